@@ -48,6 +48,8 @@ enum { VF_ROOT = 0, VF_L1 = 1, VF_L2 = 2, VF_INLINE = 3 };
 enum { VF_MLP = 0, VF_LSTM = 1 };
 enum { VF_FP32 = 0, VF_BF16 = 1 };
 enum { VF_X_RAW_I32 = 0, VF_X_SEQ_BF16 = 1 };
+/* microscaled element formats of the sequence operators, next to VF_FP32 and VF_BF16 */
+enum { VF_E4M3 = 2, VF_E2M1 = 3 };
 
 typedef struct vf_ctx vf_ctx; /* opaque; owns the state tables and scratch buffers */
 
@@ -249,6 +251,97 @@ int vf_set_noise(vf_ctx *ctx, float eps, uint64_t seed, int32_t first_rollout);
  * takes the same decisions as vf_greedy_schedule. */
 int vf_beam_search(vf_ctx *ctx, int first_stage, int last_stage, vf_state *out_states_dev,
                    int32_t *out_cids_dev, float *out_values_dev, int32_t *n_beams_dev);
+
+/* ---- sequence operators: the parts of a state-space value network ------------
+ *
+ * V(s) is a sequence model (Sec. 3.2: a recurrent network over one timestep per stage whose
+ * predictions are summed).  These operators are the parts of a block of a state-space one:
+ * residual + norm, projections with 4-bit weights, a short causal convolution with a selective
+ * scan, as whole sequences (prompts) and as single tokens behind a state that is kept per slot.
+ * They need no model, space or pipeline, keep nothing of their inputs, and work on the context's
+ * stream.  "type" is VF_FP32 or VF_BF16.  A matrix of a type has rows of `ld` elements (the
+ * distance between rows, at least their width); pointers are aligned to their elements.
+ * Sums, norms and states are fp32; every result is rounded once, ties to even.
+ *
+ * A microscaled matrix (format VF_E4M3: 8-bit floats, VF_E2M1: 4-bit floats) has kb =
+ * ceil(cols / 32) blocks of 32 columns in every row, filled up with zeros, and no gaps:
+ * scales [rows][kb], one byte e per block, the power of two 2^(e - 127), 255 = NaN (the whole block
+ * is NaN); codes [rows][32 kb] bytes (VF_E4M3) or [rows][16 kb] bytes (VF_E2M1, the even column in
+ * the low half).  codes are aligned to 16 bytes.  A value is code * scale. */
+
+/* s = x + residual; out = s / sqrt(mean(s^2) + eps) * gain, per row of `width` (1..32768) elements.
+ * x, residual (nullable) and sum (nullable: s rounded to `type`) are of `type`; sum may be x or
+ * residual itself, with its row distance.  gain[width] fp32 (nullable: ones).  out_type VF_FP32 /
+ * VF_BF16: out has rows of ld_out elements, scales is NULL; VF_E4M3 / VF_E2M1: out and scales are a
+ * microscaled matrix [rows][width] quantized as by vf_mx_quantize, ld_out is ignored. */
+int vf_rms_norm(vf_ctx *ctx, int32_t type, const void *x_dev, int64_t ld_x, const void *residual_dev, int64_t ld_residual,
+                const float *gain_dev, float eps, int64_t rows, int64_t width, void *sum_dev, int64_t ld_sum,
+                int32_t out_type, void *out_dev, int64_t ld_out, uint8_t *scales_dev);
+
+/* The block's scale is 2^(floor(log2(max |v|)) - emax) (emax 8 for VF_E4M3, 2 for VF_E2M1; exponent
+ * at least -127), a code is v / scale rounded to the format's nearest value, ties to even, at most
+ * the format's largest in magnitude (448, 6).  A block that holds an infinity or a NaN gets scale 255. */
+int vf_mx_quantize(vf_ctx *ctx, int32_t type, const void *x_dev, int64_t ld_x, int64_t rows, int64_t cols, int32_t format,
+                   uint8_t *codes_dev, uint8_t *scales_dev);
+/* The values of a microscaled matrix, rounded to `type`. */
+int vf_mx_dequantize(vf_ctx *ctx, int32_t format, const uint8_t *codes_dev, const uint8_t *scales_dev, int64_t rows,
+                     int64_t cols, int32_t type, void *out_dev, int64_t ld_out);
+/* out[m][n] = sum_k a[m][k] w[n][k] + bias[n]: a [M][K] in a_format (VF_E4M3 or VF_E2M1), w [N][K]
+ * in VF_E2M1, bias[N] fp32 (nullable), out [M][N] of out_type VF_FP32 or VF_BF16.  Products and
+ * sums are exact but for the rounding of the sums to fp32; with a in VF_E4M3 and out in VF_BF16 the terms of
+ * eight neighbouring k are cut at 2^-13 of the largest of them before.  K >= 1; N and K at most 2^24. */
+int vf_mx_matmul(vf_ctx *ctx, int32_t a_format, const uint8_t *a_codes_dev, const uint8_t *a_scales_dev,
+                 const uint8_t *w_codes_dev, const uint8_t *w_scales_dev, int64_t M, int64_t N, int64_t K,
+                 const float *bias_dev, int32_t out_type, void *out_dev, int64_t ld_out);
+
+/* A scan layer: heads H of head_dim P channels (1..256 each), groups G (divides H; head h uses the B and C
+ * of group h / (H/G)), n_state N (1..256), taps W of the convolution (1..8), C = H P + 2 G N channels [x | B | C].
+ * All arrays fp32 on the device, read by the calls: conv_w[C][W] (the last tap meets the current
+ * token), conv_b[C] (nullable: 0), a[H], d[H] (nullable: 0), dt_bias[H] (nullable: 0). */
+typedef struct {
+  int32_t heads, head_dim, groups, n_state, taps;
+  const float *conv_w_dev, *conv_b_dev, *a_dev, *d_dev, *dt_bias_dev;
+} vf_ssm;
+
+/* Inputs and outputs of a call.  Tokens are rows: xbc [tokens][C], dt [tokens][H], z [tokens][H P]
+ * (nullable), out [tokens][H P], all of `type`, each with its row distance, usually views of one
+ * projection's output.  Sequence s is rows offsets[s] .. offsets[s + 1] - 1 (offsets_dev int32
+ * [n_seq + 1]); without offsets every sequence has tokens / n_seq rows.  A range that does not lie in
+ * 0..tokens, or whose end is before its begin, counts as empty, rows of no sequence are not written.
+ * longest: the longest sequence's length, which sets how the work is split (longer ones are right, but slow).
+ * State kept per slot: conv [slots][C][W - 1] of `type` (the last inputs, oldest first) and
+ * ssm [slots][H][P][N] fp32.  Sequence s begins from slot slots_in[s] of conv_in / ssm_in (-1: from
+ * nothing, all zeros; slots_in NULL: slot s; conv_in and ssm_in NULL: every sequence from nothing) and
+ * leaves its state in slot slots_out[s] of conv_out / ssm_out (-1: nowhere; slots_out NULL: slot s;
+ * both buffers NULL: no state is left).  An empty sequence leaves the state it began from.  The
+ * buffers read and written may be the same if no sequence leaves its state in a slot that another
+ * one begins from; no two sequences may leave theirs in one slot.  A slot below -1 or past the number of
+ * slots reads as NaN and writes nowhere.  Without slots_in (slots_out) there are at least n_seq slots. */
+typedef struct {
+  int32_t type, n_seq, n_slots_in, n_slots_out;
+  int64_t tokens, longest;
+  const int32_t *offsets_dev, *slots_in_dev, *slots_out_dev;
+  const void *xbc_dev, *dt_dev, *z_dev;
+  void *out_dev;
+  int64_t ld_xbc, ld_dt, ld_z, ld_out;
+  const void *conv_in_dev;
+  const float *ssm_in_dev;
+  void *conv_out_dev;
+  float *ssm_out_dev;
+} vf_ssm_io;
+
+/* Per sequence, token by token:
+ *   u[c] = silu(conv_b[c] + sum_k conv_w[c][k] xbc[t - W + 1 + k][c]) for the channels x, B, C;
+ *   step = softplus(dt[t][h] + dt_bias[h]);
+ *   S[h][p][n] = exp(step a[h]) S[h][p][n] + step x[h][p] B[g][n];
+ *   y[h][p] = sum_n S[h][p][n] C[g][n] + d[h] x[h][p];   out = y silu(z[t]) (z NULL: y).
+ * Sequences of bf16 whose head_dim is a multiple of 16 up to 64 and n_state a multiple of 32 run in
+ * chunks on the matrix cores; others token by token in fp32.  A call may keep scratch in the context (a few long
+ * sequences are split along their length); a call whose stream is being captured takes no new scratch
+ * and does without. */
+int vf_ssm_scan(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);
+/* One token for every sequence (tokens == n_seq, offsets NULL; longest is ignored). */
+int vf_ssm_step(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);
 
 /* ---- diagnostics ---------------------------------------------------------- */
 

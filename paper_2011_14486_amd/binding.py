@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import Any, NamedTuple
 
 import numpy as np
 
@@ -18,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libvf.so")
 
 VF_OK, VF_EINVAL, VF_ESTATE, VF_ENOMEM, VF_EHIP = 0, -1, -2, -3, -4
 VF_X_RAW_I32, VF_X_SEQ_BF16 = 0, 1
+VF_FP32, VF_BF16, VF_E4M3, VF_E2M1 = 0, 1, 2, 3
 
 EXPORTS = [
     "vf_create", "vf_destroy", "vf_set_space", "vf_set_pipeline", "vf_set_model", "vf_reset_state",
@@ -25,6 +27,7 @@ EXPORTS = [
     "vf_featurize", "vf_score", "vf_score_static", "vf_score_static_max", "vf_argmin_step", "vf_greedy_schedule", "vf_beam_search", "vf_set_noise", "vf_strerror",
     "vf_last_hip_error", "vf_timer_start", "vf_timer_stop", "vf_timer_elapsed_ms",
     "vf_profile_enable", "vf_profile_read", "vf_profile_counts", "vf_set_wait_limit", "vf_sync_status",
+    "vf_rms_norm", "vf_mx_quantize", "vf_mx_dequantize", "vf_mx_matmul", "vf_ssm_scan", "vf_ssm_step",
 ]
 
 _lib = None
@@ -87,6 +90,12 @@ def lib():
         L.vf_profile_counts.argtypes = [vp, C.POINTER(i64), C.POINTER(i64)]
         L.vf_set_wait_limit.argtypes = [vp, C.c_uint]
         L.vf_sync_status.argtypes = [vp]
+        L.vf_rms_norm.argtypes = [vp, i32, vp, i64, vp, i64, vp, C.c_float, i64, i64, vp, i64, i32, vp, i64, vp]
+        L.vf_mx_quantize.argtypes = [vp, i32, vp, i64, i64, i64, i32, vp, vp]
+        L.vf_mx_dequantize.argtypes = [vp, i32, vp, vp, i64, i64, i32, vp, i64]
+        L.vf_mx_matmul.argtypes = [vp, i32, vp, vp, vp, vp, i64, i64, i64, vp, i32, vp, i64]
+        L.vf_ssm_scan.argtypes = [vp, vp, vp]
+        L.vf_ssm_step.argtypes = [vp, vp, vp]
         _lib = L
     return _lib
 
@@ -343,3 +352,253 @@ def vf_profile_counts(ctx):
     a, b = C.c_int64(), C.c_int64()
     _check(ctx, lib().vf_profile_counts(ctx.handle, C.byref(a), C.byref(b)))
     return int(a.value), int(b.value)
+
+
+# ---- sequence operators: the parts of a state-space value network ----
+#
+# They take and return torch tensors on the context's GPU.  Where torch's current stream is not the
+# context's, the context's waits for it first and it waits for the context's afterwards, so that
+# tensors may be made and used on either.  Tensors may be views; only their last dimension has to be dense.
+
+class MX(NamedTuple):
+    """A microscaled matrix of `cols` columns: codes uint8 [rows][32 kb] (VF_E4M3) or [rows][16 kb]
+    (VF_E2M1), scales uint8 [rows][kb], kb = ceil(cols / 32)."""
+    codes: Any
+    scales: Any
+    fmt: int
+    cols: int
+
+
+def _fail(what):
+    raise ValueError(what)
+
+
+def _type_of(torch, t):
+    return VF_BF16 if t.dtype == torch.bfloat16 else VF_FP32 if t.dtype == torch.float32 else _fail(
+        f"bfloat16 or float32 is wanted, not {t.dtype}")
+
+
+def _dtype_of(torch, vf_type):
+    return torch.bfloat16 if vf_type == VF_BF16 else torch.float32 if vf_type == VF_FP32 else _fail(f"no such type: {vf_type}")
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rows_of(ctx, t, rows, cols, dtype, name):
+    """Checks a matrix [rows][cols]; returns the distance of its rows."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype or t.device != ctx.device:
+        _fail(f"{name}: {dtype} [{rows}][{cols}] on {ctx.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if cols > 1 and t.stride(1) != 1:
+        _fail(f"{name}: the last dimension has to be dense")
+    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+
+
+def _vector(ctx, t, n, name, dtype=None):
+    if t is not None and (t.dtype != (dtype or ctx.torch.float32) or t.numel() != n or not t.is_contiguous() or t.device != ctx.device):
+        _fail(f"{name}: {n} dense values of {dtype or ctx.torch.float32} on {ctx.device} are wanted")
+    return _addr(t)
+
+
+def _mx_shape(fmt, cols):
+    """Bytes of codes and of scales in a row."""
+    if fmt not in (VF_E4M3, VF_E2M1):
+        _fail(f"no microscaled format: {fmt}")
+    kb = (cols + 31) // 32
+    return (32 if fmt == VF_E4M3 else 16) * kb, kb
+
+
+def _mx_check(ctx, m, name):
+    rows = m.codes.shape[0]
+    nb, kb = _mx_shape(m.fmt, m.cols)
+    for t, n in ((m.codes, nb), (m.scales, kb)):
+        if t.dtype != ctx.torch.uint8 or t.shape != (rows, n) or not t.is_contiguous() or t.device != ctx.device:
+            _fail(f"{name}: codes [{rows}][{nb}] and scales [{rows}][{kb}] as dense uint8 on {ctx.device} are wanted")
+    return rows
+
+
+def _mx_empty(ctx, rows, cols, fmt):
+    nb, kb = _mx_shape(fmt, cols)
+    u8 = ctx.torch.uint8
+    return MX(ctx.empty((rows, nb), u8), ctx.empty((rows, kb), u8), fmt, cols)
+
+
+def _call(ctx, fn, args, tensors):
+    """Runs a library call on the context's stream, ordered with torch's current one."""
+    torch = ctx.torch
+    if torch._C._cuda_getCurrentRawStream(ctx.device.index) == ctx.stream.cuda_stream:
+        _check(ctx, fn(ctx.handle, *args))
+        return
+    here = torch.cuda.current_stream(ctx.device)
+    ctx.stream.wait_stream(here)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(ctx.stream)
+    _check(ctx, fn(ctx.handle, *args))
+    here.wait_stream(ctx.stream)
+
+
+def vf_rms_norm(ctx, x, gain=None, eps=1e-5, residual=None, sum_out=None, out_type=None, out=None):
+    """(x + residual) / sqrt(mean of squares + eps) * gain for the rows of x [rows][width].
+
+    out_type VF_FP32 / VF_BF16 (default: x's): a tensor; VF_E4M3 / VF_E2M1: an MX.  Returns (out, sum): sum
+    is x + residual in x's type, written to sum_out if given (x or residual itself is fine), None without a
+    residual and a sum_out."""
+    torch = ctx.torch
+    kind = _type_of(torch, x)
+    rows, width = x.shape
+    ld_x = _rows_of(ctx, x, rows, width, x.dtype, "x")
+    ld_r = _rows_of(ctx, residual, rows, width, x.dtype, "residual") if residual is not None else 0
+    if residual is not None and sum_out is None:
+        sum_out = ctx.empty((rows, width), x.dtype)
+    ld_s = _rows_of(ctx, sum_out, rows, width, x.dtype, "sum_out") if sum_out is not None else 0
+    out_type = kind if out_type is None else out_type
+    if out_type in (VF_E4M3, VF_E2M1):
+        out = _mx_empty(ctx, rows, width, out_type) if out is None else out
+        if _mx_check(ctx, out, "out") != rows or out.fmt != out_type or out.cols != width:
+            _fail("out: another shape or format")
+        codes, scales, ld_o = out.codes, out.scales, 0
+    else:
+        dtype = _dtype_of(torch, out_type)
+        out = ctx.empty((rows, width), dtype) if out is None else out
+        codes, scales, ld_o = out, None, _rows_of(ctx, out, rows, width, dtype, "out")
+    g = _vector(ctx, gain, width, "gain")
+    _call(ctx, lib().vf_rms_norm, (kind, _addr(x), ld_x, _addr(residual), ld_r, g, eps, rows, width, _addr(sum_out), ld_s, out_type,
+                                   _addr(codes), ld_o, _addr(scales)), (x, residual, gain, sum_out, codes, scales))
+    return out, sum_out
+
+
+def vf_mx_quantize(ctx, x, fmt, out=None):
+    """x [rows][cols] as a microscaled matrix."""
+    rows, cols = x.shape
+    kind = _type_of(ctx.torch, x)
+    ld = _rows_of(ctx, x, rows, cols, x.dtype, "x")
+    q = _mx_empty(ctx, rows, cols, fmt) if out is None else out
+    if _mx_check(ctx, q, "out") != rows or q.fmt != fmt or q.cols != cols:
+        _fail("out: another shape or format")
+    _call(ctx, lib().vf_mx_quantize, (kind, _addr(x), ld, rows, cols, fmt, _addr(q.codes), _addr(q.scales)), (x, q.codes, q.scales))
+    return q
+
+
+def vf_mx_dequantize(ctx, q, out_type=VF_BF16, out=None):
+    """The values of a microscaled matrix, [rows][cols]."""
+    rows = _mx_check(ctx, q, "q")
+    dtype = _dtype_of(ctx.torch, out_type)
+    out = ctx.empty((rows, q.cols), dtype) if out is None else out
+    ld = _rows_of(ctx, out, rows, q.cols, dtype, "out")
+    _call(ctx, lib().vf_mx_dequantize, (q.fmt, _addr(q.codes), _addr(q.scales), rows, q.cols, out_type, _addr(out), ld),
+          (q.codes, q.scales, out))
+    return out
+
+
+def vf_mx_matmul(ctx, a, w, bias=None, out_type=VF_BF16, out=None):
+    """a [M][K] (MX, 8 or 4 bits) times w [N][K] (MX, VF_E2M1) transposed, plus bias[N]: [M][N]."""
+    M, N = _mx_check(ctx, a, "a"), _mx_check(ctx, w, "w")
+    if w.fmt != VF_E2M1 or a.cols != w.cols:
+        _fail("w: VF_E2M1 with the columns of a is wanted")
+    dtype = _dtype_of(ctx.torch, out_type)
+    out = ctx.empty((M, N), dtype) if out is None else out
+    ld = _rows_of(ctx, out, M, N, dtype, "out")
+    b = _vector(ctx, bias, N, "bias")
+    _call(ctx, lib().vf_mx_matmul, (a.fmt, _addr(a.codes), _addr(a.scales), _addr(w.codes), _addr(w.scales), M, N, a.cols, b, out_type,
+                                    _addr(out), ld), (a.codes, a.scales, w.codes, w.scales, bias, out))
+    return out
+
+
+class _Ssm(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("heads", "head_dim", "groups", "n_state", "taps")] + [
+        (n, C.c_void_p) for n in ("conv_w_dev", "conv_b_dev", "a_dev", "d_dev", "dt_bias_dev")]
+
+
+class _SsmIo(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("type", "n_seq", "n_slots_in", "n_slots_out")] + [
+        (n, C.c_int64) for n in ("tokens", "longest")] + [
+        (n, C.c_void_p) for n in ("offsets_dev", "slots_in_dev", "slots_out_dev", "xbc_dev", "dt_dev", "z_dev", "out_dev")] + [
+        (n, C.c_int64) for n in ("ld_xbc", "ld_dt", "ld_z", "ld_out")] + [
+        (n, C.c_void_p) for n in ("conv_in_dev", "ssm_in_dev", "conv_out_dev", "ssm_out_dev")]
+
+
+class SsmLayer:
+    """A scan layer: sizes and fp32 CUDA tensors conv_w [C][W], conv_b [C] or None, a [H], d [H] or None,
+    dt_bias [H] or None (C = H P + 2 G N).  Holds the tensors, copies nothing."""
+
+    def __init__(self, heads, head_dim, groups, n_state, conv_w, a, conv_b=None, d=None, dt_bias=None):
+        import torch
+        self.heads, self.head_dim, self.groups, self.n_state = heads, head_dim, groups, n_state
+        self.channels = heads * head_dim + 2 * groups * n_state
+        if conv_w.dim() != 2 or conv_w.shape[0] != self.channels:
+            _fail(f"conv_w: [{self.channels}][taps] is wanted, got {tuple(conv_w.shape)}")
+        self.taps = conv_w.shape[1]
+        self.device = conv_w.device
+        self.tensors = (conv_w, conv_b, a, d, dt_bias)
+        for t, n, name in ((conv_w, self.channels * self.taps, "conv_w"), (conv_b, self.channels, "conv_b"), (a, heads, "a"),
+                           (d, heads, "d"), (dt_bias, heads, "dt_bias")):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda or
+                                  t.device != self.device):
+                _fail(f"{name}: {n} dense float32 values on one GPU are wanted")
+        self.record = _Ssm(heads, head_dim, groups, n_state, self.taps, *(_addr(t) for t in self.tensors))
+        self.ref = C.byref(self.record)
+
+    def state(self, slots, dtype):
+        """Zeroed state buffers of `slots` slots: (conv [slots][C][W - 1] of dtype, ssm [slots][H][P][N] fp32)."""
+        import torch
+        return (torch.zeros((slots, self.channels, self.taps - 1), dtype=dtype, device=self.device),
+                torch.zeros((slots, self.heads, self.head_dim, self.n_state), device=self.device))
+
+
+def _ssm_state(ctx, layer, state, slots, n_seq, dtype, name):
+    """Checks one direction's buffers and slot list; returns the number of slots and the addresses."""
+    if state is None:
+        if slots is not None:
+            _fail(f"{name}: slots without state buffers")
+        return 0, None, None, None
+    conv, ssm = state
+    n = ssm.shape[0]
+    if tuple(conv.shape) != (n, layer.channels, layer.taps - 1) or conv.dtype != dtype or not conv.is_contiguous():
+        _fail(f"{name}: a dense {dtype} [{n}][{layer.channels}][{layer.taps - 1}] is wanted for the convolution")
+    if tuple(ssm.shape[1:]) != (layer.heads, layer.head_dim, layer.n_state) or ssm.dtype != ctx.torch.float32 or not ssm.is_contiguous():
+        _fail(f"{name}: a dense float32 [slots][{layer.heads}][{layer.head_dim}][{layer.n_state}] is wanted")
+    if conv.device != ctx.device or ssm.device != ctx.device:
+        _fail(f"{name}: buffers on {ctx.device} are wanted")
+    return n, conv.data_ptr(), ssm.data_ptr(), _vector(ctx, slots, n_seq, name + " slots", ctx.torch.int32)
+
+
+def _ssm_call(ctx, fn, layer, xbc, dt, z, n_seq, longest, offsets, state, slots, state_out, slots_out, out):
+    torch = ctx.torch
+    if layer.device != ctx.device:
+        _fail("the layer's weights are on another GPU")
+    kind, dtype, tokens = _type_of(torch, xbc), xbc.dtype, xbc.shape[0]
+    inner = layer.heads * layer.head_dim
+    out = ctx.empty((tokens, inner), dtype) if out is None else out
+    ld_x = _rows_of(ctx, xbc, tokens, layer.channels, dtype, "xbc")
+    ld_dt = _rows_of(ctx, dt, tokens, layer.heads, dtype, "dt")
+    ld_z = _rows_of(ctx, z, tokens, inner, dtype, "z") if z is not None else 0
+    ld_o = _rows_of(ctx, out, tokens, inner, dtype, "out")
+    off = _vector(ctx, offsets, n_seq + 1, "offsets", torch.int32)
+    n_in, conv_in, ssm_in, s_in = _ssm_state(ctx, layer, state, slots, n_seq, dtype, "state")
+    n_out, conv_out, ssm_out, s_out = _ssm_state(ctx, layer, state_out, slots_out, n_seq, dtype, "state_out")
+    io = _SsmIo(kind, n_seq, n_in, n_out, tokens, longest, off, s_in, s_out, xbc.data_ptr(), dt.data_ptr(), _addr(z), out.data_ptr(),
+                ld_x, ld_dt, ld_z, ld_o, conv_in, ssm_in, conv_out, ssm_out)
+    _call(ctx, fn, (layer.ref, C.byref(io)), (xbc, dt, z, offsets, slots, slots_out, out, *(state or ()), *(state_out or ()),
+                                              *layer.tensors))
+    return out
+
+
+def vf_ssm_scan(ctx, layer, xbc, dt, z=None, n_seq=1, longest=None, offsets=None, state=None, slots=None, state_out=None,
+                slots_out=None, out=None):
+    """Convolution, selective scan and gate over n_seq whole sequences.
+
+    xbc [tokens][C], dt [tokens][H], z [tokens][H P] (or None), one type; offsets int32 [n_seq + 1] (None: all
+    sequences have tokens / n_seq rows); longest: the longest sequence's length (default: without offsets the
+    length, with offsets all tokens).  state / state_out: (conv, ssm) buffers as SsmLayer.state makes them,
+    slots / slots_out int32 [n_seq] (None: slot s for sequence s, -1: none).  Returns out [tokens][H P]."""
+    if longest is None:
+        longest = xbc.shape[0] if offsets is not None or n_seq == 0 else xbc.shape[0] // n_seq
+    return _ssm_call(ctx, lib().vf_ssm_scan, layer, xbc, dt, z, n_seq, longest, offsets, state, slots, state_out, slots_out, out)
+
+
+def vf_ssm_step(ctx, layer, xbc, dt, z=None, state=None, slots=None, state_out=None, slots_out=None, out=None):
+    """One more token for every row: row s continues slot slots[s] of state and leaves its state in slot
+    slots_out[s] of state_out.  Arguments as vf_ssm_scan."""
+    return _ssm_call(ctx, lib().vf_ssm_step, layer, xbc, dt, z, xbc.shape[0], 1, None, state, slots, state_out, slots_out, out)

@@ -198,18 +198,6 @@ int finish_prefix(vf_ctx *c) { return c->n_sched < c->S ? vfk_seq_flush(c) : VF_
 
 int settle_whole(vf_ctx *c, bool wait);
 
-struct DeviceGuard {
-  int prev = -1;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    if (prev != dev) (void)hipSetDevice(dev);
-    else prev = -1;
-  }
-  ~DeviceGuard() {
-    if (prev >= 0) (void)hipSetDevice(prev);
-  }
-};
-
 // Looks at the outcome of the last whole-schedule launch, once.  wait = false: only if the
 // launch has finished (otherwise later).  A launch in which a bounded wait between workgroups
 // ran out has left some problems' schedules incomplete (unscheduled layers read -1 / +inf /

@@ -208,6 +208,19 @@ struct vf_prof_scope {
     }                                              \
   } while (0)
 
+// Makes the context's device the current one while an entry point runs.
+struct DeviceGuard {
+  int prev = -1;
+  explicit DeviceGuard(int dev) {
+    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+    if (prev != dev) (void)hipSetDevice(dev);
+    else prev = -1;
+  }
+  ~DeviceGuard() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+};
+
 // ---- vf_sched.hip: enumeration, featurization, commit ----
 // A packed bf16 MLP with uniform hidden width, as the fused scoring kernels take it.
 struct vf_fast_dev {
@@ -315,3 +328,15 @@ int vfk_argmin_groups(vf_ctx *c, int64_t M, int nparts, int parts_per_group, int
 // device), as a partial-minima buffer; VF_EHIP if the symbol's address cannot be had.
 int vfk_static_parts(vf_ctx *c, vf_partbuf *out);
 int vfk_ensure_parts(vf_ctx *c, size_t n);
+
+// ---- sequence operators (arguments checked by vf_ops.hip) ----
+int vfk_rms_norm(vf_ctx *c, int type, const void *x, int64_t ld_x, const void *res, int64_t ld_res, const float *gain,
+                 float eps, int64_t rows, int width, void *sum, int64_t ld_sum, int out_type, void *out, int64_t ld_out,
+                 uint8_t *scales);
+int vfk_mx_quantize(vf_ctx *c, int type, const void *x, int64_t ld, int64_t rows, int cols, int format, uint8_t *codes,
+                    uint8_t *scales);
+int vfk_mx_dequantize(vf_ctx *c, int format, const uint8_t *codes, const uint8_t *scales, int64_t rows, int cols, int type,
+                      void *out, int64_t ld);
+int vfk_mx_matmul(vf_ctx *c, int a_format, const uint8_t *a, const uint8_t *as, const uint8_t *w, const uint8_t *ws, int64_t M,
+                  int N, int K, const float *bias, int out_type, void *out, int64_t ld_out);
+int vfk_ssm(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io);
