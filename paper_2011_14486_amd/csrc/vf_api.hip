@@ -268,6 +268,7 @@ void vf_destroy(vf_ctx *c) {
                 c->d_pval,  c->d_pidx, c->d_scores, c->d_tk_val, c->d_tk_idx};
   for (void *p : ps)
     if (p) (void)hipFree(p);
+  for (int k = 0; k < c->ops_blocks; ++k) (void)hipFree(c->ops_scratch[k]);
   if (c->h_team_err) (void)hipHostFree(c->h_team_err);
   if (c->ev0) (void)hipEventDestroy(c->ev0);
   if (c->ev1) (void)hipEventDestroy(c->ev1);

@@ -160,6 +160,11 @@ struct vf_ctx {
   mutable const void *layer_kern = nullptr;            // the scorer that vfk_layer_fits found to fit, and its LDS
   mutable size_t layer_smem = 0;
 
+  // scratch of the sequence operators; a block that was too small stays until vf_destroy (a captured graph may hold it)
+  void *ops_scratch[48] = {};
+  size_t ops_bytes = 0;
+  int ops_blocks = 0;
+
   vf_partbuf static_parts = {nullptr, nullptr, 0};  // this device's static scratch array (vf_score_static)
 
   hipEvent_t ev0 = nullptr, ev1 = nullptr;
@@ -339,4 +344,6 @@ int vfk_mx_dequantize(vf_ctx *c, int format, const uint8_t *codes, const uint8_t
                       void *out, int64_t ld);
 int vfk_mx_matmul(vf_ctx *c, int a_format, const uint8_t *a, const uint8_t *as, const uint8_t *w, const uint8_t *ws, int64_t M,
                   int N, int K, const float *bias, int out_type, void *out, int64_t ld_out);
+// `bytes` of scratch, or nullptr where they cannot be had (no memory, or the stream is being captured)
+void *vfk_ops_scratch(vf_ctx *c, size_t bytes);
 int vfk_ssm(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io);

@@ -56,6 +56,26 @@ int ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io, bool one) {
 
 }  // namespace
 
+void *vfk_ops_scratch(vf_ctx *c, size_t bytes) {
+  if (bytes <= c->ops_bytes) return c->ops_scratch[c->ops_blocks - 1];
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c->stream, &st) != hipSuccess || st != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();
+    return nullptr;
+  }
+  if (c->ops_blocks == 48) return nullptr;
+  // at least twice the last block, so that what stays behind is less than what is held
+  const size_t want = bytes < 2 * c->ops_bytes ? 2 * c->ops_bytes : bytes;
+  void *p = nullptr;
+  if (hipMalloc(&p, want) != hipSuccess) {
+    (void)hipGetLastError();
+    return nullptr;
+  }
+  c->ops_scratch[c->ops_blocks++] = p;
+  c->ops_bytes = want;
+  return p;
+}
+
 extern "C" {
 
 int vf_rms_norm(vf_ctx *c, int32_t type, const void *x, int64_t ld_x, const void *res, int64_t ld_res, const float *gain,

@@ -26,6 +26,7 @@ __device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float((
 // Eight elements at an address that is aligned to one element only: global memory takes wide accesses at
 // any alignment, so that odd widths and row distances need no path of their own.
 struct __attribute__((packed, aligned(2))) u16x8 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(2))) u16x4 { uint32_t w[2]; };
 struct __attribute__((packed, aligned(4))) f32v4 { float v[4]; };
 
 __device__ __forceinline__ void load8(const uint16_t *p, float (&v)[8]) {

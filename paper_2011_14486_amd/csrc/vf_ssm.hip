@@ -25,6 +25,11 @@ struct SsmArgs {
   int H, P, G, N, W, C;
   int has_in, has_out;
   int conv_later;  // the convolution's state is written by a launch of its own: its buffers overlap
+  // Sequences in nseg segments of seg_len tokens (the last one runs to the end): seg_state [n_seq][nseg][H][P][N] holds what
+  // a segment makes of nothing (behind the launch with `local`), then the state before it (behind k_ssm_join);
+  // seg_log [n_seq][nseg][H] the logarithm of its decay.  nseg = 1: no segments.
+  int nseg, seg_len, local;
+  float *seg_state, *seg_log;
 };
 
 // Rows first .. first + count - 1 of sequence s; a range that does not lie in the tokens is empty.
@@ -37,6 +42,15 @@ __device__ __forceinline__ Span span_of(const SsmArgs &p, int s) {
   const int64_t b = p.offsets[s], e = p.offsets[s + 1];
   if (b < 0 || e < b || e > p.tokens) return {0, 0};
   return {b, (int)(e - b)};
+}
+// Tokens [begin, end) of segment `seg`, and whether the sequence ends in it
+struct Part { int begin, end; bool last; };
+__device__ __forceinline__ Part part_of(const SsmArgs &p, int count, int seg) {
+  if (p.nseg == 1) return {0, count, true};
+  // (a segment begins at most 2^31 - 1 tokens in: seg_len nseg may be more)
+  const int64_t b = (int64_t)seg * p.seg_len, e = b + p.seg_len;
+  const int begin = b < count ? (int)b : count, end = seg == p.nseg - 1 || e > count ? count : (int)e;
+  return {begin, end, end == count && (begin < count || seg == 0)};
 }
 // -1: no state, -2: a slot that is not there (reads as NaN, nothing is written)
 __device__ __forceinline__ int slot_of(const int32_t *slots, int has, int n_slots, int s) {
@@ -85,10 +99,20 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
   const float A = p.a[h], D = p.d ? p.d[h] : 0.0f, bias_dt = p.dt_bias ? p.dt_bias[h] : 0.0f;
   const bool owns_bc = h == g * (p.H / p.G) && p0 == 0;  // writes the convolution's state of its group's B and C
 
-  for (int s = blockIdx.y; s < p.n_seq; s += gridDim.y) {
+  const int64_t parts = (int64_t)p.n_seq * p.nseg, size = (int64_t)p.P * p.N;
+  for (int64_t sx = blockIdx.y; sx < parts; sx += gridDim.y) {
+    const int s = (int)(sx / p.nseg), seg = (int)(sx - (int64_t)s * p.nseg);
+    if (p.local && seg == p.nseg - 1) continue;
     const Span sp = span_of(p, s);
+    const Part pt = part_of(p, sp.count, seg);
+    if (!p.local && seg > 0 && pt.begin >= pt.end) continue;
     const int slot = slot_of(p.slots_in, p.has_in, p.n_in, s), slot_to = slot_of(p.slots_out, p.has_out, p.n_out, s);
-    float S[PI][NK][4];
+    // where the state before this part is, and where it goes
+    float *const mine = p.nseg > 1 ? p.seg_state + (sx * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+    const float *first = p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+    float *left = p.local ? mine : pt.last && slot_to >= 0 ? p.ssm_out + ((int64_t)slot_to * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+    if (p.local) first = nullptr;
+    float S[PI][NK][4], log_decay = 0.0f;
 #pragma unroll
     for (int k = 0; k < PI; ++k) {
       const int pr = 16 * k + prow;
@@ -96,9 +120,9 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
       for (int q = 0; q < NK; ++q) {
         const int n = 4 * (16 * q + i16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) S[k][q][j] = slot == -2 ? __uint_as_float(0x7fc00000u) : 0.0f;
-        if (slot >= 0 && pr < np && n < p.N) {
-          const float *from = p.ssm_in + (((int64_t)slot * p.H + h) * p.P + p0 + pr) * p.N + n;
+        for (int j = 0; j < 4; ++j) S[k][q][j] = slot == -2 && p.nseg == 1 ? __uint_as_float(0x7fc00000u) : 0.0f;
+        if (first && pr < np && n < p.N) {
+          const float *from = first + (int64_t)pr * p.N + n;
           if (n + 4 <= p.N) {
             const f32v4 v = *reinterpret_cast<const f32v4 *>(from);
 #pragma unroll
@@ -111,8 +135,8 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
         }
       }
     }
-    for (int t0 = 0; t0 < sp.count; t0 += SEQ_TOKENS) {
-      const int nt = sp.count - t0 < SEQ_TOKENS ? sp.count - t0 : SEQ_TOKENS;
+    for (int t0 = pt.begin; t0 < pt.end; t0 += SEQ_TOKENS) {
+      const int nt = pt.end - t0 < SEQ_TOKENS ? pt.end - t0 : SEQ_TOKENS;
       // convolution of this workgroup's x, and of B and C
       for (int e = tid; e < nt * nch; e += 256) {
         const int t = e / nch, k = e - t * nch;
@@ -137,6 +161,7 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
       __syncthreads();
       for (int t = 0; t < nt; ++t) {
         const float dt = udt[t], da = uda[t];
+        log_decay = fmaf(dt, A, log_decay);
         float y[PI];
 #pragma unroll
         for (int k = 0; k < PI; ++k) y[k] = 0.0f;
@@ -163,7 +188,7 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
         }
       }
       __syncthreads();
-      for (int e = tid; e < nt * np; e += 256) {
+      for (int e = tid; e < (p.local ? 0 : nt * np); e += 256) {
         const int t = e / np, k = e - t * np;
         const int64_t row = sp.first + t0 + t;
         float y = fmaf(D, ux[t * 16 * PI + k], uy[t * 16 * PI + k]);
@@ -172,7 +197,8 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
       }
       __syncthreads();
     }
-    if (slot_to < 0) continue;
+    if (p.local && tid == 0 && p0 == 0) p.seg_log[sx * p.H + h] = log_decay;
+    if (!left) continue;
 #pragma unroll
     for (int k = 0; k < PI; ++k) {
       const int pr = 16 * k + prow;
@@ -180,7 +206,7 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
       for (int q = 0; q < NK; ++q) {
         const int n = 4 * (16 * q + i16);
         if (pr >= np || n >= p.N) continue;
-        float *to = p.ssm_out + (((int64_t)slot_to * p.H + h) * p.P + p0 + pr) * p.N + n;
+        float *to = left + (int64_t)pr * p.N + n;
         if (n + 4 <= p.N) {
           f32v4 v;
 #pragma unroll
@@ -193,7 +219,7 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
         }
       }
     }
-    if (p.conv_later || p.W == 1) continue;
+    if (p.local || p.conv_later || p.W == 1) continue;
     for (int k = tid; k < (owns_bc ? nch : np); k += 256)
       conv_state<T>(p, sp, slot, slot_to, k < np ? h * p.P + p0 + k : k < np + p.N ? p.H * p.P + g * p.N + (k - np)
                                                                                    : p.H * p.P + p.G * p.N + g * p.N + (k - np - p.N));
@@ -211,28 +237,469 @@ __global__ void __launch_bounds__(256) k_ssm_conv_state(const SsmArgs p) {
   }
 }
 
+// The states before the segments of a sequence, one after the other: four neighbouring numbers a thread.
+__global__ void __launch_bounds__(256) k_ssm_join(const SsmArgs p) {
+  const int64_t size = (int64_t)p.H * p.P * p.N, total = p.n_seq * size;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int s = (int)(i / size);
+    const int64_t e = i - s * size;
+    const int h = (int)(e / ((int64_t)p.P * p.N));
+    const int slot = slot_of(p.slots_in, p.has_in, p.n_in, s);
+    float S = slot == -2 ? __uint_as_float(0x7fc00000u) : slot >= 0 ? p.ssm_in[slot * size + e] : 0.0f;
+    float *at = p.seg_state + (int64_t)s * p.nseg * size + e;
+    const float *lg = p.seg_log + (int64_t)s * p.nseg * p.H + h;
+    int seg = 0;
+    for (; seg + 8 < p.nseg; seg += 8) {
+      float own[8], d[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        own[k] = at[(seg + k) * size];
+        d[k] = lg[(seg + k) * p.H];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        at[(seg + k) * size] = S;
+        S = fmaf(__expf(d[k]), S, own[k]);
+      }
+    }
+    for (; seg < p.nseg - 1; ++seg) {
+      const float own = at[seg * size];
+      at[seg * size] = S;
+      S = fmaf(__expf(lg[seg * p.H]), S, own);
+    }
+    at[seg * size] = S;
+  }
+}
+
+inline int blocks_for(int64_t threads) {
+  const int64_t b = (threads + 255) / 256;
+  return (int)(b < (1 << 20) ? b : (1 << 20));
+}
+
+// How a call is split: segments of at least `least` tokens until there are `want` workgroups, of `each` for one segment of all
+// sequences.  Without the scratch for it (captured stream, no memory) the sequences stay whole.
+void split(vf_ctx *c, SsmArgs &p, int64_t longest, int64_t each, int64_t want, int unit, int64_t least) {
+  p.nseg = 1;
+  p.seg_len = 0;
+  if (each <= 0 || each >= want || longest < 2 * least) return;
+  int64_t n = (want + each - 1) / each;
+  if (n > longest / least) n = longest / least;
+  int64_t len = ((longest + n - 1) / n + unit - 1) / unit * unit;
+  n = (longest + len - 1) / len;
+  if (n < 2) return;
+  const int64_t states = (int64_t)p.n_seq * n * p.H * p.P * p.N, logs = (int64_t)p.n_seq * n * p.H;
+  if (states > (int64_t)1 << 31) return;
+  float *at = static_cast<float *>(vfk_ops_scratch(c, (size_t)(states + logs) * sizeof(float)));
+  if (!at) return;
+  p.nseg = (int)n;
+  p.seg_len = (int)len;
+  p.seg_state = at;
+  p.seg_log = at + states;
+}
+
+// Runs `launch` for whole sequences, or for segments: what each makes of nothing, the states before them, the rest.
+template <typename F>
+int run_parts(vf_ctx *c, SsmArgs &p, F launch) {
+  if (p.nseg > 1) {
+    p.local = 1;
+    int rc = launch();
+    if (rc != VF_OK) return rc;
+    p.local = 0;
+    k_ssm_join<<<blocks_for((int64_t)p.n_seq * p.H * p.P * p.N), 256, 0, c->stream>>>(p);
+    VF_HIP(c, hipGetLastError());
+  }
+  return launch();
+}
+
 template <typename T, int PI, int NK>
-int launch_tokens(vf_ctx *c, const SsmArgs &p) {
+int launch_tokens(vf_ctx *c, SsmArgs &p) {
   const int slices = (p.P + 16 * PI - 1) / (16 * PI), Nr = (p.N + 3) & ~3;
   const size_t smem = sizeof(float) * SEQ_TOKENS * (2 * Nr + 2 * 16 * PI + 2);
-  const dim3 grid(p.H * slices, p.n_seq < 32768 ? p.n_seq : 32768);
-  k_ssm_tokens<T, PI, NK><<<grid, 256, smem, c->stream>>>(p);
-  VF_HIP(c, hipGetLastError());
-  return VF_OK;
+  const int64_t parts = (int64_t)p.n_seq * p.nseg;
+  const dim3 grid(p.H * slices, (unsigned)(parts < 32768 ? parts : 32768));
+  return run_parts(c, p, [&] {
+    k_ssm_tokens<T, PI, NK><<<grid, 256, smem, c->stream>>>(p);
+    VF_HIP(c, hipGetLastError());
+    return VF_OK;
+  });
 }
 template <typename T>
-int tokens(vf_ctx *c, const SsmArgs &p) {
+int tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
   const int nk = (p.N + 63) / 64;
   // one slice of 64 rows unless there are too few workgroups for the compute units
-  const bool wide = p.P > 16 && (int64_t)p.n_seq * p.H >= 512;
-  int rc;
-  if (wide) rc = nk <= 1 ? launch_tokens<T, 4, 1>(c, p) : nk <= 2 ? launch_tokens<T, 4, 2>(c, p) : launch_tokens<T, 4, 4>(c, p);
-  else rc = nk <= 1 ? launch_tokens<T, 1, 1>(c, p) : nk <= 2 ? launch_tokens<T, 1, 2>(c, p) : launch_tokens<T, 1, 4>(c, p);
-  if (rc != VF_OK || !p.conv_later) return rc;
-  const int64_t blocks = ((int64_t)p.n_seq * p.C + 255) / 256;
-  k_ssm_conv_state<T><<<(int)(blocks < (1 << 20) ? blocks : (1 << 20)), 256, 0, c->stream>>>(p);
-  VF_HIP(c, hipGetLastError());
-  return VF_OK;
+  const bool wide = p.P > 16 && ((int64_t)p.n_seq * p.H >= 512 || longest >= 256);
+  split(c, p, longest, (int64_t)p.n_seq * p.H * (wide ? (p.P + 63) / 64 : (p.P + 15) / 16), 1024, SEQ_TOKENS, 64);
+  if (wide) return nk <= 1 ? launch_tokens<T, 4, 1>(c, p) : nk <= 2 ? launch_tokens<T, 4, 2>(c, p) : launch_tokens<T, 4, 4>(c, p);
+  return nk <= 1 ? launch_tokens<T, 1, 1>(c, p) : nk <= 2 ? launch_tokens<T, 1, 2>(c, p) : launch_tokens<T, 1, 4>(c, p);
+}
+
+// ---- in chunks of 32 tokens on the matrix cores ----
+//
+// With c_t = sum of step a over the chunk's tokens up to t, and the state S before the chunk:
+//   y_t = e^(c_t) S C_t + sum_(s <= t) (C_t . B_s) e^(c_t - c_s) step_s x_s + d x_t
+//   S'  = e^(c_31) S + sum_s step_s e^(c_31 - c_s) x_s B_s^T
+// A wave holds 16 PT rows p of one head's state as the accumulators of the second sum, transposed (rows n, columns p): in that
+// form a lane's numbers are, rounded to bf16, its part of an operand of the first sum's product with C, with the n of
+// a k-step in another order, which the operand read from the LDS then takes too; the same holds for the 32 x 32 matrix
+// (C_t . B_s) ... and its product with x.  So nothing but the convolved inputs passes through the LDS.
+// Rounding: the outputs are bf16, and so are the operands of their products.  The state is fp32: what
+// it takes up is in two parts of bf16 on either side, x step e^(...) and B, three products instead of one.
+//
+// The waves of a workgroup take neighbouring heads of one group and convolve its B and C together.  All bytes of x, z, out
+// pass once; what the kernel does per byte is dominated by the convolution and silu (a dozen vector operations a
+// number) and, for long states, by the 6 N / 16 matrix instructions per 16 x 32 numbers of x.
+
+constexpr int Q = 32, TS = Q + 8;  // tokens of a chunk, row of the transposed arrays in the LDS
+
+// silu of the convolution for tokens t0 .. t0 + 3 and channels c0 .. c0 + 7, zeros from token `end` and channel c0 + nc on.
+// At most four taps.
+__device__ __forceinline__ void conv_4x8(const SsmArgs &p, const Span &sp, int slot, int c0, int nc, int t0, int end, float (&v)[4][8]) {
+  if (nc <= 0 || t0 >= end) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[t][k] = 0.0f;
+    return;
+  }
+  const uint16_t *x = reinterpret_cast<const uint16_t *>(p.xbc) + sp.first * p.ld_xbc + c0;
+  u16x8 raw[7];
+#pragma unroll
+  for (int r = 0; r < 7; ++r) {
+    const int t = t0 - 3 + r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[r].w[i] = 0;
+    if (t >= 0 && t < end && nc >= 8) {
+      raw[r] = *reinterpret_cast<const u16x8 *>(x + t * p.ld_xbc);
+    } else if (t < end && t >= 1 - p.W) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < nc) raw[r].w[k >> 1] |= (uint32_t)round_bf16(conv_input<uint16_t>(p, sp, slot, c0 + k, t)) << (16 * (k & 1));
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float w[4], b = 0.0f;
+    if (k < nc) {
+      if (p.W == 4) {
+        const f32v4 q = *reinterpret_cast<const f32v4 *>(p.conv_w + (int64_t)(c0 + k) * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = q.v[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = i >= 4 - p.W ? p.conv_w[(int64_t)(c0 + k) * p.W + i - (4 - p.W)] : 0.0f;
+      }
+      if (p.conv_b) b = p.conv_b[c0 + k];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = 0.0f;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      float s = b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t q = raw[t + i].w[k >> 1];
+        const float in = __uint_as_float(k & 1 ? q & 0xffff0000u : q << 16);
+        // (a tap that is not there must not meet a NaN)
+        if (i >= 4 - p.W) s = fmaf(w[i], in, s);
+      }
+      v[t][k] = k < nc && t0 + t < end ? silu(s) : 0.0f;
+    }
+  }
+}
+__device__ __forceinline__ float low_part(float v, uint32_t hi) { return v - __uint_as_float(hi << 16); }
+
+__device__ __forceinline__ bf16x8 frag16(const uint16_t *at) { return *reinterpret_cast<const bf16x8 *>(at); }
+// k = 8 q + i of the operand is number 4 q + i, i < 4, and 16 + 4 q + i - 4 of the row: how accumulators lie
+__device__ __forceinline__ bf16x8 frag_acc(const uint16_t *row, int q) {
+  const uint2 a = *reinterpret_cast<const uint2 *>(row + 4 * q), b = *reinterpret_cast<const uint2 *>(row + 16 + 4 * q);
+  const uint4 v = make_uint4(a.x, a.y, b.x, b.y);
+  return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ bf16x8 frag_of(const f32x4 &a, const f32x4 &b) {
+  const uint4 v = make_uint4(pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3]));
+  return __builtin_bit_cast(bf16x8, v);
+}
+#define VF_MFMA16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
+
+template <int NT> constexpr size_t chunk_shared() { return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * 16 * NT * TS); }
+template <int PT> constexpr size_t chunk_wave() { return sizeof(uint16_t) * 2 * 16 * PT * TS + sizeof(float) * 3 * Q; }
+
+template <int NT, int PT, bool LOCAL>
+__global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
+  extern __shared__ __align__(16) char smem[];
+  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
+  uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + NP * TS;
+  uint16_t *XH = BtL + NP * TS + wave * 2 * PS * TS, *XL = XH + PS * TS;
+  float *cum = reinterpret_cast<float *>(BtL + NP * TS + nw * 2 * PS * TS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
+
+  // Workgroups of one part share B and C: they get neighbouring places on one of the eight dies, to which the hardware
+  // deals workgroups in turn.
+  const int slices = (p.P + PS - 1) / PS, jobs = p.H / p.G * slices, per = (jobs + nw - 1) / nw, each = per * p.G;
+  const int64_t parts = (int64_t)p.n_seq * p.nseg, total = parts * each, chunk8 = total / 8;
+  int64_t id = blockIdx.x;
+  if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
+  const int64_t sx = id / each;
+  const int wg = (int)(id - sx * each), g = wg / per, job = (wg - g * per) * nw + wave;
+  const int s = (int)(sx / p.nseg), seg = (int)(sx - (int64_t)s * p.nseg);
+  if (LOCAL && seg == p.nseg - 1) return;
+  const Span sp = span_of(p, s);
+  const Part part = part_of(p, sp.count, seg);
+  if (!LOCAL && seg > 0 && part.begin >= part.end) return;
+  const bool on = job < jobs;
+  const int h = g * (p.H / p.G) + (on ? job / slices : 0), p0 = on ? (job % slices) * PS : 0, np = p.P - p0 < PS ? p.P - p0 : PS;
+  const int slot = slot_of(p.slots_in, p.has_in, p.n_in, s), slot_to = slot_of(p.slots_out, p.has_out, p.n_out, s);
+  const int64_t size = (int64_t)p.P * p.N;
+  const float A = p.a[h], D = p.d ? p.d[h] : 0.0f, bias_dt = p.dt_bias ? p.dt_bias[h] : 0.0f;
+
+  // a lane's numbers: n = 16 i + 4 q .. + 3 of row p0 + 16 j + r
+  f32x4 S[NT][PT];
+  float *const mine = p.nseg > 1 ? p.seg_state + (sx * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+  {
+    const float *first = LOCAL ? nullptr : p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+    const float fill = !LOCAL && p.nseg == 1 && slot == -2 ? __uint_as_float(0x7fc00000u) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < PT; ++j) {
+        S[i][j] = f32x4{fill, fill, fill, fill};
+        if (first && on && 16 * j + r < np && 16 * i + 4 * q < p.N) {
+          const f32v4 v = *reinterpret_cast<const f32v4 *>(first + (int64_t)(16 * j + r) * p.N + 16 * i + 4 * q);
+          S[i][j] = f32x4{v.v[0], v.v[1], v.v[2], v.v[3]};
+        }
+      }
+  }
+  float log_decay = 0.0f;
+
+  for (int t0 = part.begin; t0 < part.end; t0 += Q) {
+    const int end = part.end - t0 < Q ? part.end : t0 + Q;
+    __syncthreads();  // (the arrays are still read for the chunk before)
+    constexpr int COLS = (LOCAL ? 1 : 2) * NP / 8;
+    for (int e = tid; e < COLS * (Q / 4); e += nthr) {
+      const int col = e % COLS, tg = e / COLS, isC = col >= NP / 8, n0 = 8 * (isC ? col - NP / 8 : col);
+      float v[4][8];
+      conv_4x8(p, sp, slot, p.H * p.P + (isC ? p.G * p.N : 0) + g * p.N + n0, p.N - n0, t0 + 4 * tg, end, v);
+      uint32_t hi[4][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) hi[t][k] = pack2(v[t][2 * k], v[t][2 * k + 1]);
+      uint16_t *rows = (isC ? Cs : Bs) + 4 * tg * NS + n0;
+      if (!LOCAL) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) *reinterpret_cast<uint4 *>(rows + t * NS) = make_uint4(hi[t][0], hi[t][1], hi[t][2], hi[t][3]);
+      }
+      if (!isC) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint32_t u[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) u[t] = k & 1 ? hi[t][k >> 1] >> 16 : hi[t][k >> 1] & 0xffffu;
+          *reinterpret_cast<uint2 *>(BtH + (n0 + k) * TS + 4 * tg) = make_uint2(u[0] | u[1] << 16, u[2] | u[3] << 16);
+          *reinterpret_cast<uint2 *>(BtL + (n0 + k) * TS + 4 * tg) =
+              make_uint2(pack2(low_part(v[0][k], u[0]), low_part(v[1][k], u[1])), pack2(low_part(v[2][k], u[2]), low_part(v[3][k], u[3])));
+        }
+      }
+    }
+    float last = 0.0f;
+    if (on) {
+      if (lane < PT * 2 * (Q / 4)) {
+        const int col = lane % (2 * PT), tg = lane / (2 * PT);
+        float v[4][8];
+        conv_4x8(p, sp, slot, h * p.P + p0 + 8 * col, np - 8 * col, t0 + 4 * tg, end, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t a = pack2(v[0][k], v[1][k]), b = pack2(v[2][k], v[3][k]);
+          *reinterpret_cast<uint2 *>(XH + (8 * col + k) * TS + 4 * tg) = make_uint2(a, b);
+          *reinterpret_cast<uint2 *>(XL + (8 * col + k) * TS + 4 * tg) =
+              make_uint2(pack2(low_part(v[0][k], a & 0xffffu), low_part(v[1][k], a >> 16)),
+                         pack2(low_part(v[2][k], b & 0xffffu), low_part(v[3][k], b >> 16)));
+        }
+      }
+      const int t = lane & (Q - 1);
+      float dt = 0.0f;
+      if (t0 + t < end) dt = softplus(load1(reinterpret_cast<const uint16_t *>(p.dt) + (sp.first + t0 + t) * p.ld_dt + h) + bias_dt);
+      float c = dt * A;
+#pragma unroll
+      for (int m = 1; m < Q; m <<= 1) {
+        const float o = __shfl_up(c, m, Q);
+        if (t >= m) c += o;
+      }
+      last = __shfl(c, Q - 1, Q);
+      if (lane < Q) {
+        cum[t] = c;
+        stp[t] = dt;
+        wgt[t] = dt * __expf(last - c);
+      }
+      log_decay += last;
+    }
+    __syncthreads();
+    if (!on) continue;
+
+    if constexpr (!LOCAL) {
+      f32x4 G[3];  // rows s, columns t: (0, 0), (0, 1), (1, 1)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) G[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < KN; ++k) {
+        const bf16x8 b0 = frag16(Bs + r * NS + 32 * k + 8 * q), b1 = frag16(Bs + (16 + r) * NS + 32 * k + 8 * q);
+        const bf16x8 c0 = frag16(Cs + r * NS + 32 * k + 8 * q), c1 = frag16(Cs + (16 + r) * NS + 32 * k + 8 * q);
+        G[0] = VF_MFMA16(b0, c0, G[0]);
+        G[1] = VF_MFMA16(b0, c1, G[1]);
+        G[2] = VF_MFMA16(b1, c1, G[2]);
+      }
+      f32x4 y[2][PT];  // rows p, columns t
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int k = 0; k < PT; ++k) y[j][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < KN; ++k) {
+        const bf16x8 c0 = frag_acc(Cs + r * NS + 32 * k, q), c1 = frag_acc(Cs + (16 + r) * NS + 32 * k, q);
+#pragma unroll
+        for (int j = 0; j < PT; ++j) {
+          const bf16x8 f = frag_of(S[2 * k][j], S[2 * k + 1][j]);
+          y[0][j] = VF_MFMA16(f, c0, y[0][j]);
+          y[1][j] = VF_MFMA16(f, c1, y[1][j]);
+        }
+      }
+      const f32x4 cs0 = *reinterpret_cast<const f32x4 *>(cum + 4 * q), cs1 = *reinterpret_cast<const f32x4 *>(cum + 16 + 4 * q);
+      const f32x4 st0 = *reinterpret_cast<const f32x4 *>(stp + 4 * q), st1 = *reinterpret_cast<const f32x4 *>(stp + 16 + 4 * q);
+      const float ct0 = cum[r], ct1 = cum[16 + r], e0 = __expf(ct0), e1 = __expf(ct1);
+      f32x4 m00, m01, m11;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // (the exponent of a later token is positive and may be large: chosen by comparison, not by a product with 0)
+        const int at = 4 * q + i;
+        const float d0 = __expf(at <= r ? ct0 - cs0[i] : 0.0f) * st0[i], d1 = __expf(at <= r ? ct1 - cs1[i] : 0.0f) * st1[i];
+        m00[i] = at <= r ? fmaf(G[0][i], d0, at == r ? D : 0.0f) : 0.0f;
+        m11[i] = at <= r ? fmaf(G[2][i], d1, at == r ? D : 0.0f) : 0.0f;
+        m01[i] = G[1][i] * __expf(ct1 - cs0[i]) * st0[i];
+      }
+      const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+      const bf16x8 f0 = frag_of(m00, zero), f1 = frag_of(m01, m11);
+#pragma unroll
+      for (int j = 0; j < PT; ++j) {
+        const bf16x8 x = frag_acc(XH + (16 * j + r) * TS, q);
+        y[0][j] *= e0;
+        y[1][j] *= e1;
+        y[0][j] = VF_MFMA16(x, f0, y[0][j]);
+        y[1][j] = VF_MFMA16(x, f1, y[1][j]);
+        // (not to be moved into the branches below, where some lanes are off)
+        asm volatile("" : "+v"(y[0][j]), "+v"(y[1][j]));
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (t0 + 16 * t + r >= end) continue;
+        const int64_t row = sp.first + t0 + 16 * t + r;
+        const uint16_t *z = p.z ? reinterpret_cast<const uint16_t *>(p.z) + row * p.ld_z + h * p.P + p0 + 4 * q : nullptr;
+        uint16_t *out = reinterpret_cast<uint16_t *>(p.out) + row * p.ld_out + h * p.P + p0 + 4 * q;
+#pragma unroll
+        for (int j = 0; j < PT; ++j) {
+          if (16 * j >= np) continue;
+          f32x4 v = y[t][j];
+          if (z) {
+            const u16x4 g4 = *reinterpret_cast<const u16x4 *>(z + 16 * j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= silu(__uint_as_float(i & 1 ? g4.w[i >> 1] & 0xffff0000u : g4.w[i >> 1] << 16));
+          }
+          u16x4 o;
+          o.w[0] = pack2(v[0], v[1]);
+          o.w[1] = pack2(v[2], v[3]);
+          *reinterpret_cast<u16x4 *>(out + 16 * j) = o;
+        }
+      }
+    }
+
+    // the state behind the chunk
+    const float el = __expf(last);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < PT; ++j) S[i][j] *= el;
+    bf16x8 vh[PT], vl[PT];
+    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(wgt + 8 * q), w1 = *reinterpret_cast<const f32x4 *>(wgt + 8 * q + 4);
+#pragma unroll
+    for (int j = 0; j < PT; ++j) {
+      const uint4 a = *reinterpret_cast<const uint4 *>(XH + (16 * j + r) * TS + 8 * q), b = *reinterpret_cast<const uint4 *>(XL + (16 * j + r) * TS + 8 * q);
+      const uint32_t ah[4] = {a.x, a.y, a.z, a.w}, al[4] = {b.x, b.y, b.z, b.w};
+      uint32_t h4[4], l4[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float wa = i < 2 ? w0[2 * i] : w1[2 * i - 4], wb = i < 2 ? w0[2 * i + 1] : w1[2 * i - 3];
+        const float x0 = wa * (__uint_as_float(ah[i] << 16) + __uint_as_float(al[i] << 16));
+        const float x1 = wb * (__uint_as_float(ah[i] & 0xffff0000u) + __uint_as_float(al[i] & 0xffff0000u));
+        h4[i] = pack2(x0, x1);
+        l4[i] = pack2(low_part(x0, h4[i] & 0xffffu), low_part(x1, h4[i] >> 16));
+      }
+      vh[j] = __builtin_bit_cast(bf16x8, make_uint4(h4[0], h4[1], h4[2], h4[3]));
+      vl[j] = __builtin_bit_cast(bf16x8, make_uint4(l4[0], l4[1], l4[2], l4[3]));
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const bf16x8 bh = frag16(BtH + (16 * i + r) * TS + 8 * q), bl = frag16(BtL + (16 * i + r) * TS + 8 * q);
+#pragma unroll
+      for (int j = 0; j < PT; ++j) {
+        S[i][j] = VF_MFMA16(bl, vh[j], S[i][j]);
+        S[i][j] = VF_MFMA16(bh, vl[j], S[i][j]);
+        S[i][j] = VF_MFMA16(bh, vh[j], S[i][j]);
+      }
+    }
+  }
+
+  float *left = LOCAL ? mine : part.last && slot_to >= 0 ? p.ssm_out + ((int64_t)slot_to * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+  if (left && on) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < PT; ++j)
+        if (16 * j + r < np && 16 * i + 4 * q < p.N) {
+          f32v4 v;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v.v[k] = S[i][j][k];
+          *reinterpret_cast<f32v4 *>(left + (int64_t)(16 * j + r) * p.N + 16 * i + 4 * q) = v;
+        }
+  }
+  if (LOCAL) {
+    if (on && lane == 0 && p0 == 0) p.seg_log[sx * p.H + h] = log_decay;
+    return;
+  }
+  if (!part.last || slot_to < 0 || p.conv_later || p.W == 1) return;
+  if (on)
+    for (int k = lane; k < np; k += 64) conv_state<uint16_t>(p, sp, slot, slot_to, h * p.P + p0 + k);
+  if (wg == g * per)
+    for (int k = tid; k < 2 * p.N; k += nthr)
+      conv_state<uint16_t>(p, sp, slot, slot_to, p.H * p.P + (k < p.N ? g * p.N + k : p.G * p.N + g * p.N + k - p.N));
+}
+
+bool chunks_fit(const SsmArgs &p) { return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4; }
+
+template <int NT, int PT>
+int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
+  const int jobs = p.H / p.G * ((p.P + 16 * PT - 1) / (16 * PT)), nw = jobs < 4 ? jobs : 4, per = (jobs + nw - 1) / nw;
+  const int64_t each = (int64_t)p.n_seq * per * p.G;
+  // two workgroups for every compute unit; a segment costs its state's way to memory and back, about 256 tokens' time
+  split(c, p, longest, each, 512, Q, 256);
+  const size_t smem = chunk_shared<NT>() + nw * chunk_wave<PT>();
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  const int64_t blocks = each * p.nseg;
+  if (blocks > (int64_t)1 << 23) return VF_EINVAL;  // (the runtime's limit of work-items in a launch)
+  return run_parts(c, p, [&] {
+    if (p.local) k_ssm_chunks<NT, PT, true><<<(unsigned)blocks, 64 * nw, smem, c->stream>>>(p);
+    else k_ssm_chunks<NT, PT, false><<<(unsigned)blocks, 64 * nw, smem, c->stream>>>(p);
+    VF_HIP(c, hipGetLastError());
+    return VF_OK;
+  });
+}
+int chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
+  // 128 accumulators for the state at most
+  const bool narrow = p.P <= 32;
+  if (p.N <= 32) return narrow ? launch_chunks<2, 2>(c, p, longest) : launch_chunks<2, 4>(c, p, longest);
+  if (p.N <= 64) return narrow ? launch_chunks<4, 2>(c, p, longest) : launch_chunks<4, 4>(c, p, longest);
+  if (p.N <= 128) return narrow ? launch_chunks<8, 2>(c, p, longest) : launch_chunks<8, 4>(c, p, longest);
+  return launch_chunks<16, 2>(c, p, longest);
 }
 
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
@@ -256,5 +723,15 @@ int vfk_ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io) {
   p.has_in = io->ssm_in_dev != nullptr; p.has_out = io->ssm_out_dev != nullptr;
   const size_t slot = (size_t)p.C * (p.W - 1) * (io->type == VF_BF16 ? 2 : 4);
   p.conv_later = overlap(p.conv_in, slot * p.n_in, p.conv_out, slot * p.n_out);
-  return io->type == VF_BF16 ? tokens<uint16_t>(c, p) : tokens<float>(c, p);
+  p.nseg = 1; p.seg_len = 0; p.local = 0; p.seg_state = p.seg_log = nullptr;
+  const int64_t longest = io->offsets_dev ? (io->longest < io->tokens ? io->longest : io->tokens) : io->tokens / io->n_seq;
+  int rc;
+  if (io->type == VF_BF16 && chunks_fit(p) && longest > 8) rc = chunks(c, p, longest);
+  else rc = io->type == VF_BF16 ? tokens<uint16_t>(c, p, longest) : tokens<float>(c, p, longest);
+  if (rc != VF_OK || !p.has_out || !p.conv_later || p.W == 1) return rc;
+  const int grid = blocks_for((int64_t)p.n_seq * p.C);
+  if (io->type == VF_BF16) k_ssm_conv_state<uint16_t><<<grid, 256, 0, c->stream>>>(p);
+  else k_ssm_conv_state<float><<<grid, 256, 0, c->stream>>>(p);
+  VF_HIP(c, hipGetLastError());
+  return VF_OK;
 }

@@ -84,13 +84,14 @@ class Case:
 
 def in_chunks(kind, sizes):
     """The documented rule for sequences on the matrix cores."""
-    return kind == "bf16" and sizes[1] % 16 == 0 and sizes[1] <= 64 and sizes[3] % 32 == 0
+    return kind == "bf16" and sizes[1] % 16 == 0 and sizes[3] % 16 == 0 and sizes[4] <= 4
 
 
 # (H, P, G, N, W): odd sizes token by token, sizes that run in chunks, shared groups, all numbers of taps
 SIZES = [(1, 1, 1, 1, 1), (2, 3, 1, 5, 2), (3, 17, 1, 30, 4), (4, 40, 2, 24, 3), (2, 100, 2, 129, 4), (1, 256, 1, 256, 8),
          (1, 16, 1, 32, 4), (4, 64, 1, 64, 4), (6, 64, 2, 128, 4), (3, 48, 1, 96, 2), (5, 32, 5, 32, 1), (8, 64, 1, 32, 8),
-         (2, 64, 1, 256, 4), (7, 16, 1, 160, 3), (2, 128, 1, 64, 4)]
+         (2, 64, 1, 256, 4), (7, 16, 1, 160, 3), (2, 128, 1, 64, 4), (1, 256, 1, 256, 4), (3, 80, 1, 16, 4),
+         (2, 112, 2, 48, 4)]
 LENS = [[1], [2], [50, 50], [64], [65, 0, 1, 63, 2], [7, 130, 3], [33, 31, 32, 96, 97]]
 
 
