@@ -342,107 +342,145 @@ int tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
 // form a lane's numbers are, rounded to bf16, its part of an operand of the first sum's product with C, with the n of
 // a k-step in another order, which the operand read from the LDS then takes too; the same holds for the 32 x 32 matrix
 // (C_t . B_s) ... and its product with x.  So nothing but the convolved inputs passes through the LDS.
-// Rounding: the outputs are bf16, and so are the operands of their products.  The state is fp32: what
-// it takes up is in two parts of bf16 on either side, x step e^(...) and B, three products instead of one.
+// Rounding: the outputs are bf16; B and C (for C_t . B_s) and S and C (for S C_t) are rounded to bf16 as operands, the
+// 32 x 32 matrix with d on its diagonal and x are in two parts of bf16.  The state is fp32: what it takes up,
+// x step e^(...) and B, is in two parts of fp16 each, 22 bits together, scaled by powers of two to fp16's range (x by
+// the wave's largest, B by its row's), which the sum takes back.
 //
 // The waves of a workgroup take neighbouring heads of one group and convolve its B and C together.  All bytes of x, z, out
-// pass once; what the kernel does per byte is dominated by the convolution and silu (a dozen vector operations a
-// number) and, for long states, by the 6 N / 16 matrix instructions per 16 x 32 numbers of x.
+// pass once; what bounds the kernel is the vector work on them: convolution, silu (two quarter-rate
+// functions a number) and the operands' parts.
 
-constexpr int Q = 32, TS = Q + 8;  // tokens of a chunk, row of the transposed arrays in the LDS
+constexpr int Q = 32;            // tokens of a chunk
+constexpr int XS = Q + 4;        // row of x in the LDS, floats
+// place of row n of the transposed B, in fp16 numbers: 80 bytes a row and 16 more after eight, so that the eight-token pieces that
+// neighbouring lanes write (channels four apart) lie in different banks
+__device__ __forceinline__ int bt_row(int n) { return n * (Q + 8) + (n >> 3) * 8; }
+constexpr int bt_size(int np) { return np * (Q + 8) + (np >> 3) * 8; }
 
-// silu of the convolution for tokens t0 .. t0 + 3 and channels c0 .. c0 + 7, zeros from token `end` and channel c0 + nc on.
-// At most four taps.
-__device__ __forceinline__ void conv_4x8(const SsmArgs &p, const Span &sp, int slot, int c0, int nc, int t0, int end, float (&v)[4][8]) {
-  if (nc <= 0 || t0 >= end) {
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ uint32_t pack_h(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+// what is left of two numbers behind their parts in fp16 / bf16
+__device__ __forceinline__ uint32_t rest_h(float a, float b, uint32_t hi) {
+  const f16x2 h = __builtin_bit_cast(f16x2, hi);
+  return pack_h(a - (float)h[0], b - (float)h[1]);
+}
+__device__ __forceinline__ uint32_t rest_b(float a, float b, uint32_t hi) {
+  return pack2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+}
+// 2^k that brings a magnitude below 2^15, and its reciprocal; k is cut where either would leave the normal numbers
+__device__ __forceinline__ float scale_to_f16(float top) {
+  const int e = (int)(__float_as_uint(top) >> 23);
+  return __uint_as_float((uint32_t)min(max(268 - e, 1), 253) << 23);
+}
+__device__ __forceinline__ float power_reciprocal(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
+
+// silu of the convolution for tokens t0 .. t0 + 7 (t0 >= 0) and channels c0 .. c0 + 3.  Tokens from `end` on get some token's inputs: what
+// they give is multiplied by a step of zero or not written.  At most four taps.  `x`: row `base` of xbc, channel c0; `inner`:
+// the rows t0 - 3 .. t0 + 7 all lie in the sequence's part (uniform over the chunk).
+__device__ __forceinline__ void conv_8x4(const SsmArgs &p, const Span &sp, int slot, const char *x, uint32_t ld2, int base, int c0,
+                                         int t0, int end, bool inner, float (&v)[8][4]) {
+  u16x4 raw[11];
+  if (inner) {
+    const uint32_t o = (uint32_t)(t0 - 3 - base) * ld2;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int r = 0; r < 11; ++r) raw[r] = *reinterpret_cast<const u16x4 *>(x + (o + r * ld2));
+  } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[t][k] = 0.0f;
-    return;
-  }
-  const uint16_t *x = reinterpret_cast<const uint16_t *>(p.xbc) + sp.first * p.ld_xbc + c0;
-  u16x8 raw[7];
+    for (int r = 0; r < 11; ++r) {
+      const int t = min(max(t0 - 3 + r, 0), end - 1);
+      raw[r] = *reinterpret_cast<const u16x4 *>(x + (uint32_t)(t - base) * ld2);
+    }
+    if (t0 < 3) {  // (t0 is 0: rows -3, -2, -1 are the convolution's state, [channel][W - 1])
+      const uint32_t fill = slot == -2 ? 0x7fc07fc0u : 0u;
 #pragma unroll
-  for (int r = 0; r < 7; ++r) {
-    const int t = t0 - 3 + r;
+      for (int r = 0; r < 3; ++r) raw[r].w[0] = raw[r].w[1] = fill;
+      if (slot >= 0) {
+        const int w1 = p.W - 1;
+        const uint16_t *st = reinterpret_cast<const uint16_t *>(p.conv_in) + ((int64_t)slot * p.C + c0) * w1 - (3 - w1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) raw[r].w[i] = 0;
-    if (t >= 0 && t < end && nc >= 8) {
-      raw[r] = *reinterpret_cast<const u16x8 *>(x + t * p.ld_xbc);
-    } else if (t < end && t >= 1 - p.W) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < nc) raw[r].w[k >> 1] |= (uint32_t)round_bf16(conv_input<uint16_t>(p, sp, slot, c0 + k, t)) << (16 * (k & 1));
+        for (int r = 0; r < 3; ++r) {
+          if (r < 3 - w1) continue;
+          raw[r].w[0] = st[r] | (uint32_t)st[w1 + r] << 16;
+          raw[r].w[1] = st[2 * w1 + r] | (uint32_t)st[3 * w1 + r] << 16;
+        }
+      }
     }
   }
+  float w[4][4], b[4];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    float w[4], b = 0.0f;
-    if (k < nc) {
-      if (p.W == 4) {
-        const f32v4 q = *reinterpret_cast<const f32v4 *>(p.conv_w + (int64_t)(c0 + k) * 4);
+  for (int k = 0; k < 4; ++k) {
+    if (p.W == 4) {
+      const f32v4 q = *reinterpret_cast<const f32v4 *>(p.conv_w + (c0 + k) * 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = q.v[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = i >= 4 - p.W ? p.conv_w[(int64_t)(c0 + k) * p.W + i - (4 - p.W)] : 0.0f;
-      }
-      if (p.conv_b) b = p.conv_b[c0 + k];
+      for (int i = 0; i < 4; ++i) w[k][i] = q.v[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = 0.0f;
+      for (int i = 0; i < 4; ++i) w[k][i] = i >= 4 - p.W ? p.conv_w[(c0 + k) * p.W + i - (4 - p.W)] : 0.0f;
     }
+    b[k] = p.conv_b ? p.conv_b[c0 + k] : 0.0f;
+  }
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      float s = b;
+  for (int k = 0; k < 4; ++k) {
+    // (one channel after the other: together they would take the registers of the state)
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      float s = b[k];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t q = raw[t + i].w[k >> 1];
-        const float in = __uint_as_float(k & 1 ? q & 0xffff0000u : q << 16);
-        // (a tap that is not there must not meet a NaN)
-        if (i >= 4 - p.W) s = fmaf(w[i], in, s);
+        const uint32_t u = raw[t + i].w[k >> 1];
+        s = fmaf(w[k][i], __uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), s);
       }
-      v[t][k] = k < nc && t0 + t < end ? silu(s) : 0.0f;
+      v[t][k] = silu(s);
     }
   }
 }
-__device__ __forceinline__ float low_part(float v, uint32_t hi) { return v - __uint_as_float(hi << 16); }
 
 __device__ __forceinline__ bf16x8 frag16(const uint16_t *at) { return *reinterpret_cast<const bf16x8 *>(at); }
 // k = 8 q + i of the operand is number 4 q + i, i < 4, and 16 + 4 q + i - 4 of the row: how accumulators lie
-__device__ __forceinline__ bf16x8 frag_acc(const uint16_t *row, int q) {
+__device__ __forceinline__ uint4 frag_acc(const uint16_t *row, int q) {
   const uint2 a = *reinterpret_cast<const uint2 *>(row + 4 * q), b = *reinterpret_cast<const uint2 *>(row + 16 + 4 * q);
-  const uint4 v = make_uint4(a.x, a.y, b.x, b.y);
-  return __builtin_bit_cast(bf16x8, v);
+  return make_uint4(a.x, a.y, b.x, b.y);
 }
-__device__ __forceinline__ bf16x8 frag_of(const f32x4 &a, const f32x4 &b) {
-  const uint4 v = make_uint4(pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3]));
-  return __builtin_bit_cast(bf16x8, v);
+__device__ __forceinline__ bf16x8 as_b(const uint4 &v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ f16x8 as_h(const uint4 &v) { return __builtin_bit_cast(f16x8, v); }
+__device__ __forceinline__ uint4 frag_of(const f32x4 &a, const f32x4 &b) {
+  return make_uint4(pack2(a[0], a[1]), pack2(a[2], a[3]), pack2(b[0], b[1]), pack2(b[2], b[3]));
 }
-#define VF_MFMA16(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
+__device__ __forceinline__ uint4 rest_of(const f32x4 &a, const f32x4 &b, const uint4 &h) {
+  return make_uint4(rest_b(a[0], a[1], h.x), rest_b(a[2], a[3], h.y), rest_b(b[0], b[1], h.z), rest_b(b[2], b[3], h.w));
+}
+#define VF_MFMA_B(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
+#define VF_MFMA_H(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
 
-template <int NT> constexpr size_t chunk_shared() { return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * 16 * NT * TS); }
-template <int PT> constexpr size_t chunk_wave() { return sizeof(uint16_t) * 2 * 16 * PT * TS + sizeof(float) * 3 * Q; }
+template <int NT> constexpr size_t chunk_shared() {
+  return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * bt_size(16 * NT)) + sizeof(float) * 16 * NT;
+}
+template <int PT> constexpr size_t chunk_wave() { return sizeof(float) * (16 * PT * XS + 3 * Q); }
 
 template <int NT, int PT, bool LOCAL>
 __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
   extern __shared__ __align__(16) char smem[];
   constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
-  uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + NP * TS;
-  uint16_t *XH = BtL + NP * TS + wave * 2 * PS * TS, *XL = XH + PS * TS;
-  float *cum = reinterpret_cast<float *>(BtL + NP * TS + nw * 2 * PS * TS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
+  uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + bt_size(NP);
+  float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));  // reciprocals of the scales of B's rows
+  float *X = bscale + NP + wave * (PS * XS + 3 * Q), *cum = X + PS * XS, *stp = cum + Q, *wgt = stp + Q;
 
   // Workgroups of one part share B and C: they get neighbouring places on one of the eight dies, to which the hardware
   // deals workgroups in turn.
   const int slices = (p.P + PS - 1) / PS, jobs = p.H / p.G * slices, per = (jobs + nw - 1) / nw, each = per * p.G;
-  const int64_t parts = (int64_t)p.n_seq * p.nseg, total = parts * each, chunk8 = total / 8;
-  int64_t id = blockIdx.x;
+  const uint32_t total = (uint32_t)((int64_t)p.n_seq * p.nseg * each), chunk8 = total / 8;
+  uint32_t id = blockIdx.x;
   if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
-  const int64_t sx = id / each;
-  const int wg = (int)(id - sx * each), g = wg / per, job = (wg - g * per) * nw + wave;
-  const int s = (int)(sx / p.nseg), seg = (int)(sx - (int64_t)s * p.nseg);
+  const int sx = (int)(id / (uint32_t)each);
+  const int wg = (int)(id - (uint32_t)sx * each), g = wg / per, job = (wg - g * per) * nw + wave;
+  const int s = sx / p.nseg, seg = sx - s * p.nseg;
   if (LOCAL && seg == p.nseg - 1) return;
   const Span sp = span_of(p, s);
   const Part part = part_of(p, sp.count, seg);
@@ -455,7 +493,7 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
 
   // a lane's numbers: n = 16 i + 4 q .. + 3 of row p0 + 16 j + r
   f32x4 S[NT][PT];
-  float *const mine = p.nseg > 1 ? p.seg_state + (sx * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+  float *const mine = p.nseg > 1 ? p.seg_state + ((int64_t)sx * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
   {
     const float *first = LOCAL ? nullptr : p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
     const float fill = !LOCAL && p.nseg == 1 && slot == -2 ? __uint_as_float(0x7fc00000u) : 0.0f;
@@ -465,56 +503,72 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
       for (int j = 0; j < PT; ++j) {
         S[i][j] = f32x4{fill, fill, fill, fill};
         if (first && on && 16 * j + r < np && 16 * i + 4 * q < p.N) {
-          const f32v4 v = *reinterpret_cast<const f32v4 *>(first + (int64_t)(16 * j + r) * p.N + 16 * i + 4 * q);
+          const f32v4 v = *reinterpret_cast<const f32v4 *>(first + (16 * j + r) * p.N + 16 * i + 4 * q);
           S[i][j] = f32x4{v.v[0], v.v[1], v.v[2], v.v[3]};
         }
       }
   }
+  // rows of B and C behind N, rows of x behind P: zeros, once
+  for (int e = tid; e < (int)((chunk_shared<NT>() + nw * chunk_wave<PT>()) / 4); e += nthr) reinterpret_cast<uint32_t *>(smem)[e] = 0;
   float log_decay = 0.0f;
+  const uint32_t ld2 = (uint32_t)(2 * p.ld_xbc);
 
   for (int t0 = part.begin; t0 < part.end; t0 += Q) {
     const int end = part.end - t0 < Q ? part.end : t0 + Q;
+    const bool inner = t0 >= 3 && end == t0 + Q;
+    const int base = t0 - 3;  // (may lie before the sequence: no row before its first is read)
+    const char *rows = reinterpret_cast<const char *>(p.xbc) + 2 * ((sp.first + base) * p.ld_xbc);
     __syncthreads();  // (the arrays are still read for the chunk before)
-    constexpr int COLS = (LOCAL ? 1 : 2) * NP / 8;
-    for (int e = tid; e < COLS * (Q / 4); e += nthr) {
-      const int col = e % COLS, tg = e / COLS, isC = col >= NP / 8, n0 = 8 * (isC ? col - NP / 8 : col);
-      float v[4][8];
-      conv_4x8(p, sp, slot, p.H * p.P + (isC ? p.G * p.N : 0) + g * p.N + n0, p.N - n0, t0 + 4 * tg, end, v);
-      uint32_t hi[4][4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) hi[t][k] = pack2(v[t][2 * k], v[t][2 * k + 1]);
-      uint16_t *rows = (isC ? Cs : Bs) + 4 * tg * NS + n0;
+    // four neighbouring lanes take the 32 tokens of four channels
+    constexpr int COLS = (LOCAL ? 1 : 2) * NP / 4;
+    for (int e = tid; e < COLS * (Q / 8); e += nthr) {
+      const int col = e >> 2, tg = e & 3, isC = col >= NP / 4, n0 = 4 * (isC ? col - NP / 4 : col);
+      if (n0 >= p.N) continue;
+      const int c0 = p.H * p.P + (isC ? p.G * p.N : 0) + g * p.N + n0;
+      float v[8][4];
+      conv_8x4(p, sp, slot, rows + 2 * c0, ld2, base, c0, t0 + 8 * tg, end, inner, v);
       if (!LOCAL) {
+        uint16_t *to = (isC ? Cs : Bs) + 8 * tg * NS + n0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) *reinterpret_cast<uint4 *>(rows + t * NS) = make_uint4(hi[t][0], hi[t][1], hi[t][2], hi[t][3]);
+        for (int t = 0; t < 8; ++t) *reinterpret_cast<uint2 *>(to + t * NS) = make_uint2(pack2(v[t][0], v[t][1]), pack2(v[t][2], v[t][3]));
       }
       if (!isC) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          uint32_t u[4];
+        for (int k = 0; k < 4; ++k) {
+          float top = 0.0f;
 #pragma unroll
-          for (int t = 0; t < 4; ++t) u[t] = k & 1 ? hi[t][k >> 1] >> 16 : hi[t][k >> 1] & 0xffffu;
-          *reinterpret_cast<uint2 *>(BtH + (n0 + k) * TS + 4 * tg) = make_uint2(u[0] | u[1] << 16, u[2] | u[3] << 16);
-          *reinterpret_cast<uint2 *>(BtL + (n0 + k) * TS + 4 * tg) =
-              make_uint2(pack2(low_part(v[0][k], u[0]), low_part(v[1][k], u[1])), pack2(low_part(v[2][k], u[2]), low_part(v[3][k], u[3])));
+          for (int t = 0; t < 8; t += 2) top = fmaxf(top, fmaxf(fabsf(v[t][k]), fabsf(v[t + 1][k])));
+          top = fmaxf(top, __shfl_xor(top, 1));
+          top = fmaxf(top, __shfl_xor(top, 2));
+          const float f = scale_to_f16(top);
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const float a = v[2 * t][k] * f, b = v[2 * t + 1][k] * f;
+            hi[t] = pack_h(a, b);
+            lo[t] = rest_h(a, b, hi[t]);
+          }
+          *reinterpret_cast<uint4 *>(BtH + bt_row(n0) + k * (Q + 8) + 8 * tg) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4 *>(BtL + bt_row(n0) + k * (Q + 8) + 8 * tg) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          if (tg == 0) bscale[n0 + k] = power_reciprocal(f);
         }
       }
     }
-    float last = 0.0f;
+    float last = 0.0f, xscale = 1.0f;
     if (on) {
-      if (lane < PT * 2 * (Q / 4)) {
-        const int col = lane % (2 * PT), tg = lane / (2 * PT);
-        float v[4][8];
-        conv_4x8(p, sp, slot, h * p.P + p0 + 8 * col, np - 8 * col, t0 + 4 * tg, end, v);
+      float top = 0.0f;
+      const int col = lane >> 2, tg = lane & 3;
+      if (4 * col < np) {
+        const int c0 = h * p.P + p0 + 4 * col;
+        float v[8][4];
+        conv_8x4(p, sp, slot, rows + 2 * c0, ld2, base, c0, t0 + 8 * tg, end, inner, v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t a = pack2(v[0][k], v[1][k]), b = pack2(v[2][k], v[3][k]);
-          *reinterpret_cast<uint2 *>(XH + (8 * col + k) * TS + 4 * tg) = make_uint2(a, b);
-          *reinterpret_cast<uint2 *>(XL + (8 * col + k) * TS + 4 * tg) =
-              make_uint2(pack2(low_part(v[0][k], a & 0xffffu), low_part(v[1][k], a >> 16)),
-                         pack2(low_part(v[2][k], b & 0xffffu), low_part(v[3][k], b >> 16)));
+        for (int k = 0; k < 4; ++k) {
+          float *to = X + (4 * col + k) * XS + 8 * tg;
+          *reinterpret_cast<f32x4 *>(to) = f32x4{v[0][k], v[1][k], v[2][k], v[3][k]};
+          *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4][k], v[5][k], v[6][k], v[7][k]};
+#pragma unroll
+          for (int t = 0; t < 8; t += 2) top = fmaxf(top, fmaxf(fabsf(v[t][k]), fabsf(v[t + 1][k])));
         }
       }
       const int t = lane & (Q - 1);
@@ -527,11 +581,19 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
         if (t >= m) c += o;
       }
       last = __shfl(c, Q - 1, Q);
+      const float w = dt * __expf(last - c);
       if (lane < Q) {
         cum[t] = c;
         stp[t] = dt;
-        wgt[t] = dt * __expf(last - c);
+        wgt[t] = w;
       }
+      float wtop = w;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        top = fmaxf(top, __shfl_xor(top, m));
+        if (m < Q) wtop = fmaxf(wtop, __shfl_xor(wtop, m));
+      }
+      xscale = scale_to_f16(top * wtop);
       log_decay += last;
     }
     __syncthreads();
@@ -543,11 +605,12 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
       for (int k = 0; k < 3; ++k) G[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < KN; ++k) {
+        if (NT * PT > 16) __builtin_amdgcn_sched_barrier(0);
         const bf16x8 b0 = frag16(Bs + r * NS + 32 * k + 8 * q), b1 = frag16(Bs + (16 + r) * NS + 32 * k + 8 * q);
         const bf16x8 c0 = frag16(Cs + r * NS + 32 * k + 8 * q), c1 = frag16(Cs + (16 + r) * NS + 32 * k + 8 * q);
-        G[0] = VF_MFMA16(b0, c0, G[0]);
-        G[1] = VF_MFMA16(b0, c1, G[1]);
-        G[2] = VF_MFMA16(b1, c1, G[2]);
+        G[0] = VF_MFMA_B(b0, c0, G[0]);
+        G[1] = VF_MFMA_B(b0, c1, G[1]);
+        G[2] = VF_MFMA_B(b1, c1, G[2]);
       }
       f32x4 y[2][PT];  // rows p, columns t
 #pragma unroll
@@ -556,12 +619,13 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
         for (int k = 0; k < PT; ++k) y[j][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < KN; ++k) {
-        const bf16x8 c0 = frag_acc(Cs + r * NS + 32 * k, q), c1 = frag_acc(Cs + (16 + r) * NS + 32 * k, q);
+        if (NT * PT > 16) __builtin_amdgcn_sched_barrier(0);
+        const bf16x8 c0 = as_b(frag_acc(Cs + r * NS + 32 * k, q)), c1 = as_b(frag_acc(Cs + (16 + r) * NS + 32 * k, q));
 #pragma unroll
         for (int j = 0; j < PT; ++j) {
-          const bf16x8 f = frag_of(S[2 * k][j], S[2 * k + 1][j]);
-          y[0][j] = VF_MFMA16(f, c0, y[0][j]);
-          y[1][j] = VF_MFMA16(f, c1, y[1][j]);
+          const bf16x8 f = as_b(frag_of(S[2 * k][j], S[2 * k + 1][j]));
+          y[0][j] = VF_MFMA_B(f, c0, y[0][j]);
+          y[1][j] = VF_MFMA_B(f, c1, y[1][j]);
         }
       }
       const f32x4 cs0 = *reinterpret_cast<const f32x4 *>(cum + 4 * q), cs1 = *reinterpret_cast<const f32x4 *>(cum + 16 + 4 * q);
@@ -578,14 +642,19 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
         m01[i] = G[1][i] * __expf(ct1 - cs0[i]) * st0[i];
       }
       const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
-      const bf16x8 f0 = frag_of(m00, zero), f1 = frag_of(m01, m11);
+      const uint4 f0 = frag_of(m00, zero), f1 = frag_of(m01, m11), g0 = rest_of(m00, zero, f0), g1 = rest_of(m01, m11, f1);
 #pragma unroll
       for (int j = 0; j < PT; ++j) {
-        const bf16x8 x = frag_acc(XH + (16 * j + r) * TS, q);
+        const f32x4 xa = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q), xb = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q);
+        const uint4 xh = frag_of(xa, xb), xl = rest_of(xa, xb, xh);
         y[0][j] *= e0;
         y[1][j] *= e1;
-        y[0][j] = VF_MFMA16(x, f0, y[0][j]);
-        y[1][j] = VF_MFMA16(x, f1, y[1][j]);
+        y[0][j] = VF_MFMA_B(as_b(xl), as_b(f0), y[0][j]);
+        y[1][j] = VF_MFMA_B(as_b(xl), as_b(f1), y[1][j]);
+        y[0][j] = VF_MFMA_B(as_b(xh), as_b(g0), y[0][j]);
+        y[1][j] = VF_MFMA_B(as_b(xh), as_b(g1), y[1][j]);
+        y[0][j] = VF_MFMA_B(as_b(xh), as_b(f0), y[0][j]);
+        y[1][j] = VF_MFMA_B(as_b(xh), as_b(f1), y[1][j]);
         // (not to be moved into the branches below, where some lanes are off)
         asm volatile("" : "+v"(y[0][j]), "+v"(y[1][j]));
       }
@@ -613,37 +682,30 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
     }
 
     // the state behind the chunk
-    const float el = __expf(last);
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int j = 0; j < PT; ++j) S[i][j] *= el;
-    bf16x8 vh[PT], vl[PT];
-    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(wgt + 8 * q), w1 = *reinterpret_cast<const f32x4 *>(wgt + 8 * q + 4);
+    uint4 vh[PT], vl[PT];
+    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(wgt + 4 * q) * xscale, w1 = *reinterpret_cast<const f32x4 *>(wgt + 16 + 4 * q) * xscale;
 #pragma unroll
     for (int j = 0; j < PT; ++j) {
-      const uint4 a = *reinterpret_cast<const uint4 *>(XH + (16 * j + r) * TS + 8 * q), b = *reinterpret_cast<const uint4 *>(XL + (16 * j + r) * TS + 8 * q);
-      const uint32_t ah[4] = {a.x, a.y, a.z, a.w}, al[4] = {b.x, b.y, b.z, b.w};
-      uint32_t h4[4], l4[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float wa = i < 2 ? w0[2 * i] : w1[2 * i - 4], wb = i < 2 ? w0[2 * i + 1] : w1[2 * i - 3];
-        const float x0 = wa * (__uint_as_float(ah[i] << 16) + __uint_as_float(al[i] << 16));
-        const float x1 = wb * (__uint_as_float(ah[i] & 0xffff0000u) + __uint_as_float(al[i] & 0xffff0000u));
-        h4[i] = pack2(x0, x1);
-        l4[i] = pack2(low_part(x0, h4[i] & 0xffffu), low_part(x1, h4[i] >> 16));
-      }
-      vh[j] = __builtin_bit_cast(bf16x8, make_uint4(h4[0], h4[1], h4[2], h4[3]));
-      vl[j] = __builtin_bit_cast(bf16x8, make_uint4(l4[0], l4[1], l4[2], l4[3]));
+      const f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * w0;
+      const f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * w1;
+      vh[j] = make_uint4(pack_h(a[0], a[1]), pack_h(a[2], a[3]), pack_h(b[0], b[1]), pack_h(b[2], b[3]));
+      vl[j] = make_uint4(rest_h(a[0], a[1], vh[j].x), rest_h(a[2], a[3], vh[j].y), rest_h(b[0], b[1], vh[j].z), rest_h(b[2], b[3], vh[j].w));
     }
+    const float el = __expf(last), back = power_reciprocal(xscale);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const bf16x8 bh = frag16(BtH + (16 * i + r) * TS + 8 * q), bl = frag16(BtL + (16 * i + r) * TS + 8 * q);
+      // (no more than two rows' operands at a time: the state takes half of the registers)
+      if (NT * PT > 16 && i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+      const f16x8 bh = as_h(frag_acc(BtH + bt_row(16 * i + r), q)), bl = as_h(frag_acc(BtL + bt_row(16 * i + r), q));
+      const f32x4 sc = *reinterpret_cast<const f32x4 *>(bscale + 16 * i + 4 * q) * back;
 #pragma unroll
       for (int j = 0; j < PT; ++j) {
-        S[i][j] = VF_MFMA16(bl, vh[j], S[i][j]);
-        S[i][j] = VF_MFMA16(bh, vl[j], S[i][j]);
-        S[i][j] = VF_MFMA16(bh, vh[j], S[i][j]);
+        f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
+        u = VF_MFMA_H(bl, as_h(vh[j]), u);
+        u = VF_MFMA_H(bh, as_h(vl[j]), u);
+        u = VF_MFMA_H(bh, as_h(vh[j]), u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) S[i][j][k] = fmaf(S[i][j][k], el, u[k] * sc[k]);
       }
     }
   }
@@ -658,11 +720,11 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
           f32v4 v;
 #pragma unroll
           for (int k = 0; k < 4; ++k) v.v[k] = S[i][j][k];
-          *reinterpret_cast<f32v4 *>(left + (int64_t)(16 * j + r) * p.N + 16 * i + 4 * q) = v;
+          *reinterpret_cast<f32v4 *>(left + (16 * j + r) * p.N + 16 * i + 4 * q) = v;
         }
   }
   if (LOCAL) {
-    if (on && lane == 0 && p0 == 0) p.seg_log[sx * p.H + h] = log_decay;
+    if (on && lane == 0 && p0 == 0) p.seg_log[(int64_t)sx * p.H + h] = log_decay;
     return;
   }
   if (!part.last || slot_to < 0 || p.conv_later || p.W == 1) return;
@@ -673,7 +735,8 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
       conv_state<uint16_t>(p, sp, slot, slot_to, p.H * p.P + (k < p.N ? g * p.N + k : p.G * p.N + g * p.N + k - p.N));
 }
 
-bool chunks_fit(const SsmArgs &p) { return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4; }
+// (byte offsets within a chunk are 32 bits wide)
+bool chunks_fit(const SsmArgs &p) { return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4 && p.ld_xbc < (1 << 25); }
 
 template <int NT, int PT>
 int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
