@@ -89,8 +89,20 @@ __device__ __forceinline__ void store_upto8(T *p, int n, const float (&v)[8]) {
 
 // ---- scalar functions of the scan ----
 __device__ __forceinline__ float silu(float x) { return x * __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
-// log(1 + e^x) without the loss that 1 + e^x has where e^x is small
-__device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.0f) + log1pf(__expf(-fabsf(x))); }
+// log(1 + e^x) = max(x, 0) + log(1 + u), u = e^-|x| <= 1, by log(1 + u) = 2 artanh(s), s = u / (2 + u) <= 1 / 3: eight terms of
+// s^(2 k + 1) / (2 k + 1), the first one left out 1e-9 of the sum, and no loss where u is small
+__device__ __forceinline__ float softplus(float x) {
+  const float u = __expf(-fabsf(x)), s = u * __builtin_amdgcn_rcpf(2.0f + u), s2 = s * s;
+  float t = 2.0f / 15.0f;
+  t = fmaf(t, s2, 2.0f / 13.0f);
+  t = fmaf(t, s2, 2.0f / 11.0f);
+  t = fmaf(t, s2, 2.0f / 9.0f);
+  t = fmaf(t, s2, 2.0f / 7.0f);
+  t = fmaf(t, s2, 2.0f / 5.0f);
+  t = fmaf(t, s2, 2.0f / 3.0f);
+  t = fmaf(t, s2, 2.0f);
+  return fmaf(s, t, fmaxf(x, 0.0f));
+}
 
 // ---- microscaled formats ----
 // E4M3: sign, 4 exponent bits, 3 fraction bits, largest 448 = 1.75 * 2^8; E2M1: largest 6 = 1.5 * 2^2.

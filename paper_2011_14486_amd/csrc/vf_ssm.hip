@@ -379,66 +379,80 @@ __device__ __forceinline__ float scale_to_f16(float top) {
 }
 __device__ __forceinline__ float power_reciprocal(float s) { return __uint_as_float((254u << 23) - __float_as_uint(s)); }
 
-// silu of the convolution for tokens t0 .. t0 + 7 (t0 >= 0) and channels c0 .. c0 + 3.  Tokens from `end` on get some token's inputs: what
-// they give is multiplied by a step of zero or not written.  At most four taps.  `x`: row `base` of xbc, channel c0; `inner`:
-// the rows t0 - 3 .. t0 + 7 all lie in the sequence's part (uniform over the chunk).
-__device__ __forceinline__ void conv_8x4(const SsmArgs &p, const Span &sp, int slot, const char *x, uint32_t ld2, int base, int c0,
-                                         int t0, int end, bool inner, float (&v)[8][4]) {
-  u16x4 raw[11];
-  if (inner) {
-    const uint32_t o = (uint32_t)(t0 - 3 - base) * ld2;
+// Rows of a chunk as the memory instructions with a range check see them: a row before the sequence or behind the part
+// reads as zeros and is not written.  `at`: row `base` of the matrix; rows base .. end - 1 are there.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+struct Rows { __amdgpu_buffer_rsrc_t rsrc; uint32_t ld2; int base; };
+__device__ __forceinline__ Rows rows_of(const void *matrix, int64_t first, int64_t ld, int base, int end) {
+  const char *at = static_cast<const char *>(matrix) + 2 * ((first + base) * ld);
+  const int n = end > base ? end - base : 0;
+  return {__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(at), 0, (int)(n * (uint32_t)(2 * ld)), 0x00027000), (uint32_t)(2 * ld), base};
+}
+__device__ __forceinline__ uint2 load4(const Rows &m, int t, uint32_t byte) {
+  const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(m.rsrc, (int)((uint32_t)(t - m.base) * m.ld2 + byte), 0, 0);
+  return make_uint2(v[0], v[1]);
+}
+__device__ __forceinline__ void store4(const Rows &m, int t, uint32_t byte, const uint2 &v) {
+  const u32x2 u = {v.x, v.y};
+  __builtin_amdgcn_raw_buffer_store_b64(u, m.rsrc, (int)((uint32_t)(t - m.base) * m.ld2 + byte), 0, 0);
+}
+
+// Inputs of four channels for tokens t0 .. t0 + 7 and three before, byte `byte` of their rows
+__device__ __forceinline__ void fetch(const Rows &m, int t0, uint32_t byte, bool on, uint2 (&raw)[11]) {
+  const uint32_t at = on ? (uint32_t)(t0 - 3 - m.base) * m.ld2 + byte : 0x80000000u;  // (past the end of any chunk)
 #pragma unroll
-    for (int r = 0; r < 11; ++r) raw[r] = *reinterpret_cast<const u16x4 *>(x + (o + r * ld2));
-  } else {
-#pragma unroll
-    for (int r = 0; r < 11; ++r) {
-      const int t = min(max(t0 - 3 + r, 0), end - 1);
-      raw[r] = *reinterpret_cast<const u16x4 *>(x + (uint32_t)(t - base) * ld2);
-    }
-    if (t0 < 3) {  // (t0 is 0: rows -3, -2, -1 are the convolution's state, [channel][W - 1])
-      const uint32_t fill = slot == -2 ? 0x7fc07fc0u : 0u;
-#pragma unroll
-      for (int r = 0; r < 3; ++r) raw[r].w[0] = raw[r].w[1] = fill;
-      if (slot >= 0) {
-        const int w1 = p.W - 1;
-        const uint16_t *st = reinterpret_cast<const uint16_t *>(p.conv_in) + ((int64_t)slot * p.C + c0) * w1 - (3 - w1);
-#pragma unroll
-        for (int r = 0; r < 3; ++r) {
-          if (r < 3 - w1) continue;
-          raw[r].w[0] = st[r] | (uint32_t)st[w1 + r] << 16;
-          raw[r].w[1] = st[2 * w1 + r] | (uint32_t)st[3 * w1 + r] << 16;
-        }
-      }
-    }
+  for (int r = 0; r < 11; ++r) {
+    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(m.rsrc, (int)(at + r * m.ld2), 0, 0);
+    raw[r] = make_uint2(v[0], v[1]);
   }
-  float w[4][4], b[4];
+}
+// Rows -3, -2, -1 of channels c0 .. c0 + 3 from the convolution's state, [channel][W - 1]
+__device__ __forceinline__ void fetch_state(const SsmArgs &p, int slot, int c0, uint2 (&raw)[11]) {
+  if (slot == -1) return;
+  const int w1 = p.W - 1;
+  const uint16_t *st = reinterpret_cast<const uint16_t *>(p.conv_in) + ((int64_t)slot * p.C + c0) * w1 - (3 - w1);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (p.W == 4) {
-      const f32v4 q = *reinterpret_cast<const f32v4 *>(p.conv_w + (c0 + k) * 4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[k][i] = q.v[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[k][i] = i >= 4 - p.W ? p.conv_w[(c0 + k) * p.W + i - (4 - p.W)] : 0.0f;
-    }
-    b[k] = p.conv_b ? p.conv_b[c0 + k] : 0.0f;
+  for (int r = 0; r < 3; ++r) {
+    if (slot == -2) raw[r] = make_uint2(0x7fc07fc0u, 0x7fc07fc0u);
+    else if (r >= 3 - w1) raw[r] = make_uint2(st[r] | (uint32_t)st[w1 + r] << 16, st[2 * w1 + r] | (uint32_t)st[3 * w1 + r] << 16);
   }
+}
+// silu of the convolution for channel k of the four.  Weights in the LDS: four taps a channel (zeros before the first), and the biases.
+// Tokens that are not there give silu(bias); their steps are zero and their outputs are not written.
+__device__ __forceinline__ void convolve(const uint2 (&raw)[11], int k, const float *w, const float *b, float (&v)[8]) {
+  const f32x4 tap = *reinterpret_cast<const f32x4 *>(w + 4 * k);
+  const float bias = b[k];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    // (one channel after the other: together they would take the registers of the state)
-    __builtin_amdgcn_sched_barrier(0);
+  for (int t = 0; t < 8; ++t) {
+    float s = bias;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      float s = b[k];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t u = raw[t + i].w[k >> 1];
-        s = fmaf(w[k][i], __uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), s);
-      }
-      v[t][k] = silu(s);
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = k < 2 ? raw[t + i].x : raw[t + i].y;
+      s = fmaf(tap[i], __uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), s);
     }
+    v[t] = silu(s);
   }
+}
+// max(a, |b|, |c|) in one instruction
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+  asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(a) : "v"(a), "v"(b), "v"(c));
+  return a;
+}
+// the largest magnitude over the eight tokens of each of four neighbouring lanes
+__device__ __forceinline__ float top_of_32(const float (&v)[8]) {
+  float m = 0.0f;
+#pragma unroll
+  for (int t = 0; t < 8; t += 2) m = max_abs(m, v[t], v[t + 1]);
+  m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0xB1, 0xf, 0xf, true)));     // lanes 1 0 3 2
+  return fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x4E, 0xf, 0xf, true)));  // lanes 2 3 0 1
+}
+// the value N lanes before in the same 16, zero where there is none; and the last of the 16 before, for the second and fourth 16
+template <int N>
+__device__ __forceinline__ float lanes_before(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x110 + N, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float row_before(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
 }
 
 __device__ __forceinline__ bf16x8 frag16(const uint16_t *at) { return *reinterpret_cast<const bf16x8 *>(at); }
@@ -458,45 +472,161 @@ __device__ __forceinline__ uint4 rest_of(const f32x4 &a, const f32x4 &b, const u
 #define VF_MFMA_B(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
 #define VF_MFMA_H(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
 
-template <int NT> constexpr size_t chunk_shared() {
-  return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * bt_size(16 * NT)) + sizeof(float) * 16 * NT;
+// LDS: B and C by tokens, B by n in two parts and its scales; per wave x by p and its scales, weights of the convolution of all of
+// these channels; per wave the chunk's steps.
+constexpr int PT = 2, PS = 16 * PT, NW = 8;  // tiles and rows p of a wave, waves of a workgroup
+template <int NT> constexpr size_t chunk_lds() {
+  return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * bt_size(16 * NT)) +
+         sizeof(float) * (16 * NT + NW * PS * (XS + 1) + 6 * (32 * NT + NW * PS) + NW * 3 * Q);
 }
-template <int PT> constexpr size_t chunk_wave() { return sizeof(float) * (16 * PT * XS + 3 * Q); }
 
-template <int NT, int PT, bool LOCAL>
-__global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
+template <int NT, bool LOCAL>
+__global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT;
+  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
   uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + bt_size(NP);
-  float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));  // reciprocals of the scales of B's rows
-  float *X = bscale + NP + wave * (PS * XS + 3 * Q), *cum = X + PS * XS, *stp = cum + Q, *wgt = stp + Q;
+  float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));
+  float *Xall = bscale + NP, *xsall = Xall + NW * PS * XS, *wl = xsall + NW * PS, *bl = wl + 4 * (2 * NP + NW * PS);
+  int *chans = reinterpret_cast<int *>(bl + 2 * NP + NW * PS);
+  float *cum = bl + 2 * (2 * NP + NW * PS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
+  const float *X = Xall + wave * PS * XS, *xs = xsall + wave * PS;
 
-  // Workgroups of one part share B and C: they get neighbouring places on one of the eight dies, to which the hardware
-  // deals workgroups in turn.
   const int slices = (p.P + PS - 1) / PS, jobs = p.H / p.G * slices, per = (jobs + nw - 1) / nw, each = per * p.G;
-  const uint32_t total = (uint32_t)((int64_t)p.n_seq * p.nseg * each), chunk8 = total / 8;
+  // Workgroups of one part share B and C: they get neighbouring places on one of the eight dies, to which the hardware
+  // deals workgroups in turn.  A workgroup takes the same heads of every `stride`-th part.
+  const int parts = p.n_seq * p.nseg, stride = (int)(gridDim.x / (unsigned)each);
   uint32_t id = blockIdx.x;
+  const uint32_t chunk8 = gridDim.x / 8;
   if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
-  const int sx = (int)(id / (uint32_t)each);
-  const int wg = (int)(id - (uint32_t)sx * each), g = wg / per, job = (wg - g * per) * nw + wave;
-  const int s = sx / p.nseg, seg = sx - s * p.nseg;
-  if (LOCAL && seg == p.nseg - 1) return;
-  const Span sp = span_of(p, s);
-  const Part part = part_of(p, sp.count, seg);
-  if (!LOCAL && seg > 0 && part.begin >= part.end) return;
+  const int sx0 = (int)(id / (uint32_t)each), wg = (int)(id - (uint32_t)sx0 * each), g = wg / per, job = (wg - g * per) * nw + wave;
   const bool on = job < jobs;
   const int h = g * (p.H / p.G) + (on ? job / slices : 0), p0 = on ? (job % slices) * PS : 0, np = p.P - p0 < PS ? p.P - p0 : PS;
-  const int slot = slot_of(p.slots_in, p.has_in, p.n_in, s), slot_to = slot_of(p.slots_out, p.has_out, p.n_out, s);
-  const int64_t size = (int64_t)p.P * p.N;
+  const int size = p.P * p.N;
   const float A = p.a[h], D = p.d ? p.d[h] : 0.0f, bias_dt = p.dt_bias ? p.dt_bias[h] : 0.0f;
+
+  // Channels of the convolution as the LDS has them: B, C (NP each, zeros behind N), x of the waves (PS each, zeros behind P): their
+  // weights, and the channel of xbc, -1 where there is none.
+  if (p.N != NP || p.P % PS != 0 || nw != NW)
+    for (int e = tid; e < (int)(chunk_lds<NT>() / 4); e += nthr) reinterpret_cast<uint32_t *>(smem)[e] = 0;
+  __syncthreads();
+  auto weights = [&](int k, int c) {
+    chans[k] = c;
+    if (c < 0) return;
+    if (p.W < 4) *reinterpret_cast<f32x4 *>(wl + 4 * k) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < p.W; ++i) wl[4 * k + 4 - p.W + i] = p.conv_w[(int64_t)c * p.W + i];
+    bl[k] = p.conv_b ? p.conv_b[c] : 0.0f;
+  };
+  for (int k = tid; k < 2 * NP; k += nthr) {
+    const int n = k < NP ? k : k - NP;
+    weights(k, n < p.N ? p.H * p.P + (k < NP ? 0 : p.G * p.N) + g * p.N + n : -1);
+  }
+  if (lane < PS) weights(2 * NP + wave * PS + lane, on && lane < np ? h * p.P + p0 + lane : -1);
+  __syncthreads();
+  // A thread's work per chunk: pieces of eight tokens of four channels, first those of B and C, then of x.  The inputs of its first
+  // piece are fetched a chunk ahead; there are more where few waves share B and C.
+  constexpr int NB = (LOCAL ? NP : 2 * NP);  // pieces of B and C: NB / 4 columns of four
+  const int pieces = NB + nw * PS;
+  auto place = [&](int item) { return item < NB ? 4 * (item >> 2) : 2 * NP + 4 * ((item - NB) >> 2); };
+  // (B and C cost nearly twice what x does: with a whole workgroup the waves of their SIMDs' other half get nothing)
+  int mine0 = tid;
+  if (nw == NW && NB == 128) mine0 = wave < 2 ? tid : wave < 4 ? tid : wave < 6 ? 1 << 20 : tid - 128;
+  const int chan = mine0 < pieces ? chans[place(mine0)] : -1;
+  auto put = [&](int item, const uint2 (&raw)[11]) {
+    const int k0 = place(item), tg = item & 3;
+    // (two channels at a time, one after the other: four would take too many registers)
+    if (item < NB) {
+      const int isC = k0 >= NP, n0 = isC ? k0 - NP : k0;
+      float back[4];
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        float v[2][8];
+        convolve(raw, k, wl + 4 * k0, bl + k0, v[0]);
+        convolve(raw, k + 1, wl + 4 * k0, bl + k0, v[1]);
+        if (!LOCAL) {
+          uint16_t *to = (isC ? Cs : Bs) + 8 * tg * NS + n0 + k;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) *reinterpret_cast<uint32_t *>(to + t * NS) = pack2(v[0][t], v[1][t]);
+        }
+        if (isC) continue;
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+          const float f = scale_to_f16(top_of_32(v[o]));
+          back[k + o] = power_reciprocal(f);
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const float a = v[o][2 * t] * f, b = v[o][2 * t + 1] * f;
+            hi[t] = pack_h(a, b);
+            lo[t] = rest_h(a, b, hi[t]);
+          }
+          *reinterpret_cast<uint4 *>(BtH + bt_row(n0) + (k + o) * (Q + 8) + 8 * tg) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4 *>(BtL + bt_row(n0) + (k + o) * (Q + 8) + 8 * tg) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+      }
+      if (!isC && tg == 0) *reinterpret_cast<f32x4 *>(bscale + n0) = f32x4{back[0], back[1], back[2], back[3]};
+    } else {
+      const int x0 = k0 - 2 * NP;
+      float top[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        float v[8];
+        convolve(raw, k, wl + 4 * k0, bl + k0, v);
+        float *to = Xall + (x0 + k) * XS + 8 * tg;
+        *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        top[k] = top_of_32(v);
+      }
+      if (tg == 0) *reinterpret_cast<f32x4 *>(xsall + x0) = f32x4{top[0], top[1], top[2], top[3]};
+    }
+  };
+
+  // Inputs are fetched a chunk ahead, also from a part to the next one: the thread's first piece, and a wave's steps.
+  struct Where { Span sp; Part part; bool live; };
+  auto where = [&](int sx) {
+    Where w = {{0, 0}, {0, 0, false}, false};
+    if (sx >= parts) return w;
+    const int s = sx / p.nseg, seg = sx - s * p.nseg;
+    w.sp = span_of(p, s);
+    w.part = part_of(p, w.sp.count, seg);
+    w.live = LOCAL ? seg < p.nseg - 1 : seg == 0 || w.part.begin < w.part.end;
+    return w;
+  };
+  uint2 raw[11];
+  uint16_t dt_raw;
+  // (one place that loads, without branches: the loads are to be under way while the chunk before is worked on)
+  auto ahead = [&](const Where &w, int t0) {
+    const int end = w.live ? (w.part.end - t0 < Q ? w.part.end : t0 + Q) : 0;
+    fetch(rows_of(p.xbc, w.sp.first, p.ld_xbc, t0 >= 3 ? t0 - 3 : 0, end), t0 + 8 * (mine0 & 3), 2 * chan, chan >= 0, raw);
+    const Rows dm = rows_of(p.dt, w.sp.first, p.ld_dt, t0, end);
+    dt_raw = __builtin_amdgcn_raw_buffer_load_b16(dm.rsrc, (int)((uint32_t)(lane & (Q - 1)) * dm.ld2 + 2 * h), 0, 0);
+  };
+  Where next = where(sx0);
+  ahead(next, next.part.begin);
+
+  for (int sx = sx0; sx < parts; sx += stride) {
+  const Where here = next;
+  next = where(sx + stride);
+  if (!here.live || here.part.begin >= here.part.end) {
+    ahead(next, next.part.begin);
+    if (!here.live) continue;
+  }
+  const int s = sx / p.nseg;
+  const Span sp = here.sp;
+  const Part part = here.part;
+  const int slot = slot_of(p.slots_in, p.has_in, p.n_in, s), slot_to = slot_of(p.slots_out, p.has_out, p.n_out, s);
+  auto rows_in = [&](int t0) { return rows_of(p.xbc, sp.first, p.ld_xbc, t0 >= 3 ? t0 - 3 : 0, part.end - t0 < Q ? part.end : t0 + Q); };
 
   // a lane's numbers: n = 16 i + 4 q .. + 3 of row p0 + 16 j + r
   f32x4 S[NT][PT];
-  float *const mine = p.nseg > 1 ? p.seg_state + ((int64_t)sx * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
+  float *const mine = p.nseg > 1 ? p.seg_state + ((int64_t)sx * p.H + h) * size + p0 * p.N : nullptr;
+  float *const left = LOCAL ? mine : part.last && slot_to >= 0 ? p.ssm_out + ((int64_t)slot_to * p.H + h) * size + p0 * p.N : nullptr;
+  const float *first = LOCAL ? nullptr : p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + p0 * p.N : nullptr;
+  const bool lost = !LOCAL && p.nseg == 1 && slot == -2;
   {
-    const float *first = LOCAL ? nullptr : p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
-    const float fill = !LOCAL && p.nseg == 1 && slot == -2 ? __uint_as_float(0x7fc00000u) : 0.0f;
+    const float fill = lost ? __uint_as_float(0x7fc00000u) : 0.0f;
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -508,93 +638,69 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
         }
       }
   }
-  // rows of B and C behind N, rows of x behind P: zeros, once
-  for (int e = tid; e < (int)((chunk_shared<NT>() + nw * chunk_wave<PT>()) / 4); e += nthr) reinterpret_cast<uint32_t *>(smem)[e] = 0;
   float log_decay = 0.0f;
-  const uint32_t ld2 = (uint32_t)(2 * p.ld_xbc);
 
   for (int t0 = part.begin; t0 < part.end; t0 += Q) {
     const int end = part.end - t0 < Q ? part.end : t0 + Q;
-    const bool inner = t0 >= 3 && end == t0 + Q;
-    const int base = t0 - 3;  // (may lie before the sequence: no row before its first is read)
-    const char *rows = reinterpret_cast<const char *>(p.xbc) + 2 * ((sp.first + base) * p.ld_xbc);
     __syncthreads();  // (the arrays are still read for the chunk before)
-    // four neighbouring lanes take the 32 tokens of four channels
-    constexpr int COLS = (LOCAL ? 1 : 2) * NP / 4;
-    for (int e = tid; e < COLS * (Q / 8); e += nthr) {
-      const int col = e >> 2, tg = e & 3, isC = col >= NP / 4, n0 = 4 * (isC ? col - NP / 4 : col);
-      if (n0 >= p.N) continue;
-      const int c0 = p.H * p.P + (isC ? p.G * p.N : 0) + g * p.N + n0;
-      float v[8][4];
-      conv_8x4(p, sp, slot, rows + 2 * c0, ld2, base, c0, t0 + 8 * tg, end, inner, v);
-      if (!LOCAL) {
-        uint16_t *to = (isC ? Cs : Bs) + 8 * tg * NS + n0;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) *reinterpret_cast<uint2 *>(to + t * NS) = make_uint2(pack2(v[t][0], v[t][1]), pack2(v[t][2], v[t][3]));
+    if (chan >= 0) {
+      if (t0 == 0 && (mine0 & 3) == 0) {
+        int c = chan;
+        asm volatile("" : "+v"(c));  // (addresses of a path taken once are not to be kept in registers)
+        fetch_state(p, slot, c, raw);
       }
-      if (!isC) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float top = 0.0f;
-#pragma unroll
-          for (int t = 0; t < 8; t += 2) top = fmaxf(top, fmaxf(fabsf(v[t][k]), fabsf(v[t + 1][k])));
-          top = fmaxf(top, __shfl_xor(top, 1));
-          top = fmaxf(top, __shfl_xor(top, 2));
-          const float f = scale_to_f16(top);
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const float a = v[2 * t][k] * f, b = v[2 * t + 1][k] * f;
-            hi[t] = pack_h(a, b);
-            lo[t] = rest_h(a, b, hi[t]);
-          }
-          *reinterpret_cast<uint4 *>(BtH + bt_row(n0) + k * (Q + 8) + 8 * tg) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4 *>(BtL + bt_row(n0) + k * (Q + 8) + 8 * tg) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          if (tg == 0) bscale[n0 + k] = power_reciprocal(f);
-        }
-      }
+      put(mine0, raw);
     }
-    float last = 0.0f, xscale = 1.0f;
+    int more = nw == NW && NB == 128 ? pieces : tid + nthr;
+    asm volatile("" : "+v"(more));
+    for (int item = more; item < pieces; item += nthr) {
+      const int c = chans[place(item)];
+      if (c < 0) continue;
+      uint2 now[11];
+      fetch(rows_in(t0), t0 + 8 * (item & 3), 2 * c, true, now);
+      if (t0 == 0 && (item & 3) == 0) fetch_state(p, slot, c, now);
+      put(item, now);
+    }
+    // (behind the convolution, whose inputs are waited for together with whatever was asked for before)
+    uint2 zr[2][PT];
+    if (!LOCAL && p.z && on) {
+      const Rows zm = rows_of(p.z, sp.first, p.ld_z, t0, end);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < PT; ++j) zr[t][j] = load4(zm, t0 + 16 * t + r, 16 * j < np ? 2 * (h * p.P + p0 + 16 * j + 4 * q) : 0);
+    }
+    float last = 0.0f, wtop = 0.0f;
     if (on) {
-      float top = 0.0f;
-      const int col = lane >> 2, tg = lane & 3;
-      if (4 * col < np) {
-        const int c0 = h * p.P + p0 + 4 * col;
-        float v[8][4];
-        conv_8x4(p, sp, slot, rows + 2 * c0, ld2, base, c0, t0 + 8 * tg, end, inner, v);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          float *to = X + (4 * col + k) * XS + 8 * tg;
-          *reinterpret_cast<f32x4 *>(to) = f32x4{v[0][k], v[1][k], v[2][k], v[3][k]};
-          *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4][k], v[5][k], v[6][k], v[7][k]};
-#pragma unroll
-          for (int t = 0; t < 8; t += 2) top = fmaxf(top, fmaxf(fabsf(v[t][k]), fabsf(v[t + 1][k])));
-        }
-      }
       const int t = lane & (Q - 1);
-      float dt = 0.0f;
-      if (t0 + t < end) dt = softplus(load1(reinterpret_cast<const uint16_t *>(p.dt) + (sp.first + t0 + t) * p.ld_dt + h) + bias_dt);
+      const float dt = t0 + t < end ? softplus(bf16_f32(dt_raw) + bias_dt) : 0.0f;
+      // sums and then maxima over the 32 lanes up to a lane
       float c = dt * A;
-#pragma unroll
-      for (int m = 1; m < Q; m <<= 1) {
-        const float o = __shfl_up(c, m, Q);
-        if (t >= m) c += o;
-      }
-      last = __shfl(c, Q - 1, Q);
+      c += lanes_before<1>(c);
+      c += lanes_before<2>(c);
+      c += lanes_before<4>(c);
+      c += lanes_before<8>(c);
+      c += row_before(c);
+      last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(c), Q - 1));
       const float w = dt * __expf(last - c);
       if (lane < Q) {
         cum[t] = c;
         stp[t] = dt;
         wgt[t] = w;
       }
-      float wtop = w;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        top = fmaxf(top, __shfl_xor(top, m));
-        if (m < Q) wtop = fmaxf(wtop, __shfl_xor(wtop, m));
-      }
-      xscale = scale_to_f16(top * wtop);
+      float m = w;
+      m = fmaxf(m, lanes_before<1>(m));
+      m = fmaxf(m, lanes_before<2>(m));
+      m = fmaxf(m, lanes_before<4>(m));
+      m = fmaxf(m, lanes_before<8>(m));
+      m = fmaxf(m, row_before(m));
+      wtop = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), Q - 1));
       log_decay += last;
+    }
+    {
+      const bool more = t0 + Q < part.end;
+      const Where w = {{more ? sp.first : next.sp.first, 0}, {0, more ? part.end : next.part.end, false}, more || next.live};
+      ahead(w, more ? t0 + Q : next.part.begin);
     }
     __syncthreads();
     if (!on) continue;
@@ -605,32 +711,38 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
       for (int k = 0; k < 3; ++k) G[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < KN; ++k) {
-        if (NT * PT > 16) __builtin_amdgcn_sched_barrier(0);
         const bf16x8 b0 = frag16(Bs + r * NS + 32 * k + 8 * q), b1 = frag16(Bs + (16 + r) * NS + 32 * k + 8 * q);
         const bf16x8 c0 = frag16(Cs + r * NS + 32 * k + 8 * q), c1 = frag16(Cs + (16 + r) * NS + 32 * k + 8 * q);
         G[0] = VF_MFMA_B(b0, c0, G[0]);
         G[1] = VF_MFMA_B(b0, c1, G[1]);
         G[2] = VF_MFMA_B(b1, c1, G[2]);
       }
+      const f32x4 cs0 = *reinterpret_cast<const f32x4 *>(cum + 4 * q), cs1 = *reinterpret_cast<const f32x4 *>(cum + 16 + 4 * q);
+      const f32x4 st0 = *reinterpret_cast<const f32x4 *>(stp + 4 * q), st1 = *reinterpret_cast<const f32x4 *>(stp + 16 + 4 * q);
+      const float ct0 = cum[r], ct1 = cum[16 + r];
       f32x4 y[2][PT];  // rows p, columns t
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int k = 0; k < PT; ++k) y[j][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (t0 > part.begin || first || lost) {  // (otherwise the state is zero)
+        const float e0 = __expf(ct0), e1 = __expf(ct1);
 #pragma unroll
-      for (int k = 0; k < KN; ++k) {
-        if (NT * PT > 16) __builtin_amdgcn_sched_barrier(0);
-        const bf16x8 c0 = as_b(frag_acc(Cs + r * NS + 32 * k, q)), c1 = as_b(frag_acc(Cs + (16 + r) * NS + 32 * k, q));
+        for (int k = 0; k < KN; ++k) {
+          const bf16x8 c0 = as_b(frag_acc(Cs + r * NS + 32 * k, q)), c1 = as_b(frag_acc(Cs + (16 + r) * NS + 32 * k, q));
+#pragma unroll
+          for (int j = 0; j < PT; ++j) {
+            const bf16x8 f = as_b(frag_of(S[2 * k][j], S[2 * k + 1][j]));
+            y[0][j] = VF_MFMA_B(f, c0, y[0][j]);
+            y[1][j] = VF_MFMA_B(f, c1, y[1][j]);
+          }
+        }
 #pragma unroll
         for (int j = 0; j < PT; ++j) {
-          const bf16x8 f = as_b(frag_of(S[2 * k][j], S[2 * k + 1][j]));
-          y[0][j] = VF_MFMA_B(f, c0, y[0][j]);
-          y[1][j] = VF_MFMA_B(f, c1, y[1][j]);
+          y[0][j] *= e0;
+          y[1][j] *= e1;
         }
       }
-      const f32x4 cs0 = *reinterpret_cast<const f32x4 *>(cum + 4 * q), cs1 = *reinterpret_cast<const f32x4 *>(cum + 16 + 4 * q);
-      const f32x4 st0 = *reinterpret_cast<const f32x4 *>(stp + 4 * q), st1 = *reinterpret_cast<const f32x4 *>(stp + 16 + 4 * q);
-      const float ct0 = cum[r], ct1 = cum[16 + r], e0 = __expf(ct0), e1 = __expf(ct1);
       f32x4 m00, m01, m11;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -647,70 +759,59 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
       for (int j = 0; j < PT; ++j) {
         const f32x4 xa = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q), xb = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q);
         const uint4 xh = frag_of(xa, xb), xl = rest_of(xa, xb, xh);
-        y[0][j] *= e0;
-        y[1][j] *= e1;
         y[0][j] = VF_MFMA_B(as_b(xl), as_b(f0), y[0][j]);
         y[1][j] = VF_MFMA_B(as_b(xl), as_b(f1), y[1][j]);
         y[0][j] = VF_MFMA_B(as_b(xh), as_b(g0), y[0][j]);
         y[1][j] = VF_MFMA_B(as_b(xh), as_b(g1), y[1][j]);
         y[0][j] = VF_MFMA_B(as_b(xh), as_b(f0), y[0][j]);
         y[1][j] = VF_MFMA_B(as_b(xh), as_b(f1), y[1][j]);
-        // (not to be moved into the branches below, where some lanes are off)
-        asm volatile("" : "+v"(y[0][j]), "+v"(y[1][j]));
       }
+      const Rows om = rows_of(p.out, sp.first, p.ld_out, t0, end);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t0 + 16 * t + r >= end) continue;
-        const int64_t row = sp.first + t0 + 16 * t + r;
-        const uint16_t *z = p.z ? reinterpret_cast<const uint16_t *>(p.z) + row * p.ld_z + h * p.P + p0 + 4 * q : nullptr;
-        uint16_t *out = reinterpret_cast<uint16_t *>(p.out) + row * p.ld_out + h * p.P + p0 + 4 * q;
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < PT; ++j) {
-          if (16 * j >= np) continue;
           f32x4 v = y[t][j];
-          if (z) {
-            const u16x4 g4 = *reinterpret_cast<const u16x4 *>(z + 16 * j);
+          if (p.z) {
+            const uint32_t z4[2] = {zr[t][j].x, zr[t][j].y};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= silu(__uint_as_float(i & 1 ? g4.w[i >> 1] & 0xffff0000u : g4.w[i >> 1] << 16));
+            for (int i = 0; i < 4; ++i) v[i] *= silu(__uint_as_float(i & 1 ? z4[i >> 1] & 0xffff0000u : z4[i >> 1] << 16));
           }
-          u16x4 o;
-          o.w[0] = pack2(v[0], v[1]);
-          o.w[1] = pack2(v[2], v[3]);
-          *reinterpret_cast<u16x4 *>(out + 16 * j) = o;
+          if (16 * j < np) store4(om, t0 + 16 * t + r, 2 * (h * p.P + p0 + 16 * j + 4 * q), make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])));
         }
-      }
     }
 
     // the state behind the chunk
+    if (!LOCAL && t0 + Q >= part.end && !left) continue;
     uint4 vh[PT], vl[PT];
-    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(wgt + 4 * q) * xscale, w1 = *reinterpret_cast<const f32x4 *>(wgt + 16 + 4 * q) * xscale;
+    float back[PT];
+    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(wgt + 4 * q), w1 = *reinterpret_cast<const f32x4 *>(wgt + 16 + 4 * q);
 #pragma unroll
     for (int j = 0; j < PT; ++j) {
-      const f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * w0;
-      const f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * w1;
+      const float f = scale_to_f16(xs[16 * j + r] * wtop);
+      back[j] = power_reciprocal(f);
+      const f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * (w0 * f);
+      const f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * (w1 * f);
       vh[j] = make_uint4(pack_h(a[0], a[1]), pack_h(a[2], a[3]), pack_h(b[0], b[1]), pack_h(b[2], b[3]));
       vl[j] = make_uint4(rest_h(a[0], a[1], vh[j].x), rest_h(a[2], a[3], vh[j].y), rest_h(b[0], b[1], vh[j].z), rest_h(b[2], b[3], vh[j].w));
     }
-    const float el = __expf(last), back = power_reciprocal(xscale);
+    const float el = __expf(last);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      // (no more than two rows' operands at a time: the state takes half of the registers)
-      if (NT * PT > 16 && i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-      const f16x8 bh = as_h(frag_acc(BtH + bt_row(16 * i + r), q)), bl = as_h(frag_acc(BtL + bt_row(16 * i + r), q));
-      const f32x4 sc = *reinterpret_cast<const f32x4 *>(bscale + 16 * i + 4 * q) * back;
+      const f16x8 bh = as_h(frag_acc(BtH + bt_row(16 * i + r), q)), bl2 = as_h(frag_acc(BtL + bt_row(16 * i + r), q));
+      const f32x4 sc = *reinterpret_cast<const f32x4 *>(bscale + 16 * i + 4 * q);
 #pragma unroll
       for (int j = 0; j < PT; ++j) {
         f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
-        u = VF_MFMA_H(bl, as_h(vh[j]), u);
+        u = VF_MFMA_H(bl2, as_h(vh[j]), u);
         u = VF_MFMA_H(bh, as_h(vl[j]), u);
         u = VF_MFMA_H(bh, as_h(vh[j]), u);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) S[i][j][k] = fmaf(S[i][j][k], el, u[k] * sc[k]);
+        for (int k = 0; k < 4; ++k) S[i][j][k] = fmaf(S[i][j][k], el, u[k] * (sc[k] * back[j]));
       }
     }
   }
 
-  float *left = LOCAL ? mine : part.last && slot_to >= 0 ? p.ssm_out + ((int64_t)slot_to * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
   if (left && on) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
@@ -725,44 +826,49 @@ __global__ void __launch_bounds__(256, 2) k_ssm_chunks(const SsmArgs p) {
   }
   if (LOCAL) {
     if (on && lane == 0 && p0 == 0) p.seg_log[(int64_t)sx * p.H + h] = log_decay;
-    return;
+    continue;
   }
-  if (!part.last || slot_to < 0 || p.conv_later || p.W == 1) return;
+  if (!part.last || slot_to < 0 || p.conv_later || p.W == 1) continue;
   if (on)
     for (int k = lane; k < np; k += 64) conv_state<uint16_t>(p, sp, slot, slot_to, h * p.P + p0 + k);
   if (wg == g * per)
     for (int k = tid; k < 2 * p.N; k += nthr)
       conv_state<uint16_t>(p, sp, slot, slot_to, p.H * p.P + (k < p.N ? g * p.N + k : p.G * p.N + g * p.N + k - p.N));
+  }
 }
 
-// (byte offsets within a chunk are 32 bits wide)
-bool chunks_fit(const SsmArgs &p) { return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4 && p.ld_xbc < (1 << 25); }
+// (byte offsets within a chunk are 32 bits wide, and a launch takes less than 2^32 threads)
+bool chunks_fit(const SsmArgs &p) {
+  constexpr int64_t most = 1 << 24;
+  if ((int64_t)p.n_seq * p.H * ((p.P + PS - 1) / PS) > (1 << 30) || (int64_t)p.H * ((p.P + PS - 1) / PS) > (1 << 22)) return false;
+  return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4 && p.ld_xbc < most && p.ld_dt < most && p.ld_out < most && (!p.z || p.ld_z < most);
+}
 
-template <int NT, int PT>
+template <int NT>
 int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
-  const int jobs = p.H / p.G * ((p.P + 16 * PT - 1) / (16 * PT)), nw = jobs < 4 ? jobs : 4, per = (jobs + nw - 1) / nw;
+  const int jobs = p.H / p.G * ((p.P + PS - 1) / PS), nw = jobs < NW ? jobs : NW, per = (jobs + nw - 1) / nw;
   const int64_t each = (int64_t)p.n_seq * per * p.G;
-  // two workgroups for every compute unit; a segment costs its state's way to memory and back, about 256 tokens' time
-  split(c, p, longest, each, 512, Q, 256);
-  const size_t smem = chunk_shared<NT>() + nw * chunk_wave<PT>();
-  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  const int64_t blocks = each * p.nseg;
-  if (blocks > (int64_t)1 << 23) return VF_EINVAL;  // (the runtime's limit of work-items in a launch)
+  // workgroups for every compute unit; a segment costs its state's way to memory and back, about 256 tokens' time
+  split(c, p, longest, each, NT <= 4 ? 512 : 256, Q, 256);
+  const size_t smem = chunk_lds<NT>();
+  if (smem > 65536) {
+    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  }
+  // many short parts: a workgroup takes several, so that its weights are fetched once for them, but there are eight times as many
+  // workgroups as run at a time, for the sake of unequal parts
+  const int64_t wgs = (int64_t)per * p.G, parts = (int64_t)p.n_seq * p.nseg, most = 2048 / wgs > 1 ? 2048 / wgs : 1;
+  const unsigned blocks = (unsigned)((parts < most ? parts : most) * wgs);
   return run_parts(c, p, [&] {
-    if (p.local) k_ssm_chunks<NT, PT, true><<<(unsigned)blocks, 64 * nw, smem, c->stream>>>(p);
-    else k_ssm_chunks<NT, PT, false><<<(unsigned)blocks, 64 * nw, smem, c->stream>>>(p);
+    if (p.local) k_ssm_chunks<NT, true><<<blocks, 64 * nw, smem, c->stream>>>(p);
+    else k_ssm_chunks<NT, false><<<blocks, 64 * nw, smem, c->stream>>>(p);
     VF_HIP(c, hipGetLastError());
     return VF_OK;
   });
 }
 int chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
-  // 128 accumulators for the state at most
-  const bool narrow = p.P <= 32;
-  if (p.N <= 32) return narrow ? launch_chunks<2, 2>(c, p, longest) : launch_chunks<2, 4>(c, p, longest);
-  if (p.N <= 64) return narrow ? launch_chunks<4, 2>(c, p, longest) : launch_chunks<4, 4>(c, p, longest);
-  if (p.N <= 128) return narrow ? launch_chunks<8, 2>(c, p, longest) : launch_chunks<8, 4>(c, p, longest);
-  return launch_chunks<16, 2>(c, p, longest);
+  return p.N <= 32 ? launch_chunks<2>(c, p, longest) : p.N <= 64 ? launch_chunks<4>(c, p, longest)
+       : p.N <= 128 ? launch_chunks<8>(c, p, longest) : launch_chunks<16>(c, p, longest);
 }
 
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
