@@ -397,17 +397,19 @@ __device__ __forceinline__ void store4(const Rows &m, int t, uint32_t byte, cons
   __builtin_amdgcn_raw_buffer_store_b64(u, m.rsrc, (int)((uint32_t)(t - m.base) * m.ld2 + byte), 0, 0);
 }
 
-// Inputs of four channels for tokens t0 .. t0 + 7 and three before, byte `byte` of their rows
-__device__ __forceinline__ void fetch(const Rows &m, int t0, uint32_t byte, bool on, uint2 (&raw)[11]) {
+// Inputs of four channels for tokens t0 - 3 .. t0 - 4 + NR, byte `byte` of their rows
+template <int NR>
+__device__ __forceinline__ void fetch(const Rows &m, int t0, uint32_t byte, bool on, uint2 (&raw)[NR]) {
   const uint32_t at = on ? (uint32_t)(t0 - 3 - m.base) * m.ld2 + byte : 0x80000000u;  // (past the end of any chunk)
 #pragma unroll
-  for (int r = 0; r < 11; ++r) {
+  for (int r = 0; r < NR; ++r) {
     const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(m.rsrc, (int)(at + r * m.ld2), 0, 0);
     raw[r] = make_uint2(v[0], v[1]);
   }
 }
 // Rows -3, -2, -1 of channels c0 .. c0 + 3 from the convolution's state, [channel][W - 1]
-__device__ __forceinline__ void fetch_state(const SsmArgs &p, int slot, int c0, uint2 (&raw)[11]) {
+template <int NR>
+__device__ __forceinline__ void fetch_state(const SsmArgs &p, int slot, int c0, uint2 (&raw)[NR]) {
   if (slot == -1) return;
   const int w1 = p.W - 1;
   const uint16_t *st = reinterpret_cast<const uint16_t *>(p.conv_in) + ((int64_t)slot * p.C + c0) * w1 - (3 - w1);
@@ -417,34 +419,44 @@ __device__ __forceinline__ void fetch_state(const SsmArgs &p, int slot, int c0, 
     else if (r >= 3 - w1) raw[r] = make_uint2(st[r] | (uint32_t)st[w1 + r] << 16, st[2 * w1 + r] | (uint32_t)st[3 * w1 + r] << 16);
   }
 }
-// silu of the convolution for channel k of the four.  Weights in the LDS: four taps a channel (zeros before the first), and the biases.
+// silu of the convolution for channel k of the four, divided by -ln 2: with weights and bias times -log2(e) the sum s is the exponent
+// of silu's exponential, and s / (1 + 2^s) the result.  The constant is taken back where the results meet steps and decays.
+// Weights in the LDS: four taps a channel (zeros before the first), and the biases.
 // Tokens that are not there give silu(bias); their steps are zero and their outputs are not written.
-__device__ __forceinline__ void convolve(const uint2 (&raw)[11], int k, const float *w, const float *b, float (&v)[8]) {
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+template <int TB>
+__device__ __forceinline__ void convolve(const uint2 (&raw)[TB + 3], int k, const float *w, const float *b, float (&v)[TB]) {
   const f32x4 tap = *reinterpret_cast<const f32x4 *>(w + 4 * k);
   const float bias = b[k];
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
+  for (int t = 0; t < TB; ++t) {
     float s = bias;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t u = k < 2 ? raw[t + i].x : raw[t + i].y;
       s = fmaf(tap[i], __uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), s);
     }
-    v[t] = silu(s);
+    v[t] = s * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s));
   }
 }
-// max(a, |b|, |c|) in one instruction
-__device__ __forceinline__ float max_abs(float a, float b, float c) {
+// The largest magnitude, as bits, of TB numbers in each of 32 / TB neighbouring lanes (magnitudes compare as integers).
+__device__ __forceinline__ uint32_t max_abs(uint32_t a, float b, float c) {
   asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(a) : "v"(a), "v"(b), "v"(c));
   return a;
 }
-// the largest magnitude over the eight tokens of each of four neighbouring lanes
-__device__ __forceinline__ float top_of_32(const float (&v)[8]) {
-  float m = 0.0f;
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_lanes(uint32_t m) {
+  return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, CTRL, 0xf, 0xf, true));
+}
+template <int TB>
+__device__ __forceinline__ float top_of_32(const float (&v)[TB]) {
+  uint32_t m = 0;
 #pragma unroll
-  for (int t = 0; t < 8; t += 2) m = max_abs(m, v[t], v[t + 1]);
-  m = fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0xB1, 0xf, 0xf, true)));     // lanes 1 0 3 2
-  return fmaxf(m, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(m), 0x4E, 0xf, 0xf, true)));  // lanes 2 3 0 1
+  for (int t = 0; t < TB; t += 2) m = max_abs(m, v[t], v[t + 1]);
+  m = max_lanes<0xB1>(m);               // lanes 1 0 3 2
+  m = max_lanes<0x4E>(m);               // lanes 2 3 0 1
+  if (TB == 4) m = max_lanes<0x141>(m); // lanes 7 .. 0 of eight
+  return __uint_as_float(m);
 }
 // the value N lanes before in the same 16, zero where there is none; and the last of the 16 before, for the second and fourth 16
 template <int N>
@@ -474,16 +486,18 @@ __device__ __forceinline__ uint4 rest_of(const f32x4 &a, const f32x4 &b, const u
 
 // LDS: B and C by tokens, B by n in two parts and its scales; per wave x by p and its scales, weights of the convolution of all of
 // these channels; per wave the chunk's steps.
-constexpr int PT = 2, PS = 16 * PT, NW = 8;  // tiles and rows p of a wave, waves of a workgroup
+constexpr int ROWS = 256;  // rows p of a workgroup: PT tiles of 16 a wave
 template <int NT> constexpr size_t chunk_lds() {
   return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * bt_size(16 * NT)) +
-         sizeof(float) * (16 * NT + NW * PS * (XS + 1) + 6 * (32 * NT + NW * PS) + NW * 3 * Q);
+         sizeof(float) * (16 * NT + ROWS * (XS + 1) + 6 * (32 * NT + ROWS) + 8 * 3 * Q);
 }
 
-template <int NT, bool LOCAL>
-__global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
+template <int NT, int PT, bool LOCAL>
+__global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2;
+  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT, NW = ROWS / PS;
+  // Tokens of B and C that a thread takes at a time, so that there is one piece of x and one of B and C for a thread, or one of either
+  constexpr int TB = PT == 4 ? 4 : 8;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
   uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + bt_size(NP);
   float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));
@@ -507,15 +521,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
 
   // Channels of the convolution as the LDS has them: B, C (NP each, zeros behind N), x of the waves (PS each, zeros behind P): their
   // weights, and the channel of xbc, -1 where there is none.
-  if (p.N != NP || p.P % PS != 0 || nw != NW)
+  if (p.N != NP || p.P % PS != 0 || jobs % NW != 0)
     for (int e = tid; e < (int)(chunk_lds<NT>() / 4); e += nthr) reinterpret_cast<uint32_t *>(smem)[e] = 0;
   __syncthreads();
   auto weights = [&](int k, int c) {
     chans[k] = c;
     if (c < 0) return;
     if (p.W < 4) *reinterpret_cast<f32x4 *>(wl + 4 * k) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i = 0; i < p.W; ++i) wl[4 * k + 4 - p.W + i] = p.conv_w[(int64_t)c * p.W + i];
-    bl[k] = p.conv_b ? p.conv_b[c] : 0.0f;
+    for (int i = 0; i < p.W; ++i) wl[4 * k + 4 - p.W + i] = p.conv_w[(int64_t)c * p.W + i] * -LOG2E;
+    bl[k] = p.conv_b ? p.conv_b[c] * -LOG2E : 0.0f;
   };
   for (int k = tid; k < 2 * NP; k += nthr) {
     const int n = k < NP ? k : k - NP;
@@ -523,65 +537,71 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
   }
   if (lane < PS) weights(2 * NP + wave * PS + lane, on && lane < np ? h * p.P + p0 + lane : -1);
   __syncthreads();
-  // A thread's work per chunk: pieces of eight tokens of four channels, first those of B and C, then of x.  The inputs of its first
-  // piece are fetched a chunk ahead; there are more where few waves share B and C.
-  constexpr int NB = (LOCAL ? NP : 2 * NP);  // pieces of B and C: NB / 4 columns of four
-  const int pieces = NB + nw * PS;
-  auto place = [&](int item) { return item < NB ? 4 * (item >> 2) : 2 * NP + 4 * ((item - NB) >> 2); };
-  // (B and C cost nearly twice what x does: with a whole workgroup the waves of their SIMDs' other half get nothing)
-  int mine0 = tid;
-  if (nw == NW && NB == 128) mine0 = wave < 2 ? tid : wave < 4 ? tid : wave < 6 ? 1 << 20 : tid - 128;
-  const int chan = mine0 < pieces ? chans[place(mine0)] : -1;
-  auto put = [&](int item, const uint2 (&raw)[11]) {
-    const int k0 = place(item), tg = item & 3;
-    // (two channels at a time, one after the other: four would take too many registers)
-    if (item < NB) {
-      const int isC = k0 >= NP, n0 = isC ? k0 - NP : k0;
-      float back[4];
+  // A thread's work per chunk: pieces of four channels, TB tokens of B or C or eight tokens of x.
+  constexpr int NB = (LOCAL ? NP : 2 * NP) / 4 * (Q / TB);
+  const int NX = nw * PS;
+  auto put_bc = [&](int item, const uint2 (&raw)[TB + 3]) {
+    const int k0 = 4 * (item / (Q / TB)), tg = item % (Q / TB), isC = k0 >= NP, n0 = isC ? k0 - NP : k0;
+    float back[4];
+    // (two channels at a time, one pair after the other: all four would take too many registers)
 #pragma unroll
-      for (int k = 0; k < 4; k += 2) {
-        __builtin_amdgcn_sched_barrier(0);
-        float v[2][8];
-        convolve(raw, k, wl + 4 * k0, bl + k0, v[0]);
-        convolve(raw, k + 1, wl + 4 * k0, bl + k0, v[1]);
-        if (!LOCAL) {
-          uint16_t *to = (isC ? Cs : Bs) + 8 * tg * NS + n0 + k;
+    for (int k = 0; k < 4; k += 2) {
+      __builtin_amdgcn_sched_barrier(0);
+      float v[2][TB];
+      convolve<TB>(raw, k, wl + 4 * k0, bl + k0, v[0]);
+      convolve<TB>(raw, k + 1, wl + 4 * k0, bl + k0, v[1]);
+      if (!LOCAL) {
+        uint16_t *to = (isC ? Cs : Bs) + TB * tg * NS + n0 + k;
 #pragma unroll
-          for (int t = 0; t < 8; ++t) *reinterpret_cast<uint32_t *>(to + t * NS) = pack2(v[0][t], v[1][t]);
+        for (int t = 0; t < TB; ++t) *reinterpret_cast<uint32_t *>(to + t * NS) = pack2(v[0][t], v[1][t]);
+      }
+      if (isC) continue;
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const float f = scale_to_f16(top_of_32<TB>(v[o]));
+        back[k + o] = power_reciprocal(f);
+        uint32_t hi[TB / 2], lo[TB / 2];
+#pragma unroll
+        for (int t = 0; t < TB / 2; ++t) {
+          const float a = v[o][2 * t] * f, b = v[o][2 * t + 1] * f;
+          hi[t] = pack_h(a, b);
+          lo[t] = rest_h(a, b, hi[t]);
         }
-        if (isC) continue;
-#pragma unroll
-        for (int o = 0; o < 2; ++o) {
-          const float f = scale_to_f16(top_of_32(v[o]));
-          back[k + o] = power_reciprocal(f);
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const float a = v[o][2 * t] * f, b = v[o][2 * t + 1] * f;
-            hi[t] = pack_h(a, b);
-            lo[t] = rest_h(a, b, hi[t]);
-          }
-          *reinterpret_cast<uint4 *>(BtH + bt_row(n0) + (k + o) * (Q + 8) + 8 * tg) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4 *>(BtL + bt_row(n0) + (k + o) * (Q + 8) + 8 * tg) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        uint16_t *th = BtH + bt_row(n0) + (k + o) * (Q + 8) + TB * tg, *tl = th + bt_size(NP);
+        if constexpr (TB == 8) {
+          *reinterpret_cast<uint4 *>(th) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4 *>(tl) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        } else {
+          *reinterpret_cast<uint2 *>(th) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2 *>(tl) = make_uint2(lo[0], lo[1]);
         }
       }
-      if (!isC && tg == 0) *reinterpret_cast<f32x4 *>(bscale + n0) = f32x4{back[0], back[1], back[2], back[3]};
-    } else {
-      const int x0 = k0 - 2 * NP;
-      float top[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-        float v[8];
-        convolve(raw, k, wl + 4 * k0, bl + k0, v);
-        float *to = Xall + (x0 + k) * XS + 8 * tg;
-        *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4], v[5], v[6], v[7]};
-        top[k] = top_of_32(v);
-      }
-      if (tg == 0) *reinterpret_cast<f32x4 *>(xsall + x0) = f32x4{top[0], top[1], top[2], top[3]};
     }
+    if (!isC && tg == 0) *reinterpret_cast<f32x4 *>(bscale + n0) = f32x4{back[0], back[1], back[2], back[3]};
   };
+  auto put_x = [&](int item, const uint2 (&raw)[11]) {
+    const int x0 = 4 * (item >> 2), tg = item & 3;
+    float top[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+      float v[8];
+      convolve<8>(raw, k, wl + 4 * (2 * NP + x0), bl + 2 * NP + x0, v);
+      float *to = Xall + (x0 + k) * XS + 8 * tg;
+      *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4], v[5], v[6], v[7]};
+      top[k] = top_of_32<8>(v);
+    }
+    if (tg == 0) *reinterpret_cast<f32x4 *>(xsall + x0) = f32x4{top[0], top[1], top[2], top[3]};
+  };
+  // The piece whose inputs are fetched a chunk ahead.  PT = 4: a piece of x for every thread, those of B and C are asked for at the
+  // chunk's begin and taken behind x.  PT = 2: pieces of x from the last thread down, of B and C from the first one up.
+  const int xitem = PT == 4 ? tid : tid - (nthr - NX < 0 ? 0 : nthr - NX);
+  const bool is_x = xitem >= 0 && xitem < NX;
+  const int bitem = PT == 4 || !is_x ? tid : NB;  // (with more pieces than threads the rest is taken in turns)
+  const int chan = is_x ? chans[2 * NP + 4 * (xitem >> 2)] : PT == 2 && bitem < NB ? chans[4 * (bitem / (Q / TB))] : -1;
+  const int chan_bc = PT == 4 && bitem < NB ? chans[4 * (bitem / (Q / TB))] : -1, tgx = is_x ? xitem & 3 : bitem % (Q / TB);
+  const int more0 = PT == 4 ? tid + nthr : nthr - NX > 0 ? tid + nthr - NX : tid;  // first of the other pieces of B and C, and their distance
 
   // Inputs are fetched a chunk ahead, also from a part to the next one: the thread's first piece, and a wave's steps.
   struct Where { Span sp; Part part; bool live; };
@@ -599,7 +619,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
   // (one place that loads, without branches: the loads are to be under way while the chunk before is worked on)
   auto ahead = [&](const Where &w, int t0) {
     const int end = w.live ? (w.part.end - t0 < Q ? w.part.end : t0 + Q) : 0;
-    fetch(rows_of(p.xbc, w.sp.first, p.ld_xbc, t0 >= 3 ? t0 - 3 : 0, end), t0 + 8 * (mine0 & 3), 2 * chan, chan >= 0, raw);
+    fetch(rows_of(p.xbc, w.sp.first, p.ld_xbc, t0 >= 3 ? t0 - 3 : 0, end), t0 + 8 * tgx, 2 * chan, chan >= 0, raw);
     const Rows dm = rows_of(p.dt, w.sp.first, p.ld_dt, t0, end);
     dt_raw = __builtin_amdgcn_raw_buffer_load_b16(dm.rsrc, (int)((uint32_t)(lane & (Q - 1)) * dm.ld2 + 2 * h), 0, 0);
   };
@@ -642,24 +662,40 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
 
   for (int t0 = part.begin; t0 < part.end; t0 += Q) {
     const int end = part.end - t0 < Q ? part.end : t0 + Q;
+    uint2 raw_bc[TB + 3];
+    if constexpr (PT == 4) fetch(rows_in(t0), t0 + TB * (bitem % (Q / TB)), 2 * chan_bc, chan_bc >= 0, raw_bc);
     __syncthreads();  // (the arrays are still read for the chunk before)
     if (chan >= 0) {
-      if (t0 == 0 && (mine0 & 3) == 0) {
+      if (t0 == 0 && tgx == 0) {
         int c = chan;
         asm volatile("" : "+v"(c));  // (addresses of a path taken once are not to be kept in registers)
         fetch_state(p, slot, c, raw);
       }
-      put(mine0, raw);
+      if (is_x) {
+        put_x(xitem, raw);
+      } else {
+        if constexpr (PT == 2) put_bc(bitem, raw);
+      }
     }
-    int more = nw == NW && NB == 128 ? pieces : tid + nthr;
+    if constexpr (PT == 4) {
+      if (chan_bc >= 0) {
+        if (t0 == 0 && bitem % (Q / TB) == 0) {
+          int c = chan_bc;
+          asm volatile("" : "+v"(c));
+          fetch_state(p, slot, c, raw_bc);
+        }
+        put_bc(bitem, raw_bc);
+      }
+    }
+    int more = more0;
     asm volatile("" : "+v"(more));
-    for (int item = more; item < pieces; item += nthr) {
-      const int c = chans[place(item)];
+    for (int item = more; item < NB; item += nthr) {
+      const int c = chans[4 * (item / (Q / TB))];
       if (c < 0) continue;
-      uint2 now[11];
-      fetch(rows_in(t0), t0 + 8 * (item & 3), 2 * c, true, now);
-      if (t0 == 0 && (item & 3) == 0) fetch_state(p, slot, c, now);
-      put(item, now);
+      uint2 now[TB + 3];
+      fetch(rows_in(t0), t0 + TB * (item % (Q / TB)), 2 * c, true, now);
+      if (t0 == 0 && item % (Q / TB) == 0) fetch_state(p, slot, c, now);
+      put_bc(item, now);
     }
     // (behind the convolution, whose inputs are waited for together with whatever was asked for before)
     uint2 zr[2][PT];
@@ -682,10 +718,10 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
       c += lanes_before<8>(c);
       c += row_before(c);
       last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(c), Q - 1));
-      const float w = dt * __expf(last - c);
+      const float w = dt * __expf(last - c) * (LN2 * LN2);
       if (lane < Q) {
         cum[t] = c;
-        stp[t] = dt;
+        stp[t] = dt * -(LN2 * LN2 * LN2);  // (x, B and C are each to be multiplied by -ln 2)
         wgt[t] = w;
       }
       float m = w;
@@ -726,7 +762,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
 #pragma unroll
         for (int k = 0; k < PT; ++k) y[j][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       if (t0 > part.begin || first || lost) {  // (otherwise the state is zero)
-        const float e0 = __expf(ct0), e1 = __expf(ct1);
+        const float e0 = __expf(ct0) * -LN2, e1 = __expf(ct1) * -LN2;
 #pragma unroll
         for (int k = 0; k < KN; ++k) {
           const bf16x8 c0 = as_b(frag_acc(Cs + r * NS + 32 * k, q)), c1 = as_b(frag_acc(Cs + (16 + r) * NS + 32 * k, q));
@@ -749,8 +785,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
         // (the exponent of a later token is positive and may be large: chosen by comparison, not by a product with 0)
         const int at = 4 * q + i;
         const float d0 = __expf(at <= r ? ct0 - cs0[i] : 0.0f) * st0[i], d1 = __expf(at <= r ? ct1 - cs1[i] : 0.0f) * st1[i];
-        m00[i] = at <= r ? fmaf(G[0][i], d0, at == r ? D : 0.0f) : 0.0f;
-        m11[i] = at <= r ? fmaf(G[2][i], d1, at == r ? D : 0.0f) : 0.0f;
+        m00[i] = at <= r ? fmaf(G[0][i], d0, at == r ? D * -LN2 : 0.0f) : 0.0f;
+        m11[i] = at <= r ? fmaf(G[2][i], d1, at == r ? D * -LN2 : 0.0f) : 0.0f;
         m01[i] = G[1][i] * __expf(ct1 - cs0[i]) * st0[i];
       }
       const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -840,35 +876,39 @@ __global__ void __launch_bounds__(64 * NW, 2) k_ssm_chunks(const SsmArgs p) {
 // (byte offsets within a chunk are 32 bits wide, and a launch takes less than 2^32 threads)
 bool chunks_fit(const SsmArgs &p) {
   constexpr int64_t most = 1 << 24;
-  if ((int64_t)p.n_seq * p.H * ((p.P + PS - 1) / PS) > (1 << 30) || (int64_t)p.H * ((p.P + PS - 1) / PS) > (1 << 22)) return false;
+  if ((int64_t)p.H * ((p.P + 31) / 32) > (1 << 22)) return false;
   return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4 && p.ld_xbc < most && p.ld_dt < most && p.ld_out < most && (!p.z || p.ld_z < most);
 }
 
-template <int NT>
+template <int NT, int PT>
 int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
+  constexpr int PS = 16 * PT, NW = ROWS / PS;
   const int jobs = p.H / p.G * ((p.P + PS - 1) / PS), nw = jobs < NW ? jobs : NW, per = (jobs + nw - 1) / nw;
   const int64_t each = (int64_t)p.n_seq * per * p.G;
-  // workgroups for every compute unit; a segment costs its state's way to memory and back, about 256 tokens' time
-  split(c, p, longest, each, NT <= 4 ? 512 : 256, Q, 256);
+  const int64_t at_once = PT == 4 ? 512 : 256;  // workgroups that run at a time
+  // a segment costs its state's way to memory and back, about 256 tokens' time
+  split(c, p, longest, each, at_once, Q, 256);
   const size_t smem = chunk_lds<NT>();
   if (smem > 65536) {
-    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   }
   // many short parts: a workgroup takes several, so that its weights are fetched once for them, but there are eight times as many
   // workgroups as run at a time, for the sake of unequal parts
-  const int64_t wgs = (int64_t)per * p.G, parts = (int64_t)p.n_seq * p.nseg, most = 2048 / wgs > 1 ? 2048 / wgs : 1;
+  const int64_t wgs = (int64_t)per * p.G, parts = (int64_t)p.n_seq * p.nseg, most = 8 * at_once / wgs > 1 ? 8 * at_once / wgs : 1;
   const unsigned blocks = (unsigned)((parts < most ? parts : most) * wgs);
   return run_parts(c, p, [&] {
-    if (p.local) k_ssm_chunks<NT, true><<<blocks, 64 * nw, smem, c->stream>>>(p);
-    else k_ssm_chunks<NT, false><<<blocks, 64 * nw, smem, c->stream>>>(p);
+    if (p.local) k_ssm_chunks<NT, PT, true><<<blocks, 64 * nw, smem, c->stream>>>(p);
+    else k_ssm_chunks<NT, PT, false><<<blocks, 64 * nw, smem, c->stream>>>(p);
     VF_HIP(c, hipGetLastError());
     return VF_OK;
   });
 }
 int chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
-  return p.N <= 32 ? launch_chunks<2>(c, p, longest) : p.N <= 64 ? launch_chunks<4>(c, p, longest)
-       : p.N <= 128 ? launch_chunks<8>(c, p, longest) : launch_chunks<16>(c, p, longest);
+  // Four waves of 64 rows, two workgroups on a compute unit, where the state leaves registers for it; else eight waves of 32 rows.
+  if (p.P > 32 && p.N <= 64) return p.N <= 32 ? launch_chunks<2, 4>(c, p, longest) : launch_chunks<4, 4>(c, p, longest);
+  return p.N <= 32 ? launch_chunks<2, 2>(c, p, longest) : p.N <= 64 ? launch_chunks<4, 2>(c, p, longest)
+       : p.N <= 128 ? launch_chunks<8, 2>(c, p, longest) : launch_chunks<16, 2>(c, p, longest);
 }
 
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
