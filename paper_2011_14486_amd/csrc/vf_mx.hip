@@ -190,13 +190,217 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
   }
 }
 
+// Many rows: tiles of BM rows by BN columns in the LDS.
+//
+// A stage of the k loop is 128 bytes of every row of a (128 k in 8 bits, 256 in 4) and as many k of the weights.  Its bytes go from memory
+// straight to the LDS, one stage ahead (two where the LDS has room), in pieces of 16 bytes; where a piece lies is
+// chosen by which lane fetches it: piece c of row m at place c ^ (m % 8), so that the 16 rows that lanes read at a time meet all
+// banks.  Scales travel as bytes, each to a word of its own.  Eight waves, each 64 rows by BN / 2 columns (BM = 256) of
+// accumulators; the weights are the first operand, with the columns dealt to the operand's 16 rows in such an order that a
+// lane ends up with neighbouring columns: 4 (BN / 32) of one row.
+//
+// What bounds it: the matrix cores, and next to them the LDS, of which a stage reads (BM BN / (64 BN / 2)) times the tile.
+template <int AF> constexpr int stage_steps() { return AF == VF_E4M3 ? 1 : 2; }  // k-steps of 128
+template <int AF, int BM, int BN> constexpr int stage_bytes() {
+  return BM * 128 + BN * 64 * stage_steps<AF>() + (BM + BN) * 16 * stage_steps<AF>();
+}
+
+// 64 lanes fetch 16 bytes (or one byte, into a word) each from addresses of their own to consecutive places of the LDS from `to` on.
+// The compiler does not know of these loads: they are waited for by wait_loads.
+__device__ __forceinline__ void to_lds16(const uint8_t *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void to_lds1(const uint8_t *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(to), "v"(from) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+template <int AF, bool EXACT, int BM, int BN, int STAGES>
+__global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tiles_n, int tiles) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  constexpr int KS = stage_steps<AF>(), WB = 64 * KS, KB = 4 * KS;  // k-steps, bytes of a row of weights, blocks of a stage
+  constexpr int WM = BM / 64, WN = 8 / WM, CN = BN / WN, NT = CN / 16;  // waves along rows and columns, a wave's columns and their tiles
+  constexpr int SB = stage_bytes<AF, BM, BN>();
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+  // Workgroups are dealt to the eight dies in turn: each die gets neighbouring tiles, in blocks of eight rows of tiles that pass over
+  // the columns, so that its cache keeps what they share.
+  int id = blockIdx.x;
+  const int chunk8 = tiles / 8;
+  if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
+  const int tiles_m = tiles / tiles_n, band = id / (8 * tiles_n), in_band = id - band * 8 * tiles_n;
+  const int high = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8;
+  const int64_t m0 = (int64_t)(8 * band + in_band % high) * BM;
+  const int n0 = in_band / high * BN;
+  const int steps = (p.kb + KB - 1) / KB;  // stages
+
+  // Pieces that this thread fetches in every stage: their sources at block 0 of the row, and their block within the stage
+  constexpr int PA = BM * 8 / 512, PW = BN * (WB / 16) / 512, PS = (BM + BN) * KB / 512;
+  const uint8_t *src_a[PA], *src_w[PW], *src_s[PS];
+  int blk_a[PA], blk_w[PW], blk_s[PS];
+#pragma unroll
+  for (int i = 0; i < PA; ++i) {
+    const int e = i * 512 + tid, row = e >> 3, c = (e & 7) ^ (row & 7);
+    const int64_t m = m0 + row < p.M ? m0 + row : p.M - 1;
+    src_a[i] = p.a + m * p.kb * mx<AF>::bytes32 + (AF == VF_E4M3 ? 16 * (c & 1) : 0);
+    blk_a[i] = AF == VF_E4M3 ? c >> 1 : c;
+  }
+#pragma unroll
+  for (int i = 0; i < PW; ++i) {
+    // rows of the LDS are the operand's rows: row 16 j + x of a wave's CN is its column 4 NT (x / 4) + 4 j + x % 4
+    const int e = i * 512 + tid, row = e / (WB / 16), x = row & 15, j = (row % CN) >> 4;
+    const int c = KS == 1 ? (e & 3) ^ ((row >> 2) & 3) : (e & 7) ^ (row & 7);
+    const int col = n0 + row / CN * CN + 4 * NT * (x >> 2) + 4 * j + (x & 3);
+    src_w[i] = p.w + (int64_t)(col < p.N ? col : p.N - 1) * p.kb * 16;
+    blk_w[i] = c;
+  }
+#pragma unroll
+  for (int i = 0; i < PS; ++i) {
+    const int e = i * 512 + tid, row = e / KB;
+    blk_s[i] = e % KB;
+    if (row < BM) {
+      const int64_t m = m0 + row < p.M ? m0 + row : p.M - 1;
+      src_s[i] = p.as + m * p.kb;
+    } else {
+      const int x = (row - BM) & 15, j = ((row - BM) % CN) >> 4;
+      const int col = n0 + (row - BM) / CN * CN + 4 * NT * (x >> 2) + 4 * j + (x & 3);
+      src_s[i] = p.ws + (int64_t)(col < p.N ? col : p.N - 1) * p.kb;
+    }
+  }
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+  const uint32_t wave_at = __builtin_amdgcn_readfirstlane(wave);
+  // (blocks behind the row's end: the row's last block, which is there; its k of a are then cleared)
+  auto fetch = [&](int st) {
+    const uint32_t at = base + (uint32_t)(st % STAGES) * SB;
+    const int b0 = st * KB;
+#pragma unroll
+    for (int i = 0; i < PA; ++i) {
+      const int b = b0 + blk_a[i];
+      to_lds16(src_a[i] + (int64_t)(b < p.kb ? b : p.kb - 1) * mx<AF>::bytes32, at + (i * 512 + wave_at * 64) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < PW; ++i) {
+      const int b = b0 + blk_w[i];
+      to_lds16(src_w[i] + (int64_t)(b < p.kb ? b : p.kb - 1) * 16, at + BM * 128 + (i * 512 + wave_at * 64) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < PS; ++i) {
+      const int b = b0 + blk_s[i];
+      to_lds1(src_s[i] + (b < p.kb ? b : p.kb - 1), at + BM * 128 + BN * WB + (i * 512 + wave_at * 64) * 4);
+    }
+  };
+  constexpr int LOADS = PA + PW + PS;
+
+  f32x4 acc[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int wm = wave % WM, wn = wave / WM;
+
+#pragma unroll
+  for (int st = 0; st < STAGES - 1; ++st)
+    if (st < steps) fetch(st);
+  for (int st = 0; st < steps; ++st) {
+    // this stage is there; the newest one may still be under way
+    if (STAGES > 2 && st + 1 < steps) wait_loads<LOADS>();
+    else wait_loads<0>();
+    __syncthreads();  // and everybody is done with the stage whose place the next fetch takes
+    uint8_t *const at = lds + (st % STAGES) * SB;
+    if (st == steps - 1 && p.kb % KB != 0) {
+      // the last blocks of a that are not there
+      constexpr int per = AF == VF_E4M3 ? 2 : 1;
+      const int have = (p.kb % KB) * per;
+      for (int e = tid; e < BM * (8 - have); e += 512) {
+        const int row = e / (8 - have), c = have + e % (8 - have);
+        *reinterpret_cast<uint4 *>(at + row * 128 + 16 * (c ^ (row & 7))) = make_uint4(0, 0, 0, 0);
+      }
+      __syncthreads();
+    }
+    if (st + STAGES - 1 < steps) fetch(st + STAGES - 1);
+    const uint32_t *sc = reinterpret_cast<const uint32_t *>(at + BM * 128 + BN * WB);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      i32x8 fa[4];
+      int sa[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = wm * 64 + 16 * i + r;
+        const uint8_t *q = at + row * 128;
+        if constexpr (AF == VF_E4M3) {
+          // 16 k at 16 g and 16 at 64 + 16 g
+          const uint4 u = *reinterpret_cast<const uint4 *>(q + 16 * (g ^ (row & 7))), v = *reinterpret_cast<const uint4 *>(q + 16 * ((4 + g) ^ (row & 7)));
+          fa[i] = i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, (int)v.x, (int)v.y, (int)v.z, (int)v.w};
+        } else {
+          const uint4 u = *reinterpret_cast<const uint4 *>(q + 16 * ((4 * ks + g) ^ (row & 7)));
+          fa[i] = i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
+        }
+        sa[i] = (int)sc[row * KB + 4 * ks + g];
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int row = wn * CN + 16 * j + r;
+        const int place = KS == 1 ? g ^ ((row >> 2) & 3) : (4 * ks + g) ^ (row & 7);
+        const uint4 u = *reinterpret_cast<const uint4 *>(at + BM * 128 + row * WB + 16 * place);
+        const i32x8 fw = {(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
+        const int sw = (int)sc[(BM + row) * KB + 4 * ks + g];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] = mfma128<AF, EXACT>(fw, fa[i], acc[j][i], sw, sa[i]);
+      }
+    }
+  }
+  // a lane has columns n .. n + 4 NT - 1 of rows r, 16 + r, 32 + r, 48 + r
+  const int n = n0 + wn * CN + 4 * NT * g;
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[j][i]));
+#pragma unroll
+  for (int j = 0; j < NT; j += 2) {
+    float b[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) b[k] = p.bias && n + 4 * j + k < p.N ? p.bias[n + 4 * j + k] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t m = m0 + wm * 64 + 16 * i + r;
+      if (m >= p.M || n + 4 * j >= p.N) continue;
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = acc[j + (k >> 2)][i][k & 3] + b[k];
+      if (p.out_bf16) store_upto8(reinterpret_cast<uint16_t *>(p.out) + m * p.ld_out + n + 4 * j, p.N - n - 4 * j, y);
+      else store_upto8(reinterpret_cast<float *>(p.out) + m * p.ld_out + n + 4 * j, p.N - n - 4 * j, y);
+    }
+  }
+}
+
 inline int blocks_for(int64_t threads) {
   const int64_t g = (threads + 255) / 256;
   return (int)(g < (1 << 20) ? g : (1 << 20));
 }
 
+template <int AF, bool EXACT, int BM, int BN, int STAGES>
+int launch_tile(vf_ctx *c, const MatmulArgs &p) {
+  constexpr int smem = STAGES * stage_bytes<AF, BM, BN>();
+  const int tiles_n = (p.N + BN - 1) / BN;
+  // (less than 2^22 workgroups in a launch; the rows are taken in several)
+  const int64_t most = ((int64_t)1 << 22) / tiles_n, per = (most > 1 ? most : 1) * BM;
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_mx_tile<AF, EXACT, BM, BN, STAGES>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
+  for (int64_t m = 0; m < p.M; m += per) {
+    MatmulArgs q = p;
+    q.a += m * p.kb * mx<AF>::bytes32;
+    q.as += m * p.kb;
+    q.M = p.M - m < per ? p.M - m : per;
+    q.out = static_cast<char *>(p.out) + m * p.ld_out * (p.out_bf16 ? 2 : 4);
+    const int tiles = (int)((q.M + BM - 1) / BM) * tiles_n;
+    k_mx_tile<AF, EXACT, BM, BN, STAGES><<<tiles, 512, smem, c->stream>>>(q, tiles_n, tiles);
+    VF_HIP(c, hipGetLastError());
+  }
+  return VF_OK;
+}
+
 template <int AF, bool EXACT>
 int matmul(vf_ctx *c, const MatmulArgs &p) {
+  const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256);
+  if (p.M > 64 && big >= 64) return launch_tile<AF, EXACT, 256, 256, AF == VF_E4M3 ? 2 : 2>(c, p);
   const int nb = (p.N + 15) / 16;
   const int MT = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
   // rows beyond the grid's second dimension are taken in further launches

@@ -234,7 +234,14 @@ def test_product(vf, ctx, M, N, K, a_fmt):
     assert bool((big[:, :3] == 5).all()) and bool((big[:, 3 + N:] == 5).all())
 
 
-@pytest.mark.parametrize("M,N,K", [(4, 64, 384), (300, 512, 1056), (1500, 700, 260)])
+@pytest.mark.parametrize("M,N,K", [(2100, 2100, 160), (2048, 2048, 256), (2000, 2049, 993), (16500, 255, 96), (1800, 2310, 33)])
+@pytest.mark.parametrize("a_fmt", [2, 3])
+def test_product_in_tiles(vf, ctx, M, N, K, a_fmt):
+    """Sizes that are cut into large tiles: edges in every direction, ends of k inside a stage."""
+    test_product(vf, ctx, M, N, K, a_fmt)
+
+
+@pytest.mark.parametrize("M,N,K", [(4, 64, 384), (300, 512, 1056), (1500, 700, 260), (2300, 2000, 416)])
 @pytest.mark.parametrize("a_fmt", [2, 3])
 def test_product_of_whole_numbers_is_exact(vf, ctx, M, N, K, a_fmt):
     """Codes of small whole numbers and scales of one: every partial sum is exact, so any order gives the same."""
