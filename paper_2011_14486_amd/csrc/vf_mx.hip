@@ -190,20 +190,21 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
   }
 }
 
-// Many rows: tiles of BM rows by BN columns in the LDS.
+// Many rows: tiles of 64 MI rows by 256 columns in the LDS, eight waves of 16 MI rows by 128 columns of accumulators.
 //
-// A stage of the k loop is 128 bytes of every row of a (128 k in 8 bits, 256 in 4) and as many k of the weights.  Its bytes go from memory
-// straight to the LDS, one stage ahead (two where the LDS has room), in pieces of 16 bytes; where a piece lies is
-// chosen by which lane fetches it: piece c of row m at place c ^ (m % 8), so that the 16 rows that lanes read at a time meet all
-// banks.  Scales travel as bytes, each to a word of its own.  Eight waves, each 64 rows by BN / 2 columns (BM = 256) of
-// accumulators; the weights are the first operand, with the columns dealt to the operand's 16 rows in such an order that a
-// lane ends up with neighbouring columns: 4 (BN / 32) of one row.
+// A stage of the k loop is 128 k.  Its bytes go from memory straight to the LDS, in pieces of 16 bytes; where a piece lies is
+// chosen by which lane fetches it: piece c of row m at place c ^ (m % 8) of eight, or c ^ (m / 4 % 4) of four, so that the 16 rows that
+// lanes read at a time meet all banks.  The weights are the first operand, with the columns dealt to the operand's 16
+// rows in such an order that a lane ends up with 32 neighbouring columns of a row of the output.
 //
-// What bounds it: the matrix cores, and next to them the LDS, of which a stage reads (BM BN / (64 BN / 2)) times the tile.
-template <int AF> constexpr int stage_steps() { return AF == VF_E4M3 ? 1 : 2; }  // k-steps of 128
-template <int AF, int BM, int BN> constexpr int stage_bytes() {
-  return BM * 128 + BN * 64 * stage_steps<AF>() + (BM + BN) * 16 * stage_steps<AF>();
-}
+// The weights' operands are read two tiles ahead, across the end of a stage too.  The only barrier is in a stage's middle: behind it
+// the next stage's bytes are there for everybody, and nobody reads the stage before any more, whose place the
+// newest fetch takes.  Of the two waves of a SIMD one has priority, so that they do not reach the reads of a's operands, at a
+// stage's begin, together.
+template <int AF> constexpr int a_bytes() { return AF == VF_E4M3 ? 128 : 64; }   // of a row, in a stage
+template <int AF> constexpr int stages() { return AF == VF_E4M3 ? 3 : 4; }       // that the LDS holds
+// (S4: scales four to a word; else each in a word of its own)
+template <int AF, int MI, bool S4> constexpr int stage_bytes() { return 64 * MI * a_bytes<AF>() + 256 * 64 + (64 * MI + 256) * (S4 ? 4 : 16); }
 
 // 64 lanes fetch 16 bytes (or one byte, into a word) each from addresses of their own to consecutive places of the LDS from `to` on.
 // The compiler does not know of these loads: they are waited for by wait_loads.
@@ -213,155 +214,178 @@ __device__ __forceinline__ void to_lds16(const uint8_t *from, uint32_t to) {
 __device__ __forceinline__ void to_lds1(const uint8_t *from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(to), "v"(from) : "memory");
 }
+__device__ __forceinline__ void to_lds4(const uint8_t *from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+}
+// (accesses of the LDS are not moved across it)
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-template <int AF, bool EXACT, int BM, int BN, int STAGES>
+template <int AF, bool EXACT, int MI, bool S4>
 __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tiles_n, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
-  constexpr int KS = stage_steps<AF>(), WB = 64 * KS, KB = 4 * KS;  // k-steps, bytes of a row of weights, blocks of a stage
-  constexpr int WM = BM / 64, WN = 8 / WM, CN = BN / WN, NT = CN / 16;  // waves along rows and columns, a wave's columns and their tiles
-  constexpr int SB = stage_bytes<AF, BM, BN>();
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
+  constexpr int BM = 64 * MI, AB = a_bytes<AF>(), NT = 8, NST = stages<AF>(), SB = stage_bytes<AF, MI, S4>();
+  constexpr int WAT = BM * AB, SAT = WAT + 256 * 64;  // the weights and the scales in a stage
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4, wm = wave & 3, wn = wave >> 2;
   // Workgroups are dealt to the eight dies in turn: each die gets neighbouring tiles, in blocks of eight rows of tiles that pass over
   // the columns, so that its cache keeps what they share.
   int id = blockIdx.x;
   const int chunk8 = tiles / 8;
   if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
   const int tiles_m = tiles / tiles_n, band = id / (8 * tiles_n), in_band = id - band * 8 * tiles_n;
-  const int high = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8;
-  const int64_t m0 = (int64_t)(8 * band + in_band % high) * BM;
-  const int n0 = in_band / high * BN;
-  const int steps = (p.kb + KB - 1) / KB;  // stages
+  const int high = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8, mt = 8 * band + in_band % high;
+  const int64_t m0 = (int64_t)mt * BM;
+  const int n0 = in_band / high * 256;
+  const int steps = (p.kb + 3) >> 2;
 
   // Pieces that this thread fetches in every stage: their sources at block 0 of the row, and their block within the stage
-  constexpr int PA = BM * 8 / 512, PW = BN * (WB / 16) / 512, PS = (BM + BN) * KB / 512;
+  constexpr int PA = BM * (AB / 16) / 512, PW = 2, PS = ((BM + 256) * (S4 ? 1 : 4) + 511) / 512;
   const uint8_t *src_a[PA], *src_w[PW], *src_s[PS];
   int blk_a[PA], blk_w[PW], blk_s[PS];
+  auto row_a = [&](int row) { return m0 + row < p.M ? m0 + row : p.M - 1; };
+  // row 16 j + x of a wave's 128 rows of weights is its column 32 (x / 4) + 4 j + x % 4
+  auto col_w = [&](int row) {
+    const int col = n0 + (row & 128) + 32 * ((row & 15) >> 2) + 4 * ((row & 127) >> 4) + (row & 3);
+    return col < p.N ? col : p.N - 1;
+  };
 #pragma unroll
   for (int i = 0; i < PA; ++i) {
-    const int e = i * 512 + tid, row = e >> 3, c = (e & 7) ^ (row & 7);
-    const int64_t m = m0 + row < p.M ? m0 + row : p.M - 1;
-    src_a[i] = p.a + m * p.kb * mx<AF>::bytes32 + (AF == VF_E4M3 ? 16 * (c & 1) : 0);
+    const int e = i * 512 + tid, row = e / (AB / 16), c = AB == 128 ? (e & 7) ^ (row & 7) : (e & 3) ^ ((row >> 2) & 3);
+    src_a[i] = p.a + row_a(row) * p.kb * mx<AF>::bytes32 + (AF == VF_E4M3 ? 16 * (c & 1) : 0);
     blk_a[i] = AF == VF_E4M3 ? c >> 1 : c;
   }
 #pragma unroll
   for (int i = 0; i < PW; ++i) {
-    // rows of the LDS are the operand's rows: row 16 j + x of a wave's CN is its column 4 NT (x / 4) + 4 j + x % 4
-    const int e = i * 512 + tid, row = e / (WB / 16), x = row & 15, j = (row % CN) >> 4;
-    const int c = KS == 1 ? (e & 3) ^ ((row >> 2) & 3) : (e & 7) ^ (row & 7);
-    const int col = n0 + row / CN * CN + 4 * NT * (x >> 2) + 4 * j + (x & 3);
-    src_w[i] = p.w + (int64_t)(col < p.N ? col : p.N - 1) * p.kb * 16;
-    blk_w[i] = c;
+    const int e = i * 512 + tid, row = e >> 2;
+    src_w[i] = p.w + (int64_t)col_w(row) * p.kb * 16;
+    blk_w[i] = (e & 3) ^ ((row >> 2) & 3);
   }
 #pragma unroll
   for (int i = 0; i < PS; ++i) {
-    const int e = i * 512 + tid, row = e / KB;
-    blk_s[i] = e % KB;
-    if (row < BM) {
-      const int64_t m = m0 + row < p.M ? m0 + row : p.M - 1;
-      src_s[i] = p.as + m * p.kb;
-    } else {
-      const int x = (row - BM) & 15, j = ((row - BM) % CN) >> 4;
-      const int col = n0 + (row - BM) / CN * CN + 4 * NT * (x >> 2) + 4 * j + (x & 3);
-      src_s[i] = p.ws + (int64_t)(col < p.N ? col : p.N - 1) * p.kb;
-    }
+    const int e = i * 512 + tid, row = S4 ? e : e >> 2;
+    blk_s[i] = S4 ? 0 : e & 3;
+    src_s[i] = row < BM ? p.as + row_a(row) * p.kb : p.ws + (int64_t)col_w(row - BM) * p.kb;
   }
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
   const uint32_t wave_at = __builtin_amdgcn_readfirstlane(wave);
   // (blocks behind the row's end: the row's last block, which is there; its k of a are then cleared)
   auto fetch = [&](int st) {
-    const uint32_t at = base + (uint32_t)(st % STAGES) * SB;
-    const int b0 = st * KB;
+    const uint32_t at = base + (uint32_t)(st % NST) * SB;
+    const int b0 = 4 * (st < steps ? st : steps - 1);
+    const bool whole = b0 + 4 <= p.kb;
+    auto block = [&](int b) { return whole || b0 + b < p.kb ? b0 + b : p.kb - 1; };
 #pragma unroll
-    for (int i = 0; i < PA; ++i) {
-      const int b = b0 + blk_a[i];
-      to_lds16(src_a[i] + (int64_t)(b < p.kb ? b : p.kb - 1) * mx<AF>::bytes32, at + (i * 512 + wave_at * 64) * 16);
-    }
+    for (int i = 0; i < PA; ++i) to_lds16(src_a[i] + (int64_t)block(blk_a[i]) * mx<AF>::bytes32, at + (i * 512 + wave_at * 64) * 16);
 #pragma unroll
-    for (int i = 0; i < PW; ++i) {
-      const int b = b0 + blk_w[i];
-      to_lds16(src_w[i] + (int64_t)(b < p.kb ? b : p.kb - 1) * 16, at + BM * 128 + (i * 512 + wave_at * 64) * 16);
-    }
+    for (int i = 0; i < PW; ++i) to_lds16(src_w[i] + (int64_t)block(blk_w[i]) * 16, at + WAT + (i * 512 + wave_at * 64) * 16);
 #pragma unroll
     for (int i = 0; i < PS; ++i) {
-      const int b = b0 + blk_s[i];
-      to_lds1(src_s[i] + (b < p.kb ? b : p.kb - 1), at + BM * 128 + BN * WB + (i * 512 + wave_at * 64) * 4);
+      const uint32_t to = at + SAT + (i * 512 + wave_at * 64) * 4;
+      if (S4) to_lds4(src_s[i] + b0, to);  // (rows of scales are whole words then)
+      else to_lds1(src_s[i] + block(blk_s[i]), to);
     }
   };
   constexpr int LOADS = PA + PW + PS;
 
-  f32x4 acc[NT][4];
+  f32x4 acc[NT][MI];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int wm = wave % WM, wn = wave / WM;
+    for (int i = 0; i < MI; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+  uint4 ar[MI][AB / 64], wq[4];
+  int as[MI], ws[4];
+  // places of this lane's pieces in a stage: of row 16 i + r they lie a constant further for every i
+  constexpr int SW = S4 ? 4 : 16;  // a row's scales
+  const int sw_a = AB == 128 ? r & 7 : (r >> 2) & 3;
+  const int la0 = (wm * 16 * MI + r) * AB + 16 * (g ^ sw_a), la1 = (wm * 16 * MI + r) * AB + 16 * ((4 + g) ^ sw_a);
+  const int lw = WAT + (wn * 128 + r) * 64 + 16 * (g ^ ((r >> 2) & 3));
+  const int lsa = SAT + (wm * 16 * MI + r) * SW + g * (SW / 4), lsw = SAT + (BM + wn * 128 + r) * SW + g * (SW / 4);
+  auto read_a = [&](int st) {
+    // (16 k at 16 g and, of 8-bit rows, 16 at 64 + 16 g)
+    const uint8_t *at = lds + (st % NST) * SB;
 #pragma unroll
-  for (int st = 0; st < STAGES - 1; ++st)
-    if (st < steps) fetch(st);
-  for (int st = 0; st < steps; ++st) {
-    // this stage is there; the newest one may still be under way
-    if (STAGES > 2 && st + 1 < steps) wait_loads<LOADS>();
-    else wait_loads<0>();
-    __syncthreads();  // and everybody is done with the stage whose place the next fetch takes
-    uint8_t *const at = lds + (st % STAGES) * SB;
-    if (st == steps - 1 && p.kb % KB != 0) {
-      // the last blocks of a that are not there
-      constexpr int per = AF == VF_E4M3 ? 2 : 1;
-      const int have = (p.kb % KB) * per;
-      for (int e = tid; e < BM * (8 - have); e += 512) {
-        const int row = e / (8 - have), c = have + e % (8 - have);
-        *reinterpret_cast<uint4 *>(at + row * 128 + 16 * (c ^ (row & 7))) = make_uint4(0, 0, 0, 0);
-      }
-      __syncthreads();
+    for (int i = 0; i < MI; ++i) {
+      ar[i][0] = *reinterpret_cast<const uint4 *>(at + la0 + i * 16 * AB);
+      if (AF == VF_E4M3) ar[i][AB / 64 - 1] = *reinterpret_cast<const uint4 *>(at + la1 + i * 16 * AB);
+      as[i] = at[lsa + i * 16 * SW];
     }
-    if (st + STAGES - 1 < steps) fetch(st + STAGES - 1);
-    const uint32_t *sc = reinterpret_cast<const uint32_t *>(at + BM * 128 + BN * WB);
+  };
+  auto read_w = [&](int st, int j) {
+    const uint8_t *at = lds + (st % NST) * SB;
+    wq[j & 3] = *reinterpret_cast<const uint4 *>(at + lw + j * 16 * 64);
+    ws[j & 3] = at[lsw + j * 16 * SW];
+  };
+  auto products = [&](int j) {
+    __builtin_amdgcn_sched_barrier(0);
+    const uint4 q = wq[j & 3];
+    const i32x8 fw = {(int)q.x, (int)q.y, (int)q.z, (int)q.w, 0, 0, 0, 0};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      i32x8 fa[4];
-      int sa[4];
+    for (int i = 0; i < MI; ++i) {
+      const uint4 u = ar[i][0], v = ar[i][AB / 64 - 1];
+      const i32x8 fa = AF == VF_E4M3 ? i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, (int)v.x, (int)v.y, (int)v.z, (int)v.w}
+                                     : i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
+      acc[j][i] = mfma128<AF, EXACT>(fw, fa, acc[j][i], ws[j & 3], as[i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = wm * 64 + 16 * i + r;
-        const uint8_t *q = at + row * 128;
-        if constexpr (AF == VF_E4M3) {
-          // 16 k at 16 g and 16 at 64 + 16 g
-          const uint4 u = *reinterpret_cast<const uint4 *>(q + 16 * (g ^ (row & 7))), v = *reinterpret_cast<const uint4 *>(q + 16 * ((4 + g) ^ (row & 7)));
-          fa[i] = i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, (int)v.x, (int)v.y, (int)v.z, (int)v.w};
-        } else {
-          const uint4 u = *reinterpret_cast<const uint4 *>(q + 16 * ((4 * ks + g) ^ (row & 7)));
-          fa[i] = i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
-        }
-        sa[i] = (int)sc[row * KB + 4 * ks + g];
+  for (int st = 0; st < NST - 1; ++st) fetch(st);
+  wait_loads<0>();
+  meet();
+  if (wave < 4) __builtin_amdgcn_s_setprio(1);
+  read_w(0, 0);
+  read_w(0, 1);
+  // (no branches in this loop: the compiler would move the products past them, behind all reads.  Stages behind the last
+  // one are the last one's bytes again, in places that nobody reads.)
+  for (int st = 0; st < steps - 1; ++st) {
+    read_a(st);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      if (j == NT / 2) {
+        wait_loads<NST == 3 ? 0 : LOADS>();  // (of four stages the newest may still be under way)
+        meet();
+        fetch(st + NST - 1);
       }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int row = wn * CN + 16 * j + r;
-        const int place = KS == 1 ? g ^ ((row >> 2) & 3) : (4 * ks + g) ^ (row & 7);
-        const uint4 u = *reinterpret_cast<const uint4 *>(at + BM * 128 + row * WB + 16 * place);
-        const i32x8 fw = {(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0};
-        const int sw = (int)sc[(BM + row) * KB + 4 * ks + g];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[j][i] = mfma128<AF, EXACT>(fw, fa[i], acc[j][i], sw, sa[i]);
-      }
+      if (j + 2 < NT) read_w(st, j + 2);
+      else read_w(st + 1, j + 2 - NT);
+      products(j);
     }
   }
-  // a lane has columns n .. n + 4 NT - 1 of rows r, 16 + r, 32 + r, 48 + r
-  const int n = n0 + wn * CN + 4 * NT * g;
+  read_a(steps - 1);
+  if (p.kb % 4 != 0) {  // k behind the row's end
+    const int b0 = 4 * (steps - 1);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      if (b0 + (AF == VF_E4M3 ? g >> 1 : g) >= p.kb) ar[i][0] = make_uint4(0, 0, 0, 0);
+      if (AF == VF_E4M3 && b0 + 2 + (g >> 1) >= p.kb) ar[i][AB / 64 - 1] = make_uint4(0, 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    if (j + 2 < NT) read_w(steps - 1, j + 2);
+    products(j);
+  }
+  __builtin_amdgcn_s_setprio(0);
+  wait_loads<0>();
+  // a lane has columns n .. n + 31 of rows r, 16 + r, ...
+  const int n = n0 + wn * 128 + 32 * g;
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[j][i]));
+    for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(acc[j][i]));
 #pragma unroll
   for (int j = 0; j < NT; j += 2) {
     float b[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) b[k] = p.bias && n + 4 * j + k < p.N ? p.bias[n + 4 * j + k] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t m = m0 + wm * 64 + 16 * i + r;
+    for (int i = 0; i < MI; ++i) {
+      const int64_t m = m0 + wm * 16 * MI + 16 * i + r;
       if (m >= p.M || n + 4 * j >= p.N) continue;
       float y[8];
 #pragma unroll
@@ -377,13 +401,13 @@ inline int blocks_for(int64_t threads) {
   return (int)(g < (1 << 20) ? g : (1 << 20));
 }
 
-template <int AF, bool EXACT, int BM, int BN, int STAGES>
+template <int AF, bool EXACT, int MI, bool S4>
 int launch_tile(vf_ctx *c, const MatmulArgs &p) {
-  constexpr int smem = STAGES * stage_bytes<AF, BM, BN>();
-  const int tiles_n = (p.N + BN - 1) / BN;
+  constexpr int smem = stages<AF>() * stage_bytes<AF, MI, S4>(), BM = 64 * MI;
+  const int tiles_n = (p.N + 255) / 256;
   // (less than 2^22 workgroups in a launch; the rows are taken in several)
   const int64_t most = ((int64_t)1 << 22) / tiles_n, per = (most > 1 ? most : 1) * BM;
-  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_mx_tile<AF, EXACT, BM, BN, STAGES>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_mx_tile<AF, EXACT, MI, S4>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
   for (int64_t m = 0; m < p.M; m += per) {
     MatmulArgs q = p;
     q.a += m * p.kb * mx<AF>::bytes32;
@@ -391,16 +415,22 @@ int launch_tile(vf_ctx *c, const MatmulArgs &p) {
     q.M = p.M - m < per ? p.M - m : per;
     q.out = static_cast<char *>(p.out) + m * p.ld_out * (p.out_bf16 ? 2 : 4);
     const int tiles = (int)((q.M + BM - 1) / BM) * tiles_n;
-    k_mx_tile<AF, EXACT, BM, BN, STAGES><<<tiles, 512, smem, c->stream>>>(q, tiles_n, tiles);
+    k_mx_tile<AF, EXACT, MI, S4><<<tiles, 512, smem, c->stream>>>(q, tiles_n, tiles);
     VF_HIP(c, hipGetLastError());
   }
   return VF_OK;
 }
 
+bool aligned4(const void *p) { return (uintptr_t)p % 4 == 0; }
+
 template <int AF, bool EXACT>
 int matmul(vf_ctx *c, const MatmulArgs &p) {
   const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256);
-  if (p.M > 64 && big >= 64) return launch_tile<AF, EXACT, 256, 256, AF == VF_E4M3 ? 2 : 2>(c, p);
+  if (p.M > 64 && big >= 64) {
+    // (rows of scales that begin at whole words travel four at a time)
+    if (p.kb % 4 == 0 && aligned4(p.as) && aligned4(p.ws)) return launch_tile<AF, EXACT, 4, true>(c, p);
+    return launch_tile<AF, EXACT, 2, false>(c, p);
+  }
   const int nb = (p.N + 15) / 16;
   const int MT = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
   // rows beyond the grid's second dimension are taken in further launches
