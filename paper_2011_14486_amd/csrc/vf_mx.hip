@@ -190,32 +190,40 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
   }
 }
 
-// Many rows: tiles of 64 MI rows by 256 columns in the LDS, eight waves of 16 MI rows by 128 columns of accumulators.
+// Many rows: tiles of 256 rows by 256 columns in the LDS, eight waves of 64 rows by 128 columns of accumulators.
 //
 // A stage of the k loop is 128 k.  Its bytes go from memory straight to the LDS, in pieces of 16 bytes; where a piece lies is
 // chosen by which lane fetches it: piece c of row m at place c ^ (m % 8) of eight, or c ^ (m / 4 % 4) of four, so that the 16 rows that
 // lanes read at a time meet all banks.  The weights are the first operand, with the columns dealt to the operand's 16
-// rows in such an order that a lane ends up with 32 neighbouring columns of a row of the output.
+// rows in such an order that of a row of the output a lane ends up with eight neighbouring columns of every 32, and four
+// lanes together with all 32 of them: a store instruction writes 64 bytes of 16 rows.
 //
 // The weights' operands are read two tiles ahead, across the end of a stage too.  The only barrier is in a stage's middle: behind it
 // the next stage's bytes are there for everybody, and nobody reads the stage before any more, whose place the
 // newest fetch takes.  Of the two waves of a SIMD one has priority, so that they do not reach the reads of a's operands, at a
 // stage's begin, together.
+//
+// What bounds it besides the matrix cores is the number of requests to the second-level cache.  So scales, four bytes a row and
+// stage, are taken 16 bytes at a time, four stages' worth, through a register: a request per row and stage for them would be half of all
+// requests.  A workgroup goes on to its next tile by itself: that tile's first stages are on their way while the results of
+// the last one are stored.
 template <int AF> constexpr int a_bytes() { return AF == VF_E4M3 ? 128 : 64; }   // of a row, in a stage
 template <int AF> constexpr int stages() { return AF == VF_E4M3 ? 3 : 4; }       // that the LDS holds
-// (S4: scales four to a word; else each in a word of its own)
-template <int AF, int MI, bool S4> constexpr int stage_bytes() { return 64 * MI * a_bytes<AF>() + 256 * 64 + (64 * MI + 256) * (S4 ? 4 : 16); }
+template <int AF> constexpr int stage_bytes() { return 256 * a_bytes<AF>() + 256 * 64; }
+constexpr int SCALES = 512 * 16;  // of four stages; the LDS holds them twice
 
-// 64 lanes fetch 16 bytes (or one byte, into a word) each from addresses of their own to consecutive places of the LDS from `to` on.
+// A part of memory as the instructions with a range check see it: what lies behind its end reads as zeros.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 part_of(const uint8_t *at, int64_t bytes) {
+  const uint64_t a = (uint64_t)(uintptr_t)at;
+  const int64_t n = bytes < 0xfffffff0ll ? bytes : 0xfffffff0ll;
+  return i32x4{__builtin_amdgcn_readfirstlane((int)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xffff),
+               __builtin_amdgcn_readfirstlane((int)(uint32_t)n), 0x00027000};
+}
+// 64 lanes fetch 16 bytes each, `lane_at` + `at` into the part, to consecutive places of the LDS from `to` on.
 // The compiler does not know of these loads: they are waited for by wait_loads.
-__device__ __forceinline__ void to_lds16(const uint8_t *from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
-}
-__device__ __forceinline__ void to_lds1(const uint8_t *from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(to), "v"(from) : "memory");
-}
-__device__ __forceinline__ void to_lds4(const uint8_t *from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+__device__ __forceinline__ void to_lds16(const i32x4 &part, uint32_t lane_at, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(lane_at), "s"(part), "s"(at) : "memory");
 }
 // (accesses of the LDS are not moved across it)
 __device__ __forceinline__ void meet() {
@@ -225,100 +233,108 @@ __device__ __forceinline__ void meet() {
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-template <int AF, bool EXACT, int MI, bool S4>
+template <int N> struct phase_is { static constexpr int value = N; };
+
+template <int AF, bool EXACT>
 __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tiles_n, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
-  constexpr int BM = 64 * MI, AB = a_bytes<AF>(), NT = 8, NST = stages<AF>(), SB = stage_bytes<AF, MI, S4>();
-  constexpr int WAT = BM * AB, SAT = WAT + 256 * 64;  // the weights and the scales in a stage
+  constexpr int AB = a_bytes<AF>(), MI = 4, NT = 8, NST = stages<AF>(), SB = stage_bytes<AF>(), WAT = 256 * AB, SAT = NST * SB;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4, wm = wave & 3, wn = wave >> 2;
-  // Workgroups are dealt to the eight dies in turn: each die gets neighbouring tiles, in blocks of eight rows of tiles that pass over
-  // the columns, so that its cache keeps what they share.
-  int id = blockIdx.x;
-  const int chunk8 = tiles / 8;
-  if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
-  const int tiles_m = tiles / tiles_n, band = id / (8 * tiles_n), in_band = id - band * 8 * tiles_n;
-  const int high = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8, mt = 8 * band + in_band % high;
-  const int64_t m0 = (int64_t)mt * BM;
-  const int n0 = in_band / high * 256;
   const int steps = (p.kb + 3) >> 2;
 
-  // Pieces that this thread fetches in every stage: their sources at block 0 of the row, and their block within the stage
-  constexpr int PA = BM * (AB / 16) / 512, PW = 2, PS = ((BM + 256) * (S4 ? 1 : 4) + 511) / 512;
-  const uint8_t *src_a[PA], *src_w[PW], *src_s[PS];
-  int blk_a[PA], blk_w[PW], blk_s[PS];
-  auto row_a = [&](int row) { return m0 + row < p.M ? m0 + row : p.M - 1; };
-  // row 16 j + x of a wave's 128 rows of weights is its column 32 (x / 4) + 4 j + x % 4
-  auto col_w = [&](int row) {
-    const int col = n0 + (row & 128) + 32 * ((row & 15) >> 2) + 4 * ((row & 127) >> 4) + (row & 3);
-    return col < p.N ? col : p.N - 1;
-  };
+  // Pieces that this thread fetches in every stage, from the tile's first row and column on;
+  // and the row of a (threads 0..255) or of the weights whose scales it takes
+  constexpr int PA = AB / 32, PW = 2, LOADS = PA + PW;
+  const uint32_t row_bytes = (uint32_t)p.kb * mx<AF>::bytes32, col_bytes = (uint32_t)p.kb * 16;
+  // row 16 j + x of a wave's 128 rows of weights is its column 32 (j / 2) + 8 (x / 4) + 4 (j % 2) + x % 4
+  auto column = [](int row) { return (row & 0xe0) + 8 * ((row & 15) >> 2) + 4 * ((row >> 4) & 1) + (row & 3); };
+  uint32_t lane_a[PA], lane_w[PW];
 #pragma unroll
   for (int i = 0; i < PA; ++i) {
     const int e = i * 512 + tid, row = e / (AB / 16), c = AB == 128 ? (e & 7) ^ (row & 7) : (e & 3) ^ ((row >> 2) & 3);
-    src_a[i] = p.a + row_a(row) * p.kb * mx<AF>::bytes32 + (AF == VF_E4M3 ? 16 * (c & 1) : 0);
-    blk_a[i] = AF == VF_E4M3 ? c >> 1 : c;
+    lane_a[i] = (uint32_t)row * row_bytes + 16 * c;
   }
 #pragma unroll
   for (int i = 0; i < PW; ++i) {
-    const int e = i * 512 + tid, row = e >> 2;
-    src_w[i] = p.w + (int64_t)col_w(row) * p.kb * 16;
-    blk_w[i] = (e & 3) ^ ((row >> 2) & 3);
+    const int e = i * 512 + tid, row = e >> 2, c = (e & 3) ^ ((row >> 2) & 3);
+    lane_w[i] = (uint32_t)column(row) * col_bytes + 16 * c;
   }
-#pragma unroll
-  for (int i = 0; i < PS; ++i) {
-    const int e = i * 512 + tid, row = S4 ? e : e >> 2;
-    blk_s[i] = S4 ? 0 : e & 3;
-    src_s[i] = row < BM ? p.as + row_a(row) * p.kb : p.ws + (int64_t)col_w(row - BM) * p.kb;
-  }
+  int64_t m0;
+  int n0;
+  i32x4 part_a, part_w;
+  const uint8_t *src_s;
+  auto place = [&](int k) {  // the workgroup's k-th tile; false behind the last
+    // Workgroups are dealt to the eight dies in turn: each die gets neighbouring tiles, in blocks of eight rows of tiles that
+    // pass over the columns, so that its cache keeps what they share.
+    const int turn = k * (int)gridDim.x + (int)blockIdx.x;
+    if (turn >= tiles) return false;
+    const int chunk8 = tiles / 8, id = turn < chunk8 * 8 ? (turn & 7) * chunk8 + (turn >> 3) : turn;
+    const int tiles_m = tiles / tiles_n, band = id / (8 * tiles_n), in_band = id - band * 8 * tiles_n;
+    const int high = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8;
+    m0 = (int64_t)(8 * band + in_band % high) * 256;
+    n0 = in_band / high * 256;
+    part_a = part_of(p.a + m0 * row_bytes, (p.M - m0) * row_bytes);
+    part_w = part_of(p.w + (int64_t)n0 * col_bytes, (int64_t)(p.N - n0) * col_bytes);
+    // (rows that are not there take the last one's scales)
+    const int64_t row = tid < 256 ? (m0 + tid < p.M ? m0 + tid : p.M - 1) : (n0 + column(tid - 256) < p.N ? n0 + column(tid - 256) : p.N - 1);
+    src_s = (tid < 256 ? p.as : p.ws) + row * p.kb;
+    return true;
+  };
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
   const uint32_t wave_at = __builtin_amdgcn_readfirstlane(wave);
-  // (blocks behind the row's end: the row's last block, which is there; its k of a are then cleared)
+  // (behind a row's end lies the next row: those k of a are cleared before they are used)
   auto fetch = [&](int st) {
-    const uint32_t at = base + (uint32_t)(st % NST) * SB;
-    const int b0 = 4 * (st < steps ? st : steps - 1);
-    const bool whole = b0 + 4 <= p.kb;
-    auto block = [&](int b) { return whole || b0 + b < p.kb ? b0 + b : p.kb - 1; };
+    const uint32_t at = base + (uint32_t)(st % NST) * SB + wave_at * 1024, k = st < steps ? st : steps - 1;
 #pragma unroll
-    for (int i = 0; i < PA; ++i) to_lds16(src_a[i] + (int64_t)block(blk_a[i]) * mx<AF>::bytes32, at + (i * 512 + wave_at * 64) * 16);
+    for (int i = 0; i < PA; ++i) to_lds16(part_a, lane_a[i], k * AB, at + i * 8192);
 #pragma unroll
-    for (int i = 0; i < PW; ++i) to_lds16(src_w[i] + (int64_t)block(blk_w[i]) * 16, at + WAT + (i * 512 + wave_at * 64) * 16);
-#pragma unroll
-    for (int i = 0; i < PS; ++i) {
-      const uint32_t to = at + SAT + (i * 512 + wave_at * 64) * 4;
-      if (S4) to_lds4(src_s[i] + b0, to);  // (rows of scales are whole words then)
-      else to_lds1(src_s[i] + block(blk_s[i]), to);
-    }
+    for (int i = 0; i < PW; ++i) to_lds16(part_w, lane_w[i], k * 64, at + WAT + i * 8192);
   };
-  constexpr int LOADS = PA + PW + PS;
+  uint4 sq;  // scales on their way: of stages 4 k .. 4 k + 3
+  // 16 bytes at any address, where the row ends before: its last 16, moved down, and scales of one behind them
+  auto ask_scales = [&](int st) {
+    const int b0 = 4 * st, from = b0 + 16 <= p.kb ? b0 : p.kb - 16, sh = b0 - from < 15 ? 8 * (b0 - from) : 120;
+    const u16x8 v = *reinterpret_cast<const u16x8 *>(src_s + from);
+    const uint64_t one = 0x7f7f7f7f7f7f7f7full, lo = v.w[0] | (uint64_t)v.w[1] << 32, hi = v.w[2] | (uint64_t)v.w[3] << 32;
+    const uint64_t in = sh & 63 ? ~0ull : 0;  // (a shift by 64 is none)
+    const uint64_t lo1 = sh < 64 ? lo : hi, hi1 = sh < 64 ? hi : one;
+    const uint64_t a = lo1 >> (sh & 63) | (hi1 << (64 - (sh & 63) & 63) & in), b = hi1 >> (sh & 63) | (one << (64 - (sh & 63) & 63) & in);
+    sq = make_uint4((uint32_t)a, (uint32_t)(a >> 32), (uint32_t)(sh < 64 ? b : one), (uint32_t)((sh < 64 ? b : one) >> 32));
+  };
+  auto first_scales = [&]() {
+    if (p.kb >= 16) {
+      ask_scales(0);
+      return;
+    }
+    uint32_t w[4] = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+      if (i < p.kb) w[i >> 2] = (w[i >> 2] & ~(255u << (8 * (i & 3)))) | (uint32_t)src_s[i] << (8 * (i & 3));
+    sq = make_uint4(w[0], w[1], w[2], w[3]);
+  };
+  auto put_scales = [&](int st) { *reinterpret_cast<uint4 *>(lds + SAT + ((st >> 2) & 1) * SCALES + tid * 16) = sq; };
 
   f32x4 acc[NT][MI];
-#pragma unroll
-  for (int j = 0; j < NT; ++j)
-#pragma unroll
-    for (int i = 0; i < MI; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
   uint4 ar[MI][AB / 64], wq[4];
   int as[MI], ws[4];
   // places of this lane's pieces in a stage: of row 16 i + r they lie a constant further for every i
-  constexpr int SW = S4 ? 4 : 16;  // a row's scales
   const int sw_a = AB == 128 ? r & 7 : (r >> 2) & 3;
-  const int la0 = (wm * 16 * MI + r) * AB + 16 * (g ^ sw_a), la1 = (wm * 16 * MI + r) * AB + 16 * ((4 + g) ^ sw_a);
+  const int la0 = (wm * 64 + r) * AB + 16 * (g ^ sw_a), la1 = (wm * 64 + r) * AB + 16 * ((4 + g) ^ sw_a);
   const int lw = WAT + (wn * 128 + r) * 64 + 16 * (g ^ ((r >> 2) & 3));
-  const int lsa = SAT + (wm * 16 * MI + r) * SW + g * (SW / 4), lsw = SAT + (BM + wn * 128 + r) * SW + g * (SW / 4);
+  const int lsa = SAT + (wm * 64 + r) * 16 + g, lsw = SAT + (256 + wn * 128 + r) * 16 + g;
   auto read_a = [&](int st) {
     // (16 k at 16 g and, of 8-bit rows, 16 at 64 + 16 g)
-    const uint8_t *at = lds + (st % NST) * SB;
+    const uint8_t *at = lds + (st % NST) * SB, *sc = lds + lsa + ((st >> 2) & 1) * SCALES + 4 * (st & 3);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       ar[i][0] = *reinterpret_cast<const uint4 *>(at + la0 + i * 16 * AB);
       if (AF == VF_E4M3) ar[i][AB / 64 - 1] = *reinterpret_cast<const uint4 *>(at + la1 + i * 16 * AB);
-      as[i] = at[lsa + i * 16 * SW];
+      as[i] = sc[i * 256];
     }
   };
   auto read_w = [&](int st, int j) {
-    const uint8_t *at = lds + (st % NST) * SB;
-    wq[j & 3] = *reinterpret_cast<const uint4 *>(at + lw + j * 16 * 64);
-    ws[j & 3] = at[lsw + j * 16 * SW];
+    wq[j & 3] = *reinterpret_cast<const uint4 *>(lds + (st % NST) * SB + lw + j * 16 * 64);
+    ws[j & 3] = lds[lsw + ((st >> 2) & 1) * SCALES + 4 * (st & 3) + j * 256];
   };
   auto products = [&](int j) {
     __builtin_amdgcn_sched_barrier(0);
@@ -333,67 +349,106 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-#pragma unroll
-  for (int st = 0; st < NST - 1; ++st) fetch(st);
-  wait_loads<0>();
-  meet();
-  if (wave < 4) __builtin_amdgcn_s_setprio(1);
-  read_w(0, 0);
-  read_w(0, 1);
-  // (no branches in this loop: the compiler would move the products past them, behind all reads.  Stages behind the last
-  // one are the last one's bytes again, in places that nobody reads.)
-  for (int st = 0; st < steps - 1; ++st) {
+  // phase: st % 4, or -1: found at run time
+  auto stage = [&](int st, auto phase) {
+    const int ph = decltype(phase)::value >= 0 ? decltype(phase)::value : st & 3;
     read_a(st);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       if (j == NT / 2) {
+        if (ph == 3) {
+          put_scales(st + 1);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
         wait_loads<NST == 3 ? 0 : LOADS>();  // (of four stages the newest may still be under way)
         meet();
         fetch(st + NST - 1);
+        if (ph == 1 && (decltype(phase)::value >= 0 || st + 3 < steps)) ask_scales(st + 3);
       }
       if (j + 2 < NT) read_w(st, j + 2);
       else read_w(st + 1, j + 2 - NT);
       products(j);
     }
-  }
-  read_a(steps - 1);
-  if (p.kb % 4 != 0) {  // k behind the row's end
-    const int b0 = 4 * (steps - 1);
+  };
+
+  bool there = place(0);
+  if (there) {
+    first_scales();
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      if (b0 + (AF == VF_E4M3 ? g >> 1 : g) >= p.kb) ar[i][0] = make_uint4(0, 0, 0, 0);
-      if (AF == VF_E4M3 && b0 + 2 + (g >> 1) >= p.kb) ar[i][AB / 64 - 1] = make_uint4(0, 0, 0, 0);
+    for (int st = 0; st < NST - 1; ++st) fetch(st);
+  }
+  if (wave < 4) __builtin_amdgcn_s_setprio(1);
+  for (int k = 1; there; ++k) {
+    const int64_t m_at = m0;
+    const int n_at = n0;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) acc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    put_scales(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wait_loads<0>();
+    meet();
+    read_w(0, 0);
+    read_w(0, 1);
+    // (Four stages without branches: past a branch the compiler would move the products, behind all reads.  Stages behind the last
+    // one are the last one's bytes again, in places that nobody reads.)
+    int st = 0;
+    for (; st + 4 < steps; st += 4) {
+      stage(st, phase_is<0>());
+      stage(st + 1, phase_is<1>());
+      stage(st + 2, phase_is<2>());
+      stage(st + 3, phase_is<3>());
+    }
+    for (; st + 1 < steps; ++st) stage(st, phase_is<-1>());
+    read_a(st);
+    if (p.kb % 4 != 0) {  // k behind the row's end
+      const int b0 = 4 * st;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        if (b0 + (AF == VF_E4M3 ? g >> 1 : g) >= p.kb) ar[i][0] = make_uint4(0, 0, 0, 0);
+        if (AF == VF_E4M3 && b0 + 2 + (g >> 1) >= p.kb) ar[i][AB / 64 - 1] = make_uint4(0, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      if (j + 2 < NT) read_w(st, j + 2);
+      products(j);
+    }
+    // the next tile's first stages, into places that the last stages no longer need
+    wait_loads<0>();
+    meet();
+    there = place(k);
+    if (there) {
+      first_scales();
+#pragma unroll
+      for (int s = 0; s < NST - 1; ++s) fetch(s);
+    }
+    // a lane has columns n + 32 j / 2 .. + 7 of rows r, 16 + r, ...
+    const int n = n_at + wn * 128 + 8 * g;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(acc[j][i]));
+#pragma unroll
+    for (int j = 0; j < NT; j += 2) {
+      const int c0 = n + 16 * j;
+      float b[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) b[c] = p.bias && c0 + c < p.N ? p.bias[c0 + c] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int64_t m = m_at + wm * 64 + 16 * i + r;
+        if (m >= p.M || c0 >= p.N) continue;
+        float y[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) y[c] = acc[j + (c >> 2)][i][c & 3] + b[c];
+        if (p.out_bf16) store_upto8(reinterpret_cast<uint16_t *>(p.out) + m * p.ld_out + c0, p.N - c0, y);
+        else store_upto8(reinterpret_cast<float *>(p.out) + m * p.ld_out + c0, p.N - c0, y);
+      }
     }
   }
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    if (j + 2 < NT) read_w(steps - 1, j + 2);
-    products(j);
-  }
-  __builtin_amdgcn_s_setprio(0);
   wait_loads<0>();
-  // a lane has columns n .. n + 31 of rows r, 16 + r, ...
-  const int n = n0 + wn * 128 + 32 * g;
-#pragma unroll
-  for (int j = 0; j < NT; ++j)
-#pragma unroll
-    for (int i = 0; i < MI; ++i) asm volatile("" : "+v"(acc[j][i]));
-#pragma unroll
-  for (int j = 0; j < NT; j += 2) {
-    float b[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) b[k] = p.bias && n + 4 * j + k < p.N ? p.bias[n + 4 * j + k] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int64_t m = m0 + wm * 16 * MI + 16 * i + r;
-      if (m >= p.M || n + 4 * j >= p.N) continue;
-      float y[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = acc[j + (k >> 2)][i][k & 3] + b[k];
-      if (p.out_bf16) store_upto8(reinterpret_cast<uint16_t *>(p.out) + m * p.ld_out + n + 4 * j, p.N - n - 4 * j, y);
-      else store_upto8(reinterpret_cast<float *>(p.out) + m * p.ld_out + n + 4 * j, p.N - n - 4 * j, y);
-    }
-  }
 }
 
 inline int blocks_for(int64_t threads) {
@@ -401,36 +456,31 @@ inline int blocks_for(int64_t threads) {
   return (int)(g < (1 << 20) ? g : (1 << 20));
 }
 
-template <int AF, bool EXACT, int MI, bool S4>
+template <int AF, bool EXACT>
 int launch_tile(vf_ctx *c, const MatmulArgs &p) {
-  constexpr int smem = stages<AF>() * stage_bytes<AF, MI, S4>(), BM = 64 * MI;
+  constexpr int smem = stages<AF>() * stage_bytes<AF>() + 2 * SCALES;
   const int tiles_n = (p.N + 255) / 256;
-  // (less than 2^22 workgroups in a launch; the rows are taken in several)
-  const int64_t most = ((int64_t)1 << 22) / tiles_n, per = (most > 1 ? most : 1) * BM;
-  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_mx_tile<AF, EXACT, MI, S4>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
+  // (tiles are counted in 32 bits; the rows are taken in several launches)
+  const int64_t most = ((int64_t)1 << 28) / tiles_n, per = (most > 1 ? most : 1) * 256;
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_mx_tile<AF, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
   for (int64_t m = 0; m < p.M; m += per) {
     MatmulArgs q = p;
     q.a += m * p.kb * mx<AF>::bytes32;
     q.as += m * p.kb;
     q.M = p.M - m < per ? p.M - m : per;
     q.out = static_cast<char *>(p.out) + m * p.ld_out * (p.out_bf16 ? 2 : 4);
-    const int tiles = (int)((q.M + BM - 1) / BM) * tiles_n;
-    k_mx_tile<AF, EXACT, MI, S4><<<tiles, 512, smem, c->stream>>>(q, tiles_n, tiles);
+    const int tiles = (int)((q.M + 255) / 256) * tiles_n;
+    k_mx_tile<AF, EXACT><<<tiles < 256 ? tiles : 256, 512, smem, c->stream>>>(q, tiles_n, tiles);
     VF_HIP(c, hipGetLastError());
   }
   return VF_OK;
 }
 
-bool aligned4(const void *p) { return (uintptr_t)p % 4 == 0; }
-
 template <int AF, bool EXACT>
 int matmul(vf_ctx *c, const MatmulArgs &p) {
   const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256);
-  if (p.M > 64 && big >= 64) {
-    // (rows of scales that begin at whole words travel four at a time)
-    if (p.kb % 4 == 0 && aligned4(p.as) && aligned4(p.ws)) return launch_tile<AF, EXACT, 4, true>(c, p);
-    return launch_tile<AF, EXACT, 2, false>(c, p);
-  }
+  // (offsets within 256 rows are 32 bits wide)
+  if (p.M > 64 && big >= 64 && p.kb <= (1 << 18)) return launch_tile<AF, EXACT>(c, p);
   const int nb = (p.N + 15) / 16;
   const int MT = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
   // rows beyond the grid's second dimension are taken in further launches
