@@ -346,4 +346,5 @@ int vfk_mx_matmul(vf_ctx *c, int a_format, const uint8_t *a, const uint8_t *as, 
                   int N, int K, const float *bias, int out_type, void *out, int64_t ld_out);
 // `bytes` of scratch, or nullptr where they cannot be had (no memory, or the stream is being captured)
 void *vfk_ops_scratch(vf_ctx *c, size_t bytes);
-int vfk_ssm(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io);
+// one: a token for every sequence
+int vfk_ssm(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io, bool one);

@@ -51,7 +51,7 @@ int ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io, bool one) {
       !state_ok(l, io, io->conv_out_dev, io->ssm_out_dev, io->slots_out_dev, io->n_slots_out))
     return VF_EINVAL;
   DeviceGuard g(c->device);
-  return vfk_ssm(c, l, io);
+  return vfk_ssm(c, l, io, one);
 }
 
 }  // namespace

@@ -80,24 +80,100 @@ __device__ __forceinline__ void conv_state(const SsmArgs &p, const Span &sp, int
     if (k < p.W - 1) store1(to + k, keep[k]);
 }
 
-// A wave's lanes 16 p + i hold p, n = 4 (16 k + i) .. + 3 of the state: 16 lanes read 256 bytes of a row of it.
-constexpr int SEQ_TOKENS = 8;  // tokens convolved at a time
+// Sums of COUNT numbers over LANES neighbouring lanes (i: which of them this one is): in each step a lane keeps half of the numbers
+// and gives the other half away, so that COUNT - 1 numbers are exchanged, not COUNT log2 LANES.
+// A lane is left with kept_of numbers, from first_kept on; where lanes share a number, all of them have it.
+template <int LANES, int COUNT> constexpr int kept_of() { return COUNT > LANES ? COUNT / LANES : 1; }
+template <int LANES, int COUNT> __device__ __forceinline__ int first_kept(int i) {
+  return COUNT >= LANES ? i * (COUNT / LANES) : i / (LANES / COUNT);
+}
+template <int LANES, int COUNT>
+__device__ __forceinline__ void sum_lanes(float (&y)[COUNT], int i) {
+  if constexpr (LANES > 1) {
+    constexpr int m = LANES / 2;
+    if constexpr (COUNT > 1) {
+      constexpr int half = COUNT / 2;
+      float rest[half];
+      const bool up = i & m;
+#pragma unroll
+      for (int k = 0; k < half; ++k) {
+        const float give = up ? y[k] : y[half + k];
+        rest[k] = (up ? y[half + k] : y[k]) + __shfl_xor(give, m);
+      }
+      sum_lanes<m, half>(rest, i);
+#pragma unroll
+      for (int k = 0; k < half; ++k) y[k] = rest[k];
+    } else {
+      y[0] += __shfl_xor(y[0], m);
+      sum_lanes<m, 1>(y, i);
+    }
+  }
+}
+// four numbers of a row of the state, `left` of which are there; zeros behind them
+__device__ __forceinline__ f32x4 load_n(const float *at, int left) {
+  if (left >= 4) {
+    const f32v4 v = *reinterpret_cast<const f32v4 *>(at);
+    return f32x4{v.v[0], v.v[1], v.v[2], v.v[3]};
+  }
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 3; ++j)
+    if (j < left) v[j] = at[j];
+  return v;
+}
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void store_n(float *at, int left, const f32x4 &v) {
+  if (left >= 4) {
+    __builtin_nontemporal_store(v, reinterpret_cast<f32x4_any *>(at));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 3; ++j)
+    if (j < left) at[j] = v[j];
+}
+template <typename T> __device__ __forceinline__ float as_f32(T v) { return load1(&v); }
+template <typename T> __device__ __forceinline__ T nan_of() { return sizeof(T) == 2 ? (T)0x7fc0 : (T)__uint_as_float(0x7fc00000u); }
 
-// Token by token: a workgroup holds 16 PI rows p of one head's state in registers, NK groups of 64 n.
-template <typename T, int PI, int NK>
+// A workgroup's channels: R of x, then those of B and of C, `span` places each.  Channel of place k, or -1; `own`: this
+// workgroup is the one that writes its convolution's state.
+__device__ __forceinline__ int channel_of(const SsmArgs &p, int k, int R, int span, int h, int g, int p0, int np) {
+  if (k < R) return k < np ? h * p.P + p0 + k : -1;
+  k -= R;
+  if (k >= 2 * span) return -1;
+  const int n = k < span ? k : k - span;
+  return n < p.N ? p.H * p.P + (k < span ? 0 : p.G * p.N) + g * p.N + n : -1;
+}
+
+// Token by token, fp32: a workgroup holds 16 PI rows p of one head's state in registers, lanes 16 p + i the n = 4 (16 q + i) .. + 3
+// of NK groups of 64.  Eight tokens are convolved at a time, a thread a channel; their inputs were fetched while
+// the eight before were worked on, and the outputs of the eight are summed over the lanes together.  What bounds it is the
+// chain of a sequence's tokens, so long sequences are split (below).
+template <typename T, int PI, int NK, int TW>
 __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
-  extern __shared__ float lds[];
+  constexpr int R = 16 * PI, SPAN = 64 * NK, PLACES = R + 2 * SPAN, NC = (PLACES + 255) / 256, TB = 8;
+  constexpr int COUNT = TB * PI, KEPT = kept_of<16, COUNT>();
+  __shared__ float ux[2][TB][R];
+  __shared__ __align__(16) float ubc[2][TB][2 * SPAN];
+  __shared__ float udt[2][TB], uda[2][TB];
   const int tid = threadIdx.x, i16 = tid & 15, prow = tid >> 4;
-  const int slices = (p.P + 16 * PI - 1) / (16 * PI);
-  const int h = (int)blockIdx.x / slices, p0 = ((int)blockIdx.x % slices) * 16 * PI;
+  const int slices = (p.P + R - 1) / R;
+  const int h = (int)blockIdx.x / slices, p0 = ((int)blockIdx.x % slices) * R;
   const int g = h / (p.H / p.G);
-  const int np = p.P - p0 < 16 * PI ? p.P - p0 : 16 * PI;
-  const int Nr = (p.N + 3) & ~3;                       // row of B and C in the LDS, zeros behind N
-  float *uB = lds, *uC = uB + SEQ_TOKENS * Nr, *ux = uC + SEQ_TOKENS * Nr, *uy = ux + SEQ_TOKENS * 16 * PI;
-  float *udt = uy + SEQ_TOKENS * 16 * PI, *uda = udt + SEQ_TOKENS;
-  const int nch = np + 2 * p.N;
+  const int np = p.P - p0 < R ? p.P - p0 : R;
   const float A = p.a[h], D = p.d ? p.d[h] : 0.0f, bias_dt = p.dt_bias ? p.dt_bias[h] : 0.0f;
   const bool owns_bc = h == g * (p.H / p.G) && p0 == 0;  // writes the convolution's state of its group's B and C
+  int chan[NC];
+  float taps[NC][TW], bias[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    chan[j] = channel_of(p, j * 256 + tid, R, SPAN, h, g, p0, np);
+    bias[j] = chan[j] >= 0 && p.conv_b ? p.conv_b[chan[j]] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < TW; ++k) taps[j][k] = chan[j] >= 0 && k >= TW - p.W ? p.conv_w[(int64_t)chan[j] * p.W + k - (TW - p.W)] : 0.0f;
+  }
+  // the outputs that are left to this lane: number v is token v / PI, row PI prow + v % PI
+  const int v0 = first_kept<16, COUNT>(i16), t_own = v0 / PI, p_own = prow * PI + v0 % PI;
+  const bool stores = !p.local && (COUNT >= 16 || i16 % (16 / (COUNT < 16 ? COUNT : 16)) == 0);
 
   const int64_t parts = (int64_t)p.n_seq * p.nseg, size = (int64_t)p.P * p.N;
   for (int64_t sx = blockIdx.y; sx < parts; sx += gridDim.y) {
@@ -112,117 +188,231 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
     const float *first = p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
     float *left = p.local ? mine : pt.last && slot_to >= 0 ? p.ssm_out + ((int64_t)slot_to * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
     if (p.local) first = nullptr;
-    float S[PI][NK][4], log_decay = 0.0f;
+    f32x4 S[PI][NK];
+    float log_decay = 0.0f;
+    const float fill = slot == -2 && p.nseg == 1 ? __uint_as_float(0x7fc00000u) : 0.0f;
 #pragma unroll
-    for (int k = 0; k < PI; ++k) {
-      const int pr = 16 * k + prow;
+    for (int k = 0; k < PI; ++k)
 #pragma unroll
       for (int q = 0; q < NK; ++q) {
-        const int n = 4 * (16 * q + i16);
+        const int n = 4 * (16 * q + i16), pr = prow * PI + k;
+        S[k][q] = f32x4{fill, fill, fill, fill};
+        if (first && pr < np && n < p.N) S[k][q] = load_n(first + (int64_t)pr * p.N + n, p.N - n);
+      }
+    float past[NC][TW - 1];
+    T raw[NC][TB], raw_z[KEPT], raw_dt = 0;
+    // (tokens behind the end: the last one again, taken as zeros)
+    auto row_of = [&](int t) { return sp.first + (t < pt.end ? t : pt.end - 1); };
+    auto ask = [&](int t0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) S[k][q][j] = slot == -2 && p.nseg == 1 ? __uint_as_float(0x7fc00000u) : 0.0f;
-        if (first && pr < np && n < p.N) {
-          const float *from = first + (int64_t)pr * p.N + n;
-          if (n + 4 <= p.N) {
-            const f32v4 v = *reinterpret_cast<const f32v4 *>(from);
+      for (int j = 0; j < NC; ++j)
+        if (chan[j] >= 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[k][q][j] = v.v[j];
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (n + j < p.N) S[k][q][j] = from[j];
-          }
+          for (int t = 0; t < TB; ++t) raw[j][t] = reinterpret_cast<const T *>(p.xbc)[row_of(t0 + t) * p.ld_xbc + chan[j]];
         }
-      }
-    }
-    for (int t0 = pt.begin; t0 < pt.end; t0 += SEQ_TOKENS) {
-      const int nt = pt.end - t0 < SEQ_TOKENS ? pt.end - t0 : SEQ_TOKENS;
-      // convolution of this workgroup's x, and of B and C
-      for (int e = tid; e < nt * nch; e += 256) {
-        const int t = e / nch, k = e - t * nch;
-        const int c = k < np ? h * p.P + p0 + k : k < np + p.N ? p.H * p.P + g * p.N + (k - np)
-                                                               : p.H * p.P + p.G * p.N + g * p.N + (k - np - p.N);
-        float v = p.conv_b ? p.conv_b[c] : 0.0f;
-        for (int w = 0; w < p.W; ++w) v = fmaf(p.conv_w[c * p.W + w], conv_input<T>(p, sp, slot, c, t0 + t - p.W + 1 + w), v);
-        v = silu(v);
-        if (k < np) ux[t * 16 * PI + k] = v;
-        else if (k < np + p.N) uB[t * Nr + (k - np)] = v;
-        else uC[t * Nr + (k - np - p.N)] = v;
-      }
-      for (int e = tid; e < nt * (Nr - p.N); e += 256) {
-        const int t = e / (Nr - p.N), k = p.N + e % (Nr - p.N);
-        uB[t * Nr + k] = uC[t * Nr + k] = 0.0f;
-      }
-      if (tid < nt) {
-        const float dt = softplus(load1(reinterpret_cast<const T *>(p.dt) + (sp.first + t0 + tid) * p.ld_dt + h) + bias_dt);
-        udt[tid] = dt;
-        uda[tid] = __expf(dt * A);
-      }
-      __syncthreads();
-      for (int t = 0; t < nt; ++t) {
-        const float dt = udt[t], da = uda[t];
-        log_decay = fmaf(dt, A, log_decay);
-        float y[PI];
+      if (tid < TB) raw_dt = reinterpret_cast<const T *>(p.dt)[row_of(t0 + tid) * p.ld_dt + h];
+    };
+    if (pt.begin < pt.end) {
 #pragma unroll
-        for (int k = 0; k < PI; ++k) y[k] = 0.0f;
+      for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int k = 0; k < TW - 1; ++k)
+          past[j][k] = chan[j] >= 0 && k >= TW - p.W ? conv_input<T>(p, sp, slot, chan[j], pt.begin - (TW - 1) + k) : 0.0f;
+      ask(pt.begin);
+    }
+    for (int t0 = pt.begin; t0 < pt.end; t0 += TB) {
+      const int nt = pt.end - t0 < TB ? pt.end - t0 : TB, buf = (t0 - pt.begin) / TB & 1;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int k = j * 256 + tid;
+        if (k >= PLACES) continue;
+        float in[TW - 1 + TB];
+#pragma unroll
+        for (int i = 0; i < TW - 1; ++i) in[i] = past[j][i];
+#pragma unroll
+        for (int t = 0; t < TB; ++t) in[TW - 1 + t] = chan[j] >= 0 ? as_f32<T>(raw[j][t]) : 0.0f;
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          float v = bias[j];
+#pragma unroll
+          for (int i = 0; i < TW; ++i) v = i >= TW - p.W ? fmaf(taps[j][i], in[t + i], v) : v;
+          v = chan[j] >= 0 && t < nt ? silu(v) : 0.0f;
+          if (k < R) ux[buf][t][k] = v;
+          else ubc[buf][t][k - R] = v;
+        }
+#pragma unroll
+        for (int i = 0; i < TW - 1; ++i) past[j][i] = in[TB + i];
+      }
+      if (tid < TB) {
+        const float dt = tid < nt ? softplus(as_f32<T>(raw_dt) + bias_dt) : 0.0f;
+        udt[buf][tid] = dt;
+        uda[buf][tid] = __expf(dt * A);
+      }
+      const int64_t row = sp.first + t0 + t_own;
+      if (p.z && stores && t_own < nt) {
+#pragma unroll
+        for (int e = 0; e < KEPT; ++e)
+          if (p_own + e < np) raw_z[e] = reinterpret_cast<const T *>(p.z)[row * p.ld_z + h * p.P + p0 + p_own + e];
+      }
+      if (t0 + TB < pt.end) ask(t0 + TB);
+      __syncthreads();  // (two buffers: nobody writes the one that is read before all have passed the next barrier)
+      float y[COUNT];
+#pragma unroll
+      for (int t = 0; t < TB; ++t) {
+        const float dt = udt[buf][t], da = uda[buf][t];
+        log_decay = fmaf(dt, A, log_decay);
+#pragma unroll
+        for (int k = 0; k < PI; ++k) y[t * PI + k] = 0.0f;
 #pragma unroll
         for (int q = 0; q < NK; ++q) {
-          const int n = 4 * (16 * q + i16);
-          if (n >= p.N) continue;
-          const f32x4 B = *reinterpret_cast<const f32x4 *>(uB + t * Nr + n), Cv = *reinterpret_cast<const f32x4 *>(uC + t * Nr + n);
+          const f32x4 B = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][4 * (16 * q + i16)]);
+          const f32x4 Cv = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][SPAN + 4 * (16 * q + i16)]);
 #pragma unroll
           for (int k = 0; k < PI; ++k) {
-            const float dx = 16 * k + prow < np ? dt * ux[t * 16 * PI + 16 * k + prow] : 0.0f;
+            const float dx = dt * ux[buf][t][prow * PI + k];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               S[k][q][j] = fmaf(S[k][q][j], da, dx * B[j]);
-              y[k] = fmaf(S[k][q][j], Cv[j], y[k]);
+              y[t * PI + k] = fmaf(S[k][q][j], Cv[j], y[t * PI + k]);
             }
           }
         }
+      }
+      if (p.local) continue;
+      sum_lanes<16, COUNT>(y, i16);
+      if (stores && t_own < nt) {
 #pragma unroll
-        for (int k = 0; k < PI; ++k) {
-#pragma unroll
-          for (int m = 1; m < 16; m <<= 1) y[k] += __shfl_xor(y[k], m);
-          if (i16 == 0) uy[t * 16 * PI + 16 * k + prow] = y[k];
+        for (int e = 0; e < KEPT; ++e) {
+          if (p_own + e >= np) continue;
+          float v = fmaf(D, ux[buf][t_own][p_own + e], y[e]);
+          if (p.z) v *= silu(as_f32<T>(raw_z[e]));
+          store1(reinterpret_cast<T *>(p.out) + row * p.ld_out + h * p.P + p0 + p_own + e, v);
         }
       }
-      __syncthreads();
-      for (int e = tid; e < (p.local ? 0 : nt * np); e += 256) {
-        const int t = e / np, k = e - t * np;
-        const int64_t row = sp.first + t0 + t;
-        float y = fmaf(D, ux[t * 16 * PI + k], uy[t * 16 * PI + k]);
-        if (p.z) y *= silu(load1(reinterpret_cast<const T *>(p.z) + row * p.ld_z + h * p.P + p0 + k));
-        store1(reinterpret_cast<T *>(p.out) + row * p.ld_out + h * p.P + p0 + k, y);
-      }
-      __syncthreads();
     }
+    __syncthreads();  // (the next part begins with the first buffer again)
     if (p.local && tid == 0 && p0 == 0) p.seg_log[sx * p.H + h] = log_decay;
     if (!left) continue;
 #pragma unroll
-    for (int k = 0; k < PI; ++k) {
-      const int pr = 16 * k + prow;
+    for (int k = 0; k < PI; ++k)
 #pragma unroll
       for (int q = 0; q < NK; ++q) {
-        const int n = 4 * (16 * q + i16);
-        if (pr >= np || n >= p.N) continue;
-        float *to = left + (int64_t)pr * p.N + n;
-        if (n + 4 <= p.N) {
-          f32v4 v;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v.v[j] = S[k][q][j];
-          *reinterpret_cast<f32v4 *>(to) = v;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (n + j < p.N) to[j] = S[k][q][j];
-        }
+        const int n = 4 * (16 * q + i16), pr = prow * PI + k;
+        if (pr < np && n < p.N) store_n(left + (int64_t)pr * p.N + n, p.N - n, S[k][q]);
       }
-    }
     if (p.local || p.conv_later || p.W == 1) continue;
-    for (int k = tid; k < (owns_bc ? nch : np); k += 256)
-      conv_state<T>(p, sp, slot, slot_to, k < np ? h * p.P + p0 + k : k < np + p.N ? p.H * p.P + g * p.N + (k - np)
-                                                                                   : p.H * p.P + p.G * p.N + g * p.N + (k - np - p.N));
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+      if (chan[j] >= 0 && (owns_bc || j * 256 + tid < R)) conv_state<T>(p, sp, slot, slot_to, chan[j]);
+  }
+}
+
+// One token: L lanes hold a row p of the state, four numbers n each; a thread has PI rows of it.  A workgroup takes the same rows p of one
+// head for `each` sequences one after the other: the layer's weights stay in registers, and the next sequence's state and
+// inputs are on their way while this one's are worked on.  Every state is read and written once, past the caches on the
+// way out: the memory's rate bounds it.  Workgroups of one head run next to each other, so that the states of
+// parents that many rows continue come from the second-level cache.
+template <typename T, int PI, int NC, int TW>
+struct StepIn {
+  f32x4 S[PI];
+  T window[NC][TW], dt, z;
+};
+template <typename T, int L, int PI, int TW>
+__global__ void __launch_bounds__(256) k_ssm_step(const SsmArgs p, int slices, int each, int turns) {
+  constexpr int RP = 256 / L, R = RP * PI, SPAN = 4 * L, PLACES = R + 2 * SPAN, NC = (PLACES + 255) / 256;
+  __shared__ __align__(16) float u[2][PLACES];
+  const int tid = threadIdx.x, i = tid & (L - 1), prow = tid / L, n = 4 * i;
+  uint32_t id = blockIdx.x;
+  const uint32_t chunk8 = gridDim.x / 8;
+  if (id < chunk8 * 8) id = (id & 7) * chunk8 + (id >> 3);
+  const int unit = (int)(id / (uint32_t)turns), s0 = (int)(id - (uint32_t)unit * turns) * each;
+  const int s1 = p.n_seq - s0 < each ? p.n_seq : s0 + each;
+  const int h = unit / slices, p0 = (unit - h * slices) * R, g = h / (p.H / p.G);
+  const int np = p.P - p0 < R ? p.P - p0 : R;
+  const float A = p.a[h], D = p.d ? p.d[h] : 0.0f, bias_dt = p.dt_bias ? p.dt_bias[h] : 0.0f;
+  const bool owns_bc = h == g * (p.H / p.G) && p0 == 0;
+  const int64_t size = (int64_t)p.P * p.N;
+  int chan[NC];
+  float taps[NC][TW], bias[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    chan[j] = channel_of(p, j * 256 + tid, R, SPAN, h, g, p0, np);
+    bias[j] = chan[j] >= 0 && p.conv_b ? p.conv_b[chan[j]] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < TW; ++k) taps[j][k] = chan[j] >= 0 && k >= TW - p.W ? p.conv_w[(int64_t)chan[j] * p.W + k - (TW - p.W)] : 0.0f;
+  }
+  const int p_own = prow * PI + first_kept<L, PI>(i);
+  const bool stores = i % (L / PI) == 0 && p_own < np;
+
+  auto ask = [&](int s, int slot, StepIn<T, PI, NC, TW> &in) {
+#pragma unroll
+    for (int k = 0; k < PI; ++k) {
+      const int pr = prow * PI + k;
+      const float fill = slot == -2 ? __uint_as_float(0x7fc00000u) : 0.0f;
+      in.S[k] = f32x4{fill, fill, fill, fill};
+      if (slot >= 0 && pr < np && n < p.N) in.S[k] = load_n(p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)(p0 + pr) * p.N + n, p.N - n);
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+#pragma unroll
+      for (int k = 0; k < TW - 1; ++k) in.window[j][k] = slot == -2 ? nan_of<T>() : (T)0;
+      if (chan[j] < 0) continue;
+      if (slot >= 0) {
+        const T *at = reinterpret_cast<const T *>(p.conv_in) + ((int64_t)slot * p.C + chan[j]) * (p.W - 1);
+#pragma unroll
+        for (int k = 0; k < TW - 1; ++k)
+          if (k >= TW - p.W) in.window[j][k] = at[k - (TW - p.W)];
+      }
+      in.window[j][TW - 1] = reinterpret_cast<const T *>(p.xbc)[s * p.ld_xbc + chan[j]];
+    }
+    in.dt = reinterpret_cast<const T *>(p.dt)[s * p.ld_dt + h];
+    if (p.z && stores) in.z = reinterpret_cast<const T *>(p.z)[s * p.ld_z + h * p.P + p0 + p_own];
+  };
+  StepIn<T, PI, NC, TW> next;
+  if (s0 < s1) ask(s0, slot_of(p.slots_in, p.has_in, p.n_in, s0), next);
+  int slot_next = s0 + 1 < s1 ? slot_of(p.slots_in, p.has_in, p.n_in, s0 + 1) : -1;
+  for (int s = s0; s < s1; ++s) {
+    StepIn<T, PI, NC, TW> in = next;
+    const int slot_to = slot_of(p.slots_out, p.has_out, p.n_out, s);
+    if (s + 1 < s1) ask(s + 1, slot_next, next);
+    if (s + 2 < s1) slot_next = slot_of(p.slots_in, p.has_in, p.n_in, s + 2);
+    float *now = u[(s - s0) & 1];  // (two buffers: one barrier a sequence)
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int k = j * 256 + tid;
+      if (k >= PLACES) continue;
+      float v = bias[j];
+#pragma unroll
+      for (int e = 0; e < TW; ++e) v = e >= TW - p.W ? fmaf(taps[j][e], as_f32<T>(in.window[j][e]), v) : v;
+      now[k] = chan[j] >= 0 ? silu(v) : 0.0f;
+      if (chan[j] < 0 || slot_to < 0 || p.conv_later || !(owns_bc || k < R)) continue;
+      T *to = reinterpret_cast<T *>(p.conv_out) + ((int64_t)slot_to * p.C + chan[j]) * (p.W - 1);
+#pragma unroll
+      for (int e = 1; e < TW; ++e)
+        if (e > TW - p.W) to[e - 1 - (TW - p.W)] = in.window[j][e];
+    }
+    const float dt = softplus(as_f32<T>(in.dt) + bias_dt), da = __expf(dt * A);
+    __syncthreads();
+    const f32x4 B = *reinterpret_cast<const f32x4 *>(now + R + n), Cv = *reinterpret_cast<const f32x4 *>(now + R + SPAN + n);
+    float y[PI];
+#pragma unroll
+    for (int k = 0; k < PI; ++k) {
+      const float dx = dt * now[prow * PI + k];
+      y[k] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        in.S[k][j] = fmaf(in.S[k][j], da, dx * B[j]);
+        y[k] = fmaf(in.S[k][j], Cv[j], y[k]);
+      }
+      const int pr = prow * PI + k;
+      if (slot_to >= 0 && pr < np && n < p.N)
+        store_n(p.ssm_out + ((int64_t)slot_to * p.H + h) * size + (int64_t)(p0 + pr) * p.N + n, p.N - n, in.S[k]);
+    }
+    sum_lanes<L, PI>(y, i);
+    if (!stores) continue;
+    float v = fmaf(D, now[p_own], y[0]);
+    if (p.z) v *= silu(as_f32<T>(in.z));
+    store1(reinterpret_cast<T *>(p.out) + s * p.ld_out + h * p.P + p0 + p_own, v);
   }
 }
 
@@ -311,14 +501,16 @@ int run_parts(vf_ctx *c, SsmArgs &p, F launch) {
   return launch();
 }
 
+constexpr int SEQ_TOKENS = 8;  // tokens that k_ssm_tokens takes at a time
+
 template <typename T, int PI, int NK>
 int launch_tokens(vf_ctx *c, SsmArgs &p) {
-  const int slices = (p.P + 16 * PI - 1) / (16 * PI), Nr = (p.N + 3) & ~3;
-  const size_t smem = sizeof(float) * SEQ_TOKENS * (2 * Nr + 2 * 16 * PI + 2);
+  const int slices = (p.P + 16 * PI - 1) / (16 * PI);
   const int64_t parts = (int64_t)p.n_seq * p.nseg;
   const dim3 grid(p.H * slices, (unsigned)(parts < 32768 ? parts : 32768));
   return run_parts(c, p, [&] {
-    k_ssm_tokens<T, PI, NK><<<grid, 256, smem, c->stream>>>(p);
+    if (p.W <= 4) k_ssm_tokens<T, PI, NK, 4><<<grid, 256, 0, c->stream>>>(p);
+    else k_ssm_tokens<T, PI, NK, 8><<<grid, 256, 0, c->stream>>>(p);
     VF_HIP(c, hipGetLastError());
     return VF_OK;
   });
@@ -331,6 +523,34 @@ int tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
   split(c, p, longest, (int64_t)p.n_seq * p.H * (wide ? (p.P + 63) / 64 : (p.P + 15) / 16), 1024, SEQ_TOKENS, 64);
   if (wide) return nk <= 1 ? launch_tokens<T, 4, 1>(c, p) : nk <= 2 ? launch_tokens<T, 4, 2>(c, p) : launch_tokens<T, 4, 4>(c, p);
   return nk <= 1 ? launch_tokens<T, 1, 1>(c, p) : nk <= 2 ? launch_tokens<T, 1, 2>(c, p) : launch_tokens<T, 1, 4>(c, p);
+}
+
+template <typename T, int L, int PI>
+int launch_step(vf_ctx *c, const SsmArgs &p) {
+  constexpr int R = 256 / L * PI;
+  const int slices = (p.P + R - 1) / R;
+  const int64_t units = (int64_t)p.H * slices, total = units * p.n_seq;
+  // sequences a workgroup: four rounds of the workgroups that run at a time, for the sake of an even end; and at most 2^22 workgroups
+  int64_t each = total / 4096;
+  each = each < 1 ? 1 : each > 16 ? 16 : each;
+  if (each < (total >> 22) + 1) each = (total >> 22) + 1;
+  if (each > p.n_seq) each = p.n_seq;
+  const int turns = (int)((p.n_seq + each - 1) / each);
+  const unsigned blocks = (unsigned)(units * turns);
+  if (p.W <= 4) k_ssm_step<T, L, PI, 4><<<blocks, 256, 0, c->stream>>>(p, slices, (int)each, turns);
+  else k_ssm_step<T, L, PI, 8><<<blocks, 256, 0, c->stream>>>(p, slices, (int)each, turns);
+  VF_HIP(c, hipGetLastError());
+  return VF_OK;
+}
+template <typename T>
+int step(vf_ctx *c, const SsmArgs &p) {
+  // 64 rows p a workgroup (32 of more than 128 numbers n), or 16 (8) where there are too few workgroups for the compute units
+  const bool wide = (int64_t)p.n_seq * p.H * ((p.P + 63) / 64) >= 512;
+  if (p.N <= 16) return launch_step<T, 4, 1>(c, p);
+  if (p.N <= 32) return wide ? launch_step<T, 8, 2>(c, p) : launch_step<T, 8, 1>(c, p);
+  if (p.N <= 64) return wide ? launch_step<T, 16, 4>(c, p) : launch_step<T, 16, 1>(c, p);
+  if (p.N <= 128) return wide ? launch_step<T, 32, 8>(c, p) : launch_step<T, 32, 2>(c, p);
+  return wide ? launch_step<T, 64, 8>(c, p) : launch_step<T, 64, 2>(c, p);
 }
 
 // ---- in chunks of 32 tokens on the matrix cores ----
@@ -918,7 +1138,7 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
 
 }  // namespace
 
-int vfk_ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io) {
+int vfk_ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io, bool one) {
   if (io->n_seq == 0) return VF_OK;
   SsmArgs p;
   p.conv_w = l->conv_w_dev; p.conv_b = l->conv_b_dev; p.a = l->a_dev; p.d = l->d_dev; p.dt_bias = l->dt_bias_dev;
@@ -935,7 +1155,8 @@ int vfk_ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io) {
   p.nseg = 1; p.seg_len = 0; p.local = 0; p.seg_state = p.seg_log = nullptr;
   const int64_t longest = io->offsets_dev ? (io->longest < io->tokens ? io->longest : io->tokens) : io->tokens / io->n_seq;
   int rc;
-  if (io->type == VF_BF16 && chunks_fit(p) && longest > 8) rc = chunks(c, p, longest);
+  if (one) rc = io->type == VF_BF16 ? step<uint16_t>(c, p) : step<float>(c, p);
+  else if (io->type == VF_BF16 && chunks_fit(p) && longest > 8) rc = chunks(c, p, longest);
   else rc = io->type == VF_BF16 ? tokens<uint16_t>(c, p, longest) : tokens<float>(c, p, longest);
   if (rc != VF_OK || !p.has_out || !p.conv_later || p.W == 1) return rc;
   const int grid = blocks_for((int64_t)p.n_seq * p.C);
