@@ -144,18 +144,18 @@ __device__ __forceinline__ int channel_of(const SsmArgs &p, int k, int R, int sp
   return n < p.N ? p.H * p.P + (k < span ? 0 : p.G * p.N) + g * p.N + n : -1;
 }
 
-// Token by token, fp32: a workgroup holds 16 PI rows p of one head's state in registers, lanes 16 p + i the n = 4 (16 q + i) .. + 3
-// of NK groups of 64.  Eight tokens are convolved at a time, a thread a channel; their inputs were fetched while
+// Token by token, fp32: a workgroup holds 256 / L PI rows p of one head's state in registers, L lanes a row, four numbers n
+// each.  Eight tokens are convolved at a time, a thread a channel; their inputs were fetched while
 // the eight before were worked on, and the outputs of the eight are summed over the lanes together.  What bounds it is the
 // chain of a sequence's tokens, so long sequences are split (below).
-template <typename T, int PI, int NK, int TW>
-__global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
-  constexpr int R = 16 * PI, SPAN = 64 * NK, PLACES = R + 2 * SPAN, NC = (PLACES + 255) / 256, TB = 8;
-  constexpr int COUNT = TB * PI, KEPT = kept_of<16, COUNT>();
+template <typename T, int L, int PI, int TW>
+__global__ void __launch_bounds__(256, 2) k_ssm_tokens(const SsmArgs p) {
+  constexpr int R = 256 / L * PI, SPAN = 4 * L, PLACES = R + 2 * SPAN, NC = (PLACES + 255) / 256, TB = 8;
+  constexpr int COUNT = TB * PI, KEPT = kept_of<L, COUNT>();
   __shared__ float ux[2][TB][R];
   __shared__ __align__(16) float ubc[2][TB][2 * SPAN];
   __shared__ float udt[2][TB], uda[2][TB];
-  const int tid = threadIdx.x, i16 = tid & 15, prow = tid >> 4;
+  const int tid = threadIdx.x, i = tid & (L - 1), prow = tid / L, n = 4 * i;
   const int slices = (p.P + R - 1) / R;
   const int h = (int)blockIdx.x / slices, p0 = ((int)blockIdx.x % slices) * R;
   const int g = h / (p.H / p.G);
@@ -172,8 +172,8 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
     for (int k = 0; k < TW; ++k) taps[j][k] = chan[j] >= 0 && k >= TW - p.W ? p.conv_w[(int64_t)chan[j] * p.W + k - (TW - p.W)] : 0.0f;
   }
   // the outputs that are left to this lane: number v is token v / PI, row PI prow + v % PI
-  const int v0 = first_kept<16, COUNT>(i16), t_own = v0 / PI, p_own = prow * PI + v0 % PI;
-  const bool stores = !p.local && (COUNT >= 16 || i16 % (16 / (COUNT < 16 ? COUNT : 16)) == 0);
+  const int v0 = first_kept<L, COUNT>(i);
+  const bool stores = !p.local && i % (COUNT < L ? L / COUNT : 1) == 0;
 
   const int64_t parts = (int64_t)p.n_seq * p.nseg, size = (int64_t)p.P * p.N;
   for (int64_t sx = blockIdx.y; sx < parts; sx += gridDim.y) {
@@ -188,17 +188,15 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
     const float *first = p.nseg > 1 ? mine : slot >= 0 ? p.ssm_in + ((int64_t)slot * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
     float *left = p.local ? mine : pt.last && slot_to >= 0 ? p.ssm_out + ((int64_t)slot_to * p.H + h) * size + (int64_t)p0 * p.N : nullptr;
     if (p.local) first = nullptr;
-    f32x4 S[PI][NK];
+    f32x4 S[PI];
     float log_decay = 0.0f;
     const float fill = slot == -2 && p.nseg == 1 ? __uint_as_float(0x7fc00000u) : 0.0f;
 #pragma unroll
-    for (int k = 0; k < PI; ++k)
-#pragma unroll
-      for (int q = 0; q < NK; ++q) {
-        const int n = 4 * (16 * q + i16), pr = prow * PI + k;
-        S[k][q] = f32x4{fill, fill, fill, fill};
-        if (first && pr < np && n < p.N) S[k][q] = load_n(first + (int64_t)pr * p.N + n, p.N - n);
-      }
+    for (int k = 0; k < PI; ++k) {
+      const int pr = prow * PI + k;
+      S[k] = f32x4{fill, fill, fill, fill};
+      if (first && pr < np && n < p.N) S[k] = load_n(first + (int64_t)pr * p.N + n, p.N - n);
+    }
     float past[NC][TW - 1];
     T raw[NC][TB], raw_z[KEPT], raw_dt = 0;
     // (tokens behind the end: the last one again, taken as zeros)
@@ -228,31 +226,32 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
         if (k >= PLACES) continue;
         float in[TW - 1 + TB];
 #pragma unroll
-        for (int i = 0; i < TW - 1; ++i) in[i] = past[j][i];
+        for (int e = 0; e < TW - 1; ++e) in[e] = past[j][e];
 #pragma unroll
         for (int t = 0; t < TB; ++t) in[TW - 1 + t] = chan[j] >= 0 ? as_f32<T>(raw[j][t]) : 0.0f;
 #pragma unroll
         for (int t = 0; t < TB; ++t) {
           float v = bias[j];
 #pragma unroll
-          for (int i = 0; i < TW; ++i) v = i >= TW - p.W ? fmaf(taps[j][i], in[t + i], v) : v;
+          for (int e = 0; e < TW; ++e) v = e >= TW - p.W ? fmaf(taps[j][e], in[t + e], v) : v;
           v = chan[j] >= 0 && t < nt ? silu(v) : 0.0f;
           if (k < R) ux[buf][t][k] = v;
           else ubc[buf][t][k - R] = v;
         }
 #pragma unroll
-        for (int i = 0; i < TW - 1; ++i) past[j][i] = in[TB + i];
+        for (int e = 0; e < TW - 1; ++e) past[j][e] = in[TB + e];
       }
       if (tid < TB) {
         const float dt = tid < nt ? softplus(as_f32<T>(raw_dt) + bias_dt) : 0.0f;
         udt[buf][tid] = dt;
         uda[buf][tid] = __expf(dt * A);
       }
-      const int64_t row = sp.first + t0 + t_own;
-      if (p.z && stores && t_own < nt) {
+      if (p.z && stores) {
 #pragma unroll
-        for (int e = 0; e < KEPT; ++e)
-          if (p_own + e < np) raw_z[e] = reinterpret_cast<const T *>(p.z)[row * p.ld_z + h * p.P + p0 + p_own + e];
+        for (int e = 0; e < KEPT; ++e) {
+          const int t = (v0 + e) / PI, pr = prow * PI + (v0 + e) % PI;
+          if (t < nt && pr < np) raw_z[e] = reinterpret_cast<const T *>(p.z)[(sp.first + t0 + t) * p.ld_z + h * p.P + p0 + pr];
+        }
       }
       if (t0 + TB < pt.end) ask(t0 + TB);
       __syncthreads();  // (two buffers: nobody writes the one that is read before all have passed the next barrier)
@@ -261,32 +260,35 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
       for (int t = 0; t < TB; ++t) {
         const float dt = udt[buf][t], da = uda[buf][t];
         log_decay = fmaf(dt, A, log_decay);
+        const f32x4 B = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][n]);
 #pragma unroll
-        for (int k = 0; k < PI; ++k) y[t * PI + k] = 0.0f;
+        for (int k = 0; k < PI; ++k) {
+          const float dx = dt * ux[buf][t][prow * PI + k];
 #pragma unroll
-        for (int q = 0; q < NK; ++q) {
-          const f32x4 B = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][4 * (16 * q + i16)]);
-          const f32x4 Cv = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][SPAN + 4 * (16 * q + i16)]);
-#pragma unroll
-          for (int k = 0; k < PI; ++k) {
-            const float dx = dt * ux[buf][t][prow * PI + k];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              S[k][q][j] = fmaf(S[k][q][j], da, dx * B[j]);
-              y[t * PI + k] = fmaf(S[k][q][j], Cv[j], y[t * PI + k]);
-            }
-          }
+          for (int j = 0; j < 4; ++j) S[k][j] = fmaf(S[k][j], da, dx * B[j]);
         }
+        if (p.local) continue;
+        const f32x4 Cv = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][SPAN + n]);
+#pragma unroll
+        for (int k = 0; k < PI; ++k) {
+          y[t * PI + k] = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[t * PI + k] = fmaf(S[k][j], Cv[j], y[t * PI + k]);
+        }
+        // (these sums are made here: moved behind the last token they would keep eight tokens' states in registers)
+#pragma unroll
+        for (int k = 0; k < PI; ++k) asm volatile("" : "+v"(y[t * PI + k]));
       }
       if (p.local) continue;
-      sum_lanes<16, COUNT>(y, i16);
-      if (stores && t_own < nt) {
+      sum_lanes<L, COUNT>(y, i);
+      if (stores) {
 #pragma unroll
         for (int e = 0; e < KEPT; ++e) {
-          if (p_own + e >= np) continue;
-          float v = fmaf(D, ux[buf][t_own][p_own + e], y[e]);
+          const int t = (v0 + e) / PI, pr = prow * PI + (v0 + e) % PI;
+          if (t >= nt || pr >= np) continue;
+          float v = fmaf(D, ux[buf][t][pr], y[e]);
           if (p.z) v *= silu(as_f32<T>(raw_z[e]));
-          store1(reinterpret_cast<T *>(p.out) + row * p.ld_out + h * p.P + p0 + p_own + e, v);
+          store1(reinterpret_cast<T *>(p.out) + (sp.first + t0 + t) * p.ld_out + h * p.P + p0 + pr, v);
         }
       }
     }
@@ -294,12 +296,10 @@ __global__ void __launch_bounds__(256) k_ssm_tokens(const SsmArgs p) {
     if (p.local && tid == 0 && p0 == 0) p.seg_log[sx * p.H + h] = log_decay;
     if (!left) continue;
 #pragma unroll
-    for (int k = 0; k < PI; ++k)
-#pragma unroll
-      for (int q = 0; q < NK; ++q) {
-        const int n = 4 * (16 * q + i16), pr = prow * PI + k;
-        if (pr < np && n < p.N) store_n(left + (int64_t)pr * p.N + n, p.N - n, S[k][q]);
-      }
+    for (int k = 0; k < PI; ++k) {
+      const int pr = prow * PI + k;
+      if (pr < np && n < p.N) store_n(left + (int64_t)pr * p.N + n, p.N - n, S[k]);
+    }
     if (p.local || p.conv_later || p.W == 1) continue;
 #pragma unroll
     for (int j = 0; j < NC; ++j)
@@ -503,26 +503,29 @@ int run_parts(vf_ctx *c, SsmArgs &p, F launch) {
 
 constexpr int SEQ_TOKENS = 8;  // tokens that k_ssm_tokens takes at a time
 
-template <typename T, int PI, int NK>
-int launch_tokens(vf_ctx *c, SsmArgs &p) {
-  const int slices = (p.P + 16 * PI - 1) / (16 * PI);
+template <typename T, int L, int PI>
+int launch_tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
+  constexpr int R = 256 / L * PI;
+  const int slices = (p.P + R - 1) / R;
+  split(c, p, longest, (int64_t)p.n_seq * p.H * slices, 1024, SEQ_TOKENS, 64);
   const int64_t parts = (int64_t)p.n_seq * p.nseg;
   const dim3 grid(p.H * slices, (unsigned)(parts < 32768 ? parts : 32768));
   return run_parts(c, p, [&] {
-    if (p.W <= 4) k_ssm_tokens<T, PI, NK, 4><<<grid, 256, 0, c->stream>>>(p);
-    else k_ssm_tokens<T, PI, NK, 8><<<grid, 256, 0, c->stream>>>(p);
+    if (p.W <= 4) k_ssm_tokens<T, L, PI, 4><<<grid, 256, 0, c->stream>>>(p);
+    else k_ssm_tokens<T, L, PI, 8><<<grid, 256, 0, c->stream>>>(p);
     VF_HIP(c, hipGetLastError());
     return VF_OK;
   });
 }
 template <typename T>
 int tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
-  const int nk = (p.N + 63) / 64;
-  // one slice of 64 rows unless there are too few workgroups for the compute units
-  const bool wide = p.P > 16 && ((int64_t)p.n_seq * p.H >= 512 || longest >= 256);
-  split(c, p, longest, (int64_t)p.n_seq * p.H * (wide ? (p.P + 63) / 64 : (p.P + 15) / 16), 1024, SEQ_TOKENS, 64);
-  if (wide) return nk <= 1 ? launch_tokens<T, 4, 1>(c, p) : nk <= 2 ? launch_tokens<T, 4, 2>(c, p) : launch_tokens<T, 4, 4>(c, p);
-  return nk <= 1 ? launch_tokens<T, 1, 1>(c, p) : nk <= 2 ? launch_tokens<T, 1, 2>(c, p) : launch_tokens<T, 1, 4>(c, p);
+  // 64 rows p a workgroup (32 of more than 128 numbers n), or a thread's one row where there are too few workgroups for the compute units
+  const bool wide = (int64_t)p.n_seq * p.H * ((p.P + 63) / 64) >= 512 || longest >= 256;
+  if (p.N <= 16) return launch_tokens<T, 4, 1>(c, p, longest);
+  if (p.N <= 32) return wide ? launch_tokens<T, 8, 2>(c, p, longest) : launch_tokens<T, 8, 1>(c, p, longest);
+  if (p.N <= 64) return wide ? launch_tokens<T, 16, 4>(c, p, longest) : launch_tokens<T, 16, 1>(c, p, longest);
+  if (p.N <= 128) return wide ? launch_tokens<T, 32, 8>(c, p, longest) : launch_tokens<T, 32, 1>(c, p, longest);
+  return wide ? launch_tokens<T, 64, 8>(c, p, longest) : launch_tokens<T, 64, 1>(c, p, longest);
 }
 
 template <typename T, int L, int PI>
