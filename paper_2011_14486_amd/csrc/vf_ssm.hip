@@ -595,6 +595,7 @@ __device__ __forceinline__ uint32_t rest_h(float a, float b, uint32_t hi) {
 __device__ __forceinline__ uint32_t rest_b(float a, float b, uint32_t hi) {
   return pack2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
 }
+__device__ __forceinline__ bool is_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 // 2^k that brings a magnitude below 2^15, and its reciprocal; k is cut where either would leave the normal numbers
 __device__ __forceinline__ float scale_to_f16(float top) {
   const int e = (int)(__float_as_uint(top) >> 23);
@@ -662,9 +663,9 @@ __device__ __forceinline__ void convolve(const uint2 (&raw)[TB + 3], int k, cons
     v[t] = s * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s));
   }
 }
-// The largest magnitude, as bits, of TB numbers in each of 32 / TB neighbouring lanes (magnitudes compare as integers).
+// The largest magnitude, as bits, of TB numbers in each of 32 / TB neighbouring lanes (magnitudes compare as integers); NaN if one is.
 __device__ __forceinline__ uint32_t max_abs(uint32_t a, float b, float c) {
-  asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(a) : "v"(a), "v"(b), "v"(c));
+  asm("v_maximum3_f32 %0, %1, |%2|, |%3|" : "=v"(a) : "v"(a), "v"(b), "v"(c));
   return a;
 }
 template <int CTRL>
@@ -721,13 +722,14 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
   constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT, NW = ROWS / PS;
   // Tokens of B and C that a thread takes at a time, so that there is one piece of x and one of B and C for a thread, or one of either
   constexpr int TB = PT == 4 ? 4 : 8;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // (what goes by the wave is held once, not per lane)
   uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + bt_size(NP);
   float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));
   float *Xall = bscale + NP, *xsall = Xall + NW * PS * XS, *wl = xsall + NW * PS, *bl = wl + 4 * (2 * NP + NW * PS);
   int *chans = reinterpret_cast<int *>(bl + 2 * NP + NW * PS);
   float *cum = bl + 2 * (2 * NP + NW * PS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
-  const float *X = Xall + wave * PS * XS, *xs = xsall + wave * PS;
+  float *X = Xall + wave * PS * XS, *xs = xsall + wave * PS;
 
   const int slices = (p.P + PS - 1) / PS, jobs = p.H / p.G * slices, per = (jobs + nw - 1) / nw, each = per * p.G;
   // Workgroups of one part share B and C: they get neighbouring places on one of the eight dies, to which the hardware
@@ -963,7 +965,24 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
     }
     __syncthreads();
     if (!on) continue;
+    // (from here on addresses are made again for every chunk: kept in registers over the loop they would displace the state)
+    int own_lane = tid & 63;
+    asm volatile("" : "+v"(own_lane));
+    const int lane = own_lane, r = lane & 15, q = lane >> 4;
 
+    // A number of x that is not finite would, times the zeros of the matrix of tokens, reach the outputs before its own.  It is taken as
+    // zero here; behind the outputs those of its row, from its token on, are set to NaN, and it is put back for the state.
+    const bool odd = !LOCAL && __any(lane < PS && !is_finite(xs[lane & (PS - 1)]));
+    if (odd && lane < PS && !is_finite(xs[lane])) {
+      int from = Q;
+#pragma unroll 1
+      for (int t = Q - 1; t >= 0; --t)
+        if (!is_finite(X[lane * XS + t])) {
+          X[lane * XS + t] = 0.0f;
+          from = t;
+        }
+      xs[lane] = __uint_as_float(0x7fc00000u | (uint32_t)from);
+    }
     if constexpr (!LOCAL) {
       f32x4 G[3];  // rows s, columns t: (0, 0), (0, 1), (1, 1)
 #pragma unroll
@@ -979,29 +998,8 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
       const f32x4 cs0 = *reinterpret_cast<const f32x4 *>(cum + 4 * q), cs1 = *reinterpret_cast<const f32x4 *>(cum + 16 + 4 * q);
       const f32x4 st0 = *reinterpret_cast<const f32x4 *>(stp + 4 * q), st1 = *reinterpret_cast<const f32x4 *>(stp + 16 + 4 * q);
       const float ct0 = cum[r], ct1 = cum[16 + r];
-      f32x4 y[2][PT];  // rows p, columns t
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int k = 0; k < PT; ++k) y[j][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (t0 > part.begin || first || lost) {  // (otherwise the state is zero)
-        const float e0 = __expf(ct0) * -LN2, e1 = __expf(ct1) * -LN2;
-#pragma unroll
-        for (int k = 0; k < KN; ++k) {
-          const bf16x8 c0 = as_b(frag_acc(Cs + r * NS + 32 * k, q)), c1 = as_b(frag_acc(Cs + (16 + r) * NS + 32 * k, q));
-#pragma unroll
-          for (int j = 0; j < PT; ++j) {
-            const bf16x8 f = as_b(frag_of(S[2 * k][j], S[2 * k + 1][j]));
-            y[0][j] = VF_MFMA_B(f, c0, y[0][j]);
-            y[1][j] = VF_MFMA_B(f, c1, y[1][j]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < PT; ++j) {
-          y[0][j] *= e0;
-          y[1][j] *= e1;
-        }
-      }
+      const bool behind = t0 > part.begin || first || lost;  // (otherwise the state is zero)
+      const float e0 = __expf(ct0) * -LN2, e1 = __expf(ct1) * -LN2;
       f32x4 m00, m01, m11;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -1014,23 +1012,34 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
       }
       const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
       const uint4 f0 = frag_of(m00, zero), f1 = frag_of(m01, m11), g0 = rest_of(m00, zero, f0), g1 = rest_of(m01, m11, f1);
+      const Rows om = rows_of(p.out, sp.first, p.ld_out, t0, end);
+      // 16 rows p after the other, so that only theirs are in registers
 #pragma unroll
       for (int j = 0; j < PT; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 y[2] = {zero, zero};  // rows p, columns t
+        if (behind) {
+#pragma unroll
+          for (int k = 0; k < KN; ++k) {
+            const bf16x8 c0 = as_b(frag_acc(Cs + r * NS + 32 * k, q)), c1 = as_b(frag_acc(Cs + (16 + r) * NS + 32 * k, q));
+            const bf16x8 f = as_b(frag_of(S[2 * k][j], S[2 * k + 1][j]));
+            y[0] = VF_MFMA_B(f, c0, y[0]);
+            y[1] = VF_MFMA_B(f, c1, y[1]);
+          }
+          y[0] *= e0;
+          y[1] *= e1;
+        }
         const f32x4 xa = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q), xb = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q);
         const uint4 xh = frag_of(xa, xb), xl = rest_of(xa, xb, xh);
-        y[0][j] = VF_MFMA_B(as_b(xl), as_b(f0), y[0][j]);
-        y[1][j] = VF_MFMA_B(as_b(xl), as_b(f1), y[1][j]);
-        y[0][j] = VF_MFMA_B(as_b(xh), as_b(g0), y[0][j]);
-        y[1][j] = VF_MFMA_B(as_b(xh), as_b(g1), y[1][j]);
-        y[0][j] = VF_MFMA_B(as_b(xh), as_b(f0), y[0][j]);
-        y[1][j] = VF_MFMA_B(as_b(xh), as_b(f1), y[1][j]);
-      }
-      const Rows om = rows_of(p.out, sp.first, p.ld_out, t0, end);
+        y[0] = VF_MFMA_B(as_b(xl), as_b(f0), y[0]);
+        y[1] = VF_MFMA_B(as_b(xl), as_b(f1), y[1]);
+        y[0] = VF_MFMA_B(as_b(xh), as_b(g0), y[0]);
+        y[1] = VF_MFMA_B(as_b(xh), as_b(g1), y[1]);
+        y[0] = VF_MFMA_B(as_b(xh), as_b(f0), y[0]);
+        y[1] = VF_MFMA_B(as_b(xh), as_b(f1), y[1]);
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int j = 0; j < PT; ++j) {
-          f32x4 v = y[t][j];
+        for (int t = 0; t < 2; ++t) {
+          f32x4 v = y[t];
           if (p.z) {
             const uint32_t z4[2] = {zr[t][j].x, zr[t][j].y};
 #pragma unroll
@@ -1038,6 +1047,17 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
           }
           if (16 * j < np) store4(om, t0 + 16 * t + r, 2 * (h * p.P + p0 + 16 * j + 4 * q), make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])));
         }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+
+    if (odd && lane < PS && !is_finite(xs[lane])) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const int from = (int)(__float_as_uint(xs[lane]) & 63);
+#pragma unroll 1
+      for (int t = from; t < Q && t0 + t < end; ++t)
+        reinterpret_cast<uint16_t *>(p.out)[(sp.first + t0 + t) * p.ld_out + h * p.P + p0 + lane] = 0x7fc0;
+      if (from < Q) X[lane * XS + from] = __uint_as_float(0x7fc00000u);
     }
 
     // the state behind the chunk

@@ -246,6 +246,42 @@ def test_nan_and_large_steps_stay_where_they_are(vf, ctx, kind, sizes):
     assert bool(hurt[60, :1].isnan().all())
 
 
+@pytest.mark.parametrize("sizes", [(4, 64, 1, 64, 4), (2, 64, 1, 128, 4), (3, 48, 1, 32, 2), (1, 16, 1, 256, 4)], ids=str)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")], ids=str)
+@pytest.mark.parametrize("lens", [[100], [70, 40]], ids=str)
+def test_what_is_not_finite_reaches_no_token_before_its_own(vf, ctx, sizes, value, lens):
+    """In chunks: x, B, C, step or gate of one token; outputs before it are as without, and from it on NaN or infinite where the
+    formulas have it."""
+    import torch
+    H, P, G, N, W = sizes
+    c = Case(vf, sizes, lens, "bf16", seed=5)
+    args = dict(n_seq=len(lens), longest=max(lens), offsets=c.offsets)
+    clean = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, **args)
+    for part, col, at in ((c.xbc, 5, 45), (c.xbc, H * P - 1, 33), (c.xbc, H * P + 3, 50), (c.xbc, H * P + G * N + 2, 20), (c.dt, 0, 41),
+                          (c.z, 7, 35)):
+        if part is c.dt and value < 0:
+            continue    # a step of zero
+        kept = part[at, col].clone()
+        part[at, col] = value
+        hurt = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, **args)
+        part[at, col] = kept
+        assert torch.equal(hurt[:at], clean[:at])
+        assert torch.equal(hurt[lens[0]:], clean[lens[0]:])
+        if part is c.z:
+            got = torch.ones_like(hurt[at], dtype=torch.bool)
+            got[col] = False
+            assert torch.equal(hurt[at][got], clean[at][got]) and torch.equal(hurt[at + 1:], clean[at + 1:])
+            if value > 0 or value != value:
+                assert not bool(hurt[at, col].isfinite())
+        elif part is c.xbc and col < H * P:
+            others = torch.ones(H * P, dtype=torch.bool, device="cuda")
+            others[col] = False
+            assert torch.equal(hurt[:, others], clean[:, others])
+            if value > 0 or value != value:
+                lasting = hurt[at:lens[0], col]
+                assert not bool(lasting.isfinite().any())
+
+
 def test_no_sequences_and_empty_ones(vf, ctx):
     import torch
     c = Case(vf, (2, 16, 1, 32, 4), [5], "bf16", slots=3)
