@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
   auto ask_scales = [&](int st) {
     const int b0 = 4 * st, from = b0 + 16 <= p.kb ? b0 : p.kb - 16, sh = b0 - from < 15 ? 8 * (b0 - from) : 120;
     const u16x8 v = *reinterpret_cast<const u16x8 *>(src_s + from);
-    const uint64_t one = 0x7f7f7f7f7f7f7f7full, lo = v.w[0] | (uint64_t)v.w[1] << 32, hi = v.w[2] | (uint64_t)v.w[3] << 32;
+    const uint64_t one = 0x7f7f7f7f7f7f7f7full, lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
     const uint64_t in = sh & 63 ? ~0ull : 0;  // (a shift by 64 is none)
     const uint64_t lo1 = sh < 64 ? lo : hi, hi1 = sh < 64 ? hi : one;
     const uint64_t a = lo1 >> (sh & 63) | (hi1 << (64 - (sh & 63) & 63) & in), b = hi1 >> (sh & 63) | (one << (64 - (sh & 63) & 63) & in);

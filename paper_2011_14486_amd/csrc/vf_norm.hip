@@ -25,14 +25,35 @@ template <> struct out_elem<VF_FP32> { typedef float type; };
 template <> struct out_elem<VF_BF16> { typedef uint16_t type; };
 
 // NCH chunks of eight columns per thread, chunk k of a thread at columns 8 (k tpr + t).  The threads of a row are a
-// power of two of them, whole waves; a workgroup holds blockDim / tpr rows.
+// power of two of them, whole waves; a workgroup holds blockDim / tpr rows at a time and takes several, one after the other: its
+// threads keep their gains, and the next row is on its way while this one is summed.
 template <typename T, int OUT, int NCH>
 __global__ void __launch_bounds__(1024) k_rms_norm(const NormArgs a) {
-  __shared__ float part[16];
+  __shared__ float part[2][16];
   const int t = (int)threadIdx.x & (a.tpr - 1), rpw = (int)blockDim.x / a.tpr, r0 = (int)threadIdx.x / a.tpr;
   const int waves = a.tpr >> 6, wave = (int)threadIdx.x >> 6;
   const int nchunk = OUT >= VF_E4M3 ? 4 * a.kb : (a.width + 7) >> 3;
-  for (int64_t base = (int64_t)blockIdx.x * rpw; base < a.rows; base += (int64_t)gridDim.x * rpw) {
+  float gain[NCH][8];
+#pragma unroll
+  for (int k = 0; k < NCH; ++k) {
+    const int c = k * a.tpr + t, n = a.width - 8 * c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gain[k][i] = 1.0f;
+    if (a.gain && n > 0) load_upto8(a.gain + 8 * c, n, gain[k]);
+  }
+  raw8<T> x[NCH], res[NCH];
+  auto ask = [&](int64_t row) {
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) {
+      const int c = k * a.tpr + t, n = row < a.rows ? a.width - 8 * c : 0;
+      if (n <= 0) continue;
+      fetch8(reinterpret_cast<const T *>(a.x) + row * a.ld_x + 8 * c, n, x[k]);
+      if (a.res) fetch8(reinterpret_cast<const T *>(a.res) + row * a.ld_res + 8 * c, n, res[k]);
+    }
+  };
+  int64_t base = (int64_t)blockIdx.x * rpw;
+  ask(base + r0);
+  for (int turn = 0; base < a.rows; ++turn) {
     const int64_t row = base + r0;
     const bool live = row < a.rows;
     float v[NCH][8];
@@ -40,43 +61,43 @@ __global__ void __launch_bounds__(1024) k_rms_norm(const NormArgs a) {
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = k * a.tpr + t, n = live ? a.width - 8 * c : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
       if (n > 0) {
-        load_upto8(reinterpret_cast<const T *>(a.x) + row * a.ld_x + 8 * c, n, v[k]);
+        unpack8(x[k], v[k]);
         if (a.res) {
           float r[8];
-          load_upto8(reinterpret_cast<const T *>(a.res) + row * a.ld_res + 8 * c, n, r);
+          unpack8(res[k], r);
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[k][i] += r[i];
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(v[k][i], v[k][i], ss);
     }
+    base += (int64_t)gridDim.x * rpw;
+    ask(base + r0);
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = k * a.tpr + t, n = live ? a.width - 8 * c : 0;
       if (a.sum && n > 0) store_upto8(reinterpret_cast<T *>(a.sum) + row * a.ld_sum + 8 * c, n, v[k]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(v[k][i], v[k][i], ss);
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) ss += __shfl_xor(ss, m);
-    if (waves > 1) {  // (uniform over the launch)
-      if ((threadIdx.x & 63) == 0) part[wave] = ss;
+    if (waves > 1) {  // (uniform over the launch; two arrays: one barrier a row)
+      float *sums = part[turn & 1];
+      if ((threadIdx.x & 63) == 0) sums[wave] = ss;
       __syncthreads();
       ss = 0.0f;
-      for (int w = 0; w < waves; ++w) ss += part[r0 * waves + w];
-      __syncthreads();
+      for (int w = 0; w < waves; ++w) ss += sums[r0 * waves + w];
     }
     const float f = 1.0f / sqrtf(ss / (float)a.width + a.eps);
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = k * a.tpr + t, n = a.width - 8 * c;
-      float y[8], g[8];
-      if (a.gain && n > 0) load_upto8(a.gain + 8 * c, n, g);
+      float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = i < n ? v[k][i] * f * (a.gain ? g[i] : 1.0f) : 0.0f;
+      for (int i = 0; i < 8; ++i) y[i] = i < n ? v[k][i] * f * gain[k][i] : 0.0f;
       const bool on = live && c < nchunk;
       if constexpr (OUT >= VF_E4M3) {
         quantize_chunk<OUT>(y, c, on, reinterpret_cast<uint8_t *>(a.out) + row * a.kb * mx<OUT>::bytes32, a.scales + row * a.kb);
@@ -122,7 +143,9 @@ int vfk_rms_norm(vf_ctx *c, int type, const void *x, int64_t ld_x, const void *r
   a.tpr = tpr;
   const int block = tpr < 256 ? 256 : tpr, rpw = block / tpr;
   const int64_t groups = (rows + rpw - 1) / rpw;
-  const int grid = (int)(groups < (1 << 20) ? groups : (1 << 20));
+  // as many workgroups as run at a time (2048 threads on each of 256 compute units)
+  const int64_t at_once = 256 * 2048 / block;
+  const int grid = (int)(groups < at_once ? groups : at_once);
   if (type == VF_BF16) launch_out<uint16_t>(c->stream, a, out_type, nch, grid, block);
   else launch_out<float>(c->stream, a, out_type, nch, grid, block);
   VF_HIP(c, hipGetLastError());

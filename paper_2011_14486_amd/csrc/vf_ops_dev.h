@@ -25,16 +25,15 @@ __device__ __forceinline__ float bf16_f32(uint16_t b) { return __uint_as_float((
 
 // Eight elements at an address that is aligned to one element only: global memory takes wide accesses at
 // any alignment, so that odd widths and row distances need no path of their own.
-struct __attribute__((packed, aligned(2))) u16x8 { uint32_t w[4]; };
-struct __attribute__((packed, aligned(2))) u16x4 { uint32_t w[2]; };
+typedef uint32_t u16x8 __attribute__((ext_vector_type(4), aligned(2)));
 struct __attribute__((packed, aligned(4))) f32v4 { float v[4]; };
 
 __device__ __forceinline__ void load8(const uint16_t *p, float (&v)[8]) {
   const u16x8 q = *reinterpret_cast<const u16x8 *>(p);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(q.w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(q.w[i] & 0xffff0000u);
+    v[2 * i] = __uint_as_float(q[i] << 16);
+    v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
   }
 }
 __device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
@@ -47,6 +46,42 @@ __device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
 }
 __device__ __forceinline__ float load1(const uint16_t *p) { return bf16_f32(*p); }
 __device__ __forceinline__ float load1(const float *p) { return *p; }
+// Eight elements as they are in memory, fetched before they are needed; the last n of a row with zeros behind them.
+template <typename T> struct raw8 { uint32_t w[2 * sizeof(T)]; };
+__device__ __forceinline__ void fetch8(const uint16_t *p, int n, raw8<uint16_t> &r) {
+  if (n >= 8) {
+    const u16x8 q = *reinterpret_cast<const u16x8 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = q[i];
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.w[i] = (2 * i < n ? p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+}
+__device__ __forceinline__ void fetch8(const float *p, int n, raw8<float> &r) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (n >= 4 * h + 4) {
+      const f32v4 q = reinterpret_cast<const f32v4 *>(p)[h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.w[4 * h + i] = __float_as_uint(q.v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.w[4 * h + i] = 4 * h + i < n ? __float_as_uint(p[4 * h + i]) : 0u;
+    }
+  }
+}
+__device__ __forceinline__ void unpack8(const raw8<uint16_t> &r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(r.w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack8(const raw8<float> &r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+}
 // elements 0..n-1 of eight, zeros behind them
 template <typename T>
 __device__ __forceinline__ void load_upto8(const T *p, int n, float (&v)[8]) {
@@ -61,7 +96,7 @@ __device__ __forceinline__ void load_upto8(const T *p, int n, float (&v)[8]) {
 __device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {
   u16x8 q;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) q.w[i] = pack2(v[2 * i], v[2 * i + 1]);
+  for (int i = 0; i < 4; ++i) q[i] = pack2(v[2 * i], v[2 * i + 1]);
   *reinterpret_cast<u16x8 *>(p) = q;
 }
 __device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
