@@ -33,13 +33,19 @@ __global__ void __launch_bounds__(1024) k_rms_norm(const NormArgs a) {
   const int t = (int)threadIdx.x & (a.tpr - 1), rpw = (int)blockDim.x / a.tpr, r0 = (int)threadIdx.x / a.tpr;
   const int waves = a.tpr >> 6, wave = (int)threadIdx.x >> 6;
   const int nchunk = OUT >= VF_E4M3 ? 4 * a.kb : (a.width + 7) >> 3;
-  float gain[NCH][8];
-#pragma unroll
-  for (int k = 0; k < NCH; ++k) {
+  constexpr bool AHEAD = NCH < 4;  // (rows of more than 16,384 leave no registers for it)
+  auto gain_of = [&](int k, float (&v)[8]) {
     const int c = k * a.tpr + t, n = a.width - 8 * c;
+    raw8<float> g;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) gain[k][i] = 1.0f;
-    if (a.gain && n > 0) load_upto8(a.gain + 8 * c, n, gain[k]);
+    for (int i = 0; i < 8; ++i) g.w[i] = __float_as_uint(1.0f);
+    if (a.gain && n > 0) fetch8(a.gain + 8 * c, n, g);
+    unpack8(g, v);
+  };
+  float gain[AHEAD ? NCH : 1][8];
+  if constexpr (AHEAD) {
+#pragma unroll
+    for (int k = 0; k < NCH; ++k) gain_of(k, gain[k]);
   }
   raw8<T> x[NCH], res[NCH];
   auto ask = [&](int64_t row) {
@@ -52,10 +58,11 @@ __global__ void __launch_bounds__(1024) k_rms_norm(const NormArgs a) {
     }
   };
   int64_t base = (int64_t)blockIdx.x * rpw;
-  ask(base + r0);
+  if (AHEAD) ask(base + r0);
   for (int turn = 0; base < a.rows; ++turn) {
     const int64_t row = base + r0;
     const bool live = row < a.rows;
+    if (!AHEAD) ask(row);
     float v[NCH][8];
     float ss = 0.0f;
 #pragma unroll
@@ -76,7 +83,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm(const NormArgs a) {
       for (int i = 0; i < 8; ++i) ss = fmaf(v[k][i], v[k][i], ss);
     }
     base += (int64_t)gridDim.x * rpw;
-    ask(base + r0);
+    if (AHEAD) ask(base + r0);
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
       const int c = k * a.tpr + t, n = live ? a.width - 8 * c : 0;
@@ -96,8 +103,9 @@ __global__ void __launch_bounds__(1024) k_rms_norm(const NormArgs a) {
     for (int k = 0; k < NCH; ++k) {
       const int c = k * a.tpr + t, n = a.width - 8 * c;
       float y[8];
+      if constexpr (!AHEAD) gain_of(k, gain[0]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = i < n ? v[k][i] * f * gain[k][i] : 0.0f;
+      for (int i = 0; i < 8; ++i) y[i] = i < n ? v[k][i] * f * gain[AHEAD ? k : 0][i] : 0.0f;
       const bool on = live && c < nchunk;
       if constexpr (OUT >= VF_E4M3) {
         quantize_chunk<OUT>(y, c, on, reinterpret_cast<uint8_t *>(a.out) + row * a.kb * mx<OUT>::bytes32, a.scales + row * a.kb);
