@@ -125,6 +125,7 @@ class Context:
         self.device = torch.device("cuda", device)
         with torch.cuda.device(self.device):
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self.index, self.raw_stream = device, self.stream.cuda_stream
         h = C.c_void_p()
         rc = lib().vf_create(C.byref(h), device, C.c_void_p(self.stream.cuda_stream))
         self.handle = h if rc == VF_OK else None
@@ -388,17 +389,20 @@ def _addr(t):
 
 def _rows_of(ctx, t, rows, cols, dtype, name):
     """Checks a matrix [rows][cols]; returns the distance of its rows."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype or t.device != ctx.device:
+    if t.shape != (rows, cols) or t.dtype != dtype or t.device != ctx.device:
         _fail(f"{name}: {dtype} [{rows}][{cols}] on {ctx.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         _fail(f"{name}: the last dimension has to be dense")
-    return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    return ld if rows > 1 or ld > cols else cols
 
 
 def _vector(ctx, t, n, name, dtype=None):
-    if t is not None and (t.dtype != (dtype or ctx.torch.float32) or t.numel() != n or not t.is_contiguous() or t.device != ctx.device):
+    if t is None:
+        return None
+    if t.dtype != (dtype or ctx.torch.float32) or t.numel() != n or not t.is_contiguous() or t.device != ctx.device:
         _fail(f"{name}: {n} dense values of {dtype or ctx.torch.float32} on {ctx.device} are wanted")
-    return _addr(t)
+    return t.data_ptr()
 
 
 def _mx_shape(fmt, cols):
@@ -410,12 +414,21 @@ def _mx_shape(fmt, cols):
 
 
 def _mx_check(ctx, m, name):
-    rows = m.codes.shape[0]
-    nb, kb = _mx_shape(m.fmt, m.cols)
-    for t, n in ((m.codes, nb), (m.scales, kb)):
-        if t.dtype != ctx.torch.uint8 or t.shape != (rows, n) or not t.is_contiguous() or t.device != ctx.device:
-            _fail(f"{name}: codes [{rows}][{nb}] and scales [{rows}][{kb}] as dense uint8 on {ctx.device} are wanted")
+    codes, scales, fmt, cols = m
+    rows = codes.shape[0]
+    nb, kb = _mx_shape(fmt, cols)
+    u8, dev = ctx.torch.uint8, ctx.device
+    if (codes.dtype != u8 or codes.shape != (rows, nb) or not codes.is_contiguous() or codes.device != dev or
+            scales.dtype != u8 or scales.shape != (rows, kb) or not scales.is_contiguous() or scales.device != dev):
+        _fail(f"{name}: codes [{rows}][{nb}] and scales [{rows}][{kb}] as dense uint8 on {dev} are wanted")
     return rows
+
+
+def _out(ctx, out, rows, cols, dtype):
+    """The caller's matrix or a new one, and the distance of its rows."""
+    if out is None:
+        return ctx.empty((rows, cols), dtype), cols
+    return out, _rows_of(ctx, out, rows, cols, dtype, "out")
 
 
 def _mx_empty(ctx, rows, cols, fmt):
@@ -427,7 +440,7 @@ def _mx_empty(ctx, rows, cols, fmt):
 def _call(ctx, fn, args, tensors):
     """Runs a library call on the context's stream, ordered with torch's current one."""
     torch = ctx.torch
-    if torch._C._cuda_getCurrentRawStream(ctx.device.index) == ctx.stream.cuda_stream:
+    if torch._C._cuda_getCurrentRawStream(ctx.index) == ctx.raw_stream:
         _check(ctx, fn(ctx.handle, *args))
         return
     here = torch.cuda.current_stream(ctx.device)
@@ -450,19 +463,22 @@ def vf_rms_norm(ctx, x, gain=None, eps=1e-5, residual=None, sum_out=None, out_ty
     rows, width = x.shape
     ld_x = _rows_of(ctx, x, rows, width, x.dtype, "x")
     ld_r = _rows_of(ctx, residual, rows, width, x.dtype, "residual") if residual is not None else 0
-    if residual is not None and sum_out is None:
-        sum_out = ctx.empty((rows, width), x.dtype)
-    ld_s = _rows_of(ctx, sum_out, rows, width, x.dtype, "sum_out") if sum_out is not None else 0
+    if sum_out is not None:
+        ld_s = _rows_of(ctx, sum_out, rows, width, x.dtype, "sum_out")
+    elif residual is not None:
+        sum_out, ld_s = ctx.empty((rows, width), x.dtype), width
+    else:
+        ld_s = 0
     out_type = kind if out_type is None else out_type
     if out_type in (VF_E4M3, VF_E2M1):
-        out = _mx_empty(ctx, rows, width, out_type) if out is None else out
-        if _mx_check(ctx, out, "out") != rows or out.fmt != out_type or out.cols != width:
+        if out is None:
+            out = _mx_empty(ctx, rows, width, out_type)
+        elif _mx_check(ctx, out, "out") != rows or out.fmt != out_type or out.cols != width:
             _fail("out: another shape or format")
         codes, scales, ld_o = out.codes, out.scales, 0
     else:
-        dtype = _dtype_of(torch, out_type)
-        out = ctx.empty((rows, width), dtype) if out is None else out
-        codes, scales, ld_o = out, None, _rows_of(ctx, out, rows, width, dtype, "out")
+        out, ld_o = _out(ctx, out, rows, width, _dtype_of(torch, out_type))
+        codes, scales = out, None
     g = _vector(ctx, gain, width, "gain")
     _call(ctx, lib().vf_rms_norm, (kind, _addr(x), ld_x, _addr(residual), ld_r, g, eps, rows, width, _addr(sum_out), ld_s, out_type,
                                    _addr(codes), ld_o, _addr(scales)), (x, residual, gain, sum_out, codes, scales))
@@ -474,9 +490,12 @@ def vf_mx_quantize(ctx, x, fmt, out=None):
     rows, cols = x.shape
     kind = _type_of(ctx.torch, x)
     ld = _rows_of(ctx, x, rows, cols, x.dtype, "x")
-    q = _mx_empty(ctx, rows, cols, fmt) if out is None else out
-    if _mx_check(ctx, q, "out") != rows or q.fmt != fmt or q.cols != cols:
-        _fail("out: another shape or format")
+    if out is None:
+        q = _mx_empty(ctx, rows, cols, fmt)
+    else:
+        q = out
+        if _mx_check(ctx, q, "out") != rows or q.fmt != fmt or q.cols != cols:
+            _fail("out: another shape or format")
     _call(ctx, lib().vf_mx_quantize, (kind, _addr(x), ld, rows, cols, fmt, _addr(q.codes), _addr(q.scales)), (x, q.codes, q.scales))
     return q
 
@@ -484,9 +503,7 @@ def vf_mx_quantize(ctx, x, fmt, out=None):
 def vf_mx_dequantize(ctx, q, out_type=VF_BF16, out=None):
     """The values of a microscaled matrix, [rows][cols]."""
     rows = _mx_check(ctx, q, "q")
-    dtype = _dtype_of(ctx.torch, out_type)
-    out = ctx.empty((rows, q.cols), dtype) if out is None else out
-    ld = _rows_of(ctx, out, rows, q.cols, dtype, "out")
+    out, ld = _out(ctx, out, rows, q.cols, _dtype_of(ctx.torch, out_type))
     _call(ctx, lib().vf_mx_dequantize, (q.fmt, _addr(q.codes), _addr(q.scales), rows, q.cols, out_type, _addr(out), ld),
           (q.codes, q.scales, out))
     return out
@@ -497,9 +514,7 @@ def vf_mx_matmul(ctx, a, w, bias=None, out_type=VF_BF16, out=None):
     M, N = _mx_check(ctx, a, "a"), _mx_check(ctx, w, "w")
     if w.fmt != VF_E2M1 or a.cols != w.cols:
         _fail("w: VF_E2M1 with the columns of a is wanted")
-    dtype = _dtype_of(ctx.torch, out_type)
-    out = ctx.empty((M, N), dtype) if out is None else out
-    ld = _rows_of(ctx, out, M, N, dtype, "out")
+    out, ld = _out(ctx, out, M, N, _dtype_of(ctx.torch, out_type))
     b = _vector(ctx, bias, N, "bias")
     _call(ctx, lib().vf_mx_matmul, (a.fmt, _addr(a.codes), _addr(a.scales), _addr(w.codes), _addr(w.scales), M, N, a.cols, b, out_type,
                                     _addr(out), ld), (a.codes, a.scales, w.codes, w.scales, bias, out))
@@ -555,9 +570,9 @@ def _ssm_state(ctx, layer, state, slots, n_seq, dtype, name):
         return 0, None, None, None
     conv, ssm = state
     n = ssm.shape[0]
-    if tuple(conv.shape) != (n, layer.channels, layer.taps - 1) or conv.dtype != dtype or not conv.is_contiguous():
+    if conv.shape != (n, layer.channels, layer.taps - 1) or conv.dtype != dtype or not conv.is_contiguous():
         _fail(f"{name}: a dense {dtype} [{n}][{layer.channels}][{layer.taps - 1}] is wanted for the convolution")
-    if tuple(ssm.shape[1:]) != (layer.heads, layer.head_dim, layer.n_state) or ssm.dtype != ctx.torch.float32 or not ssm.is_contiguous():
+    if ssm.shape != (n, layer.heads, layer.head_dim, layer.n_state) or ssm.dtype != ctx.torch.float32 or not ssm.is_contiguous():
         _fail(f"{name}: a dense float32 [slots][{layer.heads}][{layer.head_dim}][{layer.n_state}] is wanted")
     if conv.device != ctx.device or ssm.device != ctx.device:
         _fail(f"{name}: buffers on {ctx.device} are wanted")
@@ -570,11 +585,10 @@ def _ssm_call(ctx, fn, layer, xbc, dt, z, n_seq, longest, offsets, state, slots,
         _fail("the layer's weights are on another GPU")
     kind, dtype, tokens = _type_of(torch, xbc), xbc.dtype, xbc.shape[0]
     inner = layer.heads * layer.head_dim
-    out = ctx.empty((tokens, inner), dtype) if out is None else out
+    out, ld_o = _out(ctx, out, tokens, inner, dtype)
     ld_x = _rows_of(ctx, xbc, tokens, layer.channels, dtype, "xbc")
     ld_dt = _rows_of(ctx, dt, tokens, layer.heads, dtype, "dt")
     ld_z = _rows_of(ctx, z, tokens, inner, dtype, "z") if z is not None else 0
-    ld_o = _rows_of(ctx, out, tokens, inner, dtype, "out")
     off = _vector(ctx, offsets, n_seq + 1, "offsets", torch.int32)
     n_in, conv_in, ssm_in, s_in = _ssm_state(ctx, layer, state, slots, n_seq, dtype, "state")
     n_out, conv_out, ssm_out, s_out = _ssm_state(ctx, layer, state_out, slots_out, n_seq, dtype, "state_out")

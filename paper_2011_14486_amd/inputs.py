@@ -297,6 +297,26 @@ def lstm_param_count(F, H):
     return 4 * H * F + 4 * H * H + 8 * H + H + 1
 
 
+def ssm_weights(F, width, blocks, heads, head_dim=64, groups=1, n_state=64, taps=4, seed=0):
+    """State-space value network: a dict of its sizes and, as fp32 arrays, w_in [width][F]; per block gain [width],
+    w_proj [2 H P + 2 G N + H][width] (rows: gate, x, B, C, steps), the scan layer (conv_w, conv_b, a, d, dt_bias),
+    gain_out [H P], w_out [width][H P]; gain [width], w_head [1][width], b_head [1]."""
+    rng = np.random.default_rng([seed, F, width, blocks, heads])
+    inner, C = heads * head_dim, heads * head_dim + 2 * groups * n_state
+    f32 = lambda v: np.asarray(v, np.float32)   # noqa: E731
+    made = []
+    for _ in range(blocks):
+        step = np.exp(rng.uniform(np.log(0.001), np.log(0.1), heads))
+        made.append(dict(
+            gain=f32(1 + 0.2 * rng.standard_normal(width)), w_proj=f32(rng.standard_normal((inner + C + heads, width)) / np.sqrt(width)),
+            conv_w=f32(rng.uniform(-1, 1, (C, taps)) / np.sqrt(taps)), conv_b=f32(rng.uniform(-1, 1, C) / np.sqrt(taps)),
+            a=f32(-rng.uniform(1, 16, heads)), d=f32(1 + 0.2 * rng.standard_normal(heads)), dt_bias=f32(np.log(np.expm1(step))),
+            gain_out=f32(1 + 0.2 * rng.standard_normal(inner)), w_out=f32(rng.standard_normal((width, inner)) / np.sqrt(inner))))
+    return dict(heads=heads, head_dim=head_dim, groups=groups, n_state=n_state, blocks=made,
+                w_in=f32(rng.standard_normal((width, F)) / np.sqrt(F)), gain=f32(1 + 0.2 * rng.standard_normal(width)),
+                w_head=f32(rng.standard_normal((1, width)) / np.sqrt(width)), b_head=f32(rng.standard_normal(1)))
+
+
 # ----------------------------------------------------------------------------
 # raw inputs for the scoring-only workloads
 # ----------------------------------------------------------------------------
