@@ -190,7 +190,8 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
   }
 }
 
-// Many rows: tiles of 256 rows by 256 columns in the LDS, eight waves of 64 rows by 128 columns of accumulators.
+// Many rows: tiles of 256 rows by 256 columns in the LDS, eight waves of 64 rows by 128 columns of accumulators; where these would leave
+// compute units idle, tiles of 128 by 128, four waves of 64 by 64, two workgroups on a compute unit.
 //
 // A stage of the k loop is 128 k.  Its bytes go from memory straight to the LDS, in pieces of 16 bytes; where a piece lies is
 // chosen by which lane fetches it: piece c of row m at place c ^ (m % 8) of eight, or c ^ (m / 4 % 4) of four, so that the 16 rows that
@@ -209,8 +210,15 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
 // the last one are stored.
 template <int AF> constexpr int a_bytes() { return AF == VF_E4M3 ? 128 : 64; }   // of a row, in a stage
 template <int AF> constexpr int stages() { return AF == VF_E4M3 ? 3 : 4; }       // that the LDS holds
-template <int AF> constexpr int stage_bytes() { return 256 * a_bytes<AF>() + 256 * 64; }
-constexpr int SCALES = 512 * 16;  // of four stages; the LDS holds them twice
+// WM by WN waves of 64 rows by 16 NT columns: a thread for every row and column of the tile
+template <int WM_, int WN_, int NT_> struct Tile {
+  static constexpr int WM = WM_, WN = WN_, NT = NT_, M = 64 * WM, N = 16 * NT * WN, THREADS = 64 * WM * WN;
+  static constexpr int SCALES = THREADS * 16;  // bytes of four stages' scales; the LDS holds them twice
+  static_assert(M + N == THREADS, "");
+};
+typedef Tile<4, 2, 8> Large;
+typedef Tile<2, 2, 4> Small;
+template <int AF, class TL> constexpr int stage_bytes() { return TL::M * a_bytes<AF>() + TL::N * 64; }
 
 // A part of memory as the instructions with a range check see it: what lies behind its end reads as zeros.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -235,28 +243,29 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 
 template <int N> struct phase_is { static constexpr int value = N; };
 
-template <int AF, bool EXACT>
-__global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tiles_n, int tiles) {
+template <int AF, bool EXACT, class TL>
+__global__ void __launch_bounds__(TL::THREADS, 2) k_mx_tile(const MatmulArgs p, int tiles_n, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
-  constexpr int AB = a_bytes<AF>(), MI = 4, NT = 8, NST = stages<AF>(), SB = stage_bytes<AF>(), WAT = 256 * AB, SAT = NST * SB;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4, wm = wave & 3, wn = wave >> 2;
+  constexpr int AB = a_bytes<AF>(), MI = 4, NT = TL::NT, NST = stages<AF>(), SB = stage_bytes<AF, TL>(), WAT = TL::M * AB, SAT = NST * SB;
+  constexpr int TM = TL::M, TN = TL::N, THREADS = TL::THREADS, SCALES = TL::SCALES;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4, wm = wave % TL::WM, wn = wave / TL::WM;
   const int steps = (p.kb + 3) >> 2;
 
   // Pieces that this thread fetches in every stage, from the tile's first row and column on;
-  // and the row of a (threads 0..255) or of the weights whose scales it takes
-  constexpr int PA = AB / 32, PW = 2, LOADS = PA + PW;
+  // and the row of a (the first TM threads) or of the weights whose scales it takes
+  constexpr int PA = TM * AB / 16 / THREADS, PW = TN * 4 / THREADS, LOADS = PA + PW;
   const uint32_t row_bytes = (uint32_t)p.kb * mx<AF>::bytes32, col_bytes = (uint32_t)p.kb * 16;
-  // row 16 j + x of a wave's 128 rows of weights is its column 32 (j / 2) + 8 (x / 4) + 4 (j % 2) + x % 4
+  // row 16 j + x of a wave's rows of weights is its column 32 (j / 2) + 8 (x / 4) + 4 (j % 2) + x % 4
   auto column = [](int row) { return (row & 0xe0) + 8 * ((row & 15) >> 2) + 4 * ((row >> 4) & 1) + (row & 3); };
   uint32_t lane_a[PA], lane_w[PW];
 #pragma unroll
   for (int i = 0; i < PA; ++i) {
-    const int e = i * 512 + tid, row = e / (AB / 16), c = AB == 128 ? (e & 7) ^ (row & 7) : (e & 3) ^ ((row >> 2) & 3);
+    const int e = i * THREADS + tid, row = e / (AB / 16), c = AB == 128 ? (e & 7) ^ (row & 7) : (e & 3) ^ ((row >> 2) & 3);
     lane_a[i] = (uint32_t)row * row_bytes + 16 * c;
   }
 #pragma unroll
   for (int i = 0; i < PW; ++i) {
-    const int e = i * 512 + tid, row = e >> 2, c = (e & 3) ^ ((row >> 2) & 3);
+    const int e = i * THREADS + tid, row = e >> 2, c = (e & 3) ^ ((row >> 2) & 3);
     lane_w[i] = (uint32_t)column(row) * col_bytes + 16 * c;
   }
   int64_t m0;
@@ -271,13 +280,13 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
     const int chunk8 = tiles / 8, id = turn < chunk8 * 8 ? (turn & 7) * chunk8 + (turn >> 3) : turn;
     const int tiles_m = tiles / tiles_n, band = id / (8 * tiles_n), in_band = id - band * 8 * tiles_n;
     const int high = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8;
-    m0 = (int64_t)(8 * band + in_band % high) * 256;
-    n0 = in_band / high * 256;
+    m0 = (int64_t)(8 * band + in_band % high) * TM;
+    n0 = in_band / high * TN;
     part_a = part_of(p.a + m0 * row_bytes, (p.M - m0) * row_bytes);
     part_w = part_of(p.w + (int64_t)n0 * col_bytes, (int64_t)(p.N - n0) * col_bytes);
     // (rows that are not there take the last one's scales)
-    const int64_t row = tid < 256 ? (m0 + tid < p.M ? m0 + tid : p.M - 1) : (n0 + column(tid - 256) < p.N ? n0 + column(tid - 256) : p.N - 1);
-    src_s = (tid < 256 ? p.as : p.ws) + row * p.kb;
+    const int64_t row = tid < TM ? (m0 + tid < p.M ? m0 + tid : p.M - 1) : (n0 + column(tid - TM) < p.N ? n0 + column(tid - TM) : p.N - 1);
+    src_s = (tid < TM ? p.as : p.ws) + row * p.kb;
     return true;
   };
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
@@ -286,9 +295,9 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
   auto fetch = [&](int st) {
     const uint32_t at = base + (uint32_t)(st % NST) * SB + wave_at * 1024, k = st < steps ? st : steps - 1;
 #pragma unroll
-    for (int i = 0; i < PA; ++i) to_lds16(part_a, lane_a[i], k * AB, at + i * 8192);
+    for (int i = 0; i < PA; ++i) to_lds16(part_a, lane_a[i], k * AB, at + i * THREADS * 16);
 #pragma unroll
-    for (int i = 0; i < PW; ++i) to_lds16(part_w, lane_w[i], k * 64, at + WAT + i * 8192);
+    for (int i = 0; i < PW; ++i) to_lds16(part_w, lane_w[i], k * 64, at + WAT + i * THREADS * 16);
   };
   uint4 sq;  // scales on their way: of stages 4 k .. 4 k + 3
   // 16 bytes at any address, where the row ends before: its last 16, moved down, and scales of one behind them
@@ -320,8 +329,8 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
   // places of this lane's pieces in a stage: of row 16 i + r they lie a constant further for every i
   const int sw_a = AB == 128 ? r & 7 : (r >> 2) & 3;
   const int la0 = (wm * 64 + r) * AB + 16 * (g ^ sw_a), la1 = (wm * 64 + r) * AB + 16 * ((4 + g) ^ sw_a);
-  const int lw = WAT + (wn * 128 + r) * 64 + 16 * (g ^ ((r >> 2) & 3));
-  const int lsa = SAT + (wm * 64 + r) * 16 + g, lsw = SAT + (256 + wn * 128 + r) * 16 + g;
+  const int lw = WAT + (wn * 16 * NT + r) * 64 + 16 * (g ^ ((r >> 2) & 3));
+  const int lsa = SAT + (wm * 64 + r) * 16 + g, lsw = SAT + (TM + wn * 16 * NT + r) * 16 + g;
   auto read_a = [&](int st) {
     // (16 k at 16 g and, of 8-bit rows, 16 at 64 + 16 g)
     const uint8_t *at = lds + (st % NST) * SB, *sc = lds + lsa + ((st >> 2) & 1) * SCALES + 4 * (st & 3);
@@ -377,7 +386,7 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
 #pragma unroll
     for (int st = 0; st < NST - 1; ++st) fetch(st);
   }
-  if (wave < 4) __builtin_amdgcn_s_setprio(1);
+  if (THREADS == 512 && wave < 4) __builtin_amdgcn_s_setprio(1);
   for (int k = 1; there; ++k) {
     const int64_t m_at = m0;
     const int n_at = n0;
@@ -425,7 +434,7 @@ __global__ void __launch_bounds__(512, 2) k_mx_tile(const MatmulArgs p, int tile
       for (int s = 0; s < NST - 1; ++s) fetch(s);
     }
     // a lane has columns n + 32 j / 2 .. + 7 of rows r, 16 + r, ...
-    const int n = n_at + wn * 128 + 8 * g;
+    const int n = n_at + wn * 16 * NT + 8 * g;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -456,21 +465,22 @@ inline int blocks_for(int64_t threads) {
   return (int)(g < (1 << 20) ? g : (1 << 20));
 }
 
-template <int AF, bool EXACT>
+template <int AF, bool EXACT, class TL>
 int launch_tile(vf_ctx *c, const MatmulArgs &p) {
-  constexpr int smem = stages<AF>() * stage_bytes<AF>() + 2 * SCALES;
-  const int tiles_n = (p.N + 255) / 256;
+  constexpr int smem = stages<AF>() * stage_bytes<AF, TL>() + 2 * TL::SCALES, at_once = 256 * 512 / TL::THREADS;
+  const int tiles_n = (p.N + TL::N - 1) / TL::N;
   // (tiles are counted in 32 bits; the rows are taken in several launches)
-  const int64_t most = ((int64_t)1 << 28) / tiles_n, per = (most > 1 ? most : 1) * 256;
-  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_mx_tile<AF, EXACT>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
+  const int64_t most = ((int64_t)1 << 28) / tiles_n, per = (most > 1 ? most : 1) * TL::M;
+  const auto kernel = k_mx_tile<AF, EXACT, TL>;
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
   for (int64_t m = 0; m < p.M; m += per) {
     MatmulArgs q = p;
     q.a += m * p.kb * mx<AF>::bytes32;
     q.as += m * p.kb;
     q.M = p.M - m < per ? p.M - m : per;
     q.out = static_cast<char *>(p.out) + m * p.ld_out * (p.out_bf16 ? 2 : 4);
-    const int tiles = (int)((q.M + 255) / 256) * tiles_n;
-    k_mx_tile<AF, EXACT><<<tiles < 256 ? tiles : 256, 512, smem, c->stream>>>(q, tiles_n, tiles);
+    const int tiles = (int)((q.M + TL::M - 1) / TL::M) * tiles_n;
+    kernel<<<tiles < at_once ? tiles : at_once, TL::THREADS, smem, c->stream>>>(q, tiles_n, tiles);
     VF_HIP(c, hipGetLastError());
   }
   return VF_OK;
@@ -478,10 +488,21 @@ int launch_tile(vf_ctx *c, const MatmulArgs &p) {
 
 template <int AF, bool EXACT>
 int matmul(vf_ctx *c, const MatmulArgs &p) {
-  const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256);
-  // (offsets within 256 rows are 32 bits wide)
-  if (p.M > 64 && big >= 64 && p.kb <= (1 << 18)) return launch_tile<AF, EXACT>(c, p);
   const int nb = (p.N + 15) / 16;
+  // Tiles from 33 rows on, where the workgroups of k_mx_rows are more than the compute units (8-bit rows, K 4096, us: 64 rows, 4384
+  // columns 27.8 in rows, 21.8 in tiles; 200 rows, 1024 columns 15.9 and 21.5; 1000 rows, 4384 columns 219 and 33).
+  // (Offsets within 256 rows are 32 bits wide.)
+  if (p.M > 32 && nb * ((p.M + 63) / 64) > 256 && p.kb <= (1 << 18)) {
+    // By rounds of tiles: one of 256 large tiles takes 50 us, one of 512 small ones 34, of up to 256 small ones 22 (K 4096): 300 rows, 4384
+    // columns 48 large, 22 small; 1400 rows 52 and 35; 3000 rows 55 and 68.  With rows taken in two parts the large ones' operands
+    // do not fit the registers: 16384 rows 762 large, 540 small.
+    const int64_t large = (((p.M + 255) / 256) * ((p.N + 255) / 256) + 255) / 256, small = ((p.M + 127) / 128) * ((p.N + 127) / 128);
+    const int64_t rest = small % 512, small_cost = small / 512 * 34 + (rest == 0 ? 0 : rest <= 256 ? 22 : 34);
+    if constexpr (!EXACT) {
+      if (50 * large <= small_cost) return launch_tile<AF, EXACT, Large>(c, p);
+    }
+    return launch_tile<AF, EXACT, Small>(c, p);
+  }
   const int MT = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4;
   // rows beyond the grid's second dimension are taken in further launches
   const int64_t per = (int64_t)65535 * 16 * MT;

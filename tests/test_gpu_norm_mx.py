@@ -326,3 +326,24 @@ def test_other_streams_and_a_graph(vf):
         assert torch.equal(gy, ey) and torch.equal(gs, es)
         torch.cuda.synchronize()
     vf.vf_destroy(c)
+
+
+@pytest.mark.parametrize("M,N,K", [(33, 4112, 96), (129, 2100, 512), (257, 1300, 333), (640, 520, 2049), (1025, 4100, 64), (2100, 4097, 160)])
+@pytest.mark.parametrize("a_fmt", [2, 3])
+@pytest.mark.parametrize("out_type", [0, 1])
+def test_product_in_small_and_large_tiles(vf, ctx, M, N, K, a_fmt, out_type):
+    """Sizes on both sides of the lines between the ways; sums of K exact products in fp32 (2^-24 each of the magnitudes' sum, four
+    waves' parts), the cut of the 8-bit terms (2^-13 of each) where the output is bf16, and the output's rounding."""
+    import torch
+    rng = np.random.default_rng([M, N, K])
+    a, w = (vf.vf_mx_quantize(ctx, torch.from_numpy(rng.standard_normal(s)).float().cuda(), f) for s, f in (((M, K), a_fmt), ((N, K), 3)))
+    bias = torch.from_numpy(rng.standard_normal(N)).float().cuda()
+    big = torch.full((M + 1, N + 3), 7.0, dtype=torch.float32 if out_type == 0 else torch.bfloat16, device="cuda")
+    got = vf.vf_mx_matmul(ctx, a, w, bias, out_type, out=big[:M, 1:1 + N]).double()
+    av, wv = (vf.vf_mx_dequantize(ctx, m, vf.VF_FP32).double() for m in (a, w))
+    want = av @ wv.t().contiguous() + bias.double()
+    mag = av.abs() @ wv.abs().t().contiguous() + bias.double().abs()
+    cut = 2.0 ** -13 if a_fmt == 2 and out_type == 1 else 0.0
+    tol = ((K + 8) * R.U32 + cut) * mag + (R.U32 if out_type == 0 else R.UBF) * want.abs()
+    assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() / tol).max())
+    assert bool((big[M] == 7).all()) and bool((big[:, 0] == 7).all()) and bool((big[:, 1 + N:] == 7).all())
