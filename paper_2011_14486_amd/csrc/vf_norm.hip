@@ -2,7 +2,8 @@
 //
 // s = x + r; y = s / sqrt(mean(s^2) + eps) * gain.  Every element is read once and held in registers while
 // the row's sum of squares is taken, so the kernel moves x, r, sum and out once each: it is bound by the memory's
-// rate, and for a single row by the latency of a launch.
+// rate, and for a single row by the latency of a launch.  MI355X: 32768 x 2048 in bf16 with residual, 537 MB, 102 us = 5.26 TB/s, as
+// a copy reaches (123 us with a workgroup for every row, which reads the gains again); one row of 1024 2.4 us.
 #include "vf_internal.h"
 #include "vf_ops_dev.h"
 

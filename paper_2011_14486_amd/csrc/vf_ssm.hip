@@ -147,7 +147,8 @@ __device__ __forceinline__ int channel_of(const SsmArgs &p, int k, int R, int sp
 // Token by token, fp32: a workgroup holds 256 / L PI rows p of one head's state in registers, L lanes a row, four numbers n
 // each.  Eight tokens are convolved at a time, a thread a channel; their inputs were fetched while
 // the eight before were worked on, and the outputs of the eight are summed over the lanes together.  What bounds it is the
-// chain of a sequence's tokens, so long sequences are split (below).
+// chain of a sequence's tokens, so long sequences are split (below).  MI355X: 37 sequences of up to 300 tokens, 5 heads of 40 x 24 in
+// fp32, 64 us (240 with inputs asked for when they are needed and every token's outputs summed by themselves).
 template <typename T, int L, int PI, int TW>
 __global__ void __launch_bounds__(256, 2) k_ssm_tokens(const SsmArgs p) {
   constexpr int R = 256 / L * PI, SPAN = 4 * L, PLACES = R + 2 * SPAN, NC = (PLACES + 255) / 256, TB = 8;
@@ -311,7 +312,8 @@ __global__ void __launch_bounds__(256, 2) k_ssm_tokens(const SsmArgs p) {
 // head for `each` sequences one after the other: the layer's weights stay in registers, and the next sequence's state and
 // inputs are on their way while this one's are worked on.  Every state is read and written once, past the caches on the
 // way out: the memory's rate bounds it.  Workgroups of one head run next to each other, so that the states of
-// parents that many rows continue come from the second-level cache.
+// parents that many rows continue come from the second-level cache.  MI355X: 1024 rows of 32 heads of 64 x 128 behind 64 parents, 1.17 GB,
+// 225 us = 5.2 TB/s (554 by k_ssm_tokens as it was, where a token's loads wait for each other); one row 5.5 us.
 template <typename T, int PI, int NC, int TW>
 struct StepIn {
   f32x4 S[PI];
@@ -572,7 +574,8 @@ int step(vf_ctx *c, const SsmArgs &p) {
 //
 // The waves of a workgroup take neighbouring heads of one group and convolve its B and C together.  All bytes of x, z, out
 // pass once; what bounds the kernel is the vector work on them: convolution, silu (two quarter-rate
-// functions a number) and the operands' parts.
+// functions a number) and the operands' parts.  MI355X: 16,384 sequences of 50 tokens, 4 heads of 64 x 64, 626 - 654 us = 2.3 TB/s;
+// a prompt of 16,384 tokens, 32 heads of 64 x 128, 255 us: local states 92, join 13, outputs 166.
 
 constexpr int Q = 32;            // tokens of a chunk
 constexpr int XS = Q + 4;        // row of x in the LDS, floats
