@@ -145,8 +145,10 @@ int vfk_rms_norm(vf_ctx *c, int type, const void *x, int64_t ld_x, const void *r
   a.ld_x = ld_x; a.ld_res = ld_res; a.ld_sum = ld_sum; a.ld_out = ld_out; a.rows = rows;
   a.width = width; a.kb = (width + 31) / 32; a.eps = eps;
   const int nchunk = out_type >= VF_E4M3 ? 4 * a.kb : (width + 7) / 8;
+  // a thread takes one chunk up to 256 threads a row, then two, then four with 1024 threads
   int tpr = 64;
-  while (tpr < nchunk && tpr < 1024) tpr *= 2;
+  while (tpr < nchunk && tpr < 256) tpr *= 2;
+  while (2 * tpr < nchunk && tpr < 1024) tpr *= 2;
   int nch = 1;
   while (nch * tpr < nchunk) nch *= 2;
   a.tpr = tpr;

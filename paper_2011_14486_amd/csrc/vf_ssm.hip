@@ -4,6 +4,8 @@
 //
 // Token by token a state of P x N numbers is read and written once per sequence, five operations a number and
 // token; in chunks (below) the same sums are products of matrices.
+#include <algorithm>
+
 #include "vf_internal.h"
 #include "vf_ops_dev.h"
 
@@ -511,7 +513,10 @@ int launch_tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
   const int slices = (p.P + R - 1) / R;
   split(c, p, longest, (int64_t)p.n_seq * p.H * slices, 1024, SEQ_TOKENS, 64);
   const int64_t parts = (int64_t)p.n_seq * p.nseg;
-  const dim3 grid(p.H * slices, (unsigned)(parts < 32768 ? parts : 32768));
+  // Many parts: a workgroup takes several one after the other, up to 16, and keeps the layer's weights for them; there are four times as
+  // many workgroups as run at a time (five of four waves on a compute unit), for the sake of unequal parts.
+  const int64_t x = (int64_t)p.H * slices, most = std::max((int64_t)4 * 1280 / x, (parts + 15) / 16);
+  const dim3 grid((unsigned)x, (unsigned)std::min(std::min(parts, std::max(most, (int64_t)1)), (int64_t)32768));
   return run_parts(c, p, [&] {
     if (p.W <= 4) k_ssm_tokens<T, L, PI, 4><<<grid, 256, 0, c->stream>>>(p);
     else k_ssm_tokens<T, L, PI, 8><<<grid, 256, 0, c->stream>>>(p);
@@ -582,7 +587,7 @@ constexpr int XS = Q + 4;        // row of x in the LDS, floats
 // place of row n of the transposed B, in fp16 numbers: 80 bytes a row and 16 more after eight, so that the eight-token pieces that
 // neighbouring lanes write (channels four apart) lie in different banks
 __device__ __forceinline__ int bt_row(int n) { return n * (Q + 8) + (n >> 3) * 8; }
-constexpr int bt_size(int np) { return np * (Q + 8) + (np >> 3) * 8; }
+__host__ __device__ constexpr int bt_size(int np) { return np * (Q + 8) + (np >> 3) * 8; }
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -713,25 +718,26 @@ __device__ __forceinline__ uint4 rest_of(const f32x4 &a, const f32x4 &b, const u
 
 // LDS: B and C by tokens, B by n in two parts and its scales; per wave x by p and its scales, weights of the convolution of all of
 // these channels; per wave the chunk's steps.
-constexpr int ROWS = 256;  // rows p of a workgroup: PT tiles of 16 a wave
-template <int NT> constexpr size_t chunk_lds() {
+constexpr int ROWS = 256;  // most rows p of a workgroup: PT tiles of 16 a wave
+// `rows` of them, in `nw` waves
+template <int NT> __host__ __device__ constexpr size_t chunk_lds(int rows, int nw) {
   return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * bt_size(16 * NT)) +
-         sizeof(float) * (16 * NT + ROWS * (XS + 1) + 6 * (32 * NT + ROWS) + 8 * 3 * Q);
+         sizeof(float) * (16 * NT + rows * (XS + 1) + 6 * (32 * NT + rows) + nw * 3 * Q);
 }
 
 template <int NT, int PT, bool LOCAL>
 __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
   extern __shared__ __align__(16) char smem[];
-  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT, NW = ROWS / PS;
+  constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT;
   // Tokens of B and C that a thread takes at a time, so that there is one piece of x and one of B and C for a thread, or one of either
   constexpr int TB = PT == 4 ? 4 : 8;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4, nthr = blockDim.x, nw = nthr >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // (what goes by the wave is held once, not per lane)
   uint16_t *Bs = reinterpret_cast<uint16_t *>(smem), *Cs = Bs + Q * NS, *BtH = Cs + Q * NS, *BtL = BtH + bt_size(NP);
   float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));
-  float *Xall = bscale + NP, *xsall = Xall + NW * PS * XS, *wl = xsall + NW * PS, *bl = wl + 4 * (2 * NP + NW * PS);
-  int *chans = reinterpret_cast<int *>(bl + 2 * NP + NW * PS);
-  float *cum = bl + 2 * (2 * NP + NW * PS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
+  float *Xall = bscale + NP, *xsall = Xall + nw * PS * XS, *wl = xsall + nw * PS, *bl = wl + 4 * (2 * NP + nw * PS);
+  int *chans = reinterpret_cast<int *>(bl + 2 * NP + nw * PS);
+  float *cum = bl + 2 * (2 * NP + nw * PS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
   float *X = Xall + wave * PS * XS, *xs = xsall + wave * PS;
 
   const int slices = (p.P + PS - 1) / PS, jobs = p.H / p.G * slices, per = (jobs + nw - 1) / nw, each = per * p.G;
@@ -749,8 +755,8 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
 
   // Channels of the convolution as the LDS has them: B, C (NP each, zeros behind N), x of the waves (PS each, zeros behind P): their
   // weights, and the channel of xbc, -1 where there is none.
-  if (p.N != NP || p.P % PS != 0 || jobs % NW != 0)
-    for (int e = tid; e < (int)(chunk_lds<NT>() / 4); e += nthr) reinterpret_cast<uint32_t *>(smem)[e] = 0;
+  if (p.N != NP || p.P % PS != 0 || jobs % nw != 0)
+    for (int e = tid; e < (int)(chunk_lds<NT>(nw * PS, nw) / 4); e += nthr) reinterpret_cast<uint32_t *>(smem)[e] = 0;
   __syncthreads();
   auto weights = [&](int k, int c) {
     chans[k] = c;
@@ -1131,10 +1137,11 @@ int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
   constexpr int PS = 16 * PT, NW = ROWS / PS;
   const int jobs = p.H / p.G * ((p.P + PS - 1) / PS), nw = jobs < NW ? jobs : NW, per = (jobs + nw - 1) / nw;
   const int64_t each = (int64_t)p.n_seq * per * p.G;
-  const int64_t at_once = PT == 4 ? 512 : 256;  // workgroups that run at a time
+  const size_t smem = chunk_lds<NT>(nw * PS, nw);
+  // workgroups that run at a time: two waves on a SIMD, and what the LDS holds
+  const int64_t by_waves = 8 / nw, by_lds = (int64_t)(160 * 1024 / smem), at_once = 256 * (by_waves < by_lds ? by_waves : by_lds);
   // a segment costs its state's way to memory and back, about 256 tokens' time
   split(c, p, longest, each, at_once, Q, 256);
-  const size_t smem = chunk_lds<NT>();
   if (smem > 65536) {
     VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
