@@ -260,7 +260,10 @@ __global__ void __launch_bounds__(256, 2) k_ssm_tokens(const SsmArgs p) {
       __syncthreads();  // (two buffers: nobody writes the one that is read before all have passed the next barrier)
       float y[COUNT];
 #pragma unroll
+      for (int k = 0; k < COUNT; ++k) y[k] = 0.0f;
+#pragma unroll
       for (int t = 0; t < TB; ++t) {
+        if ((t == 2 || t == 4) && nt <= t) break;  // (short sequences; a line at every token would cost the long ones 8 %)
         const float dt = udt[buf][t], da = uda[buf][t];
         log_decay = fmaf(dt, A, log_decay);
         const f32x4 B = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][n]);
@@ -274,7 +277,6 @@ __global__ void __launch_bounds__(256, 2) k_ssm_tokens(const SsmArgs p) {
         const f32x4 Cv = *reinterpret_cast<const f32x4 *>(&ubc[buf][t][SPAN + n]);
 #pragma unroll
         for (int k = 0; k < PI; ++k) {
-          y[t * PI + k] = 0.0f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[t * PI + k] = fmaf(S[k][j], Cv[j], y[t * PI + k]);
         }
@@ -470,14 +472,23 @@ inline int blocks_for(int64_t threads) {
   return (int)(b < (1 << 20) ? b : (1 << 20));
 }
 
-// How a call is split: segments of at least `least` tokens until there are `want` workgroups, of `each` for one segment of all
-// sequences.  Without the scratch for it (captured stream, no memory) the sequences stay whole.
+// How a call is split: into segments of at least `least` tokens that fill one to four rounds of the `want` workgroups that run at a
+// time, `each` for one segment of all sequences, if the rounds' tokens get fewer by it: a token of a split sequence is
+// worked on twice, at about 1.6 of its cost.  Without the scratch for it (captured stream, no memory) the sequences stay whole.
 void split(vf_ctx *c, SsmArgs &p, int64_t longest, int64_t each, int64_t want, int unit, int64_t least) {
   p.nseg = 1;
   p.seg_len = 0;
   if (each <= 0 || each >= want || longest < 2 * least) return;
-  int64_t n = (want + each - 1) / each;
-  if (n > longest / least) n = longest / least;
+  int64_t n = 1, cost = longest * 10;  // (one round)
+  for (int64_t rounds = 1; rounds <= 4; ++rounds) {
+    int64_t k = rounds * want / each;
+    if (k > longest / least) k = longest / least;
+    const int64_t with = (each * k + want - 1) / want * ((longest + k - 1) / k) * 16;
+    if (k > 1 && with < cost) {
+      n = k;
+      cost = with;
+    }
+  }
   int64_t len = ((longest + n - 1) / n + unit - 1) / unit * unit;
   n = (longest + len - 1) / len;
   if (n < 2) return;
@@ -526,8 +537,9 @@ int launch_tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
 }
 template <typename T>
 int tokens(vf_ctx *c, SsmArgs &p, int64_t longest) {
-  // 64 rows p a workgroup (32 of more than 128 numbers n), or a thread's one row where there are too few workgroups for the compute units
-  const bool wide = (int64_t)p.n_seq * p.H * ((p.P + 63) / 64) >= 512 || longest >= 256;
+  // 64 rows p a workgroup (32 of more than 128 numbers n), or a thread's one row where there are too few rows, or too few workgroups
+  // for the compute units
+  const bool wide = p.P > 16 && ((int64_t)p.n_seq * p.H * ((p.P + 63) / 64) >= 512 || longest >= 256);
   if (p.N <= 16) return launch_tokens<T, 4, 1>(c, p, longest);
   if (p.N <= 32) return wide ? launch_tokens<T, 8, 2>(c, p, longest) : launch_tokens<T, 8, 1>(c, p, longest);
   if (p.N <= 64) return wide ? launch_tokens<T, 16, 4>(c, p, longest) : launch_tokens<T, 16, 1>(c, p, longest);
@@ -554,8 +566,9 @@ int launch_step(vf_ctx *c, const SsmArgs &p) {
 }
 template <typename T>
 int step(vf_ctx *c, const SsmArgs &p) {
-  // 64 rows p a workgroup (32 of more than 128 numbers n), or 16 (8) where there are too few workgroups for the compute units
-  const bool wide = (int64_t)p.n_seq * p.H * ((p.P + 63) / 64) >= 512;
+  // 64 rows p a workgroup (32 of more than 128 numbers n), or 16 (8) where there are too few rows, or too few workgroups for the compute
+  // units
+  const bool wide = p.P > 16 && (int64_t)p.n_seq * p.H * ((p.P + 63) / 64) >= 512;
   if (p.N <= 16) return launch_step<T, 4, 1>(c, p);
   if (p.N <= 32) return wide ? launch_step<T, 8, 2>(c, p) : launch_step<T, 8, 1>(c, p);
   if (p.N <= 64) return wide ? launch_step<T, 16, 4>(c, p) : launch_step<T, 16, 1>(c, p);
@@ -1135,7 +1148,8 @@ bool chunks_fit(const SsmArgs &p) {
 template <int NT, int PT>
 int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
   constexpr int PS = 16 * PT, NW = ROWS / PS;
-  const int jobs = p.H / p.G * ((p.P + PS - 1) / PS), nw = jobs < NW ? jobs : NW, per = (jobs + nw - 1) / nw;
+  // workgroups of a group's heads, each with the same number of waves but for the last
+  const int jobs = p.H / p.G * ((p.P + PS - 1) / PS), per = (jobs + NW - 1) / NW, nw = (jobs + per - 1) / per;
   const int64_t each = (int64_t)p.n_seq * per * p.G;
   const size_t smem = chunk_lds<NT>(nw * PS, nw);
   // workgroups that run at a time: two waves on a SIMD, and what the LDS holds
@@ -1188,7 +1202,7 @@ int vfk_ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io, bool one) {
   p.nseg = 1; p.seg_len = 0; p.local = 0; p.seg_state = p.seg_log = nullptr;
   const int64_t longest = io->offsets_dev ? (io->longest < io->tokens ? io->longest : io->tokens) : io->tokens / io->n_seq;
   int rc;
-  if (one) rc = io->type == VF_BF16 ? step<uint16_t>(c, p) : step<float>(c, p);
+  if (one || (!io->offsets_dev && io->tokens == io->n_seq)) rc = io->type == VF_BF16 ? step<uint16_t>(c, p) : step<float>(c, p);
   else if (io->type == VF_BF16 && chunks_fit(p) && longest > 8) rc = chunks(c, p, longest);
   else rc = io->type == VF_BF16 ? tokens<uint16_t>(c, p, longest) : tokens<float>(c, p, longest);
   if (rc != VF_OK || !p.has_out || !p.conv_later || p.W == 1) return rc;
