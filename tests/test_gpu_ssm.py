@@ -194,6 +194,37 @@ def test_state_in_place_token_by_token_equals_the_sequence(vf, ctx, sizes, kind)
     assert not state[0][[4, 6]].any() and not state[1][[4, 6]].any()
 
 
+@pytest.mark.parametrize("sizes,rows", [((4, 16, 1, 16, 4), 2600), ((4, 24, 2, 40, 3), 2100), ((8, 20, 1, 10, 8), 1300)], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_steps_of_many_rows(vf, ctx, sizes, rows, kind):
+    """More rows than workgroups: a workgroup takes several, from shared parents into slots of their own, then in place."""
+    import torch
+    rng = np.random.default_rng(rows)
+    c = Case(vf, sizes, [1] * rows, kind, slots=7)
+    slots = rng.integers(-1, 7, rows)
+    new = c.layer.state(rows, c.dtype)
+    out = vf.vf_ssm_step(ctx, c.layer, c.xbc, c.dt, c.z, state=c.state, slots=torch.from_numpy(slots.astype(np.int32)).cuda(), state_out=new)
+    c.check(out, c.ref(slots), False, new)
+    before = tuple(t.clone() for t in new)
+    out = vf.vf_ssm_step(ctx, c.layer, c.xbc, c.dt, c.z, state=new, state_out=new)
+    c.check(out, c.ref(range(rows), before), False, new)
+
+
+@pytest.mark.parametrize("sizes,kind,lens", [((4, 17, 1, 30, 4), "fp32", [2, 3, 0, 1] * 800), ((2, 64, 1, 64, 4), "bf16", [9, 0, 40, 33] * 300),
+                                             ((5, 64, 1, 128, 2), "bf16", [50] * 150), ((3, 30, 1, 20, 2), "bf16", [1] * 3000)],
+                         ids=["few tokens", "chunks, some empty", "chunks, uniform", "one token"])
+def test_many_short_sequences(vf, ctx, sizes, kind, lens):
+    """More sequences than workgroups."""
+    c = Case(vf, sizes, lens, kind)
+    new = c.layer.state(len(lens), c.dtype)
+    out = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, n_seq=len(lens), longest=max(lens), offsets=c.offsets, state_out=new)
+    ref = c.ref()
+    c.check(out, ref, in_chunks(kind, sizes) and max(lens) > 8, new)
+    if len(set(lens)) == 1:
+        out = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, n_seq=len(lens), state_out=new)
+        c.check(out, ref, in_chunks(kind, sizes) and max(lens) > 8, new)
+
+
 @pytest.mark.parametrize("kind,sizes", [("bf16", (4, 64, 1, 64, 4)), ("fp32", (3, 17, 1, 30, 4))], ids=str)
 def test_bad_slots_and_offsets(vf, ctx, kind, sizes):
     """Slots that are not there read as NaN and are not written; ranges that are not there are empty."""
