@@ -1091,8 +1091,9 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
     for (int j = 0; j < PT; ++j) {
       const float f = scale_to_f16(xs[16 * j + r] * wtop);
       back[j] = power_reciprocal(f);
-      const f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * (w0 * f);
-      const f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * (w1 * f);
+      // (first by the weight: f is up to 2^126 where a row is zero or next to it, and w f may be infinite)
+      const f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * w0 * f;
+      const f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * w1 * f;
       vh[j] = make_uint4(pack_h(a[0], a[1]), pack_h(a[2], a[3]), pack_h(b[0], b[1]), pack_h(b[2], b[3]));
       vl[j] = make_uint4(rest_h(a[0], a[1], vh[j].x), rest_h(a[2], a[3], vh[j].y), rest_h(b[0], b[1], vh[j].z), rest_h(b[2], b[3], vh[j].w));
     }
