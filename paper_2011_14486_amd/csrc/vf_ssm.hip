@@ -703,10 +703,27 @@ __device__ __forceinline__ float top_of_32(const float (&v)[TB]) {
   if (TB == 4) m = max_lanes<0x141>(m); // lanes 7 .. 0 of eight
   return __uint_as_float(m);
 }
-// the value N lanes before in the same 16, zero where there is none; and the last of the 16 before, for the second and fourth 16
+// the value N lanes before, or behind, in the same 16, zero where there is none; and the last of the 16 before, for the second and fourth 16
 template <int N>
 __device__ __forceinline__ float lanes_before(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x110 + N, 0xf, 0xf, true));
+}
+template <int N>
+__device__ __forceinline__ float lanes_behind(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x100 + N, 0xf, 0xf, true));
+}
+// sums over the 16 lanes up to a lane, and from a lane on
+__device__ __forceinline__ float sum_up_to(float v) {
+  v += lanes_before<1>(v);
+  v += lanes_before<2>(v);
+  v += lanes_before<4>(v);
+  return v + lanes_before<8>(v);
+}
+__device__ __forceinline__ float sum_from(float v) {
+  v += lanes_behind<1>(v);
+  v += lanes_behind<2>(v);
+  v += lanes_behind<4>(v);
+  return v + lanes_behind<8>(v);
 }
 __device__ __forceinline__ float row_before(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
@@ -730,12 +747,12 @@ __device__ __forceinline__ uint4 rest_of(const f32x4 &a, const f32x4 &b, const u
 #define VF_MFMA_H(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
 
 // LDS: B and C by tokens, B by n in two parts and its scales; per wave x by p and its scales, weights of the convolution of all of
-// these channels; per wave the chunk's steps.
+// these channels; per wave five numbers for each of the chunk's tokens.
 constexpr int ROWS = 256;  // most rows p of a workgroup: PT tiles of 16 a wave
 // `rows` of them, in `nw` waves
 template <int NT> __host__ __device__ constexpr size_t chunk_lds(int rows, int nw) {
   return sizeof(uint16_t) * (2 * Q * (16 * NT + 8) + 2 * bt_size(16 * NT)) +
-         sizeof(float) * (16 * NT + rows * (XS + 1) + 6 * (32 * NT + rows) + nw * 3 * Q);
+         sizeof(float) * (16 * NT + rows * (XS + 1) + 6 * (32 * NT + rows) + nw * 5 * Q);
 }
 
 template <int NT, int PT, bool LOCAL>
@@ -750,7 +767,8 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
   float *bscale = reinterpret_cast<float *>(BtL + bt_size(NP));
   float *Xall = bscale + NP, *xsall = Xall + nw * PS * XS, *wl = xsall + nw * PS, *bl = wl + 4 * (2 * NP + nw * PS);
   int *chans = reinterpret_cast<int *>(bl + 2 * NP + nw * PS);
-  float *cum = bl + 2 * (2 * NP + nw * PS) + wave * 3 * Q, *stp = cum + Q, *wgt = stp + Q;
+  // per token: exponent of its decay; their sums over the tokens of its 16 up to it, and behind it; factors of its product with B
+  float *dec = bl + 2 * (2 * NP + nw * PS) + wave * 5 * Q, *upto = dec + Q, *rest = upto + Q, *stp = rest + Q, *wgt = stp + Q;
   float *X = Xall + wave * PS * XS, *xs = xsall + wave * PS;
 
   const int slices = (p.P + PS - 1) / PS, jobs = p.H / p.G * slices, per = (jobs + nw - 1) / nw, each = per * p.G;
@@ -957,17 +975,16 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
     if (on) {
       const int t = lane & (Q - 1);
       const float dt = t0 + t < end ? softplus(bf16_f32(dt_raw) + bias_dt) : 0.0f;
-      // sums and then maxima over the 32 lanes up to a lane
-      float c = dt * A;
-      c += lanes_before<1>(c);
-      c += lanes_before<2>(c);
-      c += lanes_before<4>(c);
-      c += lanes_before<8>(c);
-      c += row_before(c);
-      last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(c), Q - 1));
-      const float w = dt * __expf(last - c) * (LN2 * LN2);
+      // Decays over some tokens have these tokens' exponents summed, never a difference of longer sums: behind a large step that
+      // would be all rounding.
+      const float v = dt * A, up = sum_up_to(v), behind = sum_from(lanes_behind<1>(v));
+      const float half = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(up), Q - 1));
+      last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(up), Q / 2 - 1)) + half;
+      const float w = dt * __expf(t < Q / 2 ? behind + half : behind) * (LN2 * LN2);
       if (lane < Q) {
-        cum[t] = c;
+        dec[t] = v;
+        upto[t] = up;
+        rest[t] = behind;
         stp[t] = dt * -(LN2 * LN2 * LN2);  // (x, B and C are each to be multiplied by -ln 2)
         wgt[t] = w;
       }
@@ -1017,20 +1034,29 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
         G[1] = VF_MFMA_B(b0, c1, G[1]);
         G[2] = VF_MFMA_B(b1, c1, G[2]);
       }
-      const f32x4 cs0 = *reinterpret_cast<const f32x4 *>(cum + 4 * q), cs1 = *reinterpret_cast<const f32x4 *>(cum + 16 + 4 * q);
       const f32x4 st0 = *reinterpret_cast<const f32x4 *>(stp + 4 * q), st1 = *reinterpret_cast<const f32x4 *>(stp + 16 + 4 * q);
-      const float ct0 = cum[r], ct1 = cum[16 + r];
+      // the exponents behind token 4 q + i up to token r, of either half: of the lane's own four tokens those that lie there, and
+      // the sum from token 4 q + 4 to r; zero for later tokens
+      auto between = [&](const float *of, float (&e)[4]) {
+        const f32x4 own = *reinterpret_cast<const f32x4 *>(of + 4 * q);
+        e[3] = sum_up_to(r >= 4 * q + 4 ? of[r] : 0.0f);
+#pragma unroll
+        for (int i = 2; i >= 0; --i) e[i] = e[i + 1] + (4 * q + i + 1 <= r ? own[i + 1] : 0.0f);
+      };
+      float e00[4], e11[4];
+      between(dec, e00);
+      between(dec + 16, e11);
+      const f32x4 rs = *reinterpret_cast<const f32x4 *>(rest + 4 * q);
+      const float up0 = upto[r], up1 = upto[16 + r];
       const bool behind = t0 > part.begin || first || lost;  // (otherwise the state is zero)
-      const float e0 = __expf(ct0) * -LN2, e1 = __expf(ct1) * -LN2;
+      const float e0 = __expf(up0) * -LN2, e1 = __expf(upto[15] + up1) * -LN2;
       f32x4 m00, m01, m11;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        // (the exponent of a later token is positive and may be large: chosen by comparison, not by a product with 0)
         const int at = 4 * q + i;
-        const float d0 = __expf(at <= r ? ct0 - cs0[i] : 0.0f) * st0[i], d1 = __expf(at <= r ? ct1 - cs1[i] : 0.0f) * st1[i];
-        m00[i] = at <= r ? fmaf(G[0][i], d0, at == r ? D * -LN2 : 0.0f) : 0.0f;
-        m11[i] = at <= r ? fmaf(G[2][i], d1, at == r ? D * -LN2 : 0.0f) : 0.0f;
-        m01[i] = G[1][i] * __expf(ct1 - cs0[i]) * st0[i];
+        m00[i] = at <= r ? fmaf(G[0][i], __expf(e00[i]) * st0[i], at == r ? D * -LN2 : 0.0f) : 0.0f;
+        m11[i] = at <= r ? fmaf(G[2][i], __expf(e11[i]) * st1[i], at == r ? D * -LN2 : 0.0f) : 0.0f;
+        m01[i] = G[1][i] * __expf(rs[i] + up1) * st0[i];
       }
       const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
       const uint4 f0 = frag_of(m00, zero), f1 = frag_of(m01, m11), g0 = rest_of(m00, zero, f0), g1 = rest_of(m01, m11, f1);

@@ -27,3 +27,24 @@ def test_rows_of_zeros_behind_large_steps(vf, ctx, sizes, lens, size):  # noqa: 
     c.check(out, c.ref(), True, new)
     if size == 0:
         assert not out[:, [3, P - 2]].any() and not new[1][:, 0, [3, P - 2]].any()
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=str)
+@pytest.mark.parametrize("lens", [[32, 64, 100], [1100]], ids=str)
+@pytest.mark.parametrize("large,small,a", [(60.0, -4.0, None), (1000.0, -4.0, None), (1e35, -10.0, -1e4)], ids=str)
+def test_small_steps_behind_large_ones(vf, ctx, sizes, lens, large, small, a):  # noqa: F811
+    """Steps that make the state forget, then small ones within the same chunk of 32 tokens: what counts are the decays of the small
+    ones alone, which are to be as exact as if the large ones were not there.  (1e35 times -1e4 is infinite in 32 bits.)"""
+    c = Case(vf, sizes, lens, "bf16", plain=True, seed=8)
+    if a is not None:
+        c.layer.tensors[2].fill_(a)
+        c.lay["a"][:] = a
+    rng = np.random.default_rng(9)
+    c.dt[:] = small
+    for first, count in zip(c.first, c.lens):
+        for chunk in range(first, first + count, 32):
+            at = chunk + rng.choice(16, 3, replace=False) + 16 * int(rng.integers(0, 2))   # in a chunk's first or second half
+            c.dt[at[at < first + count].tolist()] = large
+    new = c.layer.state(len(lens), c.dtype)
+    out = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, n_seq=len(lens), longest=max(lens), offsets=c.offsets, state_out=new)
+    c.check(out, c.ref(), True, new)
