@@ -666,11 +666,12 @@ __device__ __forceinline__ void fetch_state(const SsmArgs &p, int slot, int c0, 
 }
 // silu of the convolution for channel k of the four, divided by -ln 2: with weights and bias times -log2(e) the sum s is the exponent
 // of silu's exponential, and s / (1 + 2^s) the result.  The constant is taken back where the results meet steps and decays.
-// Weights in the LDS: four taps a channel (zeros before the first), and the biases.
+// Weights in the LDS: four taps a channel, and the biases.  Of fewer taps (FOUR false) the first 4 - W are not there: an input that is not
+// finite is not to reach tokens that do not see it by way of a zero.
 // Tokens that are not there give silu(bias); their steps are zero and their outputs are not written.
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-template <int TB>
-__device__ __forceinline__ void convolve(const uint2 (&raw)[TB + 3], int k, const float *w, const float *b, float (&v)[TB]) {
+template <int TB, bool FOUR>
+__device__ __forceinline__ void convolve(const uint2 (&raw)[TB + 3], int k, int W, const float *w, const float *b, float (&v)[TB]) {
   const f32x4 tap = *reinterpret_cast<const f32x4 *>(w + 4 * k);
   const float bias = b[k];
 #pragma unroll
@@ -679,7 +680,8 @@ __device__ __forceinline__ void convolve(const uint2 (&raw)[TB + 3], int k, cons
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t u = k < 2 ? raw[t + i].x : raw[t + i].y;
-      s = fmaf(tap[i], __uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), s);
+      const float with = fmaf(tap[i], __uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), s);
+      s = FOUR || i >= 4 - W ? with : s;
     }
     v[t] = s * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s));
   }
@@ -755,7 +757,7 @@ template <int NT> __host__ __device__ constexpr size_t chunk_lds(int rows, int n
          sizeof(float) * (16 * NT + rows * (XS + 1) + 6 * (32 * NT + rows) + nw * 5 * Q);
 }
 
-template <int NT, int PT, bool LOCAL>
+template <int NT, int PT, bool LOCAL, bool FOUR>
 __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
   extern __shared__ __align__(16) char smem[];
   constexpr int NP = 16 * NT, NS = NP + 8, KN = NT / 2, PS = 16 * PT;
@@ -792,7 +794,6 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
   auto weights = [&](int k, int c) {
     chans[k] = c;
     if (c < 0) return;
-    if (p.W < 4) *reinterpret_cast<f32x4 *>(wl + 4 * k) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     for (int i = 0; i < p.W; ++i) wl[4 * k + 4 - p.W + i] = p.conv_w[(int64_t)c * p.W + i] * -LOG2E;
     bl[k] = p.conv_b ? p.conv_b[c] * -LOG2E : 0.0f;
   };
@@ -813,8 +814,8 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
     for (int k = 0; k < 4; k += 2) {
       __builtin_amdgcn_sched_barrier(0);
       float v[2][TB];
-      convolve<TB>(raw, k, wl + 4 * k0, bl + k0, v[0]);
-      convolve<TB>(raw, k + 1, wl + 4 * k0, bl + k0, v[1]);
+      convolve<TB, FOUR>(raw, k, p.W, wl + 4 * k0, bl + k0, v[0]);
+      convolve<TB, FOUR>(raw, k + 1, p.W, wl + 4 * k0, bl + k0, v[1]);
       if (!LOCAL) {
         uint16_t *to = (isC ? Cs : Bs) + TB * tg * NS + n0 + k;
 #pragma unroll
@@ -851,7 +852,7 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
     for (int k = 0; k < 4; ++k) {
       if (k % 2 == 0) __builtin_amdgcn_sched_barrier(0);
       float v[8];
-      convolve<8>(raw, k, wl + 4 * (2 * NP + x0), bl + 2 * NP + x0, v);
+      convolve<8, FOUR>(raw, k, p.W, wl + 4 * (2 * NP + x0), bl + 2 * NP + x0, v);
       float *to = Xall + (x0 + k) * XS + 8 * tg;
       *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
       *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -1172,8 +1173,8 @@ bool chunks_fit(const SsmArgs &p) {
   return p.P % 16 == 0 && p.N % 16 == 0 && p.W <= 4 && p.ld_xbc < most && p.ld_dt < most && p.ld_out < most && (!p.z || p.ld_z < most);
 }
 
-template <int NT, int PT>
-int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
+template <int NT, int PT, bool FOUR>
+int launch_chunks_of(vf_ctx *c, SsmArgs &p, int64_t longest) {
   constexpr int PS = 16 * PT, NW = ROWS / PS;
   // workgroups of a group's heads, each with the same number of waves but for the last
   const int jobs = p.H / p.G * ((p.P + PS - 1) / PS), per = (jobs + NW - 1) / NW, nw = (jobs + per - 1) / per;
@@ -1184,19 +1185,23 @@ int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
   // a segment costs its state's way to memory and back, about 256 tokens' time
   split(c, p, longest, each, at_once, Q, 256);
   if (smem > 65536) {
-    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, false>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, true>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, false, FOUR>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(k_ssm_chunks<NT, PT, true, FOUR>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   }
   // many short parts: a workgroup takes several, so that its weights are fetched once for them, but there are eight times as many
   // workgroups as run at a time, for the sake of unequal parts
   const int64_t wgs = (int64_t)per * p.G, parts = (int64_t)p.n_seq * p.nseg, most = 8 * at_once / wgs > 1 ? 8 * at_once / wgs : 1;
   const unsigned blocks = (unsigned)((parts < most ? parts : most) * wgs);
   return run_parts(c, p, [&] {
-    if (p.local) k_ssm_chunks<NT, PT, true><<<blocks, 64 * nw, smem, c->stream>>>(p);
-    else k_ssm_chunks<NT, PT, false><<<blocks, 64 * nw, smem, c->stream>>>(p);
+    if (p.local) k_ssm_chunks<NT, PT, true, FOUR><<<blocks, 64 * nw, smem, c->stream>>>(p);
+    else k_ssm_chunks<NT, PT, false, FOUR><<<blocks, 64 * nw, smem, c->stream>>>(p);
     VF_HIP(c, hipGetLastError());
     return VF_OK;
   });
+}
+template <int NT, int PT>
+int launch_chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
+  return p.W == 4 ? launch_chunks_of<NT, PT, true>(c, p, longest) : launch_chunks_of<NT, PT, false>(c, p, longest);
 }
 int chunks(vf_ctx *c, SsmArgs &p, int64_t longest) {
   // Four waves of 64 rows, two workgroups on a compute unit, where the state leaves registers for it; else eight waves of 32 rows.

@@ -2,6 +2,7 @@
 Tolerances are those of test_gpu_ssm."""
 import numpy as np
 import pytest
+import torch
 
 from tests.test_gpu_ssm import Case, ctx, vf  # noqa: F401
 
@@ -48,3 +49,25 @@ def test_small_steps_behind_large_ones(vf, ctx, sizes, lens, large, small, a):  
     new = c.layer.state(len(lens), c.dtype)
     out = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, n_seq=len(lens), longest=max(lens), offsets=c.offsets, state_out=new)
     c.check(out, c.ref(), True, new)
+
+
+@pytest.mark.parametrize("sizes", [(4, 64, 1, 64, 3), (2, 64, 2, 128, 2), (3, 48, 1, 32, 1), (1, 16, 1, 256, 3), (4, 32, 2, 64, 4)], ids=str)
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")], ids=str)
+def test_c_that_is_not_finite_reaches_the_tokens_that_see_it(vf, ctx, sizes, value):  # noqa: F811
+    """A column of C at one token is met by the W tokens of the convolution's window from there on, by the heads of its group, and
+    nobody else: it does not go into the state."""
+    H, P, G, N, W = sizes
+    c = Case(vf, sizes, [40, 70], "bf16", seed=6)
+    args = dict(n_seq=2, longest=70, offsets=c.offsets)
+    clean = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, **args)
+    for at in (9, 31, 40 + 30, 40 + 63):
+        col = H * P + G * N + (G - 1) * N + 5
+        kept = c.xbc[at, col].clone()
+        c.xbc[at, col] = value
+        hurt = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, **args)
+        c.xbc[at, col] = kept
+        seen = torch.zeros_like(clean, dtype=torch.bool)
+        seen[at:min(at + W, 40 if at < 40 else 110), H // G * (G - 1) * P:] = True
+        assert torch.equal(hurt[~seen], clean[~seen])
+        if value != value:
+            assert bool(hurt[seen].isnan().all())
