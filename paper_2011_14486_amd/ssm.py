@@ -39,6 +39,7 @@ class SsmValue:
         self.inner = sizes[0] * sizes[1]
         self.w_in, self.gain = four(weights["w_in"]), dev(weights["gain"])
         self.w_head, self.b_head = four(weights["w_head"]), dev(weights["b_head"])
+        self.not_there = torch.tensor([float("nan"), float("nan"), 0.0], device=ctx.device)
         self.blocks = []
         for b in weights["blocks"]:
             layer = vf.SsmLayer(*sizes, **{k: dev(b[k]) for k in ("conv_w", "conv_b", "a", "d", "dt_bias")})
@@ -65,8 +66,7 @@ class SsmValue:
         return vf.vf_mx_matmul(ctx, rows, self.w_head, bias=self.b_head, out_type=vf.VF_FP32)[:, 0]
 
     def score(self, x, n_seq=1, longest=None, offsets=None, state=None, slots=None, state_out=None, slots_out=None):
-        """Values [n_seq] of whole sequences x bf16 [tokens][F]; other arguments as vf_ssm_scan; slots lie
-        within their state."""
+        """Values [n_seq] of whole sequences x bf16 [tokens][F]; other arguments as vf_ssm_scan."""
         torch = self.torch
 
         def scan(k, layer, xbc, dt, z):
@@ -82,19 +82,28 @@ class SsmValue:
         return self._totals(value, state, slots, state_out, slots_out)
 
     def extend(self, x, state, slots=None, state_out=None, slots_out=None):
-        """Values [rows] with one more stage x bf16 [rows][F]: row r continues slot slots[r] of `state` and leaves its state in
-        slot slots_out[r] of `state_out`."""
+        """Values [rows] with one more stage x bf16 [rows][F]: row r continues slot slots[r] of `state` (-1: the empty prefix) and
+        leaves its state in slot slots_out[r] of `state_out` (-1: nowhere)."""
         def scan(k, layer, xbc, dt, z):
             return vf.vf_ssm_step(self.ctx, layer, xbc, dt, z, state.blocks[k], slots, None if state_out is None else state_out.blocks[k], slots_out)
 
         return self._totals(self._tokens(x, scan), state, slots, state_out, slots_out)
 
     def _totals(self, value, state, slots, state_out, slots_out):
+        """Sums by slots as the operators have them: -1 is the empty prefix, or no place to leave one; a slot that is not there reads as
+        NaN and is not written.  (The sums with three numbers behind them: past the end, -2 and -1 as indexes.)"""
+        behind = lambda total, k: (self.torch.cat((total, self.not_there)), k.clamp(-2, total.shape[0]).long())   # noqa: E731
         if state is not None:
-            value = value + (state.total[:value.shape[0]] if slots is None else state.total[slots.long()])
+            if slots is None:
+                value = value + state.total[:value.shape[0]]
+            else:
+                sums, at = behind(state.total, slots)
+                value = value + sums[at]
         if state_out is not None:
             if slots_out is None:
                 state_out.total[:value.shape[0]] = value
             else:
-                state_out.total[slots_out.long()] = value
+                sums, at = behind(state_out.total, slots_out)
+                sums[at] = value
+                state_out.total.copy_(sums[:-3])
         return value

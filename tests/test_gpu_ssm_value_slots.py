@@ -1,0 +1,73 @@
+"""GPU: slots, offsets and numbers of sequences of the state-space value network mean what they mean for its operators."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+F, WIDTH = 16, 64
+
+
+@pytest.fixture(scope="module")
+def vf():
+    import paper_2011_14486_amd as pkg
+    return pkg.load()
+
+
+@pytest.fixture(scope="module")
+def ctx(vf):
+    c = vf.vf_create(0)
+    yield c
+    vf.vf_destroy(c)
+
+
+@pytest.fixture(scope="module")
+def net(ctx):
+    from paper_2011_14486_amd import inputs, ssm
+    return ssm.SsmValue(ctx, inputs.ssm_weights(F, WIDTH, 2, 2, 32, 1, 16, 4, seed=2))
+
+
+def stages(n, seed=0):
+    import torch
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal((n, F))).to(torch.bfloat16).cuda()
+
+
+def i32(*v):
+    import torch
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def parts(state):
+    return [t for b in state.blocks for t in b] + [state.total]
+
+
+def test_slots_of_none(net):
+    """-1 is the empty prefix where a state is taken, and no place where it is left, for the sums as for the states."""
+    import torch
+    prefixes, empty = net.state(3), net.state(4)
+    net.score(stages(30), n_seq=3, state_out=prefixes)
+    x = stages(4, 1)
+    from_nothing = net.extend(x, empty)
+    got = net.extend(x, prefixes, i32(1, -1, 2, -1))
+    assert torch.equal(got[[1, 3]], from_nothing[[1, 3]])
+    assert torch.equal(got[[0, 2]], net.extend(x, prefixes, i32(1, 0, 2, 0))[[0, 2]])
+    whole = net.score(stages(20, 2), n_seq=2, state=prefixes, slots=i32(-1, 0))
+    assert torch.equal(whole[0], net.score(stages(20, 2), n_seq=2)[0])
+    # left in slots 2 and 0 only
+    for out in (net.state(3), prefixes):
+        for t in parts(out):
+            t.fill_(2.5)
+        got = net.extend(x, empty, None, out, i32(2, -1, 0, -1))
+        assert float(out.total[2]) == float(got[0]) and float(out.total[0]) == float(got[2])
+        assert all(bool((t[1] == 2.5).all()) for t in parts(out))
+
+
+def test_slots_that_are_not_there(net):
+    """They read as NaN and are written nowhere."""
+    import torch
+    state = net.state(3)
+    x = stages(3, 3)
+    got = net.extend(x, state, i32(0, 3, -2))
+    assert torch.equal(got[0], net.extend(x, state)[0]) and bool(got[1:].isnan().all())
+    for t in parts(state):
+        t.fill_(1.5)
+    net.extend(x, net.state(3), None, state, i32(3, -2, 1))
+    assert all(bool((t[[0, 2]] == 1.5).all()) for t in parts(state)) and float(state.total[1]) != 1.5
