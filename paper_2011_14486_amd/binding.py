@@ -392,7 +392,7 @@ def _rows_of(ctx, t, rows, cols, dtype, name):
     if t.shape != (rows, cols) or t.dtype != dtype or t.device != ctx.device:
         _fail(f"{name}: {dtype} [{rows}][{cols}] on {ctx.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     ld, step = t.stride()
-    if step != 1 and cols > 1:
+    if step != 1 and cols > 1 and rows > 0:   # (tensors without elements come with any strides)
         _fail(f"{name}: the last dimension has to be dense")
     return ld if rows > 1 or ld > cols else cols
 
