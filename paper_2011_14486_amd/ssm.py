@@ -75,7 +75,7 @@ class SsmValue:
 
         each = self._tokens(x, scan)
         if offsets is None:
-            value = each.reshape(n_seq, -1).sum(1)
+            value = each.reshape(n_seq, each.shape[0] // n_seq if n_seq else 0).sum(1)
         else:
             ranges = offsets.long().clamp(0, each.shape[0]).cummax(0).values   # (segment_reduce looks at no bounds)
             value = torch.segment_reduce(each, "sum", offsets=ranges, unsafe=True, initial=0)

@@ -71,3 +71,21 @@ def test_slots_that_are_not_there(net):
         t.fill_(1.5)
     net.extend(x, net.state(3), None, state, i32(3, -2, 1))
     assert all(bool((t[[0, 2]] == 1.5).all()) for t in parts(state)) and float(state.total[1]) != 1.5
+
+
+def test_no_sequences(net):
+    state = net.state(2)
+    for t in parts(state):
+        t.fill_(0.5)
+    for more in (dict(), dict(offsets=i32(0)), dict(state=net.state(2)), dict(state_out=state), dict(slots_out=i32(), state_out=state)):
+        assert net.score(stages(0), n_seq=0, **more).shape == (0,)
+    assert net.extend(stages(0), net.state(2)).shape == (0,)
+    assert all(bool((t == 0.5).all()) for t in parts(state))
+
+
+def test_sequences_without_tokens(net):
+    import torch
+    kept = net.state(3)
+    want = net.score(stages(30), n_seq=3, state_out=kept)
+    assert torch.equal(net.score(stages(0), n_seq=3, state=kept), want)
+    assert not net.score(stages(0), n_seq=3).any()
