@@ -67,8 +67,6 @@ class SsmValue:
 
     def score(self, x, n_seq=1, longest=None, offsets=None, state=None, slots=None, state_out=None, slots_out=None):
         """Values [n_seq] of whole sequences x bf16 [tokens][F]; other arguments as vf_ssm_scan."""
-        torch = self.torch
-
         def scan(k, layer, xbc, dt, z):
             return vf.vf_ssm_scan(self.ctx, layer, xbc, dt, z, n_seq, longest, offsets, None if state is None else state.blocks[k], slots,
                                   None if state_out is None else state_out.blocks[k], slots_out)
@@ -77,9 +75,22 @@ class SsmValue:
         if offsets is None:
             value = each.reshape(n_seq, each.shape[0] // n_seq if n_seq else 0).sum(1)
         else:
-            ranges = offsets.long().clamp(0, each.shape[0]).cummax(0).values   # (segment_reduce looks at no bounds)
-            value = torch.segment_reduce(each, "sum", offsets=ranges, unsafe=True, initial=0)
+            value = self._sums(each, offsets.long())
         return self._totals(value, state, slots, state_out, slots_out)
+
+    def _sums(self, each, offsets):
+        """Sums of the sequences' predictions; ranges as the scan takes them: one that does not lie in the tokens is empty."""
+        torch, tokens = self.torch, each.shape[0]
+        begin, end = offsets[:-1], offsets[1:]
+        if tokens == 0 or begin.shape[0] == 0:
+            return each.new_zeros(begin.shape[0])
+        there = (begin >= 0) & (end >= begin) & (end <= tokens)
+        # in the order of their begins, so that begins and ends ascend (segment_reduce looks at nothing); every second segment lies
+        # between two ranges
+        begin, order = torch.where(there, begin, tokens).sort(stable=True)
+        ranges = torch.stack((begin, torch.where(there, end, tokens)[order]), 1).reshape(-1).cummax(0).values
+        sums = torch.segment_reduce(each, "sum", offsets=ranges, unsafe=True, initial=0)
+        return torch.empty_like(sums[::2]).index_copy_(0, order, sums[::2])
 
     def extend(self, x, state, slots=None, state_out=None, slots_out=None):
         """Values [rows] with one more stage x bf16 [rows][F]: row r continues slot slots[r] of `state` (-1: the empty prefix) and

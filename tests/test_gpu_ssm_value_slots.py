@@ -89,3 +89,23 @@ def test_sequences_without_tokens(net):
     want = net.score(stages(30), n_seq=3, state_out=kept)
     assert torch.equal(net.score(stages(0), n_seq=3, state=kept), want)
     assert not net.score(stages(0), n_seq=3).any()
+
+
+@pytest.mark.parametrize("offsets", [(12, 20, 0, 5, 12), (0, 5, 25, 30, 20), (-3, 5, 10, 15, 20), (3, 5, 10, 15, 17), (0, 5, -1, 12, 20)], ids=str)
+def test_ranges_that_are_not_there_are_empty(net, offsets):
+    """A sequence whose range does not lie in the tokens, or ends before its begin, has the value of no tokens, and others have
+    their whole ranges', in any order."""
+    import torch
+    x = stages(20, 4)
+    state, left = net.state(4), net.state(4)
+    net.score(stages(8, 5), n_seq=4, state_out=state)
+    got = net.score(x, n_seq=4, longest=20, offsets=i32(*offsets), state=state, state_out=left)
+    assert torch.equal(left.total, got)
+    for s in range(4):
+        a, b = offsets[s], offsets[s + 1]
+        if a < 0 or b < a or b > 20 or a == b:
+            assert float(got[s]) == float(state.total[s])
+            continue
+        alone = net.score(x, n_seq=1, longest=20, offsets=i32(a, b), state=state, slots=i32(s))
+        # (sums of the same fp32 predictions in some order: at most 20 of them, each under 10)
+        assert abs(float(got[s]) - float(alone[0])) <= 1e-4 * max(1.0, abs(float(alone[0])))
