@@ -336,8 +336,8 @@ typedef struct {
  *   S[h][p][n] = exp(step a[h]) S[h][p][n] + step x[h][p] B[g][n];
  *   y[h][p] = sum_n S[h][p][n] C[g][n] + d[h] x[h][p];   out = y silu(z[t]) (z NULL: y).
  * Sequences of bf16 with head_dim and n_state multiples of 16 and at most four taps run in chunks on the matrix
- * cores, where operands of the outputs' products are rounded to bf16 and outputs behind an x that is not finite are
- * NaN; others run token by token in fp32.  A call may keep scratch in the context (a few long
+ * cores, where B and C are rounded to bf16 for what tokens add to outputs up to 31 tokens behind them, and outputs behind an
+ * x, a state or a C that is not finite may be NaN in place of an infinity; others run token by token in fp32.  A call may keep scratch in the context (a few long
  * sequences are split along their length); a call whose stream is being captured takes no new scratch
  * and does without.  A graph that holds such a call is replayed on the context's stream, or ordered with it. */
 int vf_ssm_scan(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);

@@ -71,3 +71,20 @@ def test_c_that_is_not_finite_reaches_the_tokens_that_see_it(vf, ctx, sizes, val
         assert torch.equal(hurt[~seen], clean[~seen])
         if value != value:
             assert bool(hurt[seen].isnan().all())
+
+
+@pytest.mark.parametrize("sizes", SIZES + [(7, 16, 1, 160, 3)], ids=str)
+@pytest.mark.parametrize("lens", [[20, 50, 33], [1100]], ids=str)
+def test_outputs_behind_a_state(vf, ctx, sizes, lens):  # noqa: F811
+    """Inputs of zeros, small steps: outputs are the products of the state that the sequences began from with C.  Both are in two parts
+    of bf16: what is left out of either, and the product of the two second parts, is 2^-16 each."""
+    c = Case(vf, sizes, lens, "bf16", plain=True, slots=len(lens), seed=11)
+    H, P, G, N, W = sizes
+    c.state[0][:, :H * P] = 0
+    c.xbc[:, :H * P] = 0
+    c.dt[:] = -9.0
+    out = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, n_seq=len(lens), longest=max(lens), offsets=c.offsets, state=c.state)
+    want, _, _, omag, _ = c.ref()
+    err = np.abs(out.double().cpu().numpy() - want)
+    tol = (3 * 2.0 ** -16 + (128 + max(lens) + N) * 2.0 ** -24) * omag + 2.0 ** -8 * np.abs(want)
+    assert (err <= tol).all(), float((err / tol).max())
