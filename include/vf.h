@@ -307,7 +307,7 @@ typedef struct {
  * (nullable), out [tokens][H P], all of `type`, each with its row distance, usually views of one
  * projection's output.  Sequence s is rows offsets[s] .. offsets[s + 1] - 1 (offsets_dev int32
  * [n_seq + 1]); without offsets every sequence has tokens / n_seq rows.  A range that does not lie in
- * 0..tokens, or whose end is before its begin, counts as empty, rows of no sequence are not written.
+ * 0..tokens, or whose end is before its begin, counts as empty, rows of no sequence are not written; ranges do not overlap.
  * longest: the longest sequence's length, which sets how the work is split (longer ones are right, but slow).
  * State kept per slot: conv [slots][C][W - 1] of `type` (the last inputs, oldest first) and
  * ssm [slots][H][P][N] fp32.  Sequence s begins from slot slots_in[s] of conv_in / ssm_in (-1: from
@@ -337,9 +337,9 @@ typedef struct {
  *   y[h][p] = sum_n S[h][p][n] C[g][n] + d[h] x[h][p];   out = y silu(z[t]) (z NULL: y).
  * Sequences of bf16 with head_dim and n_state multiples of 16 and at most four taps run in chunks on the matrix
  * cores, where B and C are rounded to bf16 for what tokens add to outputs up to 31 tokens behind them, and outputs behind an
- * x, a state or a C that is not finite may be NaN in place of an infinity; others run token by token in fp32.  A call may keep scratch in the context (a few long
- * sequences are split along their length); a call whose stream is being captured takes no new scratch
- * and does without.  A graph that holds such a call is replayed on the context's stream, or ordered with it. */
+ * x, a state or a C that is not finite may be NaN in place of an infinity; others run token by token in fp32.
+ * A call may keep scratch in the context until vf_destroy, up to 260 MiB for a call and 1 GiB in all (a few long sequences are split along
+ * their length); a call whose stream is being captured takes no new scratch and does without.  A graph that holds such a call is replayed on the context's stream, or ordered with it. */
 int vf_ssm_scan(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);
 /* One token for every sequence (tokens == n_seq, offsets NULL; longest is ignored). */
 int vf_ssm_step(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);

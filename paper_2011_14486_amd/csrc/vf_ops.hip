@@ -64,7 +64,8 @@ void *vfk_ops_scratch(vf_ctx *c, size_t bytes) {
     return nullptr;
   }
   if (c->ops_blocks == 48) return nullptr;
-  // at least twice the last block, so that what stays behind is less than what is held
+  // at least twice the last block, so that what stays behind is less than what is held (no call asks for more than 260 MiB, so all
+  // blocks together stay below 1 GiB)
   const size_t want = bytes < 2 * c->ops_bytes ? 2 * c->ops_bytes : bytes;
   void *p = nullptr;
   if (hipMalloc(&p, want) != hipSuccess) {

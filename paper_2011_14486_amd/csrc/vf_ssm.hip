@@ -492,8 +492,8 @@ void split(vf_ctx *c, SsmArgs &p, int64_t longest, int64_t each, int64_t want, i
   int64_t len = ((longest + n - 1) / n + unit - 1) / unit * unit;
   n = (longest + len - 1) / len;
   if (n < 2) return;
+  // (at most 256 MiB of states: 8192 numbers for each wave of four rounds, which are eight waves on each of 256 compute units)
   const int64_t states = (int64_t)p.n_seq * n * p.H * p.P * p.N, logs = (int64_t)p.n_seq * n * p.H;
-  if (states > (int64_t)1 << 31) return;
   float *at = static_cast<float *>(vfk_ops_scratch(c, (size_t)(states + logs) * sizeof(float)));
   if (!at) return;
   p.nseg = (int)n;
