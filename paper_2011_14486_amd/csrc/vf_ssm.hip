@@ -589,8 +589,8 @@ int step(vf_ctx *c, const SsmArgs &p) {
 // bf16; B and C (for C_t . B_s) are rounded to one, which is less than 2 % of an output's own rounding over 300 tokens (error to the
 // outputs' size in root mean square 1.68e-3, of exact outputs rounded 1.66e-3; with S and C in one part behind a state of the
 // outputs' size 2.8e-3, and 3 - 7 % less time).  The state is fp32: what it takes up,
-// x step e^(...) and B, is in two parts of fp16 each, 22 bits together, scaled by powers of two to fp16's range (x by
-// the wave's largest, B by its row's), which the sum takes back.
+// x step e^(...) and B, is in two parts of fp16 each, 22 bits together, scaled by powers of two to fp16's range (the products with
+// x by their row's largest, B by its row's), which the sum takes back.
 //
 // The waves of a workgroup take neighbouring heads of one group and convolve its B and C together.  All bytes of x, z, out
 // pass once; what bounds the kernel is the vector work on them: convolution, silu (two quarter-rate
@@ -697,6 +697,13 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t max_lanes(uint32_t m) {
   return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, CTRL, 0xf, 0xf, true));
 }
+// over the lanes r, 16 + r, 32 + r, 48 + r
+__device__ __forceinline__ uint32_t max_rows(uint32_t m) {
+  const auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  m = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return max((uint32_t)b[0], (uint32_t)b[1]);
+}
 template <int TB>
 __device__ __forceinline__ float top_of_32(const float (&v)[TB]) {
   uint32_t m = 0;
@@ -707,7 +714,7 @@ __device__ __forceinline__ float top_of_32(const float (&v)[TB]) {
   if (TB == 4) m = max_lanes<0x141>(m); // lanes 7 .. 0 of eight
   return __uint_as_float(m);
 }
-// the value N lanes before, or behind, in the same 16, zero where there is none; and the last of the 16 before, for the second and fourth 16
+// the value N lanes before, or behind, in the same 16, zero where there is none
 template <int N>
 __device__ __forceinline__ float lanes_before(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x110 + N, 0xf, 0xf, true));
@@ -729,9 +736,6 @@ __device__ __forceinline__ float sum_from(float v) {
   v += lanes_behind<4>(v);
   return v + lanes_behind<8>(v);
 }
-__device__ __forceinline__ float row_before(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
-}
 
 __device__ __forceinline__ bf16x8 frag16(const uint16_t *at) { return *reinterpret_cast<const bf16x8 *>(at); }
 // k = 8 q + i of the operand is number 4 q + i, i < 4, and 16 + 4 q + i - 4 of the row: how accumulators lie
@@ -750,7 +754,7 @@ __device__ __forceinline__ uint4 rest_of(const f32x4 &a, const f32x4 &b, const u
 #define VF_MFMA_B(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0)
 #define VF_MFMA_H(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0)
 
-// LDS: B and C by tokens, C's second part, B by n in two parts and its scales; per wave x by p and its scales, weights of the convolution of all of
+// LDS: B and C by tokens, C's second part, B by n in two parts and its scales; per wave x by p and its rows' largest, weights of the convolution of all of
 // these channels; per wave five numbers for each of the chunk's tokens.
 constexpr int ROWS = 256;  // most rows p of a workgroup: PT tiles of 16 a wave
 // `rows` of them, in `nw` waves
@@ -862,9 +866,9 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
       float *to = Xall + (x0 + k) * XS + 8 * tg;
       *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
       *reinterpret_cast<f32x4 *>(to + 4) = f32x4{v[4], v[5], v[6], v[7]};
-      top[k] = top_of_32<8>(v);
+      if (!LOCAL) top[k] = top_of_32<8>(v);
     }
-    if (tg == 0) *reinterpret_cast<f32x4 *>(xsall + x0) = f32x4{top[0], top[1], top[2], top[3]};
+    if (!LOCAL && tg == 0) *reinterpret_cast<f32x4 *>(xsall + x0) = f32x4{top[0], top[1], top[2], top[3]};
   };
   // The piece whose inputs are fetched a chunk ahead.  PT = 4: a piece of x for every thread, those of B and C are asked for at the
   // chunk's begin and taken behind x.  PT = 2: pieces of x from the last thread down, of B and C from the first one up.
@@ -978,7 +982,7 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
 #pragma unroll
         for (int j = 0; j < PT; ++j) zr[t][j] = load4(zm, t0 + 16 * t + r, 16 * j < np ? 2 * (h * p.P + p0 + 16 * j + 4 * q) : 0);
     }
-    float last = 0.0f, wtop = 0.0f;
+    float last = 0.0f;
     if (on) {
       const int t = lane & (Q - 1);
       const float dt = t0 + t < end ? softplus(bf16_f32(dt_raw) + bias_dt) : 0.0f;
@@ -995,13 +999,6 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
         stp[t] = dt * -(LN2 * LN2 * LN2);  // (x, B and C are each to be multiplied by -ln 2)
         wgt[t] = w;
       }
-      float m = w;
-      m = fmaxf(m, lanes_before<1>(m));
-      m = fmaxf(m, lanes_before<2>(m));
-      m = fmaxf(m, lanes_before<4>(m));
-      m = fmaxf(m, lanes_before<8>(m));
-      m = fmaxf(m, row_before(m));
-      wtop = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), Q - 1));
       log_decay += last;
     }
     {
@@ -1127,11 +1124,14 @@ __global__ void __launch_bounds__(1024 / PT, 2) k_ssm_chunks(const SsmArgs p) {
     const f32x4 w0 = *reinterpret_cast<const f32x4 *>(wgt + 4 * q), w1 = *reinterpret_cast<const f32x4 *>(wgt + 16 + 4 * q);
 #pragma unroll
     for (int j = 0; j < PT; ++j) {
-      const float f = scale_to_f16(xs[16 * j + r] * wtop);
+      // (The scale goes by the products, not by the largest x and weight: where a large step meets zeros these are far from all products.
+      // Up to 2^126 where a row is zero, it comes last: times a weight it may be infinite.)
+      f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * w0;
+      f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * w1;
+      const float f = scale_to_f16(__uint_as_float(max_rows(max_abs(max_abs(max_abs(max_abs(0, a[0], a[1]), a[2], a[3]), b[0], b[1]), b[2], b[3]))));
       back[j] = power_reciprocal(f);
-      // (first by the weight: f is up to 2^126 where a row is zero or next to it, and w f may be infinite)
-      const f32x4 a = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 4 * q) * w0 * f;
-      const f32x4 b = *reinterpret_cast<const f32x4 *>(X + (16 * j + r) * XS + 16 + 4 * q) * w1 * f;
+      a *= f;
+      b *= f;
       vh[j] = make_uint4(pack_h(a[0], a[1]), pack_h(a[2], a[3]), pack_h(b[0], b[1]), pack_h(b[2], b[3]));
       vl[j] = make_uint4(rest_h(a[0], a[1], vh[j].x), rest_h(a[2], a[3], vh[j].y), rest_h(b[0], b[1], vh[j].z), rest_h(b[2], b[3], vh[j].w));
     }

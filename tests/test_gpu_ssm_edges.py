@@ -88,3 +88,23 @@ def test_outputs_behind_a_state(vf, ctx, sizes, lens):  # noqa: F811
     err = np.abs(out.double().cpu().numpy() - want)
     tol = (3 * 2.0 ** -16 + (128 + max(lens) + N) * 2.0 ** -24) * omag + 2.0 ** -8 * np.abs(want)
     assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=str)
+@pytest.mark.parametrize("lens", [[32, 64, 100], [1100]], ids=str)
+@pytest.mark.parametrize("large", [1000.0, 1e6, 1e12], ids=str)
+def test_large_steps_that_meet_zeros(vf, ctx, sizes, lens, large):  # noqa: F811
+    """A large step where all of x is zero clears the state and adds nothing: what small steps (1.2e-4) add in the same chunk is as
+    exact as without it."""
+    c = Case(vf, sizes, lens, "bf16", plain=True, seed=12)
+    H, P, G, N, W = sizes
+    rng = np.random.default_rng(13)
+    c.dt[:] = -9.0
+    for first, count in zip(c.first, c.lens):
+        for chunk in range(first, first + count, 32):
+            t = min(chunk + int(rng.integers(0, 28)), first + count - 1)
+            c.dt[t] = large
+            c.xbc[max(t - W + 1, first):t + 1, :H * P] = 0.0
+    new = c.layer.state(len(lens), c.dtype)
+    out = vf.vf_ssm_scan(ctx, c.layer, c.xbc, c.dt, c.z, n_seq=len(lens), longest=max(lens), offsets=c.offsets, state_out=new)
+    c.check(out, c.ref(), True, new)
