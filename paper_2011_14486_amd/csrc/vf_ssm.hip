@@ -594,8 +594,9 @@ int step(vf_ctx *c, const SsmArgs &p) {
 //
 // The waves of a workgroup take neighbouring heads of one group and convolve its B and C together.  All bytes of x, z, out
 // pass once; what bounds the kernel is the vector work on them: convolution, silu (two quarter-rate
-// functions a number) and the operands' parts.  MI355X: 16,384 sequences of 50 tokens, 4 heads of 64 x 64, 626 - 654 us = 2.3 TB/s;
-// a prompt of 16,384 tokens, 32 heads of 64 x 128, 255 us: local states 92, join 13, outputs 166.
+// functions a number) and the operands' parts, among it 220 to 340 scalar registers that do not fit and are kept in lanes of vector
+// registers.  MI355X: 16,384 sequences of 50 tokens, 4 heads of 64 x 64, 670 us = 2.2 TB/s; a prompt of 16,384 tokens, 32 heads of 64 x 128, 268 us
+// (under the profiler local states 90, join 13, outputs 185).  More than 128 numbers n: 268 bytes a lane are in memory.
 
 constexpr int Q = 32;            // tokens of a chunk
 constexpr int XS = Q + 4;        // row of x in the LDS, floats
