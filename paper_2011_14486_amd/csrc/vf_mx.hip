@@ -212,6 +212,7 @@ __global__ void __launch_bounds__(256) k_mx_rows(const MatmulArgs p) {
 // the last one are stored.
 // MI355X: 16384 x 8192 x 4096 with 8-bit rows 455 us = 2.4 PFLOP/s (the vendor library's product of 8-bit by 8-bit numbers 2.65 at 8192^3;
 // 0.74 ms with a barrier at a stage's end and scales fetched every stage), 5000 x 4384 x 4096 in 4 bits 78 - 87 us.
+// The matrix cores are busy 53 % of the cycles there, and 26 % in 4 bits, where an instruction takes half the time.
 template <int AF> constexpr int a_bytes() { return AF == VF_E4M3 ? 128 : 64; }   // of a row, in a stage
 template <int AF> constexpr int stages() { return AF == VF_E4M3 ? 3 : 4; }       // that the LDS holds
 // WM by WN waves of 64 rows by 16 NT columns: a thread for every row and column of the tile

@@ -588,7 +588,7 @@ int step(vf_ctx *c, const SsmArgs &p) {
 // Rounding: the outputs are bf16.  As operands S and C (for S C_t), the 32 x 32 matrix with d on its diagonal, and x are in two parts of
 // bf16; B and C (for C_t . B_s) are rounded to one, which is less than 2 % of an output's own rounding over 300 tokens (error to the
 // outputs' size in root mean square 1.68e-3, of exact outputs rounded 1.66e-3; with S and C in one part behind a state of the
-// outputs' size 2.8e-3, and 3 - 7 % less time).  The state is fp32: what it takes up,
+// outputs' size 2.8e-3, and 3 - 15 % less time).  The state is fp32: what it takes up,
 // x step e^(...) and B, is in two parts of fp16 each, 22 bits together, scaled by powers of two to fp16's range (the products with
 // x by their row's largest, B by its row's), which the sum takes back.
 //
