@@ -93,11 +93,13 @@ def draw(rng):
         case.update(longest=longest, seqs=max(1, min(_log(rng, 1, 256), (1 << 27) // (each * longest))), heads=kv_heads)
         return case
     longest = 1 if rng.random() < 0.5 else _log(rng, 2, 4096)
-    past = 0 if longest > 1 and rng.random() < 0.4 else _log(rng, 16, 131072 if rng.random() < 0.5 else 4096)
+    causal = rng.random() < 0.8
+    past = 0 if causal and longest > 1 and rng.random() < 0.4 else _log(rng, 16, 131072 if rng.random() < 0.5 else 4096)
     past = min(past, CACHE // 2 // each - longest, max(0, (SCORES // 4) // (heads * longest) - longest))
+    past = max(past, 0 if causal else 1)
     both = past + longest
     seqs = min(_log(rng, 1, 4096), SCORES // 4 // (heads * longest * both), CACHE // (2 * each * both))
-    case.update(longest=longest, past=max(0, past), seqs=max(1, seqs), causal=rng.random() < 0.8,
+    case.update(longest=longest, past=past, seqs=max(1, seqs), causal=causal,
                 window=_log(rng, 8, 4096) if rng.random() < 0.25 else 0, shared=0)
     if longest == 1 and case["seqs"] >= 4 and rng.random() < 0.4:   # extensions of fewer prefixes than rows
         case["shared"] = max(1, case["seqs"] // rng.choice([2, 4, 16]))
