@@ -89,8 +89,9 @@ def draw(rng):
         case["past"] = min(case["past"], CACHE // 8 // (case["seqs"] * each))
         return case
     if op == "read":
-        longest = min(_log(rng, 1, 8192), (1 << 27) // each)
-        case.update(longest=longest, seqs=max(1, min(_log(rng, 1, 256), (1 << 27) // (each * longest))), heads=kv_heads)
+        most = (1 << 26 if kind == "fp32" else 1 << 27) // each
+        longest = min(_log(rng, 1, 8192), most)
+        case.update(longest=longest, seqs=max(1, min(_log(rng, 1, 256), most // longest)), heads=kv_heads)
         return case
     longest = 1 if rng.random() < 0.5 else _log(rng, 2, 4096)
     causal = rng.random() < 0.8
