@@ -344,6 +344,76 @@ int vf_ssm_scan(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host)
 /* One token for every sequence (tokens == n_seq, offsets NULL; longest is ignored). */
 int vf_ssm_step(vf_ctx *ctx, const vf_ssm *layer_host, const vf_ssm_io *io_host);
 
+/* ---- attention operators: a paged cache of keys and values -------------------
+ *
+ * The other form of a sequence network: every stage attends to the stages before it, whose keys and
+ * values are kept.  vf_kv_append writes new tokens' keys and values into the cache (turning queries and keys by
+ * their positions on the way), vf_kv_attend is the attention of the new tokens over the cache, vf_kv_read takes
+ * rows out of it again.  As the sequence operators: no model is needed, "type" is VF_FP32 or VF_BF16, rows of a matrix
+ * are `ld` elements apart, pointers are aligned to their elements, sums and softmax statistics are fp32, every result is
+ * rounded once.
+ *
+ * A cache has `pages` pages (at least one) of `page` tokens (a power of two from 16 to 1024), kv_heads heads of
+ * head_dim numbers (1..256).  format VF_FP32 or VF_BF16: k_dev and v_dev are [pages][kv_heads][page][w], w = head_dim
+ * filled up with zeros to a multiple of 8.  VF_E4M3: k_dev and v_dev hold codes [pages][kv_heads][page][32 kb] and
+ * k_scales_dev, v_scales_dev their scales [pages][kv_heads][page][kb], every row as in a microscaled matrix, kb =
+ * ceil(head_dim / 32).  k_dev and v_dev are aligned to 16 bytes.  What fills a row up is zeros also where the
+ * caller writes rows without vf_kv_append. */
+typedef struct {
+  int32_t format, kv_heads, head_dim, page, pages;
+  void *k_dev, *v_dev;
+  uint8_t *k_scales_dev, *v_scales_dev;
+} vf_kv;
+
+/* The sequences of a call.  Sequence s has the rows offsets[s] .. offsets[s + 1] - 1 of the call's matrices (offsets_dev
+ * int32 [n_seq + 1]; without offsets every sequence has tokens / n_seq rows), m of them; a range that does not lie in 0..tokens, or
+ * whose end is before its begin, counts as empty, rows of no sequence are not written, ranges do not overlap.
+ * lengths_dev int32 [n_seq]: its keys in the cache, the new ones among them, taken as 0 if negative and as max_pages * page
+ * if more; row i of the sequence has position length - m + i.  table_dev int32 [n_seq][max_pages], rows ld_table apart:
+ * position t is at place t % page of page table[s][t / page].  Sequences may share pages that no call writes
+ * to; a token's place in the cache is written by one sequence of a call.  An entry -1 is no page: nothing is written there, its
+ * keys are left out, its rows read as zeros.  Any other entry that is not a page reads as NaN and is not written.
+ * longest: the most rows of a sequence, which sets how the work is split (more are right, but slow).
+ * max_pages * page is at most 2^30. */
+typedef struct {
+  int32_t n_seq, max_pages;
+  int64_t tokens, longest, ld_table;
+  const int32_t *offsets_dev, *lengths_dev, *table_dev;
+} vf_kv_seqs;
+
+/* Rotary positions: the first `rotary` numbers of a head (even, 0..head_dim) are pairs (a, b), numbers j and j + rotary / 2,
+ * or interleaved numbers 2 j and 2 j + 1.  At position t pair j becomes (a c - b s, b c + a s) with c = magnitude cos(t f[j]),
+ * s = magnitude sin(t f[j]).  freq_dev: f[rotary / 2], radians a position, in 64 bits; angles are taken in 64 bits too.  Frequencies and
+ * magnitudes of scaled contexts are the caller's. */
+typedef struct {
+  int32_t rotary, interleaved;
+  const double *freq_dev;
+  float magnitude;
+} vf_rope;
+
+/* Writes k and v [tokens][kv_heads head_dim] of `type` to their positions in the cache, k turned by `rope` (NULL: as it
+ * is), converted to the cache's format: `type` itself, or VF_E4M3, quantized from the turned numbers in fp32 as by vf_mx_quantize.
+ * q [tokens][heads head_dim] (nullable, heads 0) is turned into q_out, which may be q itself with its row distance.  A row whose
+ * position is negative turns by that, and its key and value are not written. */
+int vf_kv_append(vf_ctx *ctx, const vf_kv *cache_host, const vf_kv_seqs *seqs_host, const vf_rope *rope_host, int32_t type,
+                 const void *k_dev, int64_t ld_k, const void *v_dev, int64_t ld_v, int32_t heads, const void *q_dev, int64_t ld_q,
+                 void *q_out_dev, int64_t ld_q_out);
+/* Keys and values of the rows' positions, k and v [tokens][kv_heads head_dim] of `type` (either may be NULL): what vf_kv_append wrote for the
+ * same sequences, as the cache holds it.  Rows with negative positions are zeros. */
+int vf_kv_read(vf_ctx *ctx, const vf_kv *cache_host, const vf_kv_seqs *seqs_host, int32_t type, void *k_dev, int64_t ld_k, void *v_dev,
+               int64_t ld_v);
+/* out[r][h] = sum_t p[t] v[t], p = softmax over the keys t that row r sees of scale q[r][h] . k[t].  q and out [tokens][heads head_dim]
+ * of `type`; heads is a multiple of kv_heads, head h meets head h / (heads / kv_heads) of the cache; the cache's format is `type` or
+ * VF_E4M3.  scale >= 0, finite.  causal: a row at position t sees keys 0..t, with a window w > 0 only the last w of them; a row with
+ * a negative position sees none.  Otherwise (window 0) every row sees all keys, however many rows there are.  A key that a row does not see takes no
+ * part in it, whatever it and its value hold.  Rows that see no key, and rows all of whose scores are -inf, are zeros.  In bf16 the weights p are rounded to bf16 for
+ * their products with the values, and numbers that are not finite may come out as NaN where they would be infinite.  longest_kv: the longest length, which sets how
+ * the work is split (longer ones are right, but slow).  A call may keep scratch in the context until vf_destroy, up to 260 MiB for a call and 1 GiB
+ * in all (few rows behind many keys are split along the keys); a call whose stream is being captured takes no new scratch and does without.  A
+ * graph that holds such a call is replayed on the context's stream, or ordered with it. */
+int vf_kv_attend(vf_ctx *ctx, const vf_kv *cache_host, const vf_kv_seqs *seqs_host, int32_t type, int32_t heads, const void *q_dev,
+                 int64_t ld_q, int32_t causal, int32_t window, float scale, int64_t longest_kv, void *out_dev, int64_t ld_out);
+
 /* ---- diagnostics ---------------------------------------------------------- */
 
 /* Static description of an error code. */

@@ -28,6 +28,7 @@ EXPORTS = [
     "vf_last_hip_error", "vf_timer_start", "vf_timer_stop", "vf_timer_elapsed_ms",
     "vf_profile_enable", "vf_profile_read", "vf_profile_counts", "vf_set_wait_limit", "vf_sync_status",
     "vf_rms_norm", "vf_mx_quantize", "vf_mx_dequantize", "vf_mx_matmul", "vf_ssm_scan", "vf_ssm_step",
+    "vf_kv_append", "vf_kv_read", "vf_kv_attend",
 ]
 
 _lib = None
@@ -96,6 +97,9 @@ def lib():
         L.vf_mx_matmul.argtypes = [vp, i32, vp, vp, vp, vp, i64, i64, i64, vp, i32, vp, i64]
         L.vf_ssm_scan.argtypes = [vp, vp, vp]
         L.vf_ssm_step.argtypes = [vp, vp, vp]
+        L.vf_kv_append.argtypes = [vp, vp, vp, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64]
+        L.vf_kv_read.argtypes = [vp, vp, vp, i32, vp, i64, vp, i64]
+        L.vf_kv_attend.argtypes = [vp, vp, vp, i32, i32, vp, i64, i32, i32, C.c_float, i64, vp, i64]
         _lib = L
     return _lib
 
@@ -616,3 +620,166 @@ def vf_ssm_step(ctx, layer, xbc, dt, z=None, state=None, slots=None, state_out=N
     """One more token for every row: row s continues slot slots[s] of state and leaves its state in slot
     slots_out[s] of state_out.  Arguments as vf_ssm_scan."""
     return _ssm_call(ctx, lib().vf_ssm_step, layer, xbc, dt, z, xbc.shape[0], 1, None, state, slots, state_out, slots_out, out)
+
+
+# ---- attention operators: a paged cache of keys and values ----
+
+class _Kv(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("format", "kv_heads", "head_dim", "page", "pages")] + [
+        (n, C.c_void_p) for n in ("k_dev", "v_dev", "k_scales_dev", "v_scales_dev")]
+
+
+class _KvSeqs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "max_pages")] + [(n, C.c_int64) for n in ("tokens", "longest", "ld_table")] + [
+        (n, C.c_void_p) for n in ("offsets_dev", "lengths_dev", "table_dev")]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("rotary", C.c_int32), ("interleaved", C.c_int32), ("freq_dev", C.c_void_p), ("magnitude", C.c_float)]
+
+
+class KvCache:
+    """A paged cache of keys and values on one GPU.  Holds the tensors, copies nothing.
+
+    VF_FP32 / VF_BF16: k and v are dense [pages][kv_heads][page][w] of that type, w = head_dim filled up with zeros to a multiple of
+    8; VF_E4M3: k and v are codes, uint8 [pages][kv_heads][page][32 kb], k_scales and v_scales uint8 [pages][kv_heads][page][kb],
+    kb = ceil(head_dim / 32).  `page` tokens: a power of two, 16..1024."""
+
+    def __init__(self, fmt, head_dim, k, v, k_scales=None, v_scales=None):
+        import torch
+        kb = (head_dim + 31) // 32
+        if fmt not in (VF_FP32, VF_BF16, VF_E4M3):
+            _fail(f"no format of a cache: {fmt}")
+        if not 1 <= head_dim <= 256:
+            _fail(f"head_dim: 1..256 is wanted, not {head_dim}")
+        dtype, width = (torch.uint8, 32 * kb) if fmt == VF_E4M3 else (_dtype_of(torch, fmt), (head_dim + 7) // 8 * 8)
+        if k.dim() != 4:
+            _fail(f"k: [pages][kv_heads][page][{width}] is wanted, got {tuple(k.shape)}")
+        shape = tuple(k.shape[:3])
+        rows = [(k, width, dtype, "k"), (v, width, dtype, "v")]
+        if fmt == VF_E4M3:
+            rows += [(k_scales, kb, torch.uint8, "k_scales"), (v_scales, kb, torch.uint8, "v_scales")]
+        elif k_scales is not None or v_scales is not None:
+            _fail("scales belong to VF_E4M3")
+        for t, w, dt, name in rows:
+            if t is None or t.shape != (*shape, w) or t.dtype != dt or not t.is_contiguous() or not t.is_cuda or t.device != k.device:
+                _fail(f"{name}: dense {dt} {[*shape, w]} on one GPU are wanted")
+        if shape[0] < 1 or shape[1] < 1 or shape[2] not in (16, 32, 64, 128, 256, 512, 1024):
+            _fail(f"a page, a head and a power of two of tokens from 16 to 1024 are wanted, not {shape}")
+        self.fmt, self.head_dim, self.device = fmt, head_dim, k.device
+        self.pages, self.kv_heads, self.page = shape
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.tensors = (k, v, k_scales, v_scales)
+        self.record = _Kv(fmt, self.kv_heads, head_dim, self.page, self.pages, *(_addr(t) for t in self.tensors))
+        self.ref = C.byref(self.record)
+
+    @classmethod
+    def zeros(cls, fmt, pages, page, kv_heads, head_dim, device="cuda"):
+        """A cache of new memory, all zeros."""
+        import torch
+        kb = (head_dim + 31) // 32
+        new = lambda w, dt: torch.zeros((pages, kv_heads, page, w), dtype=dt, device=device)   # noqa: E731
+        if fmt == VF_E4M3:
+            return cls(fmt, head_dim, new(32 * kb, torch.uint8), new(32 * kb, torch.uint8), new(kb, torch.uint8), new(kb, torch.uint8))
+        dtype, width = _dtype_of(torch, fmt), (head_dim + 7) // 8 * 8
+        return cls(fmt, head_dim, new(width, dtype), new(width, dtype))
+
+
+class Rope:
+    """Rotary positions: freq float64 [rotary / 2] on the GPU, radians a position (inputs.rotary_frequencies); pairs are numbers j and
+    j + rotary / 2 of a head, or 2 j and 2 j + 1 if interleaved; cosines and sines are multiplied by magnitude.  Holds the tensor."""
+
+    def __init__(self, freq, interleaved=False, magnitude=1.0):
+        import torch
+        if freq.dim() != 1 or freq.dtype != torch.float64 or not freq.is_contiguous() or not freq.is_cuda:
+            _fail("freq: dense float64 values on a GPU are wanted")
+        self.freq, self.interleaved, self.magnitude, self.device = freq, bool(interleaved), float(magnitude), freq.device
+        self.record = _Rope(2 * freq.numel(), int(self.interleaved), freq.data_ptr(), self.magnitude)
+        self.ref = C.byref(self.record)
+
+
+def _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest):
+    """Checks what the calls share; returns the record."""
+    torch = ctx.torch
+    if cache.device != ctx.device:
+        _fail("the cache is on another GPU")
+    if table.dim() != 2:
+        _fail(f"table: [n_seq][max_pages] is wanted, got {tuple(table.shape)}")
+    n, wide = table.shape
+    ld = _rows_of(ctx, table, n, wide, torch.int32, "table")
+    at = _vector(ctx, lengths, n, "lengths", torch.int32)
+    off = _vector(ctx, offsets, n + 1, "offsets", torch.int32)
+    if offsets is None and (tokens % n != 0 if n else tokens != 0):
+        _fail(f"{tokens} rows cannot be dealt to {n} sequences; offsets are wanted")
+    if longest is None:
+        longest = tokens if offsets is not None or n == 0 else tokens // n
+    return _KvSeqs(n, wide, tokens, longest, ld, off, at, table.data_ptr())
+
+
+def _heads_of(cache, t, name):
+    """Heads in the rows of a matrix."""
+    if t.dim() != 2 or t.shape[1] % cache.head_dim != 0:
+        _fail(f"{name}: rows of heads of {cache.head_dim} are wanted, got {tuple(t.shape)}")
+    return t.shape[1] // cache.head_dim
+
+
+def vf_kv_append(ctx, cache, k, v, table, lengths, q=None, rope=None, offsets=None, longest=None, q_out=None):
+    """Writes new tokens' keys and values k, v [tokens][kv_heads head_dim] into the cache, keys turned by `rope` (a Rope or None).
+
+    Sequence s has rows offsets[s] .. offsets[s + 1] - 1 (int32 [n_seq + 1]; None: all sequences have tokens / n_seq rows),
+    the last of its lengths[s] positions (int32 [n_seq]), which are in the pages table[s] (int32 [n_seq][max_pages]); longest: the
+    most rows of a sequence (default: without offsets their number, with offsets all tokens).  q [tokens][heads head_dim] is
+    turned into q_out (default: a new tensor; q itself is fine).  Returns q_out, None without q."""
+    torch = ctx.torch
+    kind, dtype, tokens = _type_of(torch, k), k.dtype, k.shape[0]
+    seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
+    wide = cache.kv_heads * cache.head_dim
+    ld_k = _rows_of(ctx, k, tokens, wide, dtype, "k")
+    ld_v = _rows_of(ctx, v, tokens, wide, dtype, "v")
+    heads = ld_q = ld_o = 0
+    if q is not None:
+        heads = _heads_of(cache, q, "q")
+        ld_q = _rows_of(ctx, q, tokens, heads * cache.head_dim, dtype, "q")
+        q_out, ld_o = _out(ctx, q_out, tokens, heads * cache.head_dim, dtype)
+    elif q_out is not None:
+        _fail("q_out without q")
+    if rope is not None and rope.device != ctx.device:
+        _fail("the rotation's frequencies are on another GPU")
+    _call(ctx, lib().vf_kv_append, (cache.ref, C.byref(seqs), None if rope is None else rope.ref, kind, _addr(k), ld_k, _addr(v), ld_v, heads,
+                                    _addr(q), ld_q, _addr(q_out), ld_o),
+          (k, v, q, q_out, table, lengths, offsets, None if rope is None else rope.freq, *cache.tensors))
+    return q_out
+
+
+def vf_kv_read(ctx, cache, table, lengths, tokens, offsets=None, longest=None, out_type=VF_BF16, out=None):
+    """Keys and values of the last positions of every sequence, `tokens` rows in all, as vf_kv_append deals rows to sequences: (k, v),
+    each [tokens][kv_heads head_dim] of out_type; out: a pair of matrices to write to, either may be None and is then not read."""
+    seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
+    dtype, wide = _dtype_of(ctx.torch, out_type), cache.kv_heads * cache.head_dim
+    if out is None:
+        out, ld = (ctx.empty((tokens, wide), dtype), ctx.empty((tokens, wide), dtype)), (wide, wide)
+    else:
+        ld = tuple(0 if t is None else _rows_of(ctx, t, tokens, wide, dtype, "out") for t in out)
+    k, v = out
+    _call(ctx, lib().vf_kv_read, (cache.ref, C.byref(seqs), out_type, _addr(k), ld[0], _addr(v), ld[1]),
+          (k, v, table, lengths, offsets, *cache.tensors))
+    return out
+
+
+def vf_kv_attend(ctx, cache, q, table, lengths, causal=True, window=0, scale=None, offsets=None, longest=None, longest_kv=None, out=None):
+    """Attention of the rows q [tokens][heads head_dim] over their sequences' keys and values in the cache: [tokens][heads head_dim].
+
+    heads is a multiple of the cache's; rows, table, lengths, offsets and longest as for vf_kv_append.  causal: row i of m sees the keys up
+    to position lengths[s] - m + i, with a window only the last `window` of them; otherwise all lengths[s] keys.  scale: default
+    head_dim ** -0.5.  longest_kv: the longest length (default: what the table can hold).  Rows without keys are zeros."""
+    torch = ctx.torch
+    kind, tokens, heads = _type_of(torch, q), q.shape[0], _heads_of(cache, q, "q")
+    seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
+    ld_q = _rows_of(ctx, q, tokens, heads * cache.head_dim, q.dtype, "q")
+    out, ld_o = _out(ctx, out, tokens, heads * cache.head_dim, q.dtype)
+    if longest_kv is None:
+        longest_kv = seqs.max_pages * cache.page
+    _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, _addr(q), ld_q, 1 if causal else 0, window,
+                                    cache.head_dim ** -0.5 if scale is None else scale, longest_kv, _addr(out), ld_o),
+          (q, out, table, lengths, offsets, *cache.tensors))
+    return out

@@ -1,0 +1,629 @@
+// vf_kv_attend: attention of sequences' new tokens over their keys in a paged cache.
+//
+// One pass over the keys with a running maximum m and sum l per row: for every block of keys, S = scale q k^T, p = exp(S - m),
+// l += sum p, out += p v; where a row's maximum grows, out and l shrink by exp(m_old - m_new) first, and at the end out / l is the result.
+// Exponentials are powers of two, log2(e) is part of the scale.  m follows the maximum only when that has grown by more than MARGIN powers of two:
+// p then goes up to 2^MARGIN, which no sum minds, and in nearly all blocks no lane has to ask the others.
+//
+// All heads that share a head of the cache are rows of one product (row r of a sequence: token r / group, head r % group), so its
+// keys and values are fetched once for them.  Products are made as S^T = K Q^T and out^T = V^T P^T: a lane then holds scores of one row only, and the
+// scores come out in the lanes and registers in which the second product takes them, up to the order of the keys in it, which is free as
+// long as the values follow it.
+#include <math.h>
+
+#include "vf_internal.h"
+#include "vf_kv_dev.h"
+
+namespace {
+
+using namespace vfkv;
+
+constexpr float MARGIN = 8.0f;
+constexpr float LOG2E = 1.44269504088896340736f;
+
+struct AttendArgs {
+  Cache c;
+  Seqs s;
+  const void *q;
+  void *out;
+  float *part;      // of workgroups that share a row block: [unit][rows][DP] sums, then [unit][rows] maxima, then [unit][rows] sums of weights
+  int64_t ld_q, ld_out, units;
+  float scale2;     // scale log2(e)
+  int group, causal, window, longest;
+  int blocks, splits;  // row blocks of the longest sequence; workgroups that share one along the keys
+};
+
+// The keys that row i of a sequence sees: [lo, hi).
+__device__ __forceinline__ void seen_by(const AttendArgs &a, const Span &sp, int i, int &lo, int &hi) {
+  const int pos = sp.length - sp.rows + i;
+  lo = a.window && pos >= a.window ? pos - a.window + 1 : 0;
+  hi = !a.causal ? sp.length : pos < 0 ? 0 : pos + 1;
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The maximum that weights are taken against: a row that has seen nothing yet has none.
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+
+// A row's maxima and sums where parts of it are joined.
+__device__ __forceinline__ float weight_of(float m, float top) { return exp2_(m - base_of(top)); }
+
+// ---- few rows: keys and values straight from memory into the operands ----
+//
+// A wave holds 16 RB rows; its operands' other side are 32 keys (16 in fp32) at a time.  The four waves of a workgroup share the
+// rows and take turns at the keys, or have rows of their own (ALONG false, true).
+
+template <typename T, int FMT, int DP> struct Shape;
+// K operand: the lane of key n and quarter g takes elements; V operand: lane c takes VW neighbouring numbers of a value, NH times
+template <int FMT, int DP> struct Shape<uint16_t, FMT, DP> {
+  static constexpr int STEP = 32, VW = DP >= 128 ? 8 : DP / 16, NH = DP / (16 * VW), NK = DP / 32;
+};
+template <int FMT, int DP> struct Shape<float, FMT, DP> {
+  static constexpr int STEP = 16, VW = DP >= 64 ? 4 : DP / 16, NH = DP / (16 * VW), NK = DP / 16;
+};
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d});
+}
+__device__ __forceinline__ uint32_t cvt2(uint32_t codes, float scale, bool high) {
+  const bf16x2 v = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ float scale_of(uint8_t byte) { return __uint_as_float((uint32_t)byte << 23); }
+// whether a half of a pair of bf16 is infinite or NaN, and the pair without such halves, and 1 in their places
+__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t finite_of(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0 : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0 : w & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t marks_of(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u ? 0x3f80u : 0) | ((w & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0);
+}
+
+// First of the eight numbers (four in fp32) of k-step ks that a lane of quarter g holds: whole pieces of 16 bytes of a row.
+template <typename T, int FMT, int DP>
+__device__ __forceinline__ int k_at(int ks, int g) {
+  if constexpr (sizeof(T) == 4) return 16 * ks + 4 * g;
+  else if constexpr (FMT == VF_E4M3 && DP >= 64) return ((ks >> 1) * 4 + g) * 16 + (ks & 1) * 8;
+  else return 32 * ks + 8 * g;
+}
+
+template <typename T, int FMT, int DP, int RB, bool ALONG>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const AttendArgs a) {
+  typedef Shape<T, FMT, DP> S;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int STEP = S::STEP, VW = S::VW, NH = S::NH, NK = S::NK, ROWS = 16 * RB * (ALONG ? 4 : 1), NA = NH * VW;
+  constexpr int KB = STEP / 16;  // blocks of 16 keys in a step
+  __shared__ f32x4 join[ALONG ? 1 : 2][ALONG ? 1 : RB * NA][64];
+  __shared__ float join_m[ALONG ? 1 : 4][16 * RB], join_l[ALONG ? 1 : 4][16 * RB];
+  const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Cache &c = a.c;
+  for (int64_t unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
+    // unit: heads of the cache fastest, then shares of the keys, then row blocks, then sequences
+    int64_t rest = unit / c.heads;
+    const int head = (int)(unit - rest * c.heads), split = (int)(rest % a.splits);
+    rest /= a.splits;
+    const int seq = (int)(rest / a.blocks), block0 = (int)(rest - (int64_t)seq * a.blocks);
+    const Span sp = span_of(a.s, c.shift, seq);
+    const int64_t all = (int64_t)sp.rows * a.group;
+    for (int64_t block = block0; block * ROWS < all; block += a.blocks) {
+      // (row blocks that the plan did not count on are not shared)
+      const bool shared = a.splits > 1 && block < a.blocks;
+      if (block >= a.blocks && split > 0) break;
+      const int64_t r0 = block * ROWS + (ALONG ? wave * 16 * RB : 0), r1 = r0 + 16 * RB < all ? r0 + 16 * RB : all;
+      // what the wave's rows see: all of [lo_in, hi_in), nothing outside [lo, hi)
+      int lo = 0, hi = 0, lo_in = 0, hi_in = 0;
+      if (r0 < r1) {
+        const int first = (int)(r0 / a.group), last = (int)((r1 - 1) / a.group);
+        seen_by(a, sp, first, lo, hi_in);
+        seen_by(a, sp, last, lo_in, hi);
+      }
+      int row_lo[RB], row_hi[RB];
+      const T *q_row[RB];
+      int64_t out_row[RB];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        const int64_t r = r0 + 16 * b + n;
+        row_lo[b] = row_hi[b] = 0;
+        q_row[b] = nullptr;
+        out_row[b] = -1;
+        if (r < r1) {
+          const int i = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)i * a.group);
+          seen_by(a, sp, i, row_lo[b], row_hi[b]);
+          q_row[b] = reinterpret_cast<const T *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * c.dim;
+          out_row[b] = (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
+        }
+      }
+      // queries as operands
+      uint4 q16[F32 ? 1 : RB][F32 ? 1 : NK];
+      f32x4 q32[F32 ? RB : 1][F32 ? NK : 1];
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+          const int d = k_at<T, FMT, DP>(ks, g), left = q_row[b] ? c.dim - d : 0;
+          if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q32[b][ks][i] = i < left ? q_row[b][d + i] : 0.0f;
+          } else {
+            raw8<uint16_t> w = {};
+            if (left > 0) fetch8(q_row[b] + d, left, w);
+            q16[b][ks] = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
+          }
+        }
+      f32x4 acc[RB][NA];
+      float m[RB], l[RB];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        m[b] = -INFINITY;
+        l[b] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) acc[b][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+      // the steps of this workgroup, and of this wave among them
+      const int from = lo & ~(STEP - 1);
+      int steps = hi > from ? (hi - from + STEP - 1) / STEP : 0, s0 = 0;
+      if (shared) {
+        const int each = (steps + a.splits - 1) / a.splits;
+        s0 = (int)((int64_t)each * split < steps ? each * split : steps);
+        steps = steps - s0 < each ? steps : s0 + each;
+      }
+      for (int st = s0 + (ALONG ? 0 : wave); st < steps; st += ALONG ? 1 : 4) {
+        const int t0 = from + st * STEP;
+        int entry[KB], page[KB];
+        bool fine = true;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          entry[kb] = entry_of(a.s, c.shift, seq, t0 + 16 * kb);
+          const bool there = (unsigned)entry[kb] < (unsigned)c.pages;
+          page[kb] = there ? entry[kb] : 0;   // (what is fetched there is not used)
+          fine = fine && there;
+        }
+        const bool edge = !fine || t0 < lo_in || t0 + STEP > hi_in;
+        f32x4 sc[RB][KB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) sc[b][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        // values: of key 4 g + i of each block of 16 the VW numbers at c VW of each part
+        constexpr int VD = F32 ? VW : (VW + 1) / 2;  // registers
+        uint32_t val[KB][4][NH][VD];
+
+        if constexpr (F32) {
+          const int64_t krow = row_of(c, page[0], head, t0 + n), vrow = row_of(c, page[0], head, t0 + 4 * g);
+          f32x4 key[NK];
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks) {
+            const int d = k_at<T, FMT, DP>(ks, g);
+            key[ks] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (d < c.width) {
+              if constexpr (FMT == VF_E4M3) {
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint8_t *>(c.k) + krow * c.width + d);
+                const float s = scale_of(c.ks[krow * c.kb + (d >> 5)]);
+                const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
+                key[ks] = f32x4{x[0], x[1], y[0], y[1]};
+              } else {
+                key[ks] = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(c.k) + krow * c.width + d);
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+              const int d = h * 16 * VW + n * VW;
+#pragma unroll
+              for (int x = 0; x < VD; ++x) val[0][i][h][x] = 0;
+              if (d < c.width) {
+                if constexpr (FMT == VF_E4M3) {
+                  const uint8_t *p = reinterpret_cast<const uint8_t *>(c.v) + (vrow + i) * c.width + d;
+                  uint32_t w;
+                  if constexpr (VW == 4) w = *reinterpret_cast<const uint32_t *>(p);
+                  else w = *reinterpret_cast<const uint16_t *>(p);
+                  const float s = scale_of(c.vs[(vrow + i) * c.kb + (d >> 5)]);
+                  const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
+#pragma unroll
+                  for (int e = 0; e < VW; ++e) val[0][i][h][e] = __float_as_uint(e < 2 ? x[e & 1] : y[e & 1]);
+                } else {
+                  const float *p = reinterpret_cast<const float *>(c.v) + (vrow + i) * c.width + d;
+                  typedef float fv __attribute__((ext_vector_type(VW)));
+                  const fv w = *reinterpret_cast<const fv *>(p);
+#pragma unroll
+                  for (int e = 0; e < VW; ++e) val[0][i][h][e] = __float_as_uint(w[e]);
+                }
+              }
+            }
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+              for (int b = 0; b < RB; ++b) sc[b][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(key[ks][x], q32[b][ks][x], sc[b][0], 0, 0, 0);
+        } else {
+          uint4 key[KB][NK];
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) {
+            const int64_t krow = row_of(c, page[kb], head, t0 + 16 * kb + n), vrow = row_of(c, page[kb], head, t0 + 16 * kb + 4 * g);
+            if constexpr (FMT == VF_E4M3) {
+              const uint8_t *p = reinterpret_cast<const uint8_t *>(c.k) + krow * c.width, *ps = c.ks + krow * c.kb;
+#pragma unroll
+              for (int ks = 0; ks < NK; ks += DP >= 64 ? 2 : 1) {
+                const int d = k_at<T, FMT, DP>(ks, g);
+                uint4 w = make_uint4(0, 0, 0, 0);
+                float s = 1.0f;
+                if (d < c.width) {
+                  if constexpr (DP >= 64) {
+                    w = *reinterpret_cast<const uint4 *>(p + d);
+                  } else {
+                    const uint2 w2 = *reinterpret_cast<const uint2 *>(p + d);
+                    w.x = w2.x; w.y = w2.y;
+                  }
+                  s = scale_of(ps[d >> 5]);
+                }
+                key[kb][ks] = make_uint4(cvt2(w.x, s, false), cvt2(w.x, s, true), cvt2(w.y, s, false), cvt2(w.y, s, true));
+                if constexpr (DP >= 64) key[kb][ks + 1] = make_uint4(cvt2(w.z, s, false), cvt2(w.z, s, true), cvt2(w.w, s, false), cvt2(w.w, s, true));
+              }
+            } else {
+              const uint16_t *p = reinterpret_cast<const uint16_t *>(c.k) + krow * c.width;
+#pragma unroll
+              for (int ks = 0; ks < NK; ++ks) {
+                const int d = k_at<T, FMT, DP>(ks, g);
+                key[kb][ks] = d < c.width ? *reinterpret_cast<const uint4 *>(p + d) : make_uint4(0, 0, 0, 0);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int h = 0; h < NH; ++h) {
+                const int d = h * 16 * VW + n * VW;
+#pragma unroll
+                for (int x = 0; x < VD; ++x) val[kb][i][h][x] = 0;
+                if (d >= c.width) continue;
+                if constexpr (FMT == VF_E4M3) {
+                  const uint8_t *pv = reinterpret_cast<const uint8_t *>(c.v) + (vrow + i) * c.width + d;
+                  const float s = scale_of(c.vs[(vrow + i) * c.kb + (d >> 5)]);
+                  if constexpr (VW == 8) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(pv);
+                    val[kb][i][h][0] = cvt2(w.x, s, false); val[kb][i][h][1] = cvt2(w.x, s, true);
+                    val[kb][i][h][2] = cvt2(w.y, s, false); val[kb][i][h][3] = cvt2(w.y, s, true);
+                  } else if constexpr (VW == 4) {
+                    const uint32_t w = *reinterpret_cast<const uint32_t *>(pv);
+                    val[kb][i][h][0] = cvt2(w, s, false); val[kb][i][h][1] = cvt2(w, s, true);
+                  } else {
+                    val[kb][i][h][0] = cvt2(*reinterpret_cast<const uint16_t *>(pv), s, false);
+                  }
+                } else {
+                  typedef uint32_t uv __attribute__((ext_vector_type(VD)));
+                  const uint16_t *pv = reinterpret_cast<const uint16_t *>(c.v) + (vrow + i) * c.width + d;
+                  if constexpr (VD == 1) {
+                    val[kb][i][h][0] = *reinterpret_cast<const uint32_t *>(pv);
+                  } else {
+                    const uv w = *reinterpret_cast<const uv *>(pv);
+#pragma unroll
+                    for (int x = 0; x < VD; ++x) val[kb][i][h][x] = w[x];
+                  }
+                }
+              }
+          }
+#pragma unroll
+          for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int b = 0; b < RB; ++b)
+                sc[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, key[kb][ks]), __builtin_bit_cast(bf16x8, q16[b][ks]), sc[b][kb],
+                                                                  0, 0, 0);
+        }
+
+        bool odd = false;  // whether some value that only some rows see is not finite
+        if (edge) {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int t = t0 + 16 * kb + 4 * g + i;
+              const bool there = (unsigned)entry[kb] < (unsigned)c.pages;
+#pragma unroll
+              for (int b = 0; b < RB; ++b) {
+                const bool seen = t >= row_lo[b] && t < row_hi[b] && entry[kb] != -1;
+                sc[b][kb][i] = !seen ? -INFINITY : there ? sc[b][kb][i] : __builtin_nanf("");
+              }
+              const bool any = t >= lo && t < hi && there;
+#pragma unroll
+              for (int h = 0; h < NH; ++h)
+#pragma unroll
+                for (int x = 0; x < VD; ++x) {
+                  if (!any) val[kb][i][h][x] = 0;
+                  odd = odd || (F32 ? (val[kb][i][h][x] & 0x7f800000u) == 0x7f800000u : not_finite(val[kb][i][h][x]));
+                }
+            }
+        }
+        // maxima: followed where one has grown by much
+        float top[RB];
+        bool grown = false;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          top[b] = sc[b][0][0];
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top[b] = fmaxf(top[b], sc[b][kb][i]);
+          top[b] *= a.scale2;
+          grown = grown || top[b] > m[b] + MARGIN;
+        }
+        if (__any(grown)) {
+#pragma unroll
+          for (int b = 0; b < RB; ++b) {
+            float t = fmaxf(top[b], m[b]);
+            t = fmaxf(t, __shfl_xor(t, 16));
+            t = fmaxf(t, __shfl_xor(t, 32));
+            const float f = exp2_(m[b] - base_of(t));
+            m[b] = t;
+            l[b] *= f;
+#pragma unroll
+            for (int i = 0; i < NA; ++i) acc[b][i] *= f;
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          const float base = base_of(m[b]);
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              sc[b][kb][i] = exp2_(fmaf(sc[b][kb][i], a.scale2, -base));
+              l[b] += sc[b][kb][i];
+            }
+        }
+        // values that are not finite reach the rows that see them only: they are left out of the products, and of a product of
+        // ones in their places with ones in the places of what is seen, whatever is not zero makes NaN
+        auto seen_mark = [&](int b, int kb, int i) {
+          const int t = t0 + 16 * kb + 4 * g + i;
+          return t >= row_lo[b] && t < row_hi[b] && entry[kb] != -1;
+        };
+        const bool odd_step = edge && __any(odd);
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+              for (int x = 0; x < VW; ++x) {
+                float v = __uint_as_float(val[0][i][h][x]);
+                if (odd_step) {
+                  const bool bad = (val[0][i][h][x] & 0x7f800000u) == 0x7f800000u;
+#pragma unroll
+                  for (int b = 0; b < RB; ++b) {
+                    f32x4 hit = {0.0f, 0.0f, 0.0f, 0.0f};
+                    hit = __builtin_amdgcn_mfma_f32_16x16x4f32(bad ? 1.0f : 0.0f, seen_mark(b, 0, i) ? 1.0f : 0.0f, hit, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                      if (hit[e] != 0.0f) acc[b][h * VW + x][e] = __builtin_nanf("");
+                  }
+                  v = bad ? 0.0f : v;
+                }
+#pragma unroll
+                for (int b = 0; b < RB; ++b) acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[b][0][i], acc[b][h * VW + x], 0, 0, 0);
+              }
+        } else {
+          bf16x8 p[RB];
+#pragma unroll
+          for (int b = 0; b < RB; ++b)
+            p[b] = as_bf16x8(pack2(sc[b][0][0], sc[b][0][1]), pack2(sc[b][0][2], sc[b][0][3]), pack2(sc[b][1][0], sc[b][1][1]), pack2(sc[b][1][2], sc[b][1][3]));
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int x = 0; x < VW; ++x) {
+              // (halves x % 2 of registers x / 2 of neighbouring keys)
+              const uint32_t pick = x & 1 ? 0x07060302u : 0x05040100u;
+              uint32_t w[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                w[e] = __builtin_amdgcn_perm(val[e >> 1][2 * (e & 1) + 1][h][x >> 1], val[e >> 1][2 * (e & 1)][h][x >> 1], pick);
+              if (odd_step) {
+#pragma unroll
+                for (int b = 0; b < RB; ++b) {
+                  f32x4 hit = {0.0f, 0.0f, 0.0f, 0.0f};
+                  uint32_t see[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    see[e] = (seen_mark(b, e >> 1, 2 * (e & 1)) ? 0x3f80u : 0) | (seen_mark(b, e >> 1, 2 * (e & 1) + 1) ? 0x3f800000u : 0);
+                  hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(marks_of(w[0]), marks_of(w[1]), marks_of(w[2]), marks_of(w[3])),
+                                                               as_bf16x8(see[0], see[1], see[2], see[3]), hit, 0, 0, 0);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (hit[e] != 0.0f) acc[b][h * VW + x][e] = __builtin_nanf("");
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = finite_of(w[e]);
+              }
+#pragma unroll
+              for (int b = 0; b < RB; ++b)
+                acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w[0], w[1], w[2], w[3]), p[b], acc[b][h * VW + x], 0, 0, 0);
+            }
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        l[b] += __shfl_xor(l[b], 16);
+        l[b] += __shfl_xor(l[b], 32);
+      }
+      // the waves' shares of the keys: waves 2 and 3 give theirs to 0 and 1, then 1 to 0
+      if constexpr (!ALONG) {
+        __syncthreads();
+        if (g == 0) {
+#pragma unroll
+          for (int b = 0; b < RB; ++b) {
+            join_m[wave][16 * b + n] = m[b];
+            join_l[wave][16 * b + n] = l[b];
+          }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+          float t = join_m[0][16 * b + n];
+#pragma unroll
+          for (int w = 1; w < 4; ++w) t = fmaxf(t, join_m[w][16 * b + n]);
+          l[b] = 0.0f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) l[b] += join_l[w][16 * b + n] * weight_of(join_m[w][16 * b + n], t);
+          const float f = weight_of(m[b], t);
+          m[b] = t;
+#pragma unroll
+          for (int i = 0; i < NA; ++i) acc[b][i] *= f;
+        }
+#pragma unroll
+        for (int half = 2; half >= 1; half >>= 1) {
+          if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+              for (int i = 0; i < NA; ++i) join[wave - half][b * NA + i][lane] = acc[b][i];
+          }
+          __syncthreads();
+          if (wave < half) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+              for (int i = 0; i < NA; ++i) acc[b][i] += join[wave][b * NA + i][lane];
+          }
+          __syncthreads();
+        }
+        if (wave > 0) continue;
+      }
+      // numbers h 16 VW + (4 g + e) VW + x of row n are in acc[h VW + x][e]
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        if (shared) {
+          const int64_t at = unit * ROWS + (ALONG ? wave * 16 * RB : 0) + 16 * b + n;
+          float *o = a.part + at * DP;
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int x = 0; x < VW; ++x) o[h * 16 * VW + (4 * g + e) * VW + x] = acc[b][h * VW + x][e];
+          if (g == 0) {
+            float *stat = a.part + a.units * ROWS * DP;
+            stat[at] = m[b];
+            stat[a.units * ROWS + at] = l[b];
+          }
+        } else if (out_row[b] >= 0) {
+          const float inv = l[b] == 0.0f ? 0.0f : 1.0f / l[b];
+          T *o = reinterpret_cast<T *>(a.out) + out_row[b];
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int d = h * 16 * VW + (4 * g + e) * VW;
+              float v[8];
+#pragma unroll
+              for (int x = 0; x < 8; ++x) v[x] = x < VW ? acc[b][h * VW + x % VW][e] * inv : 0.0f;
+              const int left = c.dim - d < VW ? c.dim - d : VW;
+              if (left > 0) store_upto8(o + d, left, v);
+            }
+        }
+      }
+    }
+  }
+}
+
+// Joins the parts of row blocks that several workgroups have shared: a wave a row.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int rows) {
+  const int lane = (int)threadIdx.x & 63;
+  const Cache &c = a.c;
+  const int64_t blocks = a.units / a.splits, items = blocks * rows;
+  for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
+    const int64_t ub = item / rows;   // (sequence, row block, head of the cache), heads fastest
+    const int row = (int)(item - ub * rows), head = (int)(ub % c.heads);
+    const int64_t sb = ub / c.heads;
+    const int seq = (int)(sb / a.blocks), block = (int)(sb - (int64_t)seq * a.blocks);
+    const Span sp = span_of(a.s, c.shift, seq);
+    const int64_t r = (int64_t)block * rows + row;
+    if (r >= (int64_t)sp.rows * a.group) continue;
+    const float *stat = a.part + a.units * rows * DP;
+    auto at_of = [&](int k) { return ((sb * a.splits + k) * c.heads + head) * rows + row; };
+    float top = -INFINITY;
+    for (int k = lane; k < a.splits; k += 64) top = fmaxf(top, stat[at_of(k)]);
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+    float l = 0.0f, o[(DP + 63) / 64] = {};
+    for (int k = 0; k < a.splits; ++k) {
+      const int64_t at = at_of(k);
+      const float f = weight_of(stat[at], top);
+      l += f * stat[a.units * rows + at];
+#pragma unroll
+      for (int x = 0; x < (DP + 63) / 64; ++x)
+        if (64 * x + lane < DP) o[x] += f * a.part[at * DP + 64 * x + lane];
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int i = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)i * a.group);
+    T *to = reinterpret_cast<T *>(a.out) + (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
+#pragma unroll
+    for (int x = 0; x < (DP + 63) / 64; ++x)
+      if (64 * x + lane < c.dim) store1(to + 64 * x + lane, o[x] * inv);
+  }
+}
+
+template <typename T, int FMT, int DP>
+int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
+  constexpr int STEP = Shape<T, FMT, DP>::STEP;
+  const int64_t longest = (int64_t)a.longest * a.group;
+  const int rb = longest <= 16 ? 1 : 2;
+  const bool along = longest > 32;
+  const int rows = 16 * rb * (along ? 4 : 1);
+  a.blocks = (int)((longest + rows - 1) / rows);
+  if (a.blocks < 1) a.blocks = 1;
+  // Workgroups share the keys of a row block where there would be fewer than run at a time, as long as every wave keeps some steps.
+  const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, steps = (longest_kv + STEP - 1) / STEP, most = steps / (along ? 8 : 16);
+  int64_t splits = (512 + units - 1) / units;
+  if (splits > most) splits = most;
+  if (splits > 512) splits = 512;
+  if (splits < 1) splits = 1;
+  if (splits > 1) {
+    a.part = reinterpret_cast<float *>(vfk_ops_scratch(c, (size_t)(units * splits * rows) * (DP + 2) * sizeof(float)));
+    if (!a.part) splits = 1;
+  }
+  a.splits = (int)splits;
+  a.units = units * splits;
+  const unsigned grid = (unsigned)(a.units < (1 << 20) ? a.units : 1 << 20);
+  if (along) k_attend_rows<T, FMT, DP, 2, true><<<grid, 256, 0, c->stream>>>(a);
+  else if (rb == 2) k_attend_rows<T, FMT, DP, 2, false><<<grid, 256, 0, c->stream>>>(a);
+  else k_attend_rows<T, FMT, DP, 1, false><<<grid, 256, 0, c->stream>>>(a);
+  VF_HIP(c, hipGetLastError());
+  if (splits > 1) {
+    const int64_t items = (units * rows + 3) / 4;
+    k_attend_join<T, DP><<<(unsigned)(items < 4096 ? items : 4096), 256, 0, c->stream>>>(a, rows);
+    VF_HIP(c, hipGetLastError());
+  }
+  return VF_OK;
+}
+
+template <typename T, int FMT>
+int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
+  if (a.c.dim <= 32) return launch_rows<T, FMT, 32>(c, a, longest_kv);
+  if (a.c.dim <= 64) return launch_rows<T, FMT, 64>(c, a, longest_kv);
+  if (a.c.dim <= 128) return launch_rows<T, FMT, 128>(c, a, longest_kv);
+  return launch_rows<T, FMT, 256>(c, a, longest_kv);
+}
+
+}  // namespace
+
+int vfk_kv_attend(vf_ctx *c, const vf_kv_call &call, int heads, const void *q, int64_t ld_q, bool causal, int window, float scale, int64_t longest_kv,
+                  void *out, int64_t ld_out) {
+  if (call.seqs->n_seq == 0 || call.seqs->tokens == 0) return VF_OK;
+  AttendArgs a = {};
+  a.c = cache_of(call.kv);
+  a.s = seqs_of(call.seqs);
+  a.q = q; a.out = out; a.ld_q = ld_q; a.ld_out = ld_out;
+  // (scores that a row does not see are -inf and have to stay it: the smallest number there is does for 0, as it takes every finite score below 1e-6)
+  a.scale2 = scale * LOG2E > 0.0f ? scale * LOG2E : 1.4e-45f;
+  a.group = heads / call.kv->kv_heads;
+  a.causal = causal; a.window = window;
+  a.longest = (int)longest_of(call.seqs);
+  const int64_t most = (int64_t)call.seqs->max_pages * call.kv->page;
+  if (longest_kv > most) longest_kv = most;
+  if (call.type == VF_BF16) return call.kv->format == VF_E4M3 ? launch<uint16_t, VF_E4M3>(c, a, longest_kv) : launch<uint16_t, VF_BF16>(c, a, longest_kv);
+  return call.kv->format == VF_E4M3 ? launch<float, VF_E4M3>(c, a, longest_kv) : launch<float, VF_FP32>(c, a, longest_kv);
+}

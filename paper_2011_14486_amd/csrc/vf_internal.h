@@ -348,3 +348,15 @@ int vfk_mx_matmul(vf_ctx *c, int a_format, const uint8_t *a, const uint8_t *as, 
 void *vfk_ops_scratch(vf_ctx *c, size_t bytes);
 // one: a token for every sequence
 int vfk_ssm(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io, bool one);
+
+// ---- attention operators (arguments checked by vf_ops.hip) ----
+struct vf_kv_call {  // what the three share
+  const vf_kv *kv;
+  const vf_kv_seqs *seqs;
+  int type;
+};
+int vfk_kv_append(vf_ctx *c, const vf_kv_call &call, const vf_rope *rope, const void *k, int64_t ld_k, const void *v, int64_t ld_v, int heads,
+                  const void *q, int64_t ld_q, void *q_out, int64_t ld_q_out);
+int vfk_kv_read(vf_ctx *c, const vf_kv_call &call, void *k, int64_t ld_k, void *v, int64_t ld_v);
+int vfk_kv_attend(vf_ctx *c, const vf_kv_call &call, int heads, const void *q, int64_t ld_q, bool causal, int window, float scale, int64_t longest_kv,
+                  void *out, int64_t ld_out);

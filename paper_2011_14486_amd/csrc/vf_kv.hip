@@ -1,0 +1,267 @@
+// vf_kv_append and vf_kv_read: rows of keys and values into a paged cache and out of it, rotary positions on the way.
+//
+// Both move every number once and are bound by the memory's rate, or for few rows by the latency of a launch.
+#include "vf_internal.h"
+#include "vf_kv_dev.h"
+
+namespace {
+
+using namespace vfkv;
+
+constexpr int THREADS = 256;
+
+struct AppendArgs {
+  Cache c;
+  Seqs s;
+  const double *freq;
+  const void *q, *k, *v;
+  void *q_out;
+  int64_t ld_q, ld_k, ld_v, ld_q_out;
+  float magnitude;
+  int heads, half, interleaved;  // heads of q; half: pairs of a head that turn
+  int lanes, chunks_q, tb;       // lanes of a head (a power of two), chunks of eight numbers in a head of q; rows of a workgroup
+  int blocks;                    // workgroups' worth of rows in the longest sequence
+};
+
+// cos and sin of a in 64 bits, to about 1e-16 of 1: a minus the nearest multiple n of pi / 2, which is taken off in two parts of 53 bits
+// (fma rounds once, so what is left has the error of the second part, n 2^-107), then the series in r, |r| <= pi / 4, whose first terms
+// left out are r^17 / 17! and r^18 / 18!, below 1e-16.
+__device__ __forceinline__ void cos_sin(double a, double &c, double &s) {
+  const double n = __builtin_rint(a * 0.6366197723675814);
+  double r = __builtin_fma(-n, 1.5707963267948966, a);
+  r = __builtin_fma(-n, 6.123233995736766e-17, r);
+  const double z = r * r;
+  double p = -1.0 / 1307674368000.0;
+  p = __builtin_fma(p, z, 1.0 / 6227020800.0);
+  p = __builtin_fma(p, z, -1.0 / 39916800.0);
+  p = __builtin_fma(p, z, 1.0 / 362880.0);
+  p = __builtin_fma(p, z, -1.0 / 5040.0);
+  p = __builtin_fma(p, z, 1.0 / 120.0);
+  p = __builtin_fma(p, z, -1.0 / 6.0);
+  const double sr = __builtin_fma(r * z, p, r);
+  double w = 1.0 / 20922789888000.0;
+  w = __builtin_fma(w, z, -1.0 / 87178291200.0);
+  w = __builtin_fma(w, z, 1.0 / 479001600.0);
+  w = __builtin_fma(w, z, -1.0 / 3628800.0);
+  w = __builtin_fma(w, z, 1.0 / 40320.0);
+  w = __builtin_fma(w, z, -1.0 / 720.0);
+  w = __builtin_fma(w, z, 1.0 / 24.0);
+  w = __builtin_fma(w, z, -0.5);
+  const double cr = __builtin_fma(z, w, 1.0);
+  const double q4 = n - 4.0 * __builtin_floor(n * 0.25);  // 0, 1, 2, 3
+  const bool swap = q4 == 1.0 || q4 == 3.0;
+  c = swap ? sr : cr;
+  s = swap ? cr : sr;
+  if (q4 == 1.0 || q4 == 2.0) c = -c;
+  if (q4 == 2.0 || q4 == 3.0) s = -s;
+}
+
+// A thread takes eight neighbouring numbers of a head at a time, and the eight that they are paired with.  The rows'
+// cosines and sines are worked out once, for all heads, into the LDS.
+template <typename T, int FMT>
+__global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
+  extern __shared__ float2 turn[];  // [tb][half]
+  __shared__ int pages[64];         // of the rows; -1: nowhere
+  const int total = a.heads + 2 * a.c.heads, lane = (int)threadIdx.x & (a.lanes - 1);
+  const int64_t units = (int64_t)a.s.n * a.blocks;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int seq = (int)(unit / a.blocks);
+    const Span sp = span_of(a.s, a.c.shift, seq);
+    for (int64_t i0 = unit % a.blocks * a.tb; i0 < sp.rows; i0 += (int64_t)a.blocks * a.tb) {
+      const int rows = sp.rows - i0 < a.tb ? (int)(sp.rows - i0) : a.tb, pos0 = sp.length - sp.rows + (int)i0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < rows * a.half; i += THREADS) {
+        const int row = i / a.half;
+        double c, s;
+        cos_sin((double)(pos0 + row) * a.freq[i - row * a.half], c, s);
+        turn[i] = make_float2((float)(c * (double)a.magnitude), (float)(s * (double)a.magnitude));
+      }
+      if ((int)threadIdx.x < rows) {
+        const int pos = pos0 + (int)threadIdx.x, e = pos >= 0 ? entry_of(a.s, a.c.shift, seq, pos) : -1;
+        pages[threadIdx.x] = (unsigned)e < (unsigned)a.c.pages ? e : -1;
+      }
+      __syncthreads();
+      const int slots = rows * total;
+      // (a head's lanes are in one wave, so that all of them have read it before any of them writes: q_out may be q)
+      for (int slot0 = 0; slot0 < slots; slot0 += THREADS / a.lanes) {
+        const int slot = slot0 + (int)threadIdx.x / a.lanes;
+        const bool on = slot < slots;
+        const int row = on ? slot / total : 0, h = slot - row * total;
+        const bool is_q = h < a.heads, is_k = !is_q && h < a.heads + a.c.heads;
+        const int head = is_q ? h : is_k ? h - a.heads : h - a.heads - a.c.heads, D = a.c.dim;
+        const T *src = is_q ? reinterpret_cast<const T *>(a.q) + (sp.first + i0 + row) * a.ld_q
+                            : is_k ? reinterpret_cast<const T *>(a.k) + (sp.first + i0 + row) * a.ld_k
+                                   : reinterpret_cast<const T *>(a.v) + (sp.first + i0 + row) * a.ld_v;
+        src += (int64_t)head * D;
+        const int d0 = 8 * lane, n = on ? D - d0 : 0;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (n > 0) load_upto8(src + d0, n, v);
+        if (n > 0 && (is_q || is_k) && d0 < 2 * a.half) {
+          const float2 *cs = turn + row * a.half;
+          if (a.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              if (d0 + i < 2 * a.half) {
+                const float2 w = cs[(d0 + i) >> 1];
+                const float x = v[i], y = v[i + 1];
+                v[i] = x * w.x - y * w.y;
+                v[i + 1] = y * w.x + x * w.y;
+              }
+            }
+          } else if ((a.half & 7) == 0) {
+            float o[8];
+            const bool first = d0 < a.half;
+            load8(src + (first ? d0 + a.half : d0 - a.half), o);
+            cs += first ? d0 : d0 - a.half;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = first ? v[i] * cs[i].x - o[i] * cs[i].y : v[i] * cs[i].x + o[i] * cs[i].y;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int d = d0 + i;
+              if (d < 2 * a.half) {
+                const bool first = d < a.half;
+                const float o = load1(src + (first ? d + a.half : d - a.half));
+                const float2 w = cs[first ? d : d - a.half];
+                v[i] = first ? v[i] * w.x - o * w.y : v[i] * w.x + o * w.y;
+              }
+            }
+          }
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        if (is_q) {
+          if (n > 0) store_upto8(reinterpret_cast<T *>(a.q_out) + (sp.first + i0 + row) * a.ld_q_out + (int64_t)head * D + d0, n, v);
+          // (what follows holds exchanges between the lanes of a head, all of which take the same way)
+          continue;
+        }
+        const int page = on ? pages[row] : -1;
+        const bool there = page >= 0 && d0 < a.c.width;
+        const int64_t at = row_of(a.c, page < 0 ? 0 : page, head, pos0 + row);
+        if constexpr (FMT == VF_E4M3) {
+          uint8_t *codes = reinterpret_cast<uint8_t *>(is_k ? a.c.k : a.c.v) + at * a.c.width, *sc = (is_k ? a.c.ks : a.c.vs) + at * a.c.kb;
+          quantize_chunk<VF_E4M3>(v, lane, there, codes, sc);
+        } else {
+          if (there) store8(reinterpret_cast<T *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0, v);
+        }
+      }
+    }
+  }
+}
+
+struct ReadArgs {
+  Cache c;
+  Seqs s;
+  void *k, *v;
+  int64_t ld_k, ld_v;
+  int lanes, tb, blocks;
+};
+
+template <typename T, int FMT>
+__global__ void __launch_bounds__(THREADS) k_kv_read(const ReadArgs a) {
+  const int total = a.c.heads * ((a.k != nullptr) + (a.v != nullptr)), lane = (int)threadIdx.x & (a.lanes - 1);
+  const int64_t units = (int64_t)a.s.n * a.blocks;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int seq = (int)(unit / a.blocks);
+    const Span sp = span_of(a.s, a.c.shift, seq);
+    for (int64_t i0 = unit % a.blocks * a.tb; i0 < sp.rows; i0 += (int64_t)a.blocks * a.tb) {
+      const int rows = sp.rows - i0 < a.tb ? (int)(sp.rows - i0) : a.tb, pos0 = sp.length - sp.rows + (int)i0, slots = rows * total;
+      for (int slot = (int)threadIdx.x / a.lanes; slot < slots; slot += THREADS / a.lanes) {
+        const int row = slot / total, h = slot - row * total, pos = pos0 + row;
+        const bool is_k = a.k && h < a.c.heads;
+        const int head = a.k && !is_k ? h - a.c.heads : h, d0 = 8 * lane, n = a.c.dim - d0;
+        if (n <= 0) continue;
+        const int e = pos >= 0 ? entry_of(a.s, a.c.shift, seq, pos) : -1;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e == -1 ? 0.0f : __builtin_nanf("");
+        if ((unsigned)e < (unsigned)a.c.pages) {
+          const int64_t at = row_of(a.c, e, head, pos);
+          if constexpr (FMT == VF_E4M3) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0);
+            // (a scale's byte is the exponent field of 2^(byte - 127); the conversion takes 0 as 2^-127 and 255 as NaN)
+            const float sc = __uint_as_float((uint32_t)(is_k ? a.c.ks : a.c.vs)[at * a.c.kb + (d0 >> 5)] << 23);
+            const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, sc, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, sc, true);
+            const f32x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, sc, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, sc, true);
+            v[0] = p0[0]; v[1] = p0[1]; v[2] = p1[0]; v[3] = p1[1];
+            v[4] = p2[0]; v[5] = p2[1]; v[6] = p3[0]; v[7] = p3[1];
+          } else {
+            load8(reinterpret_cast<const typename kv_elem<FMT>::type *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0, v);
+          }
+        }
+        T *to = reinterpret_cast<T *>(is_k ? a.k : a.v) + (sp.first + i0 + row) * (is_k ? a.ld_k : a.ld_v) + (int64_t)head * a.c.dim + d0;
+        store_upto8(to, n, v);
+      }
+    }
+  }
+}
+
+// lanes of a head: a power of two, one for every eight numbers of a row
+int lanes_of(int width) {
+  int n = 1;
+  while (8 * n < width) n *= 2;
+  return n;
+}
+// Rows of a workgroup: eight where sequences are that long; the grid stays below what may be launched.
+int rows_at_once(int64_t longest) { return longest < 8 ? (longest < 1 ? 1 : (int)longest) : 8; }
+unsigned grid_of(int64_t units) { return (unsigned)(units < (1 << 20) ? units : 1 << 20); }
+
+}  // namespace
+
+int vfk_kv_append(vf_ctx *c, const vf_kv_call &call, const vf_rope *rope, const void *k, int64_t ld_k, const void *v, int64_t ld_v, int heads,
+                  const void *q, int64_t ld_q, void *q_out, int64_t ld_q_out) {
+  if (call.seqs->n_seq == 0 || call.seqs->tokens == 0) return VF_OK;
+  AppendArgs a;
+  a.c = cache_of(call.kv);
+  a.s = seqs_of(call.seqs);
+  a.freq = rope ? rope->freq_dev : nullptr;
+  a.magnitude = rope ? rope->magnitude : 1.0f;
+  a.half = rope ? rope->rotary / 2 : 0;
+  a.interleaved = rope ? rope->interleaved : 0;
+  a.q = q; a.k = k; a.v = v; a.q_out = q_out;
+  a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_q_out = ld_q_out;
+  a.heads = q ? heads : 0;
+  a.lanes = lanes_of(a.c.width);
+  const int64_t longest = longest_of(call.seqs);
+  a.tb = rows_at_once(longest);
+  a.blocks = (int)((longest + a.tb - 1) / a.tb);
+  if (a.blocks < 1) a.blocks = 1;
+  const unsigned grid = grid_of((int64_t)a.s.n * a.blocks), lds = (unsigned)(a.tb * a.half * sizeof(float2));
+  if (call.kv->format == VF_E4M3) {
+    if (call.type == VF_BF16) k_kv_append<uint16_t, VF_E4M3><<<grid, THREADS, lds, c->stream>>>(a);
+    else k_kv_append<float, VF_E4M3><<<grid, THREADS, lds, c->stream>>>(a);
+  } else if (call.type == VF_BF16) {
+    k_kv_append<uint16_t, VF_BF16><<<grid, THREADS, lds, c->stream>>>(a);
+  } else {
+    k_kv_append<float, VF_FP32><<<grid, THREADS, lds, c->stream>>>(a);
+  }
+  VF_HIP(c, hipGetLastError());
+  return VF_OK;
+}
+
+template <typename T>
+static void launch_read(const ReadArgs &a, int format, unsigned grid, hipStream_t st) {
+  if (format == VF_E4M3) k_kv_read<T, VF_E4M3><<<grid, THREADS, 0, st>>>(a);
+  else if (format == VF_BF16) k_kv_read<T, VF_BF16><<<grid, THREADS, 0, st>>>(a);
+  else k_kv_read<T, VF_FP32><<<grid, THREADS, 0, st>>>(a);
+}
+
+int vfk_kv_read(vf_ctx *c, const vf_kv_call &call, void *k, int64_t ld_k, void *v, int64_t ld_v) {
+  if (call.seqs->n_seq == 0 || call.seqs->tokens == 0 || (!k && !v)) return VF_OK;
+  ReadArgs a;
+  a.c = cache_of(call.kv);
+  a.s = seqs_of(call.seqs);
+  a.k = k; a.v = v; a.ld_k = ld_k; a.ld_v = ld_v;
+  a.lanes = lanes_of(a.c.width);
+  const int64_t longest = longest_of(call.seqs);
+  a.tb = rows_at_once(longest);
+  a.blocks = (int)((longest + a.tb - 1) / a.tb);
+  if (a.blocks < 1) a.blocks = 1;
+  const unsigned grid = grid_of((int64_t)a.s.n * a.blocks);
+  if (call.type == VF_BF16) launch_read<uint16_t>(a, call.kv->format, grid, c->stream);
+  else launch_read<float>(a, call.kv->format, grid, c->stream);
+  VF_HIP(c, hipGetLastError());
+  return VF_OK;
+}

@@ -7,6 +7,7 @@ namespace {
 
 bool is_type(int32_t t) { return t == VF_FP32 || t == VF_BF16; }
 bool is_mx(int32_t t) { return t == VF_E4M3 || t == VF_E2M1; }
+bool is_kv(int32_t t) { return is_type(t) || t == VF_E4M3; }
 bool aligned(const void *p, int n) { return (uintptr_t)p % (uintptr_t)n == 0; }
 int bytes_of(int32_t type) { return type == VF_BF16 ? 2 : 4; }
 
@@ -52,6 +53,23 @@ int ssm(vf_ctx *c, const vf_ssm *l, const vf_ssm_io *io, bool one) {
     return VF_EINVAL;
   DeviceGuard g(c->device);
   return vfk_ssm(c, l, io, one);
+}
+
+bool kv_ok(const vf_kv *kv, int32_t type) {
+  if (kv->format != type && kv->format != VF_E4M3) return false;
+  if (kv->kv_heads < 1 || kv->kv_heads > 65536 || kv->head_dim < 1 || kv->head_dim > 256 || kv->pages < 1) return false;
+  if (kv->page < 16 || kv->page > 1024 || (kv->page & (kv->page - 1)) != 0) return false;
+  if (!kv->k_dev || !kv->v_dev || !aligned(kv->k_dev, 16) || !aligned(kv->v_dev, 16)) return false;
+  return (kv->format == VF_E4M3) == (kv->k_scales_dev != nullptr) && (kv->format == VF_E4M3) == (kv->v_scales_dev != nullptr);
+}
+
+// the sequences, whose rows are looked at by the caller
+bool seqs_ok(const vf_kv_seqs *s, const vf_kv *kv) {
+  if (s->n_seq < 0 || s->tokens < 0 || s->tokens >= ((int64_t)1 << 31) || s->longest < 0) return false;
+  if (!s->offsets_dev && (s->n_seq == 0 ? s->tokens != 0 : s->tokens % s->n_seq != 0)) return false;
+  if (s->max_pages < 0 || (int64_t)s->max_pages * kv->page > ((int64_t)1 << 30) || s->ld_table < s->max_pages || s->ld_table > MAX_LD) return false;
+  if (!aligned(s->offsets_dev, 4) || !aligned(s->lengths_dev, 4) || !aligned(s->table_dev, 4)) return false;
+  return s->n_seq == 0 || (s->lengths_dev && (s->table_dev || s->max_pages == 0));
 }
 
 }  // namespace
@@ -120,5 +138,42 @@ int vf_mx_matmul(vf_ctx *c, int32_t a_format, const uint8_t *a, const uint8_t *a
 
 int vf_ssm_scan(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io) { return ssm(c, layer, io, false); }
 int vf_ssm_step(vf_ctx *c, const vf_ssm *layer, const vf_ssm_io *io) { return ssm(c, layer, io, true); }
+
+int vf_kv_append(vf_ctx *c, const vf_kv *kv, const vf_kv_seqs *seqs, const vf_rope *rope, int32_t type, const void *k, int64_t ld_k,
+                 const void *v, int64_t ld_v, int32_t heads, const void *q, int64_t ld_q, void *q_out, int64_t ld_q_out) {
+  if (!c || !kv || !seqs || !is_type(type) || !kv_ok(kv, type) || !seqs_ok(seqs, kv)) return VF_EINVAL;
+  const int64_t n = seqs->tokens;
+  if (heads < 0 || heads > 65536 || (n > 0 && ((heads > 0) != (q != nullptr) || (heads > 0) != (q_out != nullptr)))) return VF_EINVAL;
+  const int64_t each = (int64_t)kv->kv_heads * kv->head_dim, HD = (int64_t)heads * kv->head_dim;
+  if (!matrix_ok(k, ld_k, n, each, type) || !matrix_ok(v, ld_v, n, each, type)) return VF_EINVAL;
+  if (q && (!matrix_ok(q, ld_q, n, HD, type) || !matrix_ok(q_out, ld_q_out, n, HD, type) || (q_out == q && ld_q_out != ld_q))) return VF_EINVAL;
+  if (rope && (rope->rotary < 0 || rope->rotary > kv->head_dim || rope->rotary % 2 != 0 || !aligned(rope->freq_dev, 8) ||
+               (rope->rotary > 0 && !rope->freq_dev) || !isfinite(rope->magnitude)))
+    return VF_EINVAL;
+  DeviceGuard g(c->device);
+  return vfk_kv_append(c, vf_kv_call{kv, seqs, type}, rope, k, ld_k, v, ld_v, heads, q, ld_q, q_out, ld_q_out);
+}
+
+int vf_kv_read(vf_ctx *c, const vf_kv *kv, const vf_kv_seqs *seqs, int32_t type, void *k, int64_t ld_k, void *v, int64_t ld_v) {
+  if (!c || !kv || !seqs || !is_type(type) || !kv_ok(kv, kv->format == VF_E4M3 ? type : kv->format) || !is_kv(kv->format) || !seqs_ok(seqs, kv))
+    return VF_EINVAL;
+  const int64_t n = seqs->tokens, each = (int64_t)kv->kv_heads * kv->head_dim;
+  if ((k && !matrix_ok(k, ld_k, n, each, type)) || (v && !matrix_ok(v, ld_v, n, each, type))) return VF_EINVAL;
+  DeviceGuard g(c->device);
+  return vfk_kv_read(c, vf_kv_call{kv, seqs, type}, k, ld_k, v, ld_v);
+}
+
+int vf_kv_attend(vf_ctx *c, const vf_kv *kv, const vf_kv_seqs *seqs, int32_t type, int32_t heads, const void *q, int64_t ld_q, int32_t causal,
+                 int32_t window, float scale, int64_t longest_kv, void *out, int64_t ld_out) {
+  if (!c || !kv || !seqs || !is_type(type) || !kv_ok(kv, type) || !seqs_ok(seqs, kv)) return VF_EINVAL;
+  if (heads < 1 || heads > 65536 || heads % kv->kv_heads != 0) return VF_EINVAL;
+  if (causal < 0 || causal > 1 || window < 0 || (window > 0 && !causal) || !(scale >= 0.0f) || !isfinite(scale) || longest_kv < 0) return VF_EINVAL;
+  // (rows of one head of the cache are counted in 32 bits)
+  if (seqs->tokens * (int64_t)(heads / kv->kv_heads) >= ((int64_t)1 << 31)) return VF_EINVAL;
+  const int64_t HD = (int64_t)heads * kv->head_dim;
+  if (!matrix_ok(q, ld_q, seqs->tokens, HD, type) || !matrix_ok(out, ld_out, seqs->tokens, HD, type)) return VF_EINVAL;
+  DeviceGuard g(c->device);
+  return vfk_kv_attend(c, vf_kv_call{kv, seqs, type}, heads, q, ld_q, causal != 0, window, scale, longest_kv, out, ld_out);
+}
 
 }  // extern "C"
