@@ -528,9 +528,329 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
   }
 }
 
+// ---- many rows: keys and values through the LDS ----
+//
+// A wave holds 32 rows, a workgroup four waves; a tile is 64 keys, keys and values of two tiles are in the LDS.  Pieces of 16 bytes go there straight from
+// memory (numbers in 8 bits through registers, where they become bf16); which lane fetches a piece says where it lies: piece x of key t at place x ^ key_turn(t), so
+// that the 16 keys whose pieces lanes read at a time meet all banks, and values in pairs of pieces at pair ^ value_turn(t).  S^T is made by products of
+// 32 keys by 32 rows; values are read with the reads that turn a 4 by 16 block around, so that a lane gets four keys' numbers of one column.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int TK = 64;  // keys of a tile
+template <int DP> constexpr int tile_bytes() { return TK * DP * 2; }   // of keys, or of values
+template <int DP> __device__ __forceinline__ int key_turn(int t) { return DP == 64 ? (t >> 1) & 7 : t & 15; }
+template <int DP> __device__ __forceinline__ int value_turn(int t) { return DP == 64 ? (t >> 1) & 3 : t & 7; }
+
+// A part of memory as the instructions with a range check see it: what lies behind its end reads as zeros.
+__device__ __forceinline__ i32x4 part_of(const void *at, int bytes) {
+  const uint64_t a = (uint64_t)(uintptr_t)at;
+  return i32x4{__builtin_amdgcn_readfirstlane((int)a), __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xffff), __builtin_amdgcn_readfirstlane(bytes), 0x00027000};
+}
+// 64 lanes fetch 16 bytes each, `lane_at` into the part, to consecutive places of the LDS from `to` on.  The compiler does not know
+// of these loads: they are waited for by wait_loads.
+__device__ __forceinline__ void to_lds16(const i32x4 &part, uint32_t lane_at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(lane_at), "s"(part) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+template <int FMT, int DP>
+__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const AttendArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  __shared__ int odd_any;
+  constexpr int TB = tile_bytes<DP>(), RB = DP * 2, ROWS = 128, NK = DP / 16, ND = DP / 32;
+  constexpr int PIECES = DP / 8, TURNS = TK * PIECES / 256;  // pieces of 16 bytes in a row; of a tile, for every thread
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Cache &c = a.c;
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+
+  // a thread's pieces: of the keys 16 wave .. 16 wave + 15 of a tile, whose page is one
+  int from_k[TURNS], from_v[TURNS];
+#pragma unroll
+  for (int i = 0; i < TURNS; ++i) {
+    const int e = i * 64 + lane, t = 16 * wave + e / PIECES, x = e % PIECES, last = (c.width >> 3) - 1;
+    const int xk = x ^ key_turn<DP>(t), xv = ((x >> 1 ^ value_turn<DP>(t)) << 1) | (x & 1);
+    // (pieces behind a row's end are the last one again: the queries are zero there, and such columns of the output are not kept)
+    from_k[i] = e / PIECES * c.width + 8 * (xk < last ? xk : last);
+    from_v[i] = e / PIECES * c.width + 8 * (xv < last ? xv : last);
+  }
+  // places that a lane reads: of keys n (and 32 + n, a constant further), of values 4 g .. 4 g + 3 (and further ones)
+  int at_k[NK], at_v[ND];
+#pragma unroll
+  for (int ks = 0; ks < NK; ++ks) at_k[ks] = n * RB + 16 * ((2 * ks + g) ^ key_turn<DP>(n));
+#pragma unroll
+  for (int d = 0; d < ND; ++d) {
+    const int t = 4 * g + ((lane & 15) >> 2), pair = 2 * d + ((lane >> 4) & 1);
+    at_v[d] = TB + t * RB + 32 * (pair ^ value_turn<DP>(t)) + 8 * (lane & 3);
+  }
+
+  for (int64_t unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
+    // unit: heads of the cache fastest, then shares of the keys, then row blocks (those that see the most keys first), then sequences
+    int64_t rest = unit / c.heads;
+    const int head = (int)(unit - rest * c.heads), split = (int)(rest % a.splits);
+    rest /= a.splits;
+    const int seq = (int)(rest / a.blocks), block0 = a.blocks - 1 - (int)(rest - (int64_t)seq * a.blocks);
+    const Span sp = span_of(a.s, c.shift, seq);
+    const int64_t all = (int64_t)sp.rows * a.group;
+    for (int64_t block = block0; block * ROWS < all; block += a.blocks) {
+      // (row blocks that the plan did not count on are not shared)
+      const bool shared = a.splits > 1 && block < a.blocks;
+      if (block >= a.blocks && split > 0) break;
+      const int64_t w0 = block * ROWS, w1 = w0 + ROWS < all ? w0 + ROWS : all, r0 = w0 + 32 * wave, r1 = r0 + 32 < w1 ? r0 + 32 : w1;
+      // what the workgroup's rows, and the wave's, see: all of [.., in), nothing outside
+      int lo, hi, lo_in, hi_in, wlo = 0, whi = 0, wlo_in = 0, whi_in = 0;
+      seen_by(a, sp, (int)(w0 / a.group), lo, hi_in);
+      seen_by(a, sp, (int)((w1 - 1) / a.group), lo_in, hi);
+      if (r0 < r1) {
+        seen_by(a, sp, (int)(r0 / a.group), wlo, whi_in);
+        seen_by(a, sp, (int)((r1 - 1) / a.group), wlo_in, whi);
+      }
+      int row_lo = 0, row_hi = 0;
+      const uint16_t *q_row = nullptr;
+      int64_t out_row = -1;
+      const int64_t r = r0 + n;
+      if (r < r1) {
+        const int i = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)i * a.group);
+        seen_by(a, sp, i, row_lo, row_hi);
+        q_row = reinterpret_cast<const uint16_t *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * c.dim;
+        out_row = (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
+      }
+      const int from = lo & ~(TK - 1);
+      int tiles = hi > from ? (hi - from + TK - 1) / TK : 0, s0 = 0;
+      if (shared) {
+        const int each = (tiles + a.splits - 1) / a.splits;
+        s0 = (int)((int64_t)each * split < tiles ? each * split : tiles);
+        tiles = tiles - s0 < each ? tiles : s0 + each;
+      }
+      // The wave's share of a tile on its way: straight to the LDS, or 8-bit codes and scales in registers.
+      uint2 raw_k[FMT == VF_E4M3 ? TURNS : 1], raw_v[FMT == VF_E4M3 ? TURNS : 1];
+      uint32_t sc_k[FMT == VF_E4M3 ? TURNS : 1], sc_v[FMT == VF_E4M3 ? TURNS : 1];
+      auto entry_at = [&](int st) { return st < tiles ? __builtin_amdgcn_readfirstlane(entry_of(a.s, c.shift, seq, from + st * TK + 16 * wave)) : -1; };
+      auto fetch = [&](int st, int entry) {
+        const int page = (unsigned)entry < (unsigned)c.pages ? entry : 0;  // (what is fetched there is not used)
+        const int64_t row = row_of(c, page, head, from + st * TK + 16 * wave);
+        if constexpr (FMT == VF_E4M3) {
+          const uint8_t *k = reinterpret_cast<const uint8_t *>(c.k) + row * c.width, *v = reinterpret_cast<const uint8_t *>(c.v) + row * c.width;
+          const uint8_t *ks = c.ks + row * c.kb, *vs = c.vs + row * c.kb;
+#pragma unroll
+          for (int i = 0; i < TURNS; ++i) {
+            raw_k[i] = *reinterpret_cast<const uint2 *>(k + from_k[i]);
+            raw_v[i] = *reinterpret_cast<const uint2 *>(v + from_v[i]);
+            sc_k[i] = ks[from_k[i] >> 5];   // (a row's scales are a 32nd of its width)
+            sc_v[i] = vs[from_v[i] >> 5];
+          }
+        } else {
+          const i32x4 pk = part_of(reinterpret_cast<const uint16_t *>(c.k) + row * c.width, 32 * c.width);
+          const i32x4 pv = part_of(reinterpret_cast<const uint16_t *>(c.v) + row * c.width, 32 * c.width);
+          const uint32_t to = base + (uint32_t)((st & 1) * 2 * TB) + (uint32_t)wave * (16 * RB);
+#pragma unroll
+          for (int i = 0; i < TURNS; ++i) to_lds16(pk, 2 * (uint32_t)from_k[i], to + i * 1024);
+#pragma unroll
+          for (int i = 0; i < TURNS; ++i) to_lds16(pv, 2 * (uint32_t)from_v[i], to + TB + i * 1024);
+        }
+      };
+      auto put = [&](int st) {  // 8 bits: what has arrived becomes bf16 in the LDS
+        if constexpr (FMT == VF_E4M3) {
+          uint8_t *to = lds + (st & 1) * 2 * TB + wave * (16 * RB) + lane * 16;
+#pragma unroll
+          for (int i = 0; i < TURNS; ++i) {
+            const float fk = scale_of((uint8_t)sc_k[i]), fv = scale_of((uint8_t)sc_v[i]);
+            *reinterpret_cast<uint4 *>(to + i * 1024) = make_uint4(cvt2(raw_k[i].x, fk, false), cvt2(raw_k[i].x, fk, true), cvt2(raw_k[i].y, fk, false), cvt2(raw_k[i].y, fk, true));
+            *reinterpret_cast<uint4 *>(to + TB + i * 1024) = make_uint4(cvt2(raw_v[i].x, fv, false), cvt2(raw_v[i].x, fv, true), cvt2(raw_v[i].y, fv, false), cvt2(raw_v[i].y, fv, true));
+          }
+        }
+      };
+      __syncthreads();  // (the row block before is done with the LDS)
+      int entry_next = entry_at(s0);
+      if (s0 < tiles) fetch(s0, entry_next);
+      entry_next = entry_at(s0 + 1);
+
+      // queries as operands
+      uint4 q16[NK];
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) {
+        const int d = 16 * ks + 8 * g, left = q_row ? c.dim - d : 0;
+        raw8<uint16_t> w = {};
+        if (left > 0) fetch8(q_row + d, left, w);
+        q16[ks] = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
+      }
+      f32x16 acc[ND];
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+      float m = -INFINITY, l = 0.0f;
+
+      for (int st = s0; st < tiles; ++st) {
+        const int t0 = from + st * TK;
+        if constexpr (FMT == VF_E4M3) put(st);
+        else wait_loads<0>();
+        __syncthreads();  // the tile is there, and nobody reads the one before any more
+        if (st + 1 < tiles) fetch(st + 1, entry_next);
+        entry_next = entry_at(st + 2);
+        uint8_t *tile = lds + (st & 1) * 2 * TB;
+        // pages of the tile's blocks of 16 keys: bits of those that are there, and of entries that are no page and not -1
+        int there = 0, wrong = 0;
+#pragma unroll
+        for (int x = 0; x < TK / 16; ++x) {
+          const int e = entry_of(a.s, c.shift, seq, t0 + 16 * x);
+          there |= ((unsigned)e < (unsigned)c.pages) << x;
+          wrong |= ((unsigned)e >= (unsigned)c.pages && e != -1) << x;
+        }
+        constexpr int ALL = (1 << (TK / 16)) - 1;
+        if (t0 < lo_in || t0 + TK > hi_in || there != ALL) {
+          // Values that no row sees become zeros.  Of others that are not finite the rows that see them get NaN; then they are zeros too, so that
+          // they reach no other row.
+          if (tid == 0) odd_any = 0;
+          __syncthreads();
+          bool bad = false;
+#pragma unroll 1
+          for (int e = tid; e < TK * PIECES; e += 256) {
+            const int t = t0 + e / PIECES;
+            uint4 *at = reinterpret_cast<uint4 *>(tile + TB) + e;
+            if (t < lo || t >= hi || !(there >> (e / PIECES / 16) & 1)) *at = make_uint4(0, 0, 0, 0);
+            else bad = bad || not_finite(at->x) || not_finite(at->y) || not_finite(at->z) || not_finite(at->w);
+          }
+          if (bad) odd_any = 1;
+          __syncthreads();
+          if (odd_any) {
+#pragma unroll 1
+            for (int t = 0; t < TK; ++t) {
+              if (t0 + t < row_lo || t0 + t >= row_hi) continue;
+#pragma unroll
+              for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                  const int piece = 4 * d + (i >> 2);
+                  const uint2 w = *reinterpret_cast<const uint2 *>(tile + TB + t * RB + 32 * ((piece >> 1) ^ value_turn<DP>(t)) + 16 * (piece & 1) + 8 * g);
+                  if ((w.x & 0x7f80u) == 0x7f80u) acc[d][i] = __builtin_nanf("");
+                  if ((w.x & 0x7f800000u) == 0x7f800000u) acc[d][i + 1] = __builtin_nanf("");
+                  if ((w.y & 0x7f80u) == 0x7f80u) acc[d][i + 2] = __builtin_nanf("");
+                  if ((w.y & 0x7f800000u) == 0x7f800000u) acc[d][i + 3] = __builtin_nanf("");
+                }
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int e = tid; e < TK * PIECES; e += 256) {
+              uint4 *at = reinterpret_cast<uint4 *>(tile + TB) + e;
+              *at = make_uint4(finite_of(at->x), finite_of(at->y), finite_of(at->z), finite_of(at->w));
+            }
+            __syncthreads();
+          }
+        }
+        if (t0 >= whi || t0 + TK <= wlo) continue;  // (nothing for this wave's rows)
+
+        f32x16 sc[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const uint4 k = *reinterpret_cast<const uint4 *>(tile + at_k[ks] + b * 32 * RB);
+            sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q16[ks]), sc[b], 0, 0, 0);
+          }
+        if (there != ALL) {
+#pragma unroll
+          for (int x = 0; x < TK / 16; ++x) {
+            if (there >> x & 1) continue;
+            const float no = wrong >> x & 1 ? __builtin_nanf("") : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sc[x >> 1][8 * (x & 1) + i] = no;
+          }
+        }
+        if (t0 < wlo_in || t0 + TK > whi_in) {
+          const int rel = t0 + 4 * g - row_lo, len = row_hi - row_lo;  // (key 32 b + 8 (i / 4) + 4 g + i % 4 is in register i of block b)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[b][i] = (unsigned)(rel + 32 * b + 8 * (i >> 2) + (i & 3)) < (unsigned)len ? sc[b][i] : -INFINITY;
+        }
+        float top = sc[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+        top *= a.scale2;
+        if (__any(top > m + MARGIN)) {
+          float t = fmaxf(top, m);
+          t = fmaxf(t, __shfl_xor(t, 32));
+          const float f = exp2_(m - base_of(t));
+          m = t;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d) acc[d] *= f;
+        }
+        const float mb = base_of(m);
+        bf16x8 p[4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            sc[b][i] = exp2_(fmaf(sc[b][i], a.scale2, -mb));
+            l += sc[b][i];
+          }
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            p[2 * b + x] = as_bf16x8(pack2(sc[b][8 * x], sc[b][8 * x + 1]), pack2(sc[b][8 * x + 2], sc[b][8 * x + 3]), pack2(sc[b][8 * x + 4], sc[b][8 * x + 5]),
+                                     pack2(sc[b][8 * x + 6], sc[b][8 * x + 7]));
+        }
+        auto values = [&](int d, int x) {  // of keys 16 x + 4 g .. + 3 and 16 x + 8 + 4 g .. + 3, column 32 d + n
+          const uint8_t *at = tile + at_v[d] + x * 16 * RB;
+          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at));
+          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 8 * RB));
+          const uint2 w0 = __builtin_bit_cast(uint2, v0), w1 = __builtin_bit_cast(uint2, v1);
+          return make_uint4(w0.x, w0.y, w1.x, w1.y);
+        };
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(d, x)), p[x], acc[d], 0, 0, 0);
+      }
+      l += __shfl_xor(l, 32);
+      // numbers 32 d + 8 (i / 4) + 4 g + i % 4 of row n are in acc[d][i]
+      if (shared) {
+        const int64_t at = unit * ROWS + 32 * wave + n;
+        float *o = a.part + at * DP;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4 *>(o + 32 * d + 2 * i + 4 * g) = f32x4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+        if (g == 0) {
+          float *stat = a.part + a.units * ROWS * DP;
+          stat[at] = m;
+          stat[a.units * ROWS + at] = l;
+        }
+      } else if (out_row >= 0) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *o = reinterpret_cast<uint16_t *>(a.out) + out_row;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const int at = 32 * d + 2 * i + 4 * g, left = c.dim - at;
+            float v[8] = {};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[d][i + e] * inv;
+            if (left >= 4) {
+              typedef uint32_t u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+              *reinterpret_cast<u32x2 *>(o + at) = u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])};
+            } else if (left > 0) {
+              store_upto8(o + at, left, v);
+            }
+          }
+      }
+    }
+  }
+}
+
 // Joins the parts of row blocks that several workgroups have shared: a wave a row.
 template <typename T, int DP>
-__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int rows) {
+__global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int rows, bool last_first) {
   const int lane = (int)threadIdx.x & 63;
   const Cache &c = a.c;
   const int64_t blocks = a.units / a.splits, items = blocks * rows;
@@ -538,7 +858,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int row
     const int64_t ub = item / rows;   // (sequence, row block, head of the cache), heads fastest
     const int row = (int)(item - ub * rows), head = (int)(ub % c.heads);
     const int64_t sb = ub / c.heads;
-    const int seq = (int)(sb / a.blocks), block = (int)(sb - (int64_t)seq * a.blocks);
+    const int seq = (int)(sb / a.blocks), place = (int)(sb - (int64_t)seq * a.blocks), block = last_first ? a.blocks - 1 - place : place;
     const Span sp = span_of(a.s, c.shift, seq);
     const int64_t r = (int64_t)block * rows + row;
     if (r >= (int64_t)sp.rows * a.group) continue;
@@ -594,7 +914,34 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   VF_HIP(c, hipGetLastError());
   if (splits > 1) {
     const int64_t items = (units * rows + 3) / 4;
-    k_attend_join<T, DP><<<(unsigned)(items < 4096 ? items : 4096), 256, 0, c->stream>>>(a, rows);
+    k_attend_join<T, DP><<<(unsigned)(items < 4096 ? items : 4096), 256, 0, c->stream>>>(a, rows, false);
+    VF_HIP(c, hipGetLastError());
+  }
+  return VF_OK;
+}
+
+template <int FMT, int DP>
+int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
+  constexpr int ROWS = 128, LDS = 4 * tile_bytes<DP>(), AT_ONCE = DP <= 128 ? 512 : 256;
+  const int64_t longest = (int64_t)a.longest * a.group;
+  a.blocks = (int)((longest + ROWS - 1) / ROWS);
+  const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, most = (longest_kv + TK - 1) / TK / 4;
+  int64_t splits = (AT_ONCE + units - 1) / units;
+  if (splits > most) splits = most;
+  if (splits < 1) splits = 1;
+  if (splits > 1) {
+    a.part = reinterpret_cast<float *>(vfk_ops_scratch(c, (size_t)(units * splits * ROWS) * (DP + 2) * sizeof(float)));
+    if (!a.part) splits = 1;
+  }
+  a.splits = (int)splits;
+  a.units = units * splits;
+  const unsigned grid = (unsigned)(a.units < (1 << 20) ? a.units : 1 << 20);
+  VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(&k_attend_tile<FMT, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+  k_attend_tile<FMT, DP><<<grid, 256, LDS, c->stream>>>(a);
+  VF_HIP(c, hipGetLastError());
+  if (splits > 1) {
+    const int64_t items = (units * ROWS + 3) / 4;
+    k_attend_join<uint16_t, DP><<<(unsigned)(items < 4096 ? items : 4096), 256, 0, c->stream>>>(a, ROWS, true);
     VF_HIP(c, hipGetLastError());
   }
   return VF_OK;
@@ -602,6 +949,13 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
 
 template <typename T, int FMT>
 int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
+  if constexpr (sizeof(T) == 2) {
+    if ((int64_t)a.longest * a.group > 32) {
+      if (a.c.dim <= 64) return launch_tile<FMT, 64>(c, a, longest_kv);
+      if (a.c.dim <= 128) return launch_tile<FMT, 128>(c, a, longest_kv);
+      return launch_tile<FMT, 256>(c, a, longest_kv);
+    }
+  }
   if (a.c.dim <= 32) return launch_rows<T, FMT, 32>(c, a, longest_kv);
   if (a.c.dim <= 64) return launch_rows<T, FMT, 64>(c, a, longest_kv);
   if (a.c.dim <= 128) return launch_rows<T, FMT, 128>(c, a, longest_kv);
