@@ -27,11 +27,43 @@ struct AttendArgs {
   const void *q;
   void *out;
   float *part;      // of workgroups that share a row block: [unit][rows][DP] sums, then [unit][rows] maxima, then [unit][rows] sums of weights
-  int64_t ld_q, ld_out, units;
+  int64_t ld_q, ld_out;
   float scale2;     // scale log2(e)
   int group, causal, window, longest;
   int blocks, splits;  // row blocks of the longest sequence; workgroups that share one along the keys
+  uint32_t magic;      // r / group = r magic >> shift, see over_group
+  int shift;
 };
+
+// r / group for r below 2^31: with 2^(s - 1) < group <= 2^s and magic = 2^(31 + s) / group rounded up, the product is off by less than
+// r group <= 2^(31 + s) at the most, in units of 1 / group below the next quotient.
+__device__ __forceinline__ int over_group(const AttendArgs &a, int r) { return (int)((uint64_t)(uint32_t)r * a.magic >> a.shift); }
+void set_group(AttendArgs &a, int group) {
+  int s = 0;
+  while ((1 << s) < group) ++s;
+  a.group = group;
+  a.shift = 31 + s;
+  a.magic = (uint32_t)((((uint64_t)1 << a.shift) + (uint64_t)group - 1) / (uint64_t)group);
+}
+
+// A workgroup's place: x = head of the cache + heads (share of the keys + splits row block), y: sequence.  (The launch has at most MAX_Y
+// sequences side by side; workgroups go on to further ones.)
+constexpr int MAX_Y = 32768;
+struct Place { int head, split, block; };
+__device__ __forceinline__ Place place_of(const AttendArgs &a) {
+  Place p;
+  const unsigned x = blockIdx.x, rest = x / (unsigned)a.c.heads;
+  p.head = (int)(x - rest * (unsigned)a.c.heads);
+  p.block = a.splits > 1 ? (int)(rest / (unsigned)a.splits) : (int)rest;
+  p.split = a.splits > 1 ? (int)rest - p.block * a.splits : 0;
+  return p;
+}
+// A number that is the same in all of a launch, as one that the compiler has to take anew: what it derives from it (which of an
+// unrolled loop's numbers are there) is not kept over loops in registers that are then missing inside them.
+__device__ __forceinline__ int anew(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
 
 // The keys that row i of a sequence sees: [lo, hi).
 __device__ __forceinline__ void seen_by(const AttendArgs &a, const Span &sp, int i, int &lo, int &hi) {
@@ -98,40 +130,37 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
   __shared__ float join_m[ALONG ? 1 : 4][16 * RB], join_l[ALONG ? 1 : 4][16 * RB];
   const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Cache &c = a.c;
-  for (int64_t unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
-    // unit: heads of the cache fastest, then shares of the keys, then row blocks, then sequences
-    int64_t rest = unit / c.heads;
-    const int head = (int)(unit - rest * c.heads), split = (int)(rest % a.splits);
-    rest /= a.splits;
-    const int seq = (int)(rest / a.blocks), block0 = (int)(rest - (int64_t)seq * a.blocks);
+  const Place place = place_of(a);
+  const int head = place.head, split = place.split;
+  for (int seq = blockIdx.y; seq < a.s.n; seq += gridDim.y) {
     const Span sp = span_of(a.s, c.shift, seq);
-    const int64_t all = (int64_t)sp.rows * a.group;
-    for (int64_t block = block0; block * ROWS < all; block += a.blocks) {
+    const int all = sp.rows * a.group;
+    for (int block = place.block; (int64_t)block * ROWS < all; block += a.blocks) {
       // (row blocks that the plan did not count on are not shared)
       const bool shared = a.splits > 1 && block < a.blocks;
       if (block >= a.blocks && split > 0) break;
-      const int64_t r0 = block * ROWS + (ALONG ? wave * 16 * RB : 0), r1 = r0 + 16 * RB < all ? r0 + 16 * RB : all;
+      const int dim = anew(c.dim), width = anew(c.width);
+      const int r0 = block * ROWS + (ALONG ? wave * 16 * RB : 0), r1 = all - r0 > 16 * RB ? r0 + 16 * RB : all;
       // what the wave's rows see: all of [lo_in, hi_in), nothing outside [lo, hi)
       int lo = 0, hi = 0, lo_in = 0, hi_in = 0;
       if (r0 < r1) {
-        const int first = (int)(r0 / a.group), last = (int)((r1 - 1) / a.group);
-        seen_by(a, sp, first, lo, hi_in);
-        seen_by(a, sp, last, lo_in, hi);
+        seen_by(a, sp, over_group(a, r0), lo, hi_in);
+        seen_by(a, sp, over_group(a, r1 - 1), lo_in, hi);
       }
       int row_lo[RB], row_hi[RB];
       const T *q_row[RB];
       int64_t out_row[RB];
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
-        const int64_t r = r0 + 16 * b + n;
+        const int r = r0 + 16 * b + n;
         row_lo[b] = row_hi[b] = 0;
         q_row[b] = nullptr;
         out_row[b] = -1;
         if (r < r1) {
-          const int i = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)i * a.group);
+          const int i = over_group(a, r), h = head * a.group + r - i * a.group;
           seen_by(a, sp, i, row_lo[b], row_hi[b]);
-          q_row[b] = reinterpret_cast<const T *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * c.dim;
-          out_row[b] = (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
+          q_row[b] = reinterpret_cast<const T *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * dim;
+          out_row[b] = (sp.first + i) * a.ld_out + (int64_t)h * dim;
         }
       }
       // queries as operands
@@ -141,7 +170,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
       for (int b = 0; b < RB; ++b)
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks) {
-          const int d = k_at<T, FMT, DP>(ks, g), left = q_row[b] ? c.dim - d : 0;
+          const int d = k_at<T, FMT, DP>(ks, g), left = q_row[b] ? dim - d : 0;
           if constexpr (F32) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) q32[b][ks][i] = i < left ? q_row[b][d + i] : 0.0f;
@@ -168,153 +197,155 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
         s0 = (int)((int64_t)each * split < steps ? each * split : steps);
         steps = steps - s0 < each ? steps : s0 + each;
       }
-      for (int st = s0 + (ALONG ? 0 : wave); st < steps; st += ALONG ? 1 : 4) {
-        const int t0 = from + st * STEP;
-        int entry[KB], page[KB];
-        bool fine = true;
+      // A step's keys and values on their way: as they are in memory.  A step's are sent for when the registers of the step before are free, keys behind
+      // the scores, values behind the outputs; pages one step earlier.
+      constexpr int STRIDE = ALONG ? 1 : 4;
+      constexpr int VD = F32 ? VW : (VW + 1) / 2;                    // registers of VW values
+      constexpr int KL = F32 ? NK : FMT == VF_E4M3 && DP >= 64 ? NK / 2 : NK;   // pieces of a key
+      typedef uint32_t kv4 __attribute__((ext_vector_type(FMT == VF_E4M3 ? (F32 ? 1 : DP >= 64 ? 4 : 2) : 4)));
+      kv4 kraw[KB][KL];
+      uint32_t vraw[KB][4][NH][FMT == VF_E4M3 ? (VW + 3) / 4 : VD];
+      uint8_t kscale[KB][FMT == VF_E4M3 ? KL : 1], vscale[KB][4][FMT == VF_E4M3 ? NH : 1];
+      struct Pages { int entry[KB]; };
+      auto pages_at = [&](int st) {
+        Pages p;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) p.entry[kb] = st < steps ? entry_of(a.s, c.shift, seq, from + st * STEP + 16 * kb) : -1;
+        return p;
+      };
+      // (what is fetched of an entry that is no page, and behind a row's end, is not used)
+      auto page_of = [&](const Pages &p, int kb) { return (unsigned)p.entry[kb] < (unsigned)c.pages ? p.entry[kb] : 0; };
+      auto ask_keys = [&](int st, const Pages &p) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-          entry[kb] = entry_of(a.s, c.shift, seq, t0 + 16 * kb);
-          const bool there = (unsigned)entry[kb] < (unsigned)c.pages;
-          page[kb] = there ? entry[kb] : 0;   // (what is fetched there is not used)
-          fine = fine && there;
+          const int64_t row = row_of(c, page_of(p, kb), head, from + st * STEP + 16 * kb + n);
+          const typename kv_elem<FMT>::type *k = reinterpret_cast<const typename kv_elem<FMT>::type *>(c.k) + row * width;
+#pragma unroll
+          for (int x = 0; x < KL; ++x) {
+            int d = k_at<T, FMT, DP>(x * (NK / KL), g);
+            d = d < width ? d : 0;
+            kraw[kb][x] = *reinterpret_cast<const kv4 *>(k + d);
+            if constexpr (FMT == VF_E4M3) kscale[kb][x] = c.ks[row * c.kb + (d >> 5)];
+          }
         }
+      };
+      auto ask_values = [&](int st, const Pages &p) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const int64_t row = row_of(c, page_of(p, kb), head, from + st * STEP + 16 * kb + 4 * g);
+          const typename kv_elem<FMT>::type *v = reinterpret_cast<const typename kv_elem<FMT>::type *>(c.v) + row * width;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
+              int d = h * 16 * VW + n * VW;
+              d = d < width ? d : 0;
+              const auto *at = v + (int64_t)i * width + d;
+              if constexpr (FMT == VF_E4M3) {
+                if constexpr (VW == 8) {
+                  const uint2 w = *reinterpret_cast<const uint2 *>(at);
+                  vraw[kb][i][h][0] = w.x;
+                  vraw[kb][i][h][(VW + 3) / 4 - 1] = w.y;
+                } else if constexpr (VW == 4) {
+                  vraw[kb][i][h][0] = *reinterpret_cast<const uint32_t *>(at);
+                } else {
+                  vraw[kb][i][h][0] = *reinterpret_cast<const uint16_t *>(at);
+                }
+                vscale[kb][i][h] = c.vs[(row + i) * c.kb + (d >> 5)];
+              } else if constexpr (VD == 1) {
+                vraw[kb][i][h][0] = *reinterpret_cast<const uint32_t *>(at);
+              } else {
+                typedef uint32_t uv __attribute__((ext_vector_type(VD)));
+                const uv w = *reinterpret_cast<const uv *>(at);
+#pragma unroll
+                for (int x = 0; x < VD; ++x) vraw[kb][i][h][x] = w[x];
+              }
+            }
+        }
+      };
+      const int first = s0 + (ALONG ? 0 : wave);
+      Pages now = pages_at(first), next = pages_at(first + STRIDE);
+      if (first < steps) {
+        ask_keys(first, now);
+        ask_values(first, now);
+      }
+      for (int st = first; st < steps; st += STRIDE) {
+        const int t0 = from + st * STEP;
+        bool fine = true;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) fine = fine && (unsigned)now.entry[kb] < (unsigned)c.pages;
         const bool edge = !fine || t0 < lo_in || t0 + STEP > hi_in;
+        const int(&entry)[KB] = now.entry;
         f32x4 sc[RB][KB];
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) sc[b][kb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        // values: of key 4 g + i of each block of 16 the VW numbers at c VW of each part
-        constexpr int VD = F32 ? VW : (VW + 1) / 2;  // registers
-        uint32_t val[KB][4][NH][VD];
-
-        if constexpr (F32) {
-          const int64_t krow = row_of(c, page[0], head, t0 + n), vrow = row_of(c, page[0], head, t0 + 4 * g);
-          f32x4 key[NK];
 #pragma unroll
-          for (int ks = 0; ks < NK; ++ks) {
-            const int d = k_at<T, FMT, DP>(ks, g);
-            key[ks] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (d < c.width) {
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int x = 0; x < KL; ++x) {
+            const bool in = k_at<T, FMT, DP>(x * (NK / KL), g) < width;
+            kv4 w = kraw[kb][x];
+            if constexpr (F32) {
+              f32x4 key;
               if constexpr (FMT == VF_E4M3) {
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint8_t *>(c.k) + krow * c.width + d);
-                const float s = scale_of(c.ks[krow * c.kb + (d >> 5)]);
-                const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
-                key[ks] = f32x4{x[0], x[1], y[0], y[1]};
+                const float s = scale_of(kscale[kb][x]);
+                const f32x2 lo2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[0], s, false), hi2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[0], s, true);
+                key = f32x4{lo2[0], lo2[1], hi2[0], hi2[1]};
               } else {
-                key[ks] = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(c.k) + krow * c.width + d);
+                key = __builtin_bit_cast(f32x4, w);
               }
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int b = 0; b < RB; ++b) sc[b][kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(in ? key[e] : 0.0f, q32[b][x][e], sc[b][kb], 0, 0, 0);
+            } else if constexpr (FMT == VF_E4M3) {
+              const float s = scale_of(kscale[kb][x]);
+#pragma unroll
+              for (int half = 0; half < NK / KL; ++half) {
+                const uint32_t w0 = in ? w[2 * half] : 0, w1 = in ? w[2 * half + 1] : 0;
+                const bf16x8 key = as_bf16x8(cvt2(w0, in ? s : 1.0f, false), cvt2(w0, in ? s : 1.0f, true), cvt2(w1, in ? s : 1.0f, false), cvt2(w1, in ? s : 1.0f, true));
+#pragma unroll
+                for (int b = 0; b < RB; ++b)
+                  sc[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, __builtin_bit_cast(bf16x8, q16[b][x * (NK / KL) + half]), sc[b][kb], 0, 0, 0);
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[e] = in ? w[e] : 0;
+#pragma unroll
+              for (int b = 0; b < RB; ++b)
+                sc[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, q16[b][x]), sc[b][kb], 0, 0, 0);
             }
           }
+        if (st + STRIDE < steps) ask_keys(st + STRIDE, next);
+        const Pages after = pages_at(st + 2 * STRIDE);
+        // values as numbers: of key 4 g + i of each block of 16 the VW numbers at c VW of each part
+        uint32_t val[KB][4][NH][VD];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-              const int d = h * 16 * VW + n * VW;
+              if constexpr (FMT != VF_E4M3) {
 #pragma unroll
-              for (int x = 0; x < VD; ++x) val[0][i][h][x] = 0;
-              if (d < c.width) {
-                if constexpr (FMT == VF_E4M3) {
-                  const uint8_t *p = reinterpret_cast<const uint8_t *>(c.v) + (vrow + i) * c.width + d;
-                  uint32_t w;
-                  if constexpr (VW == 4) w = *reinterpret_cast<const uint32_t *>(p);
-                  else w = *reinterpret_cast<const uint16_t *>(p);
-                  const float s = scale_of(c.vs[(vrow + i) * c.kb + (d >> 5)]);
-                  const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false), y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true);
+                for (int x = 0; x < VD; ++x) val[kb][i][h][x] = vraw[kb][i][h][x];
+              } else {
+                const float s = scale_of(vscale[kb][i][h]);
 #pragma unroll
-                  for (int e = 0; e < VW; ++e) val[0][i][h][e] = __float_as_uint(e < 2 ? x[e & 1] : y[e & 1]);
-                } else {
-                  const float *p = reinterpret_cast<const float *>(c.v) + (vrow + i) * c.width + d;
-                  typedef float fv __attribute__((ext_vector_type(VW)));
-                  const fv w = *reinterpret_cast<const fv *>(p);
-#pragma unroll
-                  for (int e = 0; e < VW; ++e) val[0][i][h][e] = __float_as_uint(w[e]);
+                for (int x = 0; x < (VW + 1) / 2; ++x) {
+                  const uint32_t w = vraw[kb][i][h][x >> 1];
+                  if constexpr (F32) {
+                    const f32x2 v = x & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, s, false);
+                    val[kb][i][h][2 * x] = __float_as_uint(v[0]);
+                    val[kb][i][h][2 * x + 1] = __float_as_uint(v[1]);
+                  } else {
+                    val[kb][i][h][x] = cvt2(w, s, x & 1);
+                  }
                 }
               }
             }
-#pragma unroll
-          for (int ks = 0; ks < NK; ++ks)
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-              for (int b = 0; b < RB; ++b) sc[b][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(key[ks][x], q32[b][ks][x], sc[b][0], 0, 0, 0);
-        } else {
-          uint4 key[KB][NK];
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb) {
-            const int64_t krow = row_of(c, page[kb], head, t0 + 16 * kb + n), vrow = row_of(c, page[kb], head, t0 + 16 * kb + 4 * g);
-            if constexpr (FMT == VF_E4M3) {
-              const uint8_t *p = reinterpret_cast<const uint8_t *>(c.k) + krow * c.width, *ps = c.ks + krow * c.kb;
-#pragma unroll
-              for (int ks = 0; ks < NK; ks += DP >= 64 ? 2 : 1) {
-                const int d = k_at<T, FMT, DP>(ks, g);
-                uint4 w = make_uint4(0, 0, 0, 0);
-                float s = 1.0f;
-                if (d < c.width) {
-                  if constexpr (DP >= 64) {
-                    w = *reinterpret_cast<const uint4 *>(p + d);
-                  } else {
-                    const uint2 w2 = *reinterpret_cast<const uint2 *>(p + d);
-                    w.x = w2.x; w.y = w2.y;
-                  }
-                  s = scale_of(ps[d >> 5]);
-                }
-                key[kb][ks] = make_uint4(cvt2(w.x, s, false), cvt2(w.x, s, true), cvt2(w.y, s, false), cvt2(w.y, s, true));
-                if constexpr (DP >= 64) key[kb][ks + 1] = make_uint4(cvt2(w.z, s, false), cvt2(w.z, s, true), cvt2(w.w, s, false), cvt2(w.w, s, true));
-              }
-            } else {
-              const uint16_t *p = reinterpret_cast<const uint16_t *>(c.k) + krow * c.width;
-#pragma unroll
-              for (int ks = 0; ks < NK; ++ks) {
-                const int d = k_at<T, FMT, DP>(ks, g);
-                key[kb][ks] = d < c.width ? *reinterpret_cast<const uint4 *>(p + d) : make_uint4(0, 0, 0, 0);
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int h = 0; h < NH; ++h) {
-                const int d = h * 16 * VW + n * VW;
-#pragma unroll
-                for (int x = 0; x < VD; ++x) val[kb][i][h][x] = 0;
-                if (d >= c.width) continue;
-                if constexpr (FMT == VF_E4M3) {
-                  const uint8_t *pv = reinterpret_cast<const uint8_t *>(c.v) + (vrow + i) * c.width + d;
-                  const float s = scale_of(c.vs[(vrow + i) * c.kb + (d >> 5)]);
-                  if constexpr (VW == 8) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(pv);
-                    val[kb][i][h][0] = cvt2(w.x, s, false); val[kb][i][h][1] = cvt2(w.x, s, true);
-                    val[kb][i][h][2] = cvt2(w.y, s, false); val[kb][i][h][3] = cvt2(w.y, s, true);
-                  } else if constexpr (VW == 4) {
-                    const uint32_t w = *reinterpret_cast<const uint32_t *>(pv);
-                    val[kb][i][h][0] = cvt2(w, s, false); val[kb][i][h][1] = cvt2(w, s, true);
-                  } else {
-                    val[kb][i][h][0] = cvt2(*reinterpret_cast<const uint16_t *>(pv), s, false);
-                  }
-                } else {
-                  typedef uint32_t uv __attribute__((ext_vector_type(VD)));
-                  const uint16_t *pv = reinterpret_cast<const uint16_t *>(c.v) + (vrow + i) * c.width + d;
-                  if constexpr (VD == 1) {
-                    val[kb][i][h][0] = *reinterpret_cast<const uint32_t *>(pv);
-                  } else {
-                    const uv w = *reinterpret_cast<const uv *>(pv);
-#pragma unroll
-                    for (int x = 0; x < VD; ++x) val[kb][i][h][x] = w[x];
-                  }
-                }
-              }
-          }
-#pragma unroll
-          for (int ks = 0; ks < NK; ++ks)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-              for (int b = 0; b < RB; ++b)
-                sc[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, key[kb][ks]), __builtin_bit_cast(bf16x8, q16[b][ks]), sc[b][kb],
-                                                                  0, 0, 0);
-        }
-
         bool odd = false;  // whether some value that only some rows see is not finite
         if (edge) {
 #pragma unroll
@@ -333,7 +364,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
               for (int h = 0; h < NH; ++h)
 #pragma unroll
                 for (int x = 0; x < VD; ++x) {
-                  if (!any) val[kb][i][h][x] = 0;
+                  if (!any || h * 16 * VW + n * VW >= width) val[kb][i][h][x] = 0;
                   odd = odd || (F32 ? (val[kb][i][h][x] & 0x7f800000u) == 0x7f800000u : not_finite(val[kb][i][h][x]));
                 }
             }
@@ -442,6 +473,9 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
                 acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w[0], w[1], w[2], w[3]), p[b], acc[b][h * VW + x], 0, 0, 0);
             }
         }
+        if (st + STRIDE < steps) ask_values(st + STRIDE, next);
+        now = next;
+        next = after;
       }
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
@@ -495,7 +529,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         if (shared) {
-          const int64_t at = unit * ROWS + (ALONG ? wave * 16 * RB : 0) + 16 * b + n;
+          const int64_t at = ((int64_t)seq * gridDim.x + blockIdx.x) * ROWS + (ALONG ? wave * 16 * RB : 0) + 16 * b + n;
           float *o = a.part + at * DP;
 #pragma unroll
           for (int h = 0; h < NH; ++h)
@@ -504,9 +538,10 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
 #pragma unroll
               for (int x = 0; x < VW; ++x) o[h * 16 * VW + (4 * g + e) * VW + x] = acc[b][h * VW + x][e];
           if (g == 0) {
-            float *stat = a.part + a.units * ROWS * DP;
+            const int64_t parts = (int64_t)a.s.n * gridDim.x * ROWS;
+            float *stat = a.part + parts * DP;
             stat[at] = m[b];
-            stat[a.units * ROWS + at] = l[b];
+            stat[parts + at] = l[b];
           }
         } else if (out_row[b] >= 0) {
           const float inv = l[b] == 0.0f ? 0.0f : 1.0f / l[b];
@@ -519,7 +554,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
               float v[8];
 #pragma unroll
               for (int x = 0; x < 8; ++x) v[x] = x < VW ? acc[b][h * VW + x % VW][e] * inv : 0.0f;
-              const int left = c.dim - d < VW ? c.dim - d : VW;
+              const int left = dim - d < VW ? dim - d : VW;
               if (left > 0) store_upto8(o + d, left, v);
             }
         }
@@ -566,14 +601,20 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
   // a thread's pieces: of the keys 16 wave .. 16 wave + 15 of a tile, whose page is one
-  int from_k[TURNS], from_v[TURNS];
+  int from_k[TURNS], from_v[TURNS], zero = 0;
 #pragma unroll
   for (int i = 0; i < TURNS; ++i) {
     const int e = i * 64 + lane, t = 16 * wave + e / PIECES, x = e % PIECES, last = (c.width >> 3) - 1;
     const int xk = x ^ key_turn<DP>(t), xv = ((x >> 1 ^ value_turn<DP>(t)) << 1) | (x & 1);
-    // (pieces behind a row's end are the last one again: the queries are zero there, and such columns of the output are not kept)
-    from_k[i] = e / PIECES * c.width + 8 * (xk < last ? xk : last);
-    from_v[i] = e / PIECES * c.width + 8 * (xv < last ? xv : last);
+    // (pieces behind a row's end are zeros: they lie behind what the loads see, or are fetched again and not used)
+    if constexpr (FMT == VF_E4M3) {
+      from_k[i] = e / PIECES * c.width + 8 * (xk < last ? xk : last);
+      from_v[i] = e / PIECES * c.width + 8 * (xv < last ? xv : last);
+      zero |= (xk > last) << i;
+    } else {
+      from_k[i] = xk > last ? 1 << 28 : e / PIECES * c.width + 8 * xk;
+      from_v[i] = xv > last ? 1 << 28 : e / PIECES * c.width + 8 * xv;
+    }
   }
   // places that a lane reads: of keys n (and 32 + n, a constant further), of values 4 g .. 4 g + 3 (and further ones)
   int at_k[NK], at_v[ND];
@@ -585,36 +626,35 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
     at_v[d] = TB + t * RB + 32 * (pair ^ value_turn<DP>(t)) + 8 * (lane & 3);
   }
 
-  for (int64_t unit = blockIdx.x; unit < a.units; unit += gridDim.x) {
-    // unit: heads of the cache fastest, then shares of the keys, then row blocks (those that see the most keys first), then sequences
-    int64_t rest = unit / c.heads;
-    const int head = (int)(unit - rest * c.heads), split = (int)(rest % a.splits);
-    rest /= a.splits;
-    const int seq = (int)(rest / a.blocks), block0 = a.blocks - 1 - (int)(rest - (int64_t)seq * a.blocks);
+  const Place place = place_of(a);
+  const int head = place.head, split = place.split;
+  for (int seq = blockIdx.y; seq < a.s.n; seq += gridDim.y) {
     const Span sp = span_of(a.s, c.shift, seq);
-    const int64_t all = (int64_t)sp.rows * a.group;
-    for (int64_t block = block0; block * ROWS < all; block += a.blocks) {
+    const int all = sp.rows * a.group;
+    // (row blocks that see the most keys come first)
+    for (int block = a.blocks - 1 - place.block; (int64_t)block * ROWS < all; block += a.blocks) {
       // (row blocks that the plan did not count on are not shared)
       const bool shared = a.splits > 1 && block < a.blocks;
       if (block >= a.blocks && split > 0) break;
-      const int64_t w0 = block * ROWS, w1 = w0 + ROWS < all ? w0 + ROWS : all, r0 = w0 + 32 * wave, r1 = r0 + 32 < w1 ? r0 + 32 : w1;
+      const int dim = anew(c.dim);
+      const int w0 = block * ROWS, w1 = all - w0 > ROWS ? w0 + ROWS : all, r0 = w0 + 32 * wave, r1 = w1 - r0 > 32 ? r0 + 32 : w1;
       // what the workgroup's rows, and the wave's, see: all of [.., in), nothing outside
       int lo, hi, lo_in, hi_in, wlo = 0, whi = 0, wlo_in = 0, whi_in = 0;
-      seen_by(a, sp, (int)(w0 / a.group), lo, hi_in);
-      seen_by(a, sp, (int)((w1 - 1) / a.group), lo_in, hi);
+      seen_by(a, sp, over_group(a, w0), lo, hi_in);
+      seen_by(a, sp, over_group(a, w1 - 1), lo_in, hi);
       if (r0 < r1) {
-        seen_by(a, sp, (int)(r0 / a.group), wlo, whi_in);
-        seen_by(a, sp, (int)((r1 - 1) / a.group), wlo_in, whi);
+        seen_by(a, sp, over_group(a, r0), wlo, whi_in);
+        seen_by(a, sp, over_group(a, r1 - 1), wlo_in, whi);
       }
       int row_lo = 0, row_hi = 0;
       const uint16_t *q_row = nullptr;
       int64_t out_row = -1;
-      const int64_t r = r0 + n;
+      const int r = r0 + n;
       if (r < r1) {
-        const int i = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)i * a.group);
+        const int i = over_group(a, r), h = head * a.group + r - i * a.group;
         seen_by(a, sp, i, row_lo, row_hi);
-        q_row = reinterpret_cast<const uint16_t *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * c.dim;
-        out_row = (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
+        q_row = reinterpret_cast<const uint16_t *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * dim;
+        out_row = (sp.first + i) * a.ld_out + (int64_t)h * dim;
       }
       const int from = lo & ~(TK - 1);
       int tiles = hi > from ? (hi - from + TK - 1) / TK : 0, s0 = 0;
@@ -655,6 +695,10 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
           uint8_t *to = lds + (st & 1) * 2 * TB + wave * (16 * RB) + lane * 16;
 #pragma unroll
           for (int i = 0; i < TURNS; ++i) {
+            if (zero >> i & 1) {
+              raw_k[i] = make_uint2(0, 0);
+              sc_k[i] = 127;
+            }
             const float fk = scale_of((uint8_t)sc_k[i]), fv = scale_of((uint8_t)sc_v[i]);
             *reinterpret_cast<uint4 *>(to + i * 1024) = make_uint4(cvt2(raw_k[i].x, fk, false), cvt2(raw_k[i].x, fk, true), cvt2(raw_k[i].y, fk, false), cvt2(raw_k[i].y, fk, true));
             *reinterpret_cast<uint4 *>(to + TB + i * 1024) = make_uint4(cvt2(raw_v[i].x, fv, false), cvt2(raw_v[i].x, fv, true), cvt2(raw_v[i].y, fv, false), cvt2(raw_v[i].y, fv, true));
@@ -670,7 +714,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
       uint4 q16[NK];
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
-        const int d = 16 * ks + 8 * g, left = q_row ? c.dim - d : 0;
+        const int d = 16 * ks + 8 * g, left = q_row ? dim - d : 0;
         raw8<uint16_t> w = {};
         if (left > 0) fetch8(q_row + d, left, w);
         q16[ks] = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
@@ -813,7 +857,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
       l += __shfl_xor(l, 32);
       // numbers 32 d + 8 (i / 4) + 4 g + i % 4 of row n are in acc[d][i]
       if (shared) {
-        const int64_t at = unit * ROWS + 32 * wave + n;
+        const int64_t at = ((int64_t)seq * gridDim.x + blockIdx.x) * ROWS + 32 * wave + n, parts = (int64_t)a.s.n * gridDim.x * ROWS;
         float *o = a.part + at * DP;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
@@ -821,9 +865,9 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
           for (int i = 0; i < 16; i += 4)
             *reinterpret_cast<f32x4 *>(o + 32 * d + 2 * i + 4 * g) = f32x4{acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
         if (g == 0) {
-          float *stat = a.part + a.units * ROWS * DP;
+          float *stat = a.part + parts * DP;
           stat[at] = m;
-          stat[a.units * ROWS + at] = l;
+          stat[parts + at] = l;
         }
       } else if (out_row >= 0) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -832,7 +876,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
         for (int d = 0; d < ND; ++d)
 #pragma unroll
           for (int i = 0; i < 16; i += 4) {
-            const int at = 32 * d + 2 * i + 4 * g, left = c.dim - at;
+            const int at = 32 * d + 2 * i + 4 * g, left = dim - at;
             float v[8] = {};
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = acc[d][i + e] * inv;
@@ -853,17 +897,16 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int rows, bool last_first) {
   const int lane = (int)threadIdx.x & 63;
   const Cache &c = a.c;
-  const int64_t blocks = a.units / a.splits, items = blocks * rows;
+  const int64_t blocks = (int64_t)a.s.n * a.blocks * c.heads, items = blocks * rows, parts = items * a.splits;
   for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
-    const int64_t ub = item / rows;   // (sequence, row block, head of the cache), heads fastest
-    const int row = (int)(item - ub * rows), head = (int)(ub % c.heads);
-    const int64_t sb = ub / c.heads;
-    const int seq = (int)(sb / a.blocks), place = (int)(sb - (int64_t)seq * a.blocks), block = last_first ? a.blocks - 1 - place : place;
+    const int ub = (int)(item / rows);   // (sequence, row block, head of the cache), heads fastest
+    const int row = (int)(item - (int64_t)ub * rows), sb = ub / c.heads, head = ub - sb * c.heads;
+    const int seq = sb / a.blocks, place = sb - seq * a.blocks, block = last_first ? a.blocks - 1 - place : place;
     const Span sp = span_of(a.s, c.shift, seq);
-    const int64_t r = (int64_t)block * rows + row;
-    if (r >= (int64_t)sp.rows * a.group) continue;
-    const float *stat = a.part + a.units * rows * DP;
-    auto at_of = [&](int k) { return ((sb * a.splits + k) * c.heads + head) * rows + row; };
+    const int r = block * rows + row;
+    if (r >= sp.rows * a.group) continue;
+    const float *stat = a.part + parts * DP;
+    auto at_of = [&](int k) { return ((int64_t)(sb * a.splits + k) * c.heads + head) * rows + row; };
     float top = -INFINITY;
     for (int k = lane; k < a.splits; k += 64) top = fmaxf(top, stat[at_of(k)]);
 #pragma unroll
@@ -872,13 +915,13 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int row
     for (int k = 0; k < a.splits; ++k) {
       const int64_t at = at_of(k);
       const float f = weight_of(stat[at], top);
-      l += f * stat[a.units * rows + at];
+      l += f * stat[parts + at];
 #pragma unroll
       for (int x = 0; x < (DP + 63) / 64; ++x)
         if (64 * x + lane < DP) o[x] += f * a.part[at * DP + 64 * x + lane];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int i = (int)(r / a.group), h = head * a.group + (int)(r - (int64_t)i * a.group);
+    const int i = over_group(a, r), h = head * a.group + r - i * a.group;
     T *to = reinterpret_cast<T *>(a.out) + (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
 #pragma unroll
     for (int x = 0; x < (DP + 63) / 64; ++x)
@@ -886,15 +929,21 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int row
   }
 }
 
+// Row blocks that a launch counts on: those of the longest sequence, as long as the grid stays below 2^22 workgroups a sequence.
+int blocks_of(int64_t longest, int rows, int heads) {
+  const int64_t n = (longest + rows - 1) / rows, most = ((1 << 22) + heads - 1) / heads;
+  return (int)(n < 1 ? 1 : n < most ? n : most);
+}
+
 template <typename T, int FMT, int DP>
 int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int STEP = Shape<T, FMT, DP>::STEP;
   const int64_t longest = (int64_t)a.longest * a.group;
-  const int rb = longest <= 16 ? 1 : 2;
-  const bool along = longest > 32;
-  const int rows = 16 * rb * (along ? 4 : 1);
-  a.blocks = (int)((longest + rows - 1) / rows);
-  if (a.blocks < 1) a.blocks = 1;
+  // (bf16 comes here with up to 16 rows only)
+  constexpr int MORE = DP <= 64 ? 2 : 1;
+  const bool along = sizeof(T) == 4 && longest > 16;
+  const int rows = along ? 64 * MORE : 16;
+  a.blocks = blocks_of(longest, rows, a.c.heads);
   // Workgroups share the keys of a row block where there would be fewer than run at a time, as long as every wave keeps some steps.
   const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, steps = (longest_kv + STEP - 1) / STEP, most = steps / (along ? 8 : 16);
   int64_t splits = (512 + units - 1) / units;
@@ -906,11 +955,11 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
     if (!a.part) splits = 1;
   }
   a.splits = (int)splits;
-  a.units = units * splits;
-  const unsigned grid = (unsigned)(a.units < (1 << 20) ? a.units : 1 << 20);
-  if (along) k_attend_rows<T, FMT, DP, 2, true><<<grid, 256, 0, c->stream>>>(a);
-  else if (rb == 2) k_attend_rows<T, FMT, DP, 2, false><<<grid, 256, 0, c->stream>>>(a);
-  else k_attend_rows<T, FMT, DP, 1, false><<<grid, 256, 0, c->stream>>>(a);
+  const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
+  if constexpr (sizeof(T) == 4) {
+    if (along) k_attend_rows<T, FMT, DP, MORE, true><<<grid, 256, 0, c->stream>>>(a);
+  }
+  if (!along) k_attend_rows<T, FMT, DP, 1, false><<<grid, 256, 0, c->stream>>>(a);
   VF_HIP(c, hipGetLastError());
   if (splits > 1) {
     const int64_t items = (units * rows + 3) / 4;
@@ -924,7 +973,7 @@ template <int FMT, int DP>
 int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int ROWS = 128, LDS = 4 * tile_bytes<DP>(), AT_ONCE = DP <= 128 ? 512 : 256;
   const int64_t longest = (int64_t)a.longest * a.group;
-  a.blocks = (int)((longest + ROWS - 1) / ROWS);
+  a.blocks = blocks_of(longest, ROWS, a.c.heads);
   const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, most = (longest_kv + TK - 1) / TK / 4;
   int64_t splits = (AT_ONCE + units - 1) / units;
   if (splits > most) splits = most;
@@ -934,8 +983,7 @@ int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
     if (!a.part) splits = 1;
   }
   a.splits = (int)splits;
-  a.units = units * splits;
-  const unsigned grid = (unsigned)(a.units < (1 << 20) ? a.units : 1 << 20);
+  const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
   VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(&k_attend_tile<FMT, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   k_attend_tile<FMT, DP><<<grid, 256, LDS, c->stream>>>(a);
   VF_HIP(c, hipGetLastError());
@@ -950,7 +998,7 @@ int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
 template <typename T, int FMT>
 int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   if constexpr (sizeof(T) == 2) {
-    if ((int64_t)a.longest * a.group > 32) {
+    if ((int64_t)a.longest * a.group > 16) {
       if (a.c.dim <= 64) return launch_tile<FMT, 64>(c, a, longest_kv);
       if (a.c.dim <= 128) return launch_tile<FMT, 128>(c, a, longest_kv);
       return launch_tile<FMT, 256>(c, a, longest_kv);
@@ -973,7 +1021,7 @@ int vfk_kv_attend(vf_ctx *c, const vf_kv_call &call, int heads, const void *q, i
   a.q = q; a.out = out; a.ld_q = ld_q; a.ld_out = ld_out;
   // (scores that a row does not see are -inf and have to stay it: the smallest number there is does for 0, as it takes every finite score below 1e-6)
   a.scale2 = scale * LOG2E > 0.0f ? scale * LOG2E : 1.4e-45f;
-  a.group = heads / call.kv->kv_heads;
+  set_group(a, heads / call.kv->kv_heads);
   a.causal = causal; a.window = window;
   a.longest = (int)longest_of(call.seqs);
   const int64_t most = (int64_t)call.seqs->max_pages * call.kv->page;
