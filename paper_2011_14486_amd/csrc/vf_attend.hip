@@ -29,22 +29,10 @@ struct AttendArgs {
   float *part;      // of workgroups that share a row block: [unit][rows][DP] sums, then [unit][rows] maxima, then [unit][rows] sums of weights
   int64_t ld_q, ld_out;
   float scale2;     // scale log2(e)
-  int group, causal, window, longest;
+  Divisor group;
+  int causal, window, longest;
   int blocks, splits;  // row blocks of the longest sequence; workgroups that share one along the keys
-  uint32_t magic;      // r / group = r magic >> shift, see over_group
-  int shift;
 };
-
-// r / group for r below 2^31: with 2^(s - 1) < group <= 2^s and magic = 2^(31 + s) / group rounded up, the product is off by less than
-// r group <= 2^(31 + s) at the most, in units of 1 / group below the next quotient.
-__device__ __forceinline__ int over_group(const AttendArgs &a, int r) { return (int)((uint64_t)(uint32_t)r * a.magic >> a.shift); }
-void set_group(AttendArgs &a, int group) {
-  int s = 0;
-  while ((1 << s) < group) ++s;
-  a.group = group;
-  a.shift = 31 + s;
-  a.magic = (uint32_t)((((uint64_t)1 << a.shift) + (uint64_t)group - 1) / (uint64_t)group);
-}
 
 // A workgroup's place: x = head of the cache + heads (share of the keys + splits row block), y: sequence.  (The launch has at most MAX_Y
 // sequences side by side; workgroups go on to further ones.)
@@ -83,7 +71,8 @@ __device__ __forceinline__ float weight_of(float m, float top) { return exp2_(m 
 // ---- few rows: keys and values straight from memory into the operands ----
 //
 // A wave holds 16 RB rows; its operands' other side are 32 keys (16 in fp32) at a time.  The four waves of a workgroup share the
-// rows and take turns at the keys, or have rows of their own (ALONG false, true).
+// rows and take turns at the keys, or have rows of their own, or sequences.
+enum { SHARE, ROWWISE, SEQWISE };
 
 template <typename T, int FMT, int DP> struct Shape;
 // K operand: the lane of key n and quarter g takes elements; V operand: lane c takes VW neighbouring numbers of a value, NH times
@@ -120,11 +109,12 @@ __device__ __forceinline__ int k_at(int ks, int g) {
   else return 32 * ks + 8 * g;
 }
 
-template <typename T, int FMT, int DP, int RB, bool ALONG>
+template <typename T, int FMT, int DP, int RB, int MODE>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const AttendArgs a) {
   typedef Shape<T, FMT, DP> S;
+  constexpr bool ALONG = MODE != SHARE;
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int STEP = S::STEP, VW = S::VW, NH = S::NH, NK = S::NK, ROWS = 16 * RB * (ALONG ? 4 : 1), NA = NH * VW;
+  constexpr int STEP = S::STEP, VW = S::VW, NH = S::NH, NK = S::NK, ROWS = 16 * RB * (MODE == ROWWISE ? 4 : 1), NA = NH * VW;
   constexpr int KB = STEP / 16;  // blocks of 16 keys in a step
   __shared__ f32x4 join[ALONG ? 1 : 2][ALONG ? 1 : RB * NA][64];
   __shared__ float join_m[ALONG ? 1 : 4][16 * RB], join_l[ALONG ? 1 : 4][16 * RB];
@@ -132,20 +122,21 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
   const Cache &c = a.c;
   const Place place = place_of(a);
   const int head = place.head, split = place.split;
-  for (int seq = blockIdx.y; seq < a.s.n; seq += gridDim.y) {
+  constexpr int SEQS = MODE == SEQWISE ? 4 : 1;
+  for (int seq = (int)blockIdx.y * SEQS + (MODE == SEQWISE ? wave : 0); seq < a.s.n; seq += (int)gridDim.y * SEQS) {
     const Span sp = span_of(a.s, c.shift, seq);
-    const int all = sp.rows * a.group;
+    const int all = sp.rows * a.group.by;
     for (int block = place.block; (int64_t)block * ROWS < all; block += a.blocks) {
       // (row blocks that the plan did not count on are not shared)
       const bool shared = a.splits > 1 && block < a.blocks;
       if (block >= a.blocks && split > 0) break;
       const int dim = anew(c.dim), width = anew(c.width);
-      const int r0 = block * ROWS + (ALONG ? wave * 16 * RB : 0), r1 = all - r0 > 16 * RB ? r0 + 16 * RB : all;
+      const int r0 = block * ROWS + (MODE == ROWWISE ? wave * 16 * RB : 0), r1 = all - r0 > 16 * RB ? r0 + 16 * RB : all;
       // what the wave's rows see: all of [lo_in, hi_in), nothing outside [lo, hi)
       int lo = 0, hi = 0, lo_in = 0, hi_in = 0;
       if (r0 < r1) {
-        seen_by(a, sp, over_group(a, r0), lo, hi_in);
-        seen_by(a, sp, over_group(a, r1 - 1), lo_in, hi);
+        seen_by(a, sp, over(a.group, r0), lo, hi_in);
+        seen_by(a, sp, over(a.group, r1 - 1), lo_in, hi);
       }
       int row_lo[RB], row_hi[RB];
       const T *q_row[RB];
@@ -157,7 +148,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
         q_row[b] = nullptr;
         out_row[b] = -1;
         if (r < r1) {
-          const int i = over_group(a, r), h = head * a.group + r - i * a.group;
+          const int i = over(a.group, r), h = head * a.group.by + r - i * a.group.by;
           seen_by(a, sp, i, row_lo[b], row_hi[b]);
           q_row[b] = reinterpret_cast<const T *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * dim;
           out_row[b] = (sp.first + i) * a.ld_out + (int64_t)h * dim;
@@ -529,7 +520,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         if (shared) {
-          const int64_t at = ((int64_t)seq * gridDim.x + blockIdx.x) * ROWS + (ALONG ? wave * 16 * RB : 0) + 16 * b + n;
+          const int64_t at = ((int64_t)seq * gridDim.x + blockIdx.x) * ROWS + (MODE == ROWWISE ? wave * 16 * RB : 0) + 16 * b + n;
           float *o = a.part + at * DP;
 #pragma unroll
           for (int h = 0; h < NH; ++h)
@@ -630,7 +621,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
   const int head = place.head, split = place.split;
   for (int seq = blockIdx.y; seq < a.s.n; seq += gridDim.y) {
     const Span sp = span_of(a.s, c.shift, seq);
-    const int all = sp.rows * a.group;
+    const int all = sp.rows * a.group.by;
     // (row blocks that see the most keys come first)
     for (int block = a.blocks - 1 - place.block; (int64_t)block * ROWS < all; block += a.blocks) {
       // (row blocks that the plan did not count on are not shared)
@@ -640,18 +631,18 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
       const int w0 = block * ROWS, w1 = all - w0 > ROWS ? w0 + ROWS : all, r0 = w0 + 32 * wave, r1 = w1 - r0 > 32 ? r0 + 32 : w1;
       // what the workgroup's rows, and the wave's, see: all of [.., in), nothing outside
       int lo, hi, lo_in, hi_in, wlo = 0, whi = 0, wlo_in = 0, whi_in = 0;
-      seen_by(a, sp, over_group(a, w0), lo, hi_in);
-      seen_by(a, sp, over_group(a, w1 - 1), lo_in, hi);
+      seen_by(a, sp, over(a.group, w0), lo, hi_in);
+      seen_by(a, sp, over(a.group, w1 - 1), lo_in, hi);
       if (r0 < r1) {
-        seen_by(a, sp, over_group(a, r0), wlo, whi_in);
-        seen_by(a, sp, over_group(a, r1 - 1), wlo_in, whi);
+        seen_by(a, sp, over(a.group, r0), wlo, whi_in);
+        seen_by(a, sp, over(a.group, r1 - 1), wlo_in, whi);
       }
       int row_lo = 0, row_hi = 0;
       const uint16_t *q_row = nullptr;
       int64_t out_row = -1;
       const int r = r0 + n;
       if (r < r1) {
-        const int i = over_group(a, r), h = head * a.group + r - i * a.group;
+        const int i = over(a.group, r), h = head * a.group.by + r - i * a.group.by;
         seen_by(a, sp, i, row_lo, row_hi);
         q_row = reinterpret_cast<const uint16_t *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * dim;
         out_row = (sp.first + i) * a.ld_out + (int64_t)h * dim;
@@ -904,7 +895,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int row
     const int seq = sb / a.blocks, place = sb - seq * a.blocks, block = last_first ? a.blocks - 1 - place : place;
     const Span sp = span_of(a.s, c.shift, seq);
     const int r = block * rows + row;
-    if (r >= sp.rows * a.group) continue;
+    if (r >= sp.rows * a.group.by) continue;
     const float *stat = a.part + parts * DP;
     auto at_of = [&](int k) { return ((int64_t)(sb * a.splits + k) * c.heads + head) * rows + row; };
     float top = -INFINITY;
@@ -921,7 +912,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int row
         if (64 * x + lane < DP) o[x] += f * a.part[at * DP + 64 * x + lane];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    const int i = over_group(a, r), h = head * a.group + r - i * a.group;
+    const int i = over(a.group, r), h = head * a.group.by + r - i * a.group.by;
     T *to = reinterpret_cast<T *>(a.out) + (sp.first + i) * a.ld_out + (int64_t)h * c.dim;
 #pragma unroll
     for (int x = 0; x < (DP + 63) / 64; ++x)
@@ -938,9 +929,9 @@ int blocks_of(int64_t longest, int rows, int heads) {
 template <typename T, int FMT, int DP>
 int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int STEP = Shape<T, FMT, DP>::STEP;
-  const int64_t longest = (int64_t)a.longest * a.group;
+  const int64_t longest = (int64_t)a.longest * a.group.by;
   // (bf16 comes here with up to 16 rows only)
-  constexpr int MORE = DP <= 64 ? 2 : 1;
+  constexpr int MORE = 1;
   const bool along = sizeof(T) == 4 && longest > 16;
   const int rows = along ? 64 * MORE : 16;
   a.blocks = blocks_of(longest, rows, a.c.heads);
@@ -957,9 +948,16 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   a.splits = (int)splits;
   const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
   if constexpr (sizeof(T) == 4) {
-    if (along) k_attend_rows<T, FMT, DP, MORE, true><<<grid, 256, 0, c->stream>>>(a);
+    if (along) k_attend_rows<T, FMT, DP, MORE, ROWWISE><<<grid, 256, 0, c->stream>>>(a);
   }
-  if (!along) k_attend_rows<T, FMT, DP, 1, false><<<grid, 256, 0, c->stream>>>(a);
+  if (!along) {
+    if (units >= 2048 && a.s.n >= 4) {
+      const int by_four = (a.s.n + 3) / 4;
+      k_attend_rows<T, FMT, DP, 1, SEQWISE><<<dim3(grid.x, by_four < MAX_Y ? by_four : MAX_Y), 256, 0, c->stream>>>(a);
+    } else {
+      k_attend_rows<T, FMT, DP, 1, SHARE><<<grid, 256, 0, c->stream>>>(a);
+    }
+  }
   VF_HIP(c, hipGetLastError());
   if (splits > 1) {
     const int64_t items = (units * rows + 3) / 4;
@@ -972,7 +970,7 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
 template <int FMT, int DP>
 int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int ROWS = 128, LDS = 4 * tile_bytes<DP>(), AT_ONCE = DP <= 128 ? 512 : 256;
-  const int64_t longest = (int64_t)a.longest * a.group;
+  const int64_t longest = (int64_t)a.longest * a.group.by;
   a.blocks = blocks_of(longest, ROWS, a.c.heads);
   const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, most = (longest_kv + TK - 1) / TK / 4;
   int64_t splits = (AT_ONCE + units - 1) / units;
@@ -998,7 +996,7 @@ int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
 template <typename T, int FMT>
 int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   if constexpr (sizeof(T) == 2) {
-    if ((int64_t)a.longest * a.group > 16) {
+    if ((int64_t)a.longest * a.group.by > 16) {
       if (a.c.dim <= 64) return launch_tile<FMT, 64>(c, a, longest_kv);
       if (a.c.dim <= 128) return launch_tile<FMT, 128>(c, a, longest_kv);
       return launch_tile<FMT, 256>(c, a, longest_kv);
@@ -1021,7 +1019,7 @@ int vfk_kv_attend(vf_ctx *c, const vf_kv_call &call, int heads, const void *q, i
   a.q = q; a.out = out; a.ld_q = ld_q; a.ld_out = ld_out;
   // (scores that a row does not see are -inf and have to stay it: the smallest number there is does for 0, as it takes every finite score below 1e-6)
   a.scale2 = scale * LOG2E > 0.0f ? scale * LOG2E : 1.4e-45f;
-  set_group(a, heads / call.kv->kv_heads);
+  a.group = divisor_of(heads / call.kv->kv_heads);
   a.causal = causal; a.window = window;
   a.longest = (int)longest_of(call.seqs);
   const int64_t most = (int64_t)call.seqs->max_pages * call.kv->page;

@@ -8,7 +8,15 @@ namespace {
 
 using namespace vfkv;
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256, TB = 16;   // TB: most rows of a workgroup at a time
+
+// eight elements of the cache's row, whose places are aligned to eight of them
+__device__ __forceinline__ void fetch_whole(const uint8_t *p, raw8<uint8_t> &r) {
+  const uint2 w = *reinterpret_cast<const uint2 *>(p);
+  r.w[0] = w.x;
+  r.w[1] = w.y;
+}
+template <typename E> __device__ __forceinline__ void fetch_whole(const E *p, raw8<E> &r) { fetch8(p, 8, r); }
 
 struct AppendArgs {
   Cache c;
@@ -21,6 +29,7 @@ struct AppendArgs {
   int heads, half, interleaved;  // heads of q; half: pairs of a head that turn
   int lanes, chunks_q, tb;       // lanes of a head (a power of two), chunks of eight numbers in a head of q; rows of a workgroup
   int blocks;                    // workgroups' worth of rows in the longest sequence
+  Divisor total;                 // heads of a row: of q, keys and values
 };
 
 // cos and sin of a in 64 bits, to about 1e-16 of 1: a minus the nearest multiple n of pi / 2, which is taken off in two parts of 53 bits
@@ -56,18 +65,20 @@ __device__ __forceinline__ void cos_sin(double a, double &c, double &s) {
   if (q4 == 2.0 || q4 == 3.0) s = -s;
 }
 
-// A thread takes eight neighbouring numbers of a head at a time, and the eight that they are paired with.  The rows'
-// cosines and sines are worked out once, for all heads, into the LDS.
+// A thread takes eight neighbouring numbers of a head at a time, and the eight that they are paired with, of several heads at once, so that
+// their loads are on their way together.  The rows' cosines and sines are worked out once, for all heads, into the LDS.
 template <typename T, int FMT>
 __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
   extern __shared__ float2 turn[];  // [tb][half]
-  __shared__ int pages[64];         // of the rows; -1: nowhere
-  const int total = a.heads + 2 * a.c.heads, lane = (int)threadIdx.x & (a.lanes - 1);
+  __shared__ int pages[TB];         // of the rows; -1: nowhere
+  constexpr int U = sizeof(T) == 2 ? 4 : 2;
+  const int lane = (int)threadIdx.x & (a.lanes - 1), D = a.c.dim, d0 = 8 * lane, n = D - d0, step = THREADS / a.lanes;
+  const bool whole = (a.half & 7) == 0, first = d0 < a.half, turns = d0 < 2 * a.half;
   const int64_t units = (int64_t)a.s.n * a.blocks;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int seq = (int)(unit / a.blocks);
+    const int seq = a.blocks > 1 ? (int)(unit / a.blocks) : (int)unit;
     const Span sp = span_of(a.s, a.c.shift, seq);
-    for (int64_t i0 = unit % a.blocks * a.tb; i0 < sp.rows; i0 += (int64_t)a.blocks * a.tb) {
+    for (int64_t i0 = (unit - (int64_t)seq * a.blocks) * a.tb; i0 < sp.rows; i0 += (int64_t)a.blocks * a.tb) {
       const int rows = sp.rows - i0 < a.tb ? (int)(sp.rows - i0) : a.tb, pos0 = sp.length - sp.rows + (int)i0;
       __syncthreads();
       for (int i = threadIdx.x; i < rows * a.half; i += THREADS) {
@@ -81,70 +92,77 @@ __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
         pages[threadIdx.x] = (unsigned)e < (unsigned)a.c.pages ? e : -1;
       }
       __syncthreads();
-      const int slots = rows * total;
+      const int slots = rows * a.total.by;
       // (a head's lanes are in one wave, so that all of them have read it before any of them writes: q_out may be q)
-      for (int slot0 = 0; slot0 < slots; slot0 += THREADS / a.lanes) {
-        const int slot = slot0 + (int)threadIdx.x / a.lanes;
-        const bool on = slot < slots;
-        const int row = on ? slot / total : 0, h = slot - row * total;
-        const bool is_q = h < a.heads, is_k = !is_q && h < a.heads + a.c.heads;
-        const int head = is_q ? h : is_k ? h - a.heads : h - a.heads - a.c.heads, D = a.c.dim;
-        const T *src = is_q ? reinterpret_cast<const T *>(a.q) + (sp.first + i0 + row) * a.ld_q
-                            : is_k ? reinterpret_cast<const T *>(a.k) + (sp.first + i0 + row) * a.ld_k
-                                   : reinterpret_cast<const T *>(a.v) + (sp.first + i0 + row) * a.ld_v;
-        src += (int64_t)head * D;
-        const int d0 = 8 * lane, n = on ? D - d0 : 0;
-        float v[8];
+      for (int slot0 = 0; slot0 < slots; slot0 += U * step) {
+        raw8<T> own[U], other[U];
+        int row[U], head[U];   // head: of q, then of keys, then of values
+        const T *src[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        if (n > 0) load_upto8(src + d0, n, v);
-        if (n > 0 && (is_q || is_k) && d0 < 2 * a.half) {
-          const float2 *cs = turn + row * a.half;
-          if (a.interleaved) {
+        for (int u = 0; u < U; ++u) {
+          const int slot = slot0 + u * step + (int)threadIdx.x / a.lanes;
+          row[u] = slot < slots ? over(a.total, slot) : -1;
+          head[u] = slot - row[u] * a.total.by;
+          if (row[u] < 0) head[u] = a.total.by;
+          const int64_t r = sp.first + i0 + row[u];
+          const int hk = head[u] - a.heads, hv = hk - a.c.heads;
+          src[u] = hk < 0 ? reinterpret_cast<const T *>(a.q) + r * a.ld_q + (int64_t)head[u] * D
+                          : hv < 0 ? reinterpret_cast<const T *>(a.k) + r * a.ld_k + (int64_t)hk * D : reinterpret_cast<const T *>(a.v) + r * a.ld_v + (int64_t)hv * D;
+          own[u] = {};
+          if (row[u] >= 0 && n > 0) fetch8(src[u] + d0, n, own[u]);
+          if (row[u] >= 0 && hv < 0 && turns && whole && !a.interleaved) fetch8(src[u] + (first ? d0 + a.half : d0 - a.half), 8, other[u]);
+        }
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              if (d0 + i < 2 * a.half) {
-                const float2 w = cs[(d0 + i) >> 1];
-                const float x = v[i], y = v[i + 1];
-                v[i] = x * w.x - y * w.y;
-                v[i + 1] = y * w.x + x * w.y;
+        for (int u = 0; u < U; ++u) {
+          const int hk = head[u] - a.heads, hv = hk - a.c.heads;
+          float v[8];
+          unpack8(own[u], v);
+          if (row[u] >= 0 && hv < 0 && turns) {
+            const float2 *cs = turn + row[u] * a.half;
+            if (a.interleaved) {
+#pragma unroll
+              for (int i = 0; i < 8; i += 2) {
+                if (d0 + i < 2 * a.half) {
+                  const float2 w = cs[(d0 + i) >> 1];
+                  const float x = v[i], y = v[i + 1];
+                  v[i] = x * w.x - y * w.y;
+                  v[i + 1] = y * w.x + x * w.y;
+                }
               }
-            }
-          } else if ((a.half & 7) == 0) {
-            float o[8];
-            const bool first = d0 < a.half;
-            load8(src + (first ? d0 + a.half : d0 - a.half), o);
-            cs += first ? d0 : d0 - a.half;
+            } else if (whole) {
+              float o[8];
+              unpack8(other[u], o);
+              cs += first ? d0 : d0 - a.half;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = first ? v[i] * cs[i].x - o[i] * cs[i].y : v[i] * cs[i].x + o[i] * cs[i].y;
-          } else {
+              for (int i = 0; i < 8; ++i) v[i] = first ? v[i] * cs[i].x - o[i] * cs[i].y : v[i] * cs[i].x + o[i] * cs[i].y;
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int d = d0 + i;
-              if (d < 2 * a.half) {
-                const bool first = d < a.half;
-                const float o = load1(src + (first ? d + a.half : d - a.half));
-                const float2 w = cs[first ? d : d - a.half];
-                v[i] = first ? v[i] * w.x - o * w.y : v[i] * w.x + o * w.y;
+              for (int i = 0; i < 8; ++i) {
+                const int d = d0 + i;
+                if (d < 2 * a.half) {
+                  const bool low = d < a.half;
+                  const float o = load1(src[u] + (low ? d + a.half : d - a.half));
+                  const float2 w = cs[low ? d : d - a.half];
+                  v[i] = low ? v[i] * w.x - o * w.y : v[i] * w.x + o * w.y;
+                }
               }
             }
           }
-        }
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_wave_barrier();
-        if (is_q) {
-          if (n > 0) store_upto8(reinterpret_cast<T *>(a.q_out) + (sp.first + i0 + row) * a.ld_q_out + (int64_t)head * D + d0, n, v);
-          // (what follows holds exchanges between the lanes of a head, all of which take the same way)
-          continue;
-        }
-        const int page = on ? pages[row] : -1;
-        const bool there = page >= 0 && d0 < a.c.width;
-        const int64_t at = row_of(a.c, page < 0 ? 0 : page, head, pos0 + row);
-        if constexpr (FMT == VF_E4M3) {
-          uint8_t *codes = reinterpret_cast<uint8_t *>(is_k ? a.c.k : a.c.v) + at * a.c.width, *sc = (is_k ? a.c.ks : a.c.vs) + at * a.c.kb;
-          quantize_chunk<VF_E4M3>(v, lane, there, codes, sc);
-        } else {
-          if (there) store8(reinterpret_cast<T *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0, v);
+          asm volatile("" ::: "memory");
+          __builtin_amdgcn_wave_barrier();
+          if (hk < 0) {
+            if (n > 0) store_upto8(reinterpret_cast<T *>(a.q_out) + (sp.first + i0 + row[u]) * a.ld_q_out + (int64_t)head[u] * D + d0, n, v);
+          } else {
+            // (exchanges between the lanes of a head, all of which come here)
+            const int page = row[u] >= 0 ? pages[row[u]] : -1;
+            const bool there = page >= 0 && d0 < a.c.width;
+            const int64_t at = row_of(a.c, page < 0 ? 0 : page, hv < 0 ? hk : hv, pos0 + row[u]);
+            if constexpr (FMT == VF_E4M3) {
+              quantize_chunk<VF_E4M3>(v, lane, there, reinterpret_cast<uint8_t *>(hv < 0 ? a.c.k : a.c.v) + at * a.c.width, (hv < 0 ? a.c.ks : a.c.vs) + at * a.c.kb);
+            } else {
+              if (there) store8(reinterpret_cast<T *>(hv < 0 ? a.c.k : a.c.v) + at * a.c.width + d0, v);
+            }
+          }
         }
       }
     }
@@ -157,42 +175,69 @@ struct ReadArgs {
   void *k, *v;
   int64_t ld_k, ld_v;
   int lanes, tb, blocks;
+  Divisor total;  // heads of a row that are read
 };
 
 template <typename T, int FMT>
 __global__ void __launch_bounds__(THREADS) k_kv_read(const ReadArgs a) {
-  const int total = a.c.heads * ((a.k != nullptr) + (a.v != nullptr)), lane = (int)threadIdx.x & (a.lanes - 1);
+  __shared__ int entries[TB];  // of the rows' pages
+  constexpr int U = 4;
+  typedef typename kv_elem<FMT>::type E;
+  const int lane = (int)threadIdx.x & (a.lanes - 1), d0 = 8 * lane, n = a.c.dim - d0, step = THREADS / a.lanes;
   const int64_t units = (int64_t)a.s.n * a.blocks;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int seq = (int)(unit / a.blocks);
+    const int seq = a.blocks > 1 ? (int)(unit / a.blocks) : (int)unit;
     const Span sp = span_of(a.s, a.c.shift, seq);
-    for (int64_t i0 = unit % a.blocks * a.tb; i0 < sp.rows; i0 += (int64_t)a.blocks * a.tb) {
-      const int rows = sp.rows - i0 < a.tb ? (int)(sp.rows - i0) : a.tb, pos0 = sp.length - sp.rows + (int)i0, slots = rows * total;
-      for (int slot = (int)threadIdx.x / a.lanes; slot < slots; slot += THREADS / a.lanes) {
-        const int row = slot / total, h = slot - row * total, pos = pos0 + row;
-        const bool is_k = a.k && h < a.c.heads;
-        const int head = a.k && !is_k ? h - a.c.heads : h, d0 = 8 * lane, n = a.c.dim - d0;
-        if (n <= 0) continue;
-        const int e = pos >= 0 ? entry_of(a.s, a.c.shift, seq, pos) : -1;
-        float v[8];
+    for (int64_t i0 = (unit - (int64_t)seq * a.blocks) * a.tb; i0 < sp.rows; i0 += (int64_t)a.blocks * a.tb) {
+      const int rows = sp.rows - i0 < a.tb ? (int)(sp.rows - i0) : a.tb, pos0 = sp.length - sp.rows + (int)i0, slots = rows * a.total.by;
+      __syncthreads();
+      if ((int)threadIdx.x < rows) {
+        const int pos = pos0 + (int)threadIdx.x;
+        entries[threadIdx.x] = pos >= 0 ? entry_of(a.s, a.c.shift, seq, pos) : -1;
+      }
+      __syncthreads();
+      if (n <= 0) continue;
+      for (int slot0 = (int)threadIdx.x / a.lanes; slot0 < slots; slot0 += U * step) {
+        raw8<E> raw[U];
+        uint32_t scale[U];
+        int row[U], head[U], entry[U];  // head: of keys, then of values
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = e == -1 ? 0.0f : __builtin_nanf("");
-        if ((unsigned)e < (unsigned)a.c.pages) {
-          const int64_t at = row_of(a.c, e, head, pos);
-          if constexpr (FMT == VF_E4M3) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0);
-            // (a scale's byte is the exponent field of 2^(byte - 127); the conversion takes 0 as 2^-127 and 255 as NaN)
-            const float sc = __uint_as_float((uint32_t)(is_k ? a.c.ks : a.c.vs)[at * a.c.kb + (d0 >> 5)] << 23);
-            const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, sc, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.x, sc, true);
-            const f32x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, sc, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w.y, sc, true);
-            v[0] = p0[0]; v[1] = p0[1]; v[2] = p1[0]; v[3] = p1[1];
-            v[4] = p2[0]; v[5] = p2[1]; v[6] = p3[0]; v[7] = p3[1];
-          } else {
-            load8(reinterpret_cast<const typename kv_elem<FMT>::type *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0, v);
+        for (int u = 0; u < U; ++u) {
+          const int slot = slot0 + u * step;
+          row[u] = slot < slots ? over(a.total, slot) : -1;
+          head[u] = slot - row[u] * a.total.by + (a.k ? 0 : a.c.heads);
+          entry[u] = row[u] >= 0 ? entries[row[u]] : -1;
+          if ((unsigned)entry[u] < (unsigned)a.c.pages) {
+            const bool is_k = head[u] < a.c.heads;
+            const int64_t at = row_of(a.c, entry[u], is_k ? head[u] : head[u] - a.c.heads, pos0 + row[u]);
+            fetch_whole(reinterpret_cast<const E *>(is_k ? a.c.k : a.c.v) + at * a.c.width + d0, raw[u]);
+            if (FMT == VF_E4M3) scale[u] = (is_k ? a.c.ks : a.c.vs)[at * a.c.kb + (d0 >> 5)];
           }
         }
-        T *to = reinterpret_cast<T *>(is_k ? a.k : a.v) + (sp.first + i0 + row) * (is_k ? a.ld_k : a.ld_v) + (int64_t)head * a.c.dim + d0;
-        store_upto8(to, n, v);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (row[u] < 0) continue;
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = entry[u] == -1 ? 0.0f : __builtin_nanf("");
+          if ((unsigned)entry[u] < (unsigned)a.c.pages) {
+            if constexpr (FMT == VF_E4M3) {
+              // (a scale's byte is the exponent field of 2^(byte - 127); the conversion takes 0 as 2^-127 and 255 as NaN)
+              const float sc = __uint_as_float(scale[u] << 23);
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(raw[u].w[x], sc, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(raw[u].w[x], sc, true);
+                v[4 * x] = lo[0]; v[4 * x + 1] = lo[1]; v[4 * x + 2] = hi[0]; v[4 * x + 3] = hi[1];
+              }
+            } else {
+              unpack8(raw[u], v);
+            }
+          }
+          const bool is_k = head[u] < a.c.heads;
+          T *to = reinterpret_cast<T *>(is_k ? a.k : a.v) + (sp.first + i0 + row[u]) * (is_k ? a.ld_k : a.ld_v) +
+                  (int64_t)(is_k ? head[u] : head[u] - a.c.heads) * a.c.dim + d0;
+          store_upto8(to, n, v);
+        }
       }
     }
   }
@@ -204,8 +249,8 @@ int lanes_of(int width) {
   while (8 * n < width) n *= 2;
   return n;
 }
-// Rows of a workgroup: eight where sequences are that long; the grid stays below what may be launched.
-int rows_at_once(int64_t longest) { return longest < 8 ? (longest < 1 ? 1 : (int)longest) : 8; }
+// Rows of a workgroup where sequences are that long; the grid stays below what may be launched.
+int rows_at_once(int64_t longest, int most) { return longest < most ? (longest < 1 ? 1 : (int)longest) : most; }
 unsigned grid_of(int64_t units) { return (unsigned)(units < (1 << 20) ? units : 1 << 20); }
 
 }  // namespace
@@ -225,7 +270,8 @@ int vfk_kv_append(vf_ctx *c, const vf_kv_call &call, const vf_rope *rope, const 
   a.heads = q ? heads : 0;
   a.lanes = lanes_of(a.c.width);
   const int64_t longest = longest_of(call.seqs);
-  a.tb = rows_at_once(longest);
+  a.tb = rows_at_once(longest, 8);
+  a.total = divisor_of(a.heads + 2 * a.c.heads);
   a.blocks = (int)((longest + a.tb - 1) / a.tb);
   if (a.blocks < 1) a.blocks = 1;
   const unsigned grid = grid_of((int64_t)a.s.n * a.blocks), lds = (unsigned)(a.tb * a.half * sizeof(float2));
@@ -256,7 +302,8 @@ int vfk_kv_read(vf_ctx *c, const vf_kv_call &call, void *k, int64_t ld_k, void *
   a.k = k; a.v = v; a.ld_k = ld_k; a.ld_v = ld_v;
   a.lanes = lanes_of(a.c.width);
   const int64_t longest = longest_of(call.seqs);
-  a.tb = rows_at_once(longest);
+  a.tb = rows_at_once(longest, TB);
+  a.total = divisor_of(a.c.heads * ((k != nullptr) + (v != nullptr)));
   a.blocks = (int)((longest + a.tb - 1) / a.tb);
   if (a.blocks < 1) a.blocks = 1;
   const unsigned grid = grid_of((int64_t)a.s.n * a.blocks);

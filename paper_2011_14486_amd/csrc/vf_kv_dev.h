@@ -43,6 +43,23 @@ inline Seqs seqs_of(const vf_kv_seqs *s) {
   q.each = s->n_seq > 0 && !s->offsets_dev ? (int)(s->tokens / s->n_seq) : 0;
   return q;
 }
+// r / by for r below 2^31: with 2^(s - 1) < by <= 2^s and magic = 2^(31 + s) / by rounded up, the product is off by less than
+// r by <= 2^(31 + s) at the most, in units of 1 / by below the next quotient.
+struct Divisor {
+  uint32_t magic;
+  int shift, by;
+};
+inline Divisor divisor_of(int by) {
+  int s = 0;
+  while (((int64_t)1 << s) < by) ++s;
+  Divisor d;
+  d.by = by;
+  d.shift = 31 + s;
+  d.magic = (uint32_t)((((uint64_t)1 << d.shift) + (uint64_t)by - 1) / (uint64_t)by);
+  return d;
+}
+__device__ __forceinline__ int over(const Divisor &d, int r) { return (int)((uint64_t)(uint32_t)r * d.magic >> d.shift); }
+
 // The most rows of a sequence, as the caller says where lengths differ.
 inline int64_t longest_of(const vf_kv_seqs *s) {
   if (!s->offsets_dev) return s->n_seq > 0 ? s->tokens / s->n_seq : 0;
