@@ -582,9 +582,9 @@ __device__ __forceinline__ void to_lds16(const i32x4 &part, uint32_t lane_at, ui
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 template <int FMT, int DP>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const AttendArgs a) {
+__global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_attend_tile(const AttendArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
-  __shared__ int odd_any;
+  __shared__ int odd_any[2];   // by tiles in turn: whether a value that only some rows see is not finite
   constexpr int TB = tile_bytes<DP>(), RB = DP * 2, ROWS = 128, NK = DP / 16, ND = DP / 32;
   constexpr int PIECES = DP / 8, TURNS = TK * PIECES / 256;  // pieces of 16 bytes in a row; of a tile, for every thread
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -657,7 +657,26 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
       // The wave's share of a tile on its way: straight to the LDS, or 8-bit codes and scales in registers.
       uint2 raw_k[FMT == VF_E4M3 ? TURNS : 1], raw_v[FMT == VF_E4M3 ? TURNS : 1];
       uint32_t sc_k[FMT == VF_E4M3 ? TURNS : 1], sc_v[FMT == VF_E4M3 ? TURNS : 1];
-      auto entry_at = [&](int st) { return st < tiles ? __builtin_amdgcn_readfirstlane(entry_of(a.s, c.shift, seq, from + st * TK + 16 * wave)) : -1; };
+      // Pages of a tile's blocks of 16 keys, asked for two tiles ahead: the wave's own block's, and bits of those that are there, and of
+      // entries that are no page and not -1.
+      constexpr int ALL = (1 << (TK / 16)) - 1;
+      int asked[TK / 16];
+      auto ask_pages = [&](int st) {
+#pragma unroll
+        for (int x = 0; x < TK / 16; ++x) asked[x] = st < tiles ? entry_of(a.s, c.shift, seq, from + st * TK + 16 * x) : -1;
+      };
+      struct Bits { int own, there, wrong; };
+      auto bits_of = [&]() {
+        Bits b = {-1, 0, 0};
+#pragma unroll
+        for (int x = 0; x < TK / 16; ++x) {
+          const int e = __builtin_amdgcn_readfirstlane(asked[x]);
+          b.there |= ((unsigned)e < (unsigned)c.pages) << x;
+          b.wrong |= ((unsigned)e >= (unsigned)c.pages && e != -1) << x;
+          b.own = x == wave ? e : b.own;
+        }
+        return b;
+      };
       auto fetch = [&](int st, int entry) {
         const int page = (unsigned)entry < (unsigned)c.pages ? entry : 0;  // (what is fetched there is not used)
         const int64_t row = row_of(c, page, head, from + st * TK + 16 * wave);
@@ -696,10 +715,12 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
           }
         }
       };
+      ask_pages(s0);
+      Bits now = bits_of();
       __syncthreads();  // (the row block before is done with the LDS)
-      int entry_next = entry_at(s0);
-      if (s0 < tiles) fetch(s0, entry_next);
-      entry_next = entry_at(s0 + 1);
+      if (tid < 2) odd_any[tid] = 0;
+      if (s0 < tiles) fetch(s0, now.own);
+      ask_pages(s0 + 1);
 
       // queries as operands
       uint4 q16[NK];
@@ -722,23 +743,17 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
         if constexpr (FMT == VF_E4M3) put(st);
         else wait_loads<0>();
         __syncthreads();  // the tile is there, and nobody reads the one before any more
-        if (st + 1 < tiles) fetch(st + 1, entry_next);
-        entry_next = entry_at(st + 2);
-        uint8_t *tile = lds + (st & 1) * 2 * TB;
-        // pages of the tile's blocks of 16 keys: bits of those that are there, and of entries that are no page and not -1
-        int there = 0, wrong = 0;
-#pragma unroll
-        for (int x = 0; x < TK / 16; ++x) {
-          const int e = entry_of(a.s, c.shift, seq, t0 + 16 * x);
-          there |= ((unsigned)e < (unsigned)c.pages) << x;
-          wrong |= ((unsigned)e >= (unsigned)c.pages && e != -1) << x;
+        const int there = now.there, wrong = now.wrong;
+        if (st + 1 < tiles) {
+          now = bits_of();
+          fetch(st + 1, now.own);
+          ask_pages(st + 2);
         }
-        constexpr int ALL = (1 << (TK / 16)) - 1;
+        uint8_t *tile = lds + (st & 1) * 2 * TB;
+        if (tid == 0) odd_any[~st & 1] = 0;
         if (t0 < lo_in || t0 + TK > hi_in || there != ALL) {
           // Values that no row sees become zeros.  Of others that are not finite the rows that see them get NaN; then they are zeros too, so that
           // they reach no other row.
-          if (tid == 0) odd_any = 0;
-          __syncthreads();
           bool bad = false;
 #pragma unroll 1
           for (int e = tid; e < TK * PIECES; e += 256) {
@@ -747,9 +762,9 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_tile(const At
             if (t < lo || t >= hi || !(there >> (e / PIECES / 16) & 1)) *at = make_uint4(0, 0, 0, 0);
             else bad = bad || not_finite(at->x) || not_finite(at->y) || not_finite(at->z) || not_finite(at->w);
           }
-          if (bad) odd_any = 1;
+          if (bad) odd_any[st & 1] = 1;
           __syncthreads();
-          if (odd_any) {
+          if (odd_any[st & 1]) {
 #pragma unroll 1
             for (int t = 0; t < TK; ++t) {
               if (t0 + t < row_lo || t0 + t >= row_hi) continue;
