@@ -568,6 +568,12 @@ constexpr int TK = 64;  // keys of a tile
 template <int DP> constexpr int tile_bytes() { return TK * DP * 2; }   // of keys, or of values
 template <int DP> __device__ __forceinline__ int key_turn(int t) { return DP == 64 ? (t >> 1) & 7 : t & 15; }
 template <int DP> __device__ __forceinline__ int value_turn(int t) { return DP == 64 ? (t >> 1) & 3 : t & 7; }
+// place of a row's pair of pieces, before it is turned, and the other way round: of 32 lanes that read four rows' neighbouring pairs at a time, the second 16
+// are half of the banks away from the first
+template <int DP> __device__ __forceinline__ int place_of_pair(int x) {
+  return DP == 64 ? (x >> 1 & 1) | (x & 1) << 1 : (x & 8) | (x >> 1 & 3) | (x & 1) << 2;
+}
+template <int DP> __device__ __forceinline__ int pair_at(int x) { return DP == 64 ? (x >> 1 & 1) | (x & 1) << 1 : (x & 8) | (x & 3) << 1 | (x >> 2 & 1); }
 
 // A part of memory as the instructions with a range check see it: what lies behind its end reads as zeros.
 __device__ __forceinline__ i32x4 part_of(const void *at, int bytes) {
@@ -596,7 +602,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
 #pragma unroll
   for (int i = 0; i < TURNS; ++i) {
     const int e = i * 64 + lane, t = 16 * wave + e / PIECES, x = e % PIECES, last = (c.width >> 3) - 1;
-    const int xk = x ^ key_turn<DP>(t), xv = ((x >> 1 ^ value_turn<DP>(t)) << 1) | (x & 1);
+    const int xk = x ^ key_turn<DP>(t), xv = pair_at<DP>(x >> 1 ^ value_turn<DP>(t)) << 1 | (x & 1);
     // (pieces behind a row's end are zeros: they lie behind what the loads see, or are fetched again and not used)
     if constexpr (FMT == VF_E4M3) {
       from_k[i] = e / PIECES * c.width + 8 * (xk < last ? xk : last);
@@ -614,7 +620,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
 #pragma unroll
   for (int d = 0; d < ND; ++d) {
     const int t = 4 * g + ((lane & 15) >> 2), pair = 2 * d + ((lane >> 4) & 1);
-    at_v[d] = TB + t * RB + 32 * (pair ^ value_turn<DP>(t)) + 8 * (lane & 3);
+    at_v[d] = TB + t * RB + 32 * (place_of_pair<DP>(pair) ^ value_turn<DP>(t)) + 8 * (lane & 3);
   }
 
   const Place place = place_of(a);
@@ -773,7 +779,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                   const int piece = 4 * d + (i >> 2);
-                  const uint2 w = *reinterpret_cast<const uint2 *>(tile + TB + t * RB + 32 * ((piece >> 1) ^ value_turn<DP>(t)) + 16 * (piece & 1) + 8 * g);
+                  const uint2 w = *reinterpret_cast<const uint2 *>(tile + TB + t * RB + 32 * (place_of_pair<DP>(piece >> 1) ^ value_turn<DP>(t)) + 16 * (piece & 1) + 8 * g);
                   if ((w.x & 0x7f80u) == 0x7f80u) acc[d][i] = __builtin_nanf("");
                   if ((w.x & 0x7f800000u) == 0x7f800000u) acc[d][i + 1] = __builtin_nanf("");
                   if ((w.y & 0x7f80u) == 0x7f80u) acc[d][i + 2] = __builtin_nanf("");
