@@ -32,6 +32,7 @@ struct AttendArgs {
   Divisor group;
   int causal, window, longest;
   int blocks, splits;  // row blocks of the longest sequence; workgroups that share one along the keys
+  bool by_work;        // sequences with most work first
 };
 
 // A workgroup's place: x = head of the cache + heads (share of the keys + splits row block), y: sequence.  (The launch has at most MAX_Y
@@ -587,6 +588,22 @@ __device__ __forceinline__ void to_lds16(const i32x4 &part, uint32_t lane_at, ui
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
+// The sequence that comes k-th if those with most work come first, of at most 64: every lane takes one of them and counts those before it.
+__device__ __forceinline__ int kth_by_work(const AttendArgs &a, int k) {
+  const int lane = (int)threadIdx.x & 63;
+  float w = -1.0f;
+  if (lane < a.s.n) {
+    const Span sp = span_of(a.s, a.c.shift, lane);
+    w = (float)sp.rows * (float)sp.length;
+  }
+  int before = 0;
+  for (int j = 0; j < a.s.n; ++j) {
+    const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), j));
+    before += o > w || (o == w && j < lane);
+  }
+  return __ffsll((unsigned long long)__ballot(lane < a.s.n && before == k)) - 1;
+}
+
 template <int FMT, int DP>
 __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_attend_tile(const AttendArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -625,7 +642,8 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
 
   const Place place = place_of(a);
   const int head = place.head, split = place.split;
-  for (int seq = blockIdx.y; seq < a.s.n; seq += gridDim.y) {
+  for (int y = blockIdx.y; y < a.s.n; y += gridDim.y) {
+    const int seq = a.by_work ? kth_by_work(a, y) : y;
     const Span sp = span_of(a.s, c.shift, seq);
     const int all = sp.rows * a.group.by;
     // (row blocks that see the most keys come first)
@@ -1002,6 +1020,8 @@ int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
     if (!a.part) splits = 1;
   }
   a.splits = (int)splits;
+  // (where workgroups come in several rounds, long ones that come last would be waited for; with many sequences they are a small part)
+  a.by_work = a.s.n > 1 && a.s.n <= 64 && units * splits > AT_ONCE;
   const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
   VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(&k_attend_tile<FMT, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   k_attend_tile<FMT, DP><<<grid, 256, LDS, c->stream>>>(a);
