@@ -32,7 +32,7 @@ struct AttendArgs {
   Divisor group;
   int causal, window, longest;
   int blocks, splits;  // row blocks of the longest sequence; workgroups that share one along the keys
-  bool by_work;        // sequences with most work first
+  bool by_length;        // sequences with most keys first
 };
 
 // A workgroup's place: x = head of the cache + heads (share of the keys + splits row block), y: sequence.  (The launch has at most MAX_Y
@@ -588,13 +588,14 @@ __device__ __forceinline__ void to_lds16(const i32x4 &part, uint32_t lane_at, ui
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// The sequence that comes k-th if those with most work come first, of at most 64: every lane takes one of them and counts those before it.
-__device__ __forceinline__ int kth_by_work(const AttendArgs &a, int k) {
+// The sequence that comes k-th if those with most keys come first, which make the longest workgroups, of at most 64: every lane takes one of them
+// and counts those before it.
+__device__ __forceinline__ int kth_by_length(const AttendArgs &a, int k) {
   const int lane = (int)threadIdx.x & 63;
   float w = -1.0f;
   if (lane < a.s.n) {
     const Span sp = span_of(a.s, a.c.shift, lane);
-    w = (float)sp.rows * (float)sp.length;
+    w = sp.rows > 0 ? (float)sp.length : 0.0f;
   }
   int before = 0;
   for (int j = 0; j < a.s.n; ++j) {
@@ -643,7 +644,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
   const Place place = place_of(a);
   const int head = place.head, split = place.split;
   for (int y = blockIdx.y; y < a.s.n; y += gridDim.y) {
-    const int seq = a.by_work ? kth_by_work(a, y) : y;
+    const int seq = a.by_length ? kth_by_length(a, y) : y;
     const Span sp = span_of(a.s, c.shift, seq);
     const int all = sp.rows * a.group.by;
     // (row blocks that see the most keys come first)
@@ -1021,7 +1022,7 @@ int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   }
   a.splits = (int)splits;
   // (where workgroups come in several rounds, long ones that come last would be waited for; with many sequences they are a small part)
-  a.by_work = a.s.n > 1 && a.s.n <= 64 && units * splits > AT_ONCE;
+  a.by_length = a.s.n > 1 && a.s.n <= 64 && units * splits > AT_ONCE;
   const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
   VF_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void *>(&k_attend_tile<FMT, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
   k_attend_tile<FMT, DP><<<grid, 256, LDS, c->stream>>>(a);
