@@ -317,6 +317,37 @@ def ssm_weights(F, width, blocks, heads, head_dim=64, groups=1, n_state=64, taps
                 w_head=f32(rng.standard_normal((1, width)) / np.sqrt(width)), b_head=f32(rng.standard_normal(1)))
 
 
+def rotary_frequencies(rotary, theta=10000.0, factor=1.0, original=0, slow=1.0, fast=32.0):
+    """Angles a position, float64 [rotary / 2], of the pairs of a head's first `rotary` numbers: theta^(-2 j / rotary).
+
+    A factor stretches them over a context that is so many times longer.  Without `original` all are divided by it.  With it, the number
+    of positions of the context before, pairs that turn less than `slow` times over these are divided, those that
+    turn more than `fast` times are as they were, and what lies between is mixed in proportion."""
+    f = theta ** (-np.arange(0, rotary, 2, dtype=np.float64) / max(rotary, 1))
+    keep = np.clip((f * original / (2 * np.pi) - slow) / (fast - slow), 0.0, 1.0) if original else 0.0
+    return f * keep + f / factor * (1.0 - keep)
+
+
+def attention_weights(F, width, blocks, heads, kv_heads=None, head_dim=64, hidden=0, rotary=None, seed=0):
+    """Attention value network: a dict of its sizes and, as fp32 arrays, w_in [width][F]; per block gain [width], w_qkv
+    [(heads + 2 kv_heads) head_dim][width] (rows: queries, keys, values), w_out [width][heads head_dim] and, with `hidden` units, gain_up
+    [width], w_up [hidden][width], w_down [width][hidden]; gain [width], w_head [1][width], b_head [1]; freq float64 [rotary / 2]."""
+    rng = np.random.default_rng([seed, F, width, blocks, heads])
+    kv_heads = heads if kv_heads is None else kv_heads
+    f32 = lambda v: np.asarray(v, np.float32)   # noqa: E731
+    matrix = lambda n, k: f32(rng.standard_normal((n, k)) / np.sqrt(k))   # noqa: E731
+    gain = lambda: f32(1 + 0.2 * rng.standard_normal(width))   # noqa: E731
+    made = []
+    for _ in range(blocks):
+        b = dict(gain=gain(), w_qkv=matrix((heads + 2 * kv_heads) * head_dim, width), w_out=matrix(width, heads * head_dim))
+        if hidden:
+            b.update(gain_up=gain(), w_up=matrix(hidden, width), w_down=matrix(width, hidden))
+        made.append(b)
+    return dict(heads=heads, kv_heads=kv_heads, head_dim=head_dim, hidden=hidden, blocks=made, w_in=matrix(width, F), gain=gain(),
+                w_head=matrix(1, width), b_head=f32(rng.standard_normal(1)),
+                freq=rotary_frequencies(head_dim // 2 * 2 if rotary is None else rotary))
+
+
 # ----------------------------------------------------------------------------
 # raw inputs for the scoring-only workloads
 # ----------------------------------------------------------------------------

@@ -27,6 +27,21 @@ class SsmState(NamedTuple):
     total: Any
 
 
+def sums_of_ranges(torch, each, offsets):
+    """Sums of the sequences' predictions; ranges as the operators take them: one that does not lie in the tokens is empty."""
+    tokens = each.shape[0]
+    begin, end = offsets[:-1], offsets[1:]
+    if tokens == 0 or begin.shape[0] == 0:
+        return each.new_zeros(begin.shape[0])
+    there = (begin >= 0) & (end >= begin) & (end <= tokens)
+    # in the order of their begins, so that begins and ends ascend (segment_reduce looks at nothing); every second segment lies
+    # between two ranges
+    begin, order = torch.where(there, begin, tokens).sort(stable=True)
+    ranges = torch.stack((begin, torch.where(there, end, tokens)[order]), 1).reshape(-1).cummax(0).values
+    sums = torch.segment_reduce(each, "sum", offsets=ranges, unsafe=True, initial=0)
+    return torch.empty_like(sums[::2]).index_copy_(0, order, sums[::2])
+
+
 class SsmValue:
     """The network on a context's GPU; `weights` as inputs.ssm_weights makes them."""
 
@@ -79,18 +94,7 @@ class SsmValue:
         return self._totals(value, state, slots, state_out, slots_out)
 
     def _sums(self, each, offsets):
-        """Sums of the sequences' predictions; ranges as the scan takes them: one that does not lie in the tokens is empty."""
-        torch, tokens = self.torch, each.shape[0]
-        begin, end = offsets[:-1], offsets[1:]
-        if tokens == 0 or begin.shape[0] == 0:
-            return each.new_zeros(begin.shape[0])
-        there = (begin >= 0) & (end >= begin) & (end <= tokens)
-        # in the order of their begins, so that begins and ends ascend (segment_reduce looks at nothing); every second segment lies
-        # between two ranges
-        begin, order = torch.where(there, begin, tokens).sort(stable=True)
-        ranges = torch.stack((begin, torch.where(there, end, tokens)[order]), 1).reshape(-1).cummax(0).values
-        sums = torch.segment_reduce(each, "sum", offsets=ranges, unsafe=True, initial=0)
-        return torch.empty_like(sums[::2]).index_copy_(0, order, sums[::2])
+        return sums_of_ranges(self.torch, each, offsets)
 
     def extend(self, x, state, slots=None, state_out=None, slots_out=None):
         """Values [rows] with one more stage x bf16 [rows][F]: row r continues slot slots[r] of `state` (-1: the empty prefix) and
