@@ -32,7 +32,9 @@ struct AttendArgs {
   Divisor group;
   int causal, window, longest;
   int blocks, splits;  // row blocks of the longest sequence; workgroups that share one along the keys
-  bool by_length;        // sequences with most keys first
+  bool by_length;      // sequences with most keys first
+  const int2 *order;     // GROUP: sequences and their lengths, by first pages,
+  const int32_t *items;  // and where groups that go together begin
 };
 
 // A workgroup's place: x = head of the cache + heads (share of the keys + splits row block), y: sequence.  (The launch has at most MAX_Y
@@ -73,7 +75,11 @@ __device__ __forceinline__ float weight_of(float m, float top) { return exp2_(m 
 //
 // A wave holds 16 RB rows; its operands' other side are 32 keys (16 in fp32) at a time.  The four waves of a workgroup share the
 // rows and take turns at the keys, or have rows of their own, or sequences.
-enum { SHARE, ROWWISE, SEQWISE };
+//
+// Rows of a search that go on from the same prefix have the same pages in front.  GROUP takes single tokens of up to 16 / group sequences that begin
+// with the same page as the rows of one product: keys and values of blocks whose pages are the same are fetched once for all of them, others for one sequence at a
+// time, with the other sequences' rows not seeing them.
+enum { SHARE, ROWWISE, SEQWISE, GROUP };
 
 template <typename T, int FMT, int DP> struct Shape;
 // K operand: the lane of key n and quarter g takes elements; V operand: lane c takes VW neighbouring numbers of a value, NH times
@@ -111,9 +117,9 @@ __device__ __forceinline__ int k_at(int ks, int g) {
 }
 
 template <typename T, int FMT, int DP, int RB, int MODE>
-__global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const AttendArgs a) {
+__global__ void __launch_bounds__(256, MODE == GROUP && DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_attend_rows(const AttendArgs a) {
   typedef Shape<T, FMT, DP> S;
-  constexpr bool ALONG = MODE != SHARE;
+  constexpr bool ALONG = MODE == ROWWISE || MODE == SEQWISE, G = MODE == GROUP;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int STEP = S::STEP, VW = S::VW, NH = S::NH, NK = S::NK, ROWS = 16 * RB * (MODE == ROWWISE ? 4 : 1), NA = NH * VW;
   constexpr int KB = STEP / 16;  // blocks of 16 keys in a step
@@ -124,9 +130,13 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
   const Place place = place_of(a);
   const int head = place.head, split = place.split;
   constexpr int SEQS = MODE == SEQWISE ? 4 : 1;
-  for (int seq = (int)blockIdx.y * SEQS + (MODE == SEQWISE ? wave : 0); seq < a.s.n; seq += (int)gridDim.y * SEQS) {
-    const Span sp = span_of(a.s, c.shift, seq);
-    const int all = sp.rows * a.group.by;
+  for (int turn = (int)blockIdx.y * SEQS + (MODE == SEQWISE ? wave : 0); turn < a.s.n; turn += (int)gridDim.y * SEQS) {
+    // (a group: its first place in the order, its sequences)
+    const int begin = G ? a.items[turn] : 0, members = G ? a.items[turn + 1] - begin : 1;
+    if (members == 0) break;
+    const int seq = G ? 0 : turn;
+    const Span sp = G ? Span{0, 1, 0} : span_of(a.s, c.shift, seq);
+    const int all = G ? members * a.group.by : sp.rows * a.group.by;
     for (int block = place.block; (int64_t)block * ROWS < all; block += a.blocks) {
       // (row blocks that the plan did not count on are not shared)
       const bool shared = a.splits > 1 && block < a.blocks;
@@ -135,25 +145,57 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
       const int r0 = block * ROWS + (MODE == ROWWISE ? wave * 16 * RB : 0), r1 = all - r0 > 16 * RB ? r0 + 16 * RB : all;
       // what the wave's rows see: all of [lo_in, hi_in), nothing outside [lo, hi)
       int lo = 0, hi = 0, lo_in = 0, hi_in = 0;
-      if (r0 < r1) {
+      if (!G && r0 < r1) {
         seen_by(a, sp, over(a.group, r0), lo, hi_in);
         seen_by(a, sp, over(a.group, r1 - 1), lo_in, hi);
       }
-      int row_lo[RB], row_hi[RB];
+      int row_lo[RB], row_hi[RB], row_seq[RB];
       const T *q_row[RB];
       int64_t out_row[RB];
+      const int member = G ? over(a.group, n) : 0;   // of a group: the lane's row's sequence
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         const int r = r0 + 16 * b + n;
         row_lo[b] = row_hi[b] = 0;
+        row_seq[b] = seq;
         q_row[b] = nullptr;
         out_row[b] = -1;
         if (r < r1) {
-          const int i = over(a.group, r), h = head * a.group.by + r - i * a.group.by;
-          seen_by(a, sp, i, row_lo[b], row_hi[b]);
-          q_row[b] = reinterpret_cast<const T *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * dim;
-          out_row[b] = (sp.first + i) * a.ld_out + (int64_t)h * dim;
+          const int x = over(a.group, r), h = head * a.group.by + r - x * a.group.by;
+          Span own = sp;
+          if constexpr (G) {   // (a row a sequence, without offsets)
+            const int2 of = a.order[begin + x];
+            row_seq[b] = of.x;
+            own = Span{of.x, 1, of.y};
+          }
+          const int i = G ? 0 : x;
+          seen_by(a, own, i, row_lo[b], row_hi[b]);
+          q_row[b] = reinterpret_cast<const T *>(a.q) + (own.first + i) * a.ld_q + (int64_t)h * dim;
+          out_row[b] = (own.first + i) * a.ld_out + (int64_t)h * dim;
         }
+      }
+      if constexpr (G) {
+        lo = lo_in = row_lo[0];
+        hi = hi_in = row_hi[0];
+        if (n >= r1) {   // (no row: it bounds nothing)
+          lo = hi_in = 0x7fffffff;
+          hi = lo_in = 0;
+        }
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1) {
+          int o = __shfl_xor(lo, x);
+          lo = o < lo ? o : lo;
+          o = __shfl_xor(hi_in, x);
+          hi_in = o < hi_in ? o : hi_in;
+          o = __shfl_xor(hi, x);
+          hi = o > hi ? o : hi;
+          o = __shfl_xor(lo_in, x);
+          lo_in = o > lo_in ? o : lo_in;
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        lo_in = __builtin_amdgcn_readfirstlane(lo_in);
+        hi_in = __builtin_amdgcn_readfirstlane(hi_in);
       }
       // queries as operands
       uint4 q16[F32 ? 1 : RB][F32 ? 1 : NK];
@@ -198,16 +240,67 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
       kv4 kraw[KB][KL];
       uint32_t vraw[KB][4][NH][FMT == VF_E4M3 ? (VW + 3) / 4 : VD];
       uint8_t kscale[KB][FMT == VF_E4M3 ? KL : 1], vscale[KB][4][FMT == VF_E4M3 ? NH : 1];
-      struct Pages { int entry[KB]; };
+      // what a turn of the loop takes: a step's blocks of 16 keys in these pages, for all rows (who -1) or for those of one member of a group, which sees
+      // [lo, hi)
+      struct Pages { int st, who, lo, hi, entry[KB]; };
       auto pages_at = [&](int st) {
         Pages p;
+        p.st = st;
+        p.who = -1;
+        p.lo = lo;
+        p.hi = hi;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) p.entry[kb] = st < steps ? entry_of(a.s, c.shift, seq, from + st * STEP + 16 * kb) : -1;
         return p;
       };
+      // a group's: lane x asks for block x % KB of member x / KB
+      const int asker = lane / KB, asked_block = lane % KB;
+      int ask_seq = 0, ask_lo = 0, ask_hi = 0;
+      if (G && asker < members) {
+        const int2 of = a.order[begin + asker];
+        ask_seq = of.x;
+        seen_by(a, Span{of.x, 1, of.y}, 0, ask_lo, ask_hi);
+      }
+      auto entries_at = [&](int st) {
+        const int t = from + st * STEP + 16 * asked_block;
+        return asker < members && st < steps && t < ask_hi ? entry_of(a.s, c.shift, ask_seq, t) : -1;
+      };
+      // the pages of step st from member `who` on; who = members if none is left
+      auto pages_of_group = [&](int st, int entries, int who) {
+        Pages p;
+        p.st = st;
+        p.who = -1;
+        p.lo = lo;
+        p.hi = hi;
+        const int t = from + st * STEP + 16 * asked_block;
+        const bool on = asker < members && t < ask_hi && t + 16 > ask_lo;
+        bool same = true;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const unsigned long long those = __ballot(on && asked_block == kb);
+          p.entry[kb] = those ? __builtin_amdgcn_readlane(entries, (int)__ffsll(those) - 1) : -1;
+          same = same && !__ballot(on && asked_block == kb && entries != p.entry[kb]);
+        }
+        if (same) {
+          if (who > 0) p.who = members;
+          return p;
+        }
+        const unsigned long long those = __ballot(on && asker >= who);
+        p.who = those ? ((int)__ffsll(those) - 1) / KB : members;
+        if (!those) return p;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const bool sees = __ballot(on) >> (p.who * KB + kb) & 1;
+          p.entry[kb] = sees ? __builtin_amdgcn_readlane(entries, p.who * KB + kb) : -1;
+        }
+        p.lo = __builtin_amdgcn_readlane(ask_lo, p.who * KB);
+        p.hi = __builtin_amdgcn_readlane(ask_hi, p.who * KB);
+        return p;
+      };
       // (what is fetched of an entry that is no page, and behind a row's end, is not used)
       auto page_of = [&](const Pages &p, int kb) { return (unsigned)p.entry[kb] < (unsigned)c.pages ? p.entry[kb] : 0; };
-      auto ask_keys = [&](int st, const Pages &p) {
+      auto ask_keys = [&](const Pages &p) {
+        const int st = p.st;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           const int64_t row = row_of(c, page_of(p, kb), head, from + st * STEP + 16 * kb + n);
@@ -221,7 +314,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
           }
         }
       };
-      auto ask_values = [&](int st, const Pages &p) {
+      auto ask_values = [&](const Pages &p) {
+        const int st = p.st;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           const int64_t row = row_of(c, page_of(p, kb), head, from + st * STEP + 16 * kb + 4 * g);
@@ -256,17 +350,37 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
         }
       };
       const int first = s0 + (ALONG ? 0 : wave);
-      Pages now = pages_at(first), next = pages_at(first + STRIDE);
-      if (first < steps) {
-        ask_keys(first, now);
-        ask_values(first, now);
+      Pages now, next;
+      int entries = 0, entries_after = 0;   // of a group: of now's step, and of the one behind it
+      if constexpr (G) {
+        entries = entries_at(first);
+        now = pages_of_group(first, entries, 0);
+        entries_after = entries_at(first + STRIDE);
+      } else {
+        now = pages_at(first);
+        next = pages_at(first + STRIDE);
       }
-      for (int st = first; st < steps; st += STRIDE) {
-        const int t0 = from + st * STEP;
+      if (first < steps) {
+        ask_keys(now);
+        ask_values(now);
+      }
+      while (now.st < steps) {
+        const int t0 = from + now.st * STEP, who = now.who;
+        Pages after = now;
+        if constexpr (G) {
+          next = now;
+          next.who = members;
+          if (who >= 0) next = pages_of_group(now.st, entries, who + 1);
+          if (next.who == members) {
+            entries = entries_after;
+            next = pages_of_group(now.st + STRIDE, entries, 0);
+            entries_after = entries_at(now.st + 2 * STRIDE);
+          }
+        }
         bool fine = true;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) fine = fine && (unsigned)now.entry[kb] < (unsigned)c.pages;
-        const bool edge = !fine || t0 < lo_in || t0 + STEP > hi_in;
+        const bool edge = !fine || t0 < lo_in || t0 + STEP > hi_in || (G && who >= 0);
         const int(&entry)[KB] = now.entry;
         f32x4 sc[RB][KB];
 #pragma unroll
@@ -310,8 +424,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
                 sc[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, q16[b][x]), sc[b][kb], 0, 0, 0);
             }
           }
-        if (st + STRIDE < steps) ask_keys(st + STRIDE, next);
-        const Pages after = pages_at(st + 2 * STRIDE);
+        if (next.st < steps) ask_keys(next);
+        if constexpr (!G) after = pages_at(now.st + 2 * STRIDE);
         // values as numbers: of key 4 g + i of each block of 16 the VW numbers at c VW of each part
         uint32_t val[KB][4][NH][VD];
 #pragma unroll
@@ -348,10 +462,10 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
               const bool there = (unsigned)entry[kb] < (unsigned)c.pages;
 #pragma unroll
               for (int b = 0; b < RB; ++b) {
-                const bool seen = t >= row_lo[b] && t < row_hi[b] && entry[kb] != -1;
+                const bool seen = t >= row_lo[b] && t < row_hi[b] && entry[kb] != -1 && (!G || who < 0 || member == who);
                 sc[b][kb][i] = !seen ? -INFINITY : there ? sc[b][kb][i] : __builtin_nanf("");
               }
-              const bool any = t >= lo && t < hi && there;
+              const bool any = t >= now.lo && t < now.hi && there;
 #pragma unroll
               for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -402,7 +516,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
         // ones in their places with ones in the places of what is seen, whatever is not zero makes NaN
         auto seen_mark = [&](int b, int kb, int i) {
           const int t = t0 + 16 * kb + 4 * g + i;
-          return t >= row_lo[b] && t < row_hi[b] && entry[kb] != -1;
+          return t >= row_lo[b] && t < row_hi[b] && entry[kb] != -1 && (!G || who < 0 || member == who);
         };
         const bool odd_step = edge && __any(odd);
         if constexpr (F32) {
@@ -465,9 +579,9 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
                 acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w[0], w[1], w[2], w[3]), p[b], acc[b][h * VW + x], 0, 0, 0);
             }
         }
-        if (st + STRIDE < steps) ask_values(st + STRIDE, next);
+        if (next.st < steps) ask_values(next);
         now = next;
-        next = after;
+        if constexpr (!G) next = after;
       }
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
@@ -521,7 +635,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) k_attend_rows(const At
 #pragma unroll
       for (int b = 0; b < RB; ++b) {
         if (shared) {
-          const int64_t at = ((int64_t)seq * gridDim.x + blockIdx.x) * ROWS + (MODE == ROWWISE ? wave * 16 * RB : 0) + 16 * b + n;
+          const int64_t at = ((int64_t)row_seq[b] * gridDim.x + blockIdx.x) * ROWS + (G ? n - member * a.group.by : (MODE == ROWWISE ? wave * 16 * RB : 0) + 16 * b + n);
+          if (G && n >= r1) continue;
           float *o = a.part + at * DP;
 #pragma unroll
           for (int h = 0; h < NH; ++h)
@@ -923,6 +1038,107 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
   }
 }
 
+// Sorts sequences by their first page and cuts them into groups of up to `most` that have the same: order[n] = (sequence, its length), items[n + 1] = first
+// places of the groups (behind the last one n).  A sequence without keys is a group of its own.  One workgroup, a bitonic network of 64-bit keys (page,
+// sequence), key 1024 r + t in register r of thread t: neighbours up to 32 apart are exchanged between lanes, up to 512 through the LDS.
+// MI355X: 1024 sequences 9 us.
+constexpr int MAX_GROUPED = 4096;
+template <int PER>
+__global__ void __launch_bounds__(1024) k_attend_group(const AttendArgs a, int2 *order, int32_t *items, int most) {
+  __shared__ uint64_t key[1024 * PER];
+  __shared__ int total[16];
+  const int n = a.s.n, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint64_t mine[PER];
+#pragma unroll
+  for (int r = 0; r < PER; ++r) {
+    const int i = 1024 * r + tid;
+    mine[r] = ~0ull;
+    if (i < n) {
+      const Span sp = span_of(a.s, a.c.shift, i);
+      const int e = sp.length > 0 ? entry_of(a.s, a.c.shift, i, 0) : -1;
+      mine[r] = (uint64_t)((unsigned)e < (unsigned)a.c.pages ? (uint32_t)e : 0x80000000u + (uint32_t)i) << 32 | (uint32_t)i;
+    }
+  }
+  // exchanges key i with key i + d, or i - d: the one with bit d clear keeps the smaller where the run of `width` that both are in ascends
+  auto keep = [&](uint64_t &v, uint64_t o, int i, int d, int width) {
+    const bool smaller = ((i & d) == 0) == ((i & width) == 0);
+    if ((o < v) == smaller) v = o;
+  };
+#pragma unroll
+  for (int width = 2; width <= 1024 * PER; width *= 2) {
+#pragma unroll
+    for (int d = 1024 * PER / 2; d > 0; d /= 2) {
+      if (d >= width) continue;
+      if (d >= 1024) {
+#pragma unroll
+        for (int r = 0; r < PER; ++r)
+          if ((r & (d / 1024)) == 0) {
+            const uint64_t u = mine[r], v = mine[r | (d / 1024)];
+            keep(mine[r], v, 1024 * r + tid, d, width);
+            keep(mine[r | (d / 1024)], u, 1024 * (r | (d / 1024)) + tid, d, width);
+          }
+      } else if (d >= 64) {
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < PER; ++r) key[1024 * r + tid] = mine[r];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < PER; ++r) keep(mine[r], key[1024 * r + (tid ^ d)], 1024 * r + tid, d, width);
+      } else {
+#pragma unroll
+        for (int r = 0; r < PER; ++r) {
+          const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)mine[r], d), hi = (uint32_t)__shfl_xor((int)(uint32_t)(mine[r] >> 32), d);
+          keep(mine[r], (uint64_t)hi << 32 | lo, 1024 * r + tid, d, width);
+        }
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < PER; ++r) key[1024 * r + tid] = mine[r];
+  __syncthreads();
+  // places in order, 1024 at a time: where its run of equal pages begins is the largest beginning up to a place, and a group begins every
+  // `most` places of a run
+  int run_before = 0, items_before = 0;
+#pragma unroll
+  for (int r = 0; r < PER; ++r) {
+    const int i = 1024 * r + tid;
+    int run = i == 0 || (uint32_t)(mine[r] >> 32) != (uint32_t)(key[i > 0 ? i - 1 : 0] >> 32) ? i : -1;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const int o = __shfl_up(run, x);
+      run = lane >= x && o > run ? o : run;
+    }
+    if (lane == 63) total[wave] = run;
+    __syncthreads();
+    for (int w = 0; w < 16; ++w) {
+      const int o = total[w];
+      if (w < wave) run = o > run ? o : run;
+    }
+    run = run_before > run ? run_before : run;
+    __syncthreads();
+    const bool begins = i < n && (i - run) % most == 0;
+    const unsigned long long those = __ballot(begins);
+    if (lane == 63) total[wave] = __popcll(those);
+    if (tid == 1023) key[0] = (uint64_t)run;   // (its first place has been looked at)
+    __syncthreads();
+    int at = items_before + __popcll(those & ((1ull << lane) - 1));
+    for (int w = 0; w < 16; ++w) {
+      const int o = total[w];
+      at += w < wave ? o : 0;
+      items_before += o;
+    }
+    run_before = (int)key[0];
+    if (begins) items[at] = i;
+    if (i < n) {
+      const int s = (int)(uint32_t)mine[r];
+      order[i] = make_int2(s, span_of(a.s, a.c.shift, s).length);
+    }
+    __syncthreads();
+  }
+  for (int i = items_before + tid; i <= n; i += 1024) items[i] = n;
+}
+
 // Joins the parts of row blocks that several workgroups have shared: a wave a row.
 template <typename T, int DP>
 __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a, int rows, bool last_first) {
@@ -966,6 +1182,9 @@ int blocks_of(int64_t longest, int rows, int heads) {
   return (int)(n < 1 ? 1 : n < most ? n : most);
 }
 
+// (about 70 us at the memory's rate; below, the 10 us that finding the groups takes are more than what sharing saves)
+constexpr int64_t GROUP_BYTES = 384 << 20;
+
 template <typename T, int FMT, int DP>
 int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int STEP = Shape<T, FMT, DP>::STEP;
@@ -981,16 +1200,35 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   if (splits > most) splits = most;
   if (splits > 512) splits = 512;
   if (splits < 1) splits = 1;
-  if (splits > 1) {
-    a.part = reinterpret_cast<float *>(vfk_ops_scratch(c, (size_t)(units * splits * rows) * (DP + 2) * sizeof(float)));
-    if (!a.part) splits = 1;
+  // Single tokens whose keys and values take the memory longer than it takes to find out which sequences share pages
+  const int most_members = 16 / a.group.by;
+  const int64_t bytes = (int64_t)a.s.n * longest_kv * a.c.heads * a.c.width * 2 * (int64_t)sizeof(typename kv_elem<FMT>::type);
+  bool grouped = !a.s.offsets && a.s.each == 1 && most_members > 1 && a.s.n >= 16 && a.s.n <= MAX_GROUPED && bytes >= GROUP_BYTES;
+  const size_t part_bytes = splits > 1 ? (size_t)(units * splits * rows) * (DP + 2) * sizeof(float) : 0;
+  const size_t group_bytes = grouped ? (size_t)a.s.n * sizeof(int2) + ((size_t)a.s.n + 1) * sizeof(int32_t) : 0;
+  if (part_bytes + group_bytes > 0) {
+    uint8_t *scratch = reinterpret_cast<uint8_t *>(vfk_ops_scratch(c, part_bytes + group_bytes));
+    if (!scratch) {
+      splits = 1;
+      grouped = false;
+    }
+    a.part = reinterpret_cast<float *>(scratch);
+    a.order = reinterpret_cast<int2 *>(scratch + part_bytes);
+    a.items = reinterpret_cast<const int32_t *>(a.order + a.s.n);
   }
   a.splits = (int)splits;
   const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
   if constexpr (sizeof(T) == 4) {
     if (along) k_attend_rows<T, FMT, DP, MORE, ROWWISE><<<grid, 256, 0, c->stream>>>(a);
   }
-  if (!along) {
+  if (grouped) {
+    int2 *order = const_cast<int2 *>(a.order);
+    int32_t *items = const_cast<int32_t *>(a.items);
+    if (a.s.n <= 1024) k_attend_group<1><<<1, 1024, 0, c->stream>>>(a, order, items, most_members);
+    else k_attend_group<4><<<1, 1024, 0, c->stream>>>(a, order, items, most_members);
+    VF_HIP(c, hipGetLastError());
+    k_attend_rows<T, FMT, DP, 1, GROUP><<<grid, 256, 0, c->stream>>>(a);
+  } else if (!along) {
     if (units >= 2048 && a.s.n >= 4) {
       const int by_four = (a.s.n + 3) / 4;
       k_attend_rows<T, FMT, DP, 1, SEQWISE><<<dim3(grid.x, by_four < MAX_Y ? by_four : MAX_Y), 256, 0, c->stream>>>(a);
