@@ -699,21 +699,35 @@ class Rope:
 
 
 def _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest):
-    """Checks what the calls share; returns the record."""
-    torch = ctx.torch
-    if cache.device != ctx.device:
+    """Checks what the calls share; returns the record.  (Calls of single tokens are as long as this takes: one look at each thing.)"""
+    i32, dev = ctx.torch.int32, ctx.device
+    if cache.device != dev:
         _fail("the cache is on another GPU")
     if table.dim() != 2:
         _fail(f"table: [n_seq][max_pages] is wanted, got {tuple(table.shape)}")
     n, wide = table.shape
-    ld = _rows_of(ctx, table, n, wide, torch.int32, "table")
-    at = _vector(ctx, lengths, n, "lengths", torch.int32)
-    off = _vector(ctx, offsets, n + 1, "offsets", torch.int32)
-    if offsets is None and (tokens % n != 0 if n else tokens != 0):
-        _fail(f"{tokens} rows cannot be dealt to {n} sequences; offsets are wanted")
-    if longest is None:
-        longest = tokens if offsets is not None or n == 0 else tokens // n
-    return _KvSeqs(n, wide, tokens, longest, ld, off, at, table.data_ptr())
+    ld, step = table.stride()
+    if table.dtype is not i32 or table.device != dev or (step != 1 and wide > 1 and n > 0):
+        _fail(f"table: int32 rows on {dev} whose last dimension is dense are wanted, got {table.dtype} on {table.device}, strides {(ld, step)}")
+    if n <= 1 and ld < wide:
+        ld = wide
+    if lengths.dtype is not i32 or lengths.numel() != n or not lengths.is_contiguous() or lengths.device != dev:
+        _fail(f"lengths: {n} dense values of int32 on {dev} are wanted")
+    if offsets is None:
+        each = tokens // n if n else 0
+        if each * n != tokens:
+            _fail(f"{tokens} rows cannot be dealt to {n} sequences; offsets are wanted")
+        return _KvSeqs(n, wide, tokens, each if longest is None else longest, ld, None, lengths.data_ptr(), table.data_ptr())
+    return _KvSeqs(n, wide, tokens, tokens if longest is None else longest, ld, _vector(ctx, offsets, n + 1, "offsets", i32), lengths.data_ptr(),
+                   table.data_ptr())
+
+
+def _like(ctx, out, t, ld_t, rows, cols, dtype):
+    """The caller's matrix or a new one of t's sizes and type, and the distance of its rows."""
+    if out is None:
+        torch = ctx.torch
+        return torch.empty_like(t, memory_format=torch.contiguous_format), cols
+    return out, ld_t if out is t else _rows_of(ctx, out, rows, cols, dtype, "out")
 
 
 def _heads_of(cache, t, name):
@@ -739,8 +753,9 @@ def vf_kv_append(ctx, cache, k, v, table, lengths, q=None, rope=None, offsets=No
     heads = ld_q = ld_o = 0
     if q is not None:
         heads = _heads_of(cache, q, "q")
-        ld_q = _rows_of(ctx, q, tokens, heads * cache.head_dim, dtype, "q")
-        q_out, ld_o = _out(ctx, q_out, tokens, heads * cache.head_dim, dtype)
+        wide = heads * cache.head_dim
+        ld_q = _rows_of(ctx, q, tokens, wide, dtype, "q")
+        q_out, ld_o = _like(ctx, q_out, q, ld_q, tokens, wide, dtype)
     elif q_out is not None:
         _fail("q_out without q")
     if rope is not None and rope.device != ctx.device:
@@ -757,7 +772,8 @@ def vf_kv_read(ctx, cache, table, lengths, tokens, offsets=None, longest=None, o
     seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
     dtype, wide = _dtype_of(ctx.torch, out_type), cache.kv_heads * cache.head_dim
     if out is None:
-        out, ld = (ctx.empty((tokens, wide), dtype), ctx.empty((tokens, wide), dtype)), (wide, wide)
+        k = ctx.empty((tokens, wide), dtype)
+        out, ld = (k, ctx.torch.empty_like(k)), (wide, wide)
     else:
         ld = tuple(0 if t is None else _rows_of(ctx, t, tokens, wide, dtype, "out") for t in out)
     k, v = out
@@ -775,8 +791,9 @@ def vf_kv_attend(ctx, cache, q, table, lengths, causal=True, window=0, scale=Non
     torch = ctx.torch
     kind, tokens, heads = _type_of(torch, q), q.shape[0], _heads_of(cache, q, "q")
     seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
-    ld_q = _rows_of(ctx, q, tokens, heads * cache.head_dim, q.dtype, "q")
-    out, ld_o = _out(ctx, out, tokens, heads * cache.head_dim, q.dtype)
+    wide, dtype = heads * cache.head_dim, q.dtype
+    ld_q = _rows_of(ctx, q, tokens, wide, dtype, "q")
+    out, ld_o = _like(ctx, out, q, ld_q, tokens, wide, dtype)
     if longest_kv is None:
         longest_kv = seqs.max_pages * cache.page
     _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, _addr(q), ld_q, 1 if causal else 0, window,

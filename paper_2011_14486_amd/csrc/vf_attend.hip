@@ -79,7 +79,7 @@ __device__ __forceinline__ float weight_of(float m, float top) { return exp2_(m 
 // Rows of a search that go on from the same prefix have the same pages in front.  GROUP takes single tokens of up to 16 / group sequences that begin
 // with the same page as the rows of one product: keys and values of blocks whose pages are the same are fetched once for all of them, others for one sequence at a
 // time, with the other sequences' rows not seeing them.
-enum { SHARE, ROWWISE, SEQWISE, GROUP };
+enum { SHARE, ROWWISE, SEQWISE, GROUP, SHARE8 };   // SHARE8: eight waves, where there are few workgroups
 
 template <typename T, int FMT, int DP> struct Shape;
 // K operand: the lane of key n and quarter g takes elements; V operand: lane c takes VW neighbouring numbers of a value, NH times
@@ -117,14 +117,15 @@ __device__ __forceinline__ int k_at(int ks, int g) {
 }
 
 template <typename T, int FMT, int DP, int RB, int MODE>
-__global__ void __launch_bounds__(256, MODE == GROUP && DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_attend_rows(const AttendArgs a) {
+__global__ void __launch_bounds__(MODE == SHARE8 ? 512 : 256, MODE == GROUP && DP <= 64 ? 3 : DP <= 128 ? 2 : MODE == SHARE8 ? 2 : 1) k_attend_rows(const AttendArgs a) {
   typedef Shape<T, FMT, DP> S;
   constexpr bool ALONG = MODE == ROWWISE || MODE == SEQWISE, G = MODE == GROUP;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int STEP = S::STEP, VW = S::VW, NH = S::NH, NK = S::NK, ROWS = 16 * RB * (MODE == ROWWISE ? 4 : 1), NA = NH * VW;
   constexpr int KB = STEP / 16;  // blocks of 16 keys in a step
-  __shared__ f32x4 join[ALONG ? 1 : 2][ALONG ? 1 : RB * NA][64];
-  __shared__ float join_m[ALONG ? 1 : 4][16 * RB], join_l[ALONG ? 1 : 4][16 * RB];
+  constexpr int WAVES = MODE == SHARE8 ? 8 : 4;
+  __shared__ f32x4 join[ALONG ? 1 : WAVES / 2][ALONG ? 1 : RB * NA][64];
+  __shared__ float join_m[ALONG ? 1 : WAVES][16 * RB], join_l[ALONG ? 1 : WAVES][16 * RB];
   const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const Cache &c = a.c;
   const Place place = place_of(a);
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(256, MODE == GROUP && DP <= 64 ? 3 : DP <= 128
       }
       // A step's keys and values on their way: as they are in memory.  A step's are sent for when the registers of the step before are free, keys behind
       // the scores, values behind the outputs; pages one step earlier.
-      constexpr int STRIDE = ALONG ? 1 : 4;
+      constexpr int STRIDE = ALONG ? 1 : WAVES;
       constexpr int VD = F32 ? VW : (VW + 1) / 2;                    // registers of VW values
       constexpr int KL = F32 ? NK : FMT == VF_E4M3 && DP >= 64 ? NK / 2 : NK;   // pieces of a key
       typedef uint32_t kv4 __attribute__((ext_vector_type(FMT == VF_E4M3 ? (F32 ? 1 : DP >= 64 ? 4 : 2) : 4)));
@@ -588,7 +589,7 @@ __global__ void __launch_bounds__(256, MODE == GROUP && DP <= 64 ? 3 : DP <= 128
         l[b] += __shfl_xor(l[b], 16);
         l[b] += __shfl_xor(l[b], 32);
       }
-      // the waves' shares of the keys: waves 2 and 3 give theirs to 0 and 1, then 1 to 0
+      // the waves' shares of the keys: the upper half of the waves gives theirs to the lower, until one has all
       if constexpr (!ALONG) {
         __syncthreads();
         if (g == 0) {
@@ -603,17 +604,17 @@ __global__ void __launch_bounds__(256, MODE == GROUP && DP <= 64 ? 3 : DP <= 128
         for (int b = 0; b < RB; ++b) {
           float t = join_m[0][16 * b + n];
 #pragma unroll
-          for (int w = 1; w < 4; ++w) t = fmaxf(t, join_m[w][16 * b + n]);
+          for (int w = 1; w < WAVES; ++w) t = fmaxf(t, join_m[w][16 * b + n]);
           l[b] = 0.0f;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) l[b] += join_l[w][16 * b + n] * weight_of(join_m[w][16 * b + n], t);
+          for (int w = 0; w < WAVES; ++w) l[b] += join_l[w][16 * b + n] * weight_of(join_m[w][16 * b + n], t);
           const float f = weight_of(m[b], t);
           m[b] = t;
 #pragma unroll
           for (int i = 0; i < NA; ++i) acc[b][i] *= f;
         }
 #pragma unroll
-        for (int half = 2; half >= 1; half >>= 1) {
+        for (int half = WAVES / 2; half >= 1; half >>= 1) {
           if (wave >= half && wave < 2 * half) {
 #pragma unroll
             for (int b = 0; b < RB; ++b)
@@ -1195,7 +1196,7 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   const int rows = along ? 64 * MORE : 16;
   a.blocks = blocks_of(longest, rows, a.c.heads);
   // Workgroups share the keys of a row block where there would be fewer than run at a time, as long as every wave keeps some steps.
-  const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, steps = (longest_kv + STEP - 1) / STEP, most = steps / (along ? 8 : 16);
+  const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, steps = (longest_kv + STEP - 1) / STEP, most = along ? steps / 8 : (steps + 31) / 32;
   int64_t splits = (512 + units - 1) / units;
   if (splits > most) splits = most;
   if (splits > 512) splits = 512;
@@ -1233,7 +1234,10 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
       const int by_four = (a.s.n + 3) / 4;
       k_attend_rows<T, FMT, DP, 1, SEQWISE><<<dim3(grid.x, by_four < MAX_Y ? by_four : MAX_Y), 256, 0, c->stream>>>(a);
     } else {
-      k_attend_rows<T, FMT, DP, 1, SHARE><<<grid, 256, 0, c->stream>>>(a);
+      // (with one workgroup a compute unit there are registers for eight waves, up to 128 numbers a head)
+      constexpr int FEW = DP <= 128 ? SHARE8 : SHARE;
+      if (DP <= 128 && units * splits <= 256 && steps > 4) k_attend_rows<T, FMT, DP, 1, FEW><<<grid, 512, 0, c->stream>>>(a);
+      else k_attend_rows<T, FMT, DP, 1, SHARE><<<grid, 256, 0, c->stream>>>(a);
     }
   }
   VF_HIP(c, hipGetLastError());
