@@ -18,6 +18,8 @@ namespace {
 
 using namespace vfkv;
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
 constexpr float MARGIN = 8.0f;
 constexpr float LOG2E = 1.44269504088896340736f;
 
@@ -671,13 +673,247 @@ __global__ void __launch_bounds__(MODE == SHARE8 ? 512 : 256, MODE == GROUP && D
   }
 }
 
+// ---- many rows in fp32: 32 rows a wave, keys and values straight from memory ----
+//
+// Products of 32 by 32 numbers, two of the sum at a time, take so long that one wave a SIMD keeps the matrix cores busy as long as its operands are
+// there: a step's keys are sent for behind the scores of the step before, its values behind the outputs.  Lane n of half g holds key n, and takes the
+// numbers d = 8 x + 4 g + e for product (x, e); of value 8 (i / 4) + 4 g + i % 4, whose weight is in register i, it takes the VW numbers at VW n, one for each of VW products.
+// MI355X: see launch_wide.
+template <int FMT, int DP>
+__global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const AttendArgs a) {
+  constexpr int ROWS = 128, STEP = 32, NX = DP / 8, VW = DP / 32;
+  constexpr bool MX8 = FMT == VF_E4M3;
+  typedef typename kv_elem<FMT>::type E;
+  typedef uint32_t k4 __attribute__((ext_vector_type(MX8 ? 1 : 4)));
+  constexpr int VR = MX8 ? 1 : VW;   // registers of VW numbers
+  const int lane = (int)threadIdx.x & 63, n = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const Cache &c = a.c;
+  const Place place = place_of(a);
+  const int head = place.head, split = place.split;
+  for (int seq = blockIdx.y; seq < a.s.n; seq += gridDim.y) {
+    const Span sp = span_of(a.s, c.shift, seq);
+    const int all = sp.rows * a.group.by;
+    // (row blocks that see the most keys come first)
+    for (int block = a.blocks - 1 - place.block; (int64_t)block * ROWS < all; block += a.blocks) {
+      const bool shared = a.splits > 1 && block < a.blocks;
+      if (block >= a.blocks && split > 0) break;
+      const int dim = anew(c.dim), width = anew(c.width);
+      const int r0 = block * ROWS + 32 * wave, r1 = all - r0 > 32 ? r0 + 32 : all;
+      int lo = 0, hi = 0, lo_in = 0, hi_in = 0, row_lo = 0, row_hi = 0;
+      if (r0 < r1) {
+        seen_by(a, sp, over(a.group, r0), lo, hi_in);
+        seen_by(a, sp, over(a.group, r1 - 1), lo_in, hi);
+      }
+      const float *q_row = nullptr;
+      int64_t out_row = -1;
+      const int r = r0 + n;
+      if (r < r1) {
+        const int i = over(a.group, r), h = head * a.group.by + r - i * a.group.by;
+        seen_by(a, sp, i, row_lo, row_hi);
+        q_row = reinterpret_cast<const float *>(a.q) + (sp.first + i) * a.ld_q + (int64_t)h * dim;
+        out_row = (sp.first + i) * a.ld_out + (int64_t)h * dim;
+      }
+      f32x4 q[NX];
+#pragma unroll
+      for (int x = 0; x < NX; ++x) {
+        const int d = 8 * x + 4 * g, left = q_row ? dim - d : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[x][e] = e < left ? q_row[d + e] : 0.0f;
+      }
+      f32x16 acc[VW];
+#pragma unroll
+      for (int x = 0; x < VW; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[x][i] = 0.0f;
+      float m = -INFINITY, l = 0.0f;
+      const int from = lo & ~(STEP - 1);
+      int steps = hi > from ? (hi - from + STEP - 1) / STEP : 0, s0 = 0;
+      if (shared) {
+        const int each = (steps + a.splits - 1) / a.splits;
+        s0 = (int)((int64_t)each * split < steps ? each * split : steps);
+        steps = steps - s0 < each ? steps : s0 + each;
+      }
+      k4 kraw[NX];
+      uint32_t vraw[16][VR];
+      uint8_t kscale[MX8 ? VW : 1], vscale[MX8 ? 16 : 1];
+      struct Pages { int entry[2]; };
+      auto pages_at = [&](int st) {
+        Pages p;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) p.entry[kb] = st < steps ? entry_of(a.s, c.shift, seq, from + st * STEP + 16 * kb) : -1;
+        return p;
+      };
+      // (what is fetched of an entry that is no page, and behind a row's end, is not used)
+      auto page_of = [&](const Pages &p, int kb) { return (unsigned)p.entry[kb] < (unsigned)c.pages ? p.entry[kb] : 0; };
+      const int own_d = VW * n < width ? VW * n : 0;
+      auto ask_keys = [&](int st, const Pages &p) {
+        const int64_t row = row_of(c, n < 16 ? page_of(p, 0) : page_of(p, 1), head, from + st * STEP + n);
+        const E *k = reinterpret_cast<const E *>(c.k) + row * width;
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+          const int d = 8 * x + 4 * g;
+          kraw[x] = *reinterpret_cast<const k4 *>(k + (d < width ? d : 0));
+        }
+        if constexpr (MX8) {
+#pragma unroll
+          for (int b = 0; b < VW; ++b) kscale[b] = c.ks[row * c.kb + (b < c.kb ? b : 0)];
+        }
+      };
+      auto ask_values = [&](int st, const Pages &p) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int64_t row = row_of(c, page_of(p, i >> 3), head, from + st * STEP + 8 * (i >> 2) + 4 * g + (i & 3));
+          const E *v = reinterpret_cast<const E *>(c.v) + row * width + own_d;
+          if constexpr (!MX8) {
+            typedef uint32_t uv __attribute__((ext_vector_type(VW)));
+            const uv w = *reinterpret_cast<const uv *>(v);
+#pragma unroll
+            for (int x = 0; x < VW; ++x) vraw[i][x] = w[x];
+          } else {
+            if constexpr (VW == 4) vraw[i][0] = *reinterpret_cast<const uint32_t *>(v);
+            else if constexpr (VW == 2) vraw[i][0] = *reinterpret_cast<const uint16_t *>(v);
+            else vraw[i][0] = *v;
+            vscale[i] = c.vs[row * c.kb + (own_d >> 5)];
+          }
+        }
+      };
+      Pages now = pages_at(s0), next = pages_at(s0 + 1);
+      if (s0 < steps) {
+        ask_keys(s0, now);
+        ask_values(s0, now);
+      }
+      for (int st = s0; st < steps; ++st) {
+        const int t0 = from + st * STEP;
+        const bool there0 = (unsigned)now.entry[0] < (unsigned)c.pages, there1 = (unsigned)now.entry[1] < (unsigned)c.pages;
+        const bool edge = !there0 || !there1 || t0 < lo_in || t0 + STEP > hi_in;
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+          if (8 * x >= width) continue;   // (the same for all lanes)
+          f32x4 k;
+          if constexpr (MX8) {
+            const float s = scale_of(kscale[x >> 2]);
+            const f32x2 k0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(kraw[x][0], s, false), k1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(kraw[x][0], s, true);
+            k = f32x4{k0[0], k0[1], k1[0], k1[1]};
+          } else {
+            k = __builtin_bit_cast(f32x4, kraw[x]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[x][e], sc, 0, 0, 0);
+        }
+        if (st + 1 < steps) ask_keys(st + 1, next);
+        const Pages after = pages_at(st + 2);
+        float val[16][VW];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if constexpr (MX8) {
+            const float s = scale_of(vscale[i]);
+            const f32x2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(vraw[i][0], s, false), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(vraw[i][0], s, true);
+#pragma unroll
+            for (int x = 0; x < VW; ++x) val[i][x] = x < 2 ? v0[x & 1] : v1[x & 1];
+          } else {
+#pragma unroll
+            for (int x = 0; x < VW; ++x) val[i][x] = __uint_as_float(vraw[i][x]);
+          }
+        }
+        auto key_of = [&](int i) { return t0 + 8 * (i >> 2) + 4 * g + (i & 3); };
+        auto sees = [&](int i) { return key_of(i) >= row_lo && key_of(i) < row_hi && now.entry[i >> 3] != -1; };
+        bool odd = false;
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const bool there = i < 8 ? there0 : there1;
+            sc[i] = !sees(i) ? -INFINITY : there ? sc[i] : __builtin_nanf("");
+            const bool any = key_of(i) >= lo && key_of(i) < hi && there && VW * n < width;
+#pragma unroll
+            for (int x = 0; x < VW; ++x) {
+              val[i][x] = any ? val[i][x] : 0.0f;
+              odd = odd || !(fabsf(val[i][x]) < INFINITY);
+            }
+          }
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+        top *= a.scale2;
+        if (__any(top > m + MARGIN)) {
+          float t = fmaxf(top, m);
+          t = fmaxf(t, __shfl_xor(t, 32));
+          const float f = exp2_(m - base_of(t));
+          m = t;
+          l *= f;
+#pragma unroll
+          for (int x = 0; x < VW; ++x) acc[x] *= f;
+        }
+        const float mb = base_of(m);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          sc[i] = exp2_(fmaf(sc[i], a.scale2, -mb));
+          l += sc[i];
+        }
+        if (edge && __any(odd)) {
+          // (as in k_attend_rows: values that are not finite make NaN in the rows that see them, and are left out of the products)
+#pragma unroll
+          for (int x = 0; x < VW; ++x) {
+            f32x16 hit;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) hit[i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool bad = !(fabsf(val[i][x]) < INFINITY);
+              hit = __builtin_amdgcn_mfma_f32_32x32x2f32(bad ? 1.0f : 0.0f, sees(i) ? 1.0f : 0.0f, hit, 0, 0, 0);
+              val[i][x] = bad ? 0.0f : val[i][x];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (hit[i] != 0.0f) acc[x][i] = __builtin_nanf("");
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int x = 0; x < VW; ++x) acc[x] = __builtin_amdgcn_mfma_f32_32x32x2f32(val[i][x], sc[i], acc[x], 0, 0, 0);
+        if (st + 1 < steps) ask_values(st + 1, next);
+        now = next;
+        next = after;
+      }
+      l += __shfl_xor(l, 32);
+      // numbers VW (8 (i / 4) + 4 g + i % 4) + x of row n are in acc[x][i]
+      if (shared) {
+        const int64_t at = ((int64_t)seq * gridDim.x + blockIdx.x) * ROWS + 32 * wave + n, parts = (int64_t)a.s.n * gridDim.x * ROWS;
+        float *o = a.part + at * DP;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int x = 0; x < VW; ++x) o[VW * (8 * (i >> 2) + 4 * g + (i & 3)) + x] = acc[x][i];
+        if (g == 0) {
+          float *stat = a.part + parts * DP;
+          stat[at] = m;
+          stat[parts + at] = l;
+        }
+      } else if (out_row >= 0) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        float *o = reinterpret_cast<float *>(a.out) + out_row;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int x = 0; x < VW; ++x) {
+            const int d = VW * (8 * (i >> 2) + 4 * g + (i & 3)) + x;
+            if (d < dim) o[d] = acc[x][i] * inv;
+          }
+      }
+    }
+  }
+}
+
 // ---- many rows: keys and values through the LDS ----
 //
 // A wave holds 32 rows, a workgroup four waves; a tile is 64 keys, keys and values of two tiles are in the LDS.  Pieces of 16 bytes go there straight from
 // memory (numbers in 8 bits through registers, where they become bf16); which lane fetches a piece says where it lies: piece x of key t at place x ^ key_turn(t), so
 // that the 16 keys whose pieces lanes read at a time meet all banks, and values in pairs of pieces at pair ^ value_turn(t).  S^T is made by products of
 // 32 keys by 32 rows; values are read with the reads that turn a 4 by 16 block around, so that a lane gets four keys' numbers of one column.
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
@@ -1191,9 +1427,9 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int STEP = Shape<T, FMT, DP>::STEP;
   const int64_t longest = (int64_t)a.longest * a.group.by;
   // (bf16 comes here with up to 16 rows only)
-  constexpr int MORE = 1;
-  const bool along = sizeof(T) == 4 && longest > 16;
-  const int rows = along ? 64 * MORE : 16;
+  // (and fp32 with more rows if a head has more than 128 numbers)
+  const bool along = sizeof(T) == 4 && DP > 128 && longest > 16;
+  const int rows = along ? 64 : 16;
   a.blocks = blocks_of(longest, rows, a.c.heads);
   // Workgroups share the keys of a row block where there would be fewer than run at a time, as long as every wave keeps some steps.
   const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, steps = (longest_kv + STEP - 1) / STEP, most = along ? steps / 8 : (steps + 31) / 32;
@@ -1219,8 +1455,8 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   }
   a.splits = (int)splits;
   const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
-  if constexpr (sizeof(T) == 4) {
-    if (along) k_attend_rows<T, FMT, DP, MORE, ROWWISE><<<grid, 256, 0, c->stream>>>(a);
+  if constexpr (sizeof(T) == 4 && DP > 128) {
+    if (along) k_attend_rows<T, FMT, DP, 1, ROWWISE><<<grid, 256, 0, c->stream>>>(a);
   }
   if (grouped) {
     int2 *order = const_cast<int2 *>(a.order);
@@ -1277,6 +1513,32 @@ int launch_tile(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   return VF_OK;
 }
 
+// Rows of a workgroup are four waves' of 32.
+template <int FMT, int DP>
+int launch_wide(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
+  constexpr int ROWS = 128, AT_ONCE = DP <= 64 ? 512 : 256;
+  const int64_t longest = (int64_t)a.longest * a.group.by;
+  a.blocks = blocks_of(longest, ROWS, a.c.heads);
+  const int64_t units = (int64_t)a.s.n * a.blocks * a.c.heads, most = (longest_kv + 31) / 32 / 8;
+  int64_t splits = (AT_ONCE + units - 1) / units;
+  if (splits > most) splits = most;
+  if (splits < 1) splits = 1;
+  if (splits > 1) {
+    a.part = reinterpret_cast<float *>(vfk_ops_scratch(c, (size_t)(units * splits * ROWS) * (DP + 2) * sizeof(float)));
+    if (!a.part) splits = 1;
+  }
+  a.splits = (int)splits;
+  const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
+  k_attend_wide<FMT, DP><<<grid, 256, 0, c->stream>>>(a);
+  VF_HIP(c, hipGetLastError());
+  if (splits > 1) {
+    const int64_t items = (units * ROWS + 3) / 4;
+    k_attend_join<float, DP><<<(unsigned)(items < 4096 ? items : 4096), 256, 0, c->stream>>>(a, ROWS, true);
+    VF_HIP(c, hipGetLastError());
+  }
+  return VF_OK;
+}
+
 template <typename T, int FMT>
 int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   if constexpr (sizeof(T) == 2) {
@@ -1284,6 +1546,13 @@ int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
       if (a.c.dim <= 64) return launch_tile<FMT, 64>(c, a, longest_kv);
       if (a.c.dim <= 128) return launch_tile<FMT, 128>(c, a, longest_kv);
       return launch_tile<FMT, 256>(c, a, longest_kv);
+    }
+  }
+  if constexpr (sizeof(T) == 4) {
+    if ((int64_t)a.longest * a.group.by > 16 && a.c.dim <= 128) {
+      if (a.c.dim <= 32) return launch_wide<FMT, 32>(c, a, longest_kv);
+      if (a.c.dim <= 64) return launch_wide<FMT, 64>(c, a, longest_kv);
+      return launch_wide<FMT, 128>(c, a, longest_kv);
     }
   }
   if (a.c.dim <= 32) return launch_rows<T, FMT, 32>(c, a, longest_kv);
@@ -1308,6 +1577,7 @@ int vfk_kv_attend(vf_ctx *c, const vf_kv_call &call, int heads, const void *q, i
   a.longest = (int)longest_of(call.seqs);
   const int64_t most = (int64_t)call.seqs->max_pages * call.kv->page;
   if (longest_kv > most) longest_kv = most;
+  if (window > 0 && longest_kv > (int64_t)window + a.longest) longest_kv = (int64_t)window + a.longest;   // (what a sequence's rows see)
   if (call.type == VF_BF16) return call.kv->format == VF_E4M3 ? launch<uint16_t, VF_E4M3>(c, a, longest_kv) : launch<uint16_t, VF_BF16>(c, a, longest_kv);
   return call.kv->format == VF_E4M3 ? launch<float, VF_E4M3>(c, a, longest_kv) : launch<float, VF_FP32>(c, a, longest_kv);
 }

@@ -67,13 +67,14 @@ __device__ __forceinline__ void cos_sin(double a, double &c, double &s) {
 
 // A thread takes eight neighbouring numbers of a head at a time, and the eight that they are paired with, of several heads at once, so that
 // their loads are on their way together.  The rows' cosines and sines are worked out once, for all heads, into the LDS.
-template <typename T, int FMT>
+// ODD: halves of pairs that do not end between eights.
+template <typename T, int FMT, bool ODD>
 __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
   extern __shared__ float2 turn[];  // [tb][half]
   __shared__ int pages[TB];         // of the rows; -1: nowhere
   constexpr int U = sizeof(T) == 2 ? 4 : 2;
   const int lane = (int)threadIdx.x & (a.lanes - 1), D = a.c.dim, d0 = 8 * lane, n = D - d0, step = THREADS / a.lanes;
-  const bool whole = (a.half & 7) == 0, first = d0 < a.half, turns = d0 < 2 * a.half;
+  const bool first = d0 < a.half, turns = d0 < 2 * a.half;
   const int64_t units = (int64_t)a.s.n * a.blocks;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int seq = a.blocks > 1 ? (int)(unit / a.blocks) : (int)unit;
@@ -98,6 +99,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
         raw8<T> own[U], other[U];
         int row[U], head[U];   // head: of q, then of keys, then of values
         const T *src[U];
+        float each[ODD ? U : 1][8];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int slot = slot0 + u * step + (int)threadIdx.x / a.lanes;
@@ -110,7 +112,18 @@ __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
                           : hv < 0 ? reinterpret_cast<const T *>(a.k) + r * a.ld_k + (int64_t)hk * D : reinterpret_cast<const T *>(a.v) + r * a.ld_v + (int64_t)hv * D;
           own[u] = {};
           if (row[u] >= 0 && n > 0) fetch8(src[u] + d0, n, own[u]);
-          if (row[u] >= 0 && hv < 0 && turns && whole && !a.interleaved) fetch8(src[u] + (first ? d0 + a.half : d0 - a.half), 8, other[u]);
+          if (row[u] >= 0 && hv < 0 && turns && !a.interleaved) {
+            if constexpr (!ODD) {
+              fetch8(src[u] + (first ? d0 + a.half : d0 - a.half), 8, other[u]);
+            } else {
+              // (eight loads, all on their way together)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int d = d0 + i;
+                each[ODD ? u : 0][i] = load1(src[u] + (d < a.half ? d + a.half : d < 2 * a.half ? d - a.half : 0));
+              }
+            }
+          }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -129,7 +142,7 @@ __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
                   v[i + 1] = y * w.x + x * w.y;
                 }
               }
-            } else if (whole) {
+            } else if constexpr (!ODD) {
               float o[8];
               unpack8(other[u], o);
               cs += first ? d0 : d0 - a.half;
@@ -139,12 +152,11 @@ __global__ void __launch_bounds__(THREADS) k_kv_append(const AppendArgs a) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 const int d = d0 + i;
-                if (d < 2 * a.half) {
-                  const bool low = d < a.half;
-                  const float o = load1(src[u] + (low ? d + a.half : d - a.half));
-                  const float2 w = cs[low ? d : d - a.half];
-                  v[i] = low ? v[i] * w.x - o * w.y : v[i] * w.x + o * w.y;
-                }
+                const bool low = d < a.half;
+                const float2 w = cs[low ? d : d < 2 * a.half ? d - a.half : 0];
+                const float o = each[ODD ? u : 0][i];
+                const float x = low ? v[i] * w.x - o * w.y : v[i] * w.x + o * w.y;
+                v[i] = d < 2 * a.half ? x : v[i];
               }
             }
           }
@@ -253,6 +265,18 @@ int lanes_of(int width) {
 int rows_at_once(int64_t longest, int most) { return longest < most ? (longest < 1 ? 1 : (int)longest) : most; }
 unsigned grid_of(int64_t units) { return (unsigned)(units < (1 << 20) ? units : 1 << 20); }
 
+template <bool ODD>
+void launch_append(const AppendArgs &a, int type, int format, unsigned grid, unsigned lds, hipStream_t st) {
+  if (format == VF_E4M3) {
+    if (type == VF_BF16) k_kv_append<uint16_t, VF_E4M3, ODD><<<grid, THREADS, lds, st>>>(a);
+    else k_kv_append<float, VF_E4M3, ODD><<<grid, THREADS, lds, st>>>(a);
+  } else if (type == VF_BF16) {
+    k_kv_append<uint16_t, VF_BF16, ODD><<<grid, THREADS, lds, st>>>(a);
+  } else {
+    k_kv_append<float, VF_FP32, ODD><<<grid, THREADS, lds, st>>>(a);
+  }
+}
+
 }  // namespace
 
 int vfk_kv_append(vf_ctx *c, const vf_kv_call &call, const vf_rope *rope, const void *k, int64_t ld_k, const void *v, int64_t ld_v, int heads,
@@ -275,14 +299,8 @@ int vfk_kv_append(vf_ctx *c, const vf_kv_call &call, const vf_rope *rope, const 
   a.blocks = (int)((longest + a.tb - 1) / a.tb);
   if (a.blocks < 1) a.blocks = 1;
   const unsigned grid = grid_of((int64_t)a.s.n * a.blocks), lds = (unsigned)(a.tb * a.half * sizeof(float2));
-  if (call.kv->format == VF_E4M3) {
-    if (call.type == VF_BF16) k_kv_append<uint16_t, VF_E4M3><<<grid, THREADS, lds, c->stream>>>(a);
-    else k_kv_append<float, VF_E4M3><<<grid, THREADS, lds, c->stream>>>(a);
-  } else if (call.type == VF_BF16) {
-    k_kv_append<uint16_t, VF_BF16><<<grid, THREADS, lds, c->stream>>>(a);
-  } else {
-    k_kv_append<float, VF_FP32><<<grid, THREADS, lds, c->stream>>>(a);
-  }
+  if (a.half % 8 != 0 && !a.interleaved) launch_append<true>(a, call.type, call.kv->format, grid, lds, c->stream);
+  else launch_append<false>(a, call.type, call.kv->format, grid, lds, c->stream);
   VF_HIP(c, hipGetLastError());
   return VF_OK;
 }

@@ -66,24 +66,30 @@ inline int64_t longest_of(const vf_kv_seqs *s) {
   return s->longest < s->tokens ? s->longest : s->tokens;
 }
 
+// Numbers that no kernel here writes, as constant memory: from an address that is the same in all lanes they come by a scalar load, which is waited for where
+// it is used.  (A vector load of such a number would be waited for at once, and with it all loads that are on their way.)
+__device__ __forceinline__ int fixed_at(const int32_t *p, int64_t i) {
+  return ((const __attribute__((address_space(4))) int32_t *)(uintptr_t)p)[i];
+}
+
 __device__ __forceinline__ Span span_of(const Seqs &q, int shift, int s) {
   Span p;
   p.first = (int64_t)s * q.each;
   p.rows = q.each;
   if (q.offsets) {
-    const int b = q.offsets[s], e = q.offsets[s + 1];
+    const int b = fixed_at(q.offsets, s), e = fixed_at(q.offsets, (int64_t)s + 1);
     const bool fine = b >= 0 && e >= b && e <= q.tokens;
     p.first = fine ? b : 0;
     p.rows = fine ? e - b : 0;
   }
-  const int most = q.max_pages << shift, n = q.lengths[s];
+  const int most = q.max_pages << shift, n = fixed_at(q.lengths, s);
   p.length = n < 0 ? 0 : n > most ? most : n;
   return p;
 }
 // The entry of a sequence's table for position t >= 0; -1 behind the table's end.
 __device__ __forceinline__ int entry_of(const Seqs &q, int shift, int s, int t) {
   const int at = t >> shift;
-  return at < q.max_pages ? q.table[(int64_t)s * q.ld_table + at] : -1;
+  return at < q.max_pages ? fixed_at(q.table, (int64_t)s * q.ld_table + at) : -1;
 }
 // Number of position t's row in a page of a head, over all pages and heads.
 __device__ __forceinline__ int64_t row_of(const Cache &c, int page, int head, int t) {
