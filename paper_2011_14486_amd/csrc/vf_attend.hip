@@ -678,7 +678,8 @@ __global__ void __launch_bounds__(MODE == SHARE8 ? 512 : 256, MODE == GROUP && D
 // Products of 32 by 32 numbers, two of the sum at a time, take so long that one wave a SIMD keeps the matrix cores busy as long as its operands are
 // there: a step's keys are sent for behind the scores of the step before, its values behind the outputs.  Lane n of half g holds key n, and takes the
 // numbers d = 8 x + 4 g + e for product (x, e); of value 8 (i / 4) + 4 g + i % 4, whose weight is in register i, it takes the VW numbers at VW n, one for each of VW products.
-// MI355X: see launch_wide.
+// MI355X: a prompt of 2048 tokens, 32 heads of 128 over 8 of the cache, 390 us = 88 TFLOP/s, of the 154 that the vendor library's product reaches: matrix cores busy
+// 54 % of the cycles, the rest is weights and moves beside them, which nothing else hides with one wave a SIMD.
 template <int FMT, int DP>
 __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const AttendArgs a) {
   constexpr int ROWS = 128, STEP = 32, NX = DP / 8, VW = DP / 32;
@@ -765,7 +766,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const Att
           const int64_t row = row_of(c, page_of(p, i >> 3), head, from + st * STEP + 8 * (i >> 2) + 4 * g + (i & 3));
           const E *v = reinterpret_cast<const E *>(c.v) + row * width + own_d;
           if constexpr (!MX8) {
-            typedef uint32_t uv __attribute__((ext_vector_type(VW)));
+            typedef uint32_t uv __attribute__((ext_vector_type(VW), aligned(4)));
             const uv w = *reinterpret_cast<const uv *>(v);
 #pragma unroll
             for (int x = 0; x < VW; ++x) vraw[i][x] = w[x];
@@ -791,7 +792,6 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const Att
         for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
 #pragma unroll
         for (int x = 0; x < NX; ++x) {
-          if (8 * x >= width) continue;   // (the same for all lanes)
           f32x4 k;
           if constexpr (MX8) {
             const float s = scale_of(kscale[x >> 2]);
@@ -800,8 +800,9 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const Att
           } else {
             k = __builtin_bit_cast(f32x4, kraw[x]);
           }
+          const bool in = 8 * x + 4 * g < width;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[x][e], sc, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? k[e] : 0.0f, q[x][e], sc, 0, 0, 0);
         }
         if (st + 1 < steps) ask_keys(st + 1, next);
         const Pages after = pages_at(st + 2);
@@ -1427,8 +1428,8 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   constexpr int STEP = Shape<T, FMT, DP>::STEP;
   const int64_t longest = (int64_t)a.longest * a.group.by;
   // (bf16 comes here with up to 16 rows only)
-  // (and fp32 with more rows if a head has more than 128 numbers)
-  const bool along = sizeof(T) == 4 && DP > 128 && longest > 16;
+  // (and fp32 with more, see launch)
+  const bool along = sizeof(T) == 4 && longest > 16;
   const int rows = along ? 64 : 16;
   a.blocks = blocks_of(longest, rows, a.c.heads);
   // Workgroups share the keys of a row block where there would be fewer than run at a time, as long as every wave keeps some steps.
@@ -1455,7 +1456,7 @@ int launch_rows(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
   }
   a.splits = (int)splits;
   const dim3 grid((unsigned)(a.blocks * a.c.heads * a.splits), (unsigned)(a.s.n < MAX_Y ? a.s.n : MAX_Y));
-  if constexpr (sizeof(T) == 4 && DP > 128) {
+  if constexpr (sizeof(T) == 4) {
     if (along) k_attend_rows<T, FMT, DP, 1, ROWWISE><<<grid, 256, 0, c->stream>>>(a);
   }
   if (grouped) {
@@ -1549,9 +1550,13 @@ int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
     }
   }
   if constexpr (sizeof(T) == 4) {
-    if ((int64_t)a.longest * a.group.by > 16 && a.c.dim <= 128) {
+    // Rows of 32 a wave fetch half as much as rows of 16, but see more keys that are not all theirs, and there are fewer waves.  MI355X, us, 16 / 32:
+    // 37 sequences of up to 300 rows with a window of 100, heads of 40, 46 / 64; 312 of 87 behind 48, heads of 32, 129 / 135; a prompt of 2048, 32 heads of 128, 576 /
+    // 390, of 64 295 / 253.
+    if ((int64_t)a.longest * a.group.by > 16 && a.c.dim <= 128 && longest_kv >= 512) {
       if (a.c.dim <= 32) return launch_wide<FMT, 32>(c, a, longest_kv);
       if (a.c.dim <= 64) return launch_wide<FMT, 64>(c, a, longest_kv);
+      if (FMT == VF_FP32 && a.c.dim <= 96) return launch_wide<FMT, FMT == VF_FP32 ? 96 : 128>(c, a, longest_kv);
       return launch_wide<FMT, 128>(c, a, longest_kv);
     }
   }

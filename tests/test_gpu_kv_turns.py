@@ -172,3 +172,41 @@ def test_in_place_and_far_positions(vf, ctx):  # noqa: F811
     out = vf.vf_kv_attend(ctx, cache, got, table, at, window=1, longest_kv=1 << 30)
     # (one key: its weight p times the value, times 1 / p: three roundings)
     assert (np.abs(f64(out) - f64(rv)) <= 4 * 2.0 ** -24 * np.abs(f64(rv))).all()
+
+
+@pytest.mark.parametrize("cache", ["fp32", "e4m3"])
+@pytest.mark.parametrize("dim", [9, 32, 40, 64, 80, 96, 128])
+def test_rows_of_32_a_wave(vf, ctx, cache, dim):  # noqa: F811
+    """fp32 with tables of more than 512 places: ragged rows, windows, all keys, pages that are missing or none, numbers that are not finite."""
+    heads = 6
+    new, keys = [40, 1, 33, 0, 150], [60, 20, 33, 7, 600]
+    for window, causal in ((0, True), (21, True), (0, False)):
+        c = Case(vf, "fp32", cache, heads, 2, dim, new, keys, 16, extra=40)
+        q = c.matrix(heads * dim, scale=1.5)
+        table, lengths = c.where()
+        got = vf.vf_kv_attend(ctx, c.cache, q, table, lengths, causal=causal, window=window, offsets=c.dev(c.offsets))
+        c.check_attend(ctx, q, got, causal, window)
+    for where, entry in (((0, 1), -1), ((4, 20), 10 ** 7), ((4, 37), -1)):
+        c = Case(vf, "fp32", cache, heads, 2, dim, new, keys, 16, extra=40)
+        c.table[where] = entry
+        c.pool()
+        q = c.matrix(heads * dim)
+        table, lengths = c.where()
+        c.check_attend(ctx, q, vf.vf_kv_attend(ctx, c.cache, q, table, lengths, offsets=c.dev(c.offsets)))
+    for what in (float("inf"), float("nan")):
+        c = Case(vf, "fp32", cache, heads, 2, dim, new, keys, 16, extra=40)
+        clean = f64(vf.vf_kv_attend(ctx, c.cache, q, *c.where(), offsets=c.dev(c.offsets)))
+        for t in (5, 33, 59):
+            c.v[c.table[0, t // 16], 0, t % 16, dim // 2] = what
+        c.pool()
+        got = f64(vf.vf_kv_attend(ctx, c.cache, q, *c.where(), offsets=c.dev(c.offsets)))
+        first = int(c.offsets[0])
+        for r in range(c.tokens - 4):
+            row = first + r
+            hit = r < 40 and any(t <= 20 + r for t in (5, 33, 59))
+            for h in range(heads):
+                a, b = got[row, h * dim:(h + 1) * dim], clean[row, h * dim:(h + 1) * dim]
+                if hit and h < heads // 2:
+                    assert not np.isfinite(a[dim // 2])
+                else:
+                    assert np.array_equal(a, b)

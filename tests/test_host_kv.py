@@ -122,9 +122,11 @@ def ways(stub, vf, ctx):
         got = names(stub)
         assert len(got) == len(want) and all(kinds[w] in name for w, (name, _) in zip(want, got)), (sizes, got)
     # fp32: few rows share the keys, more have waves of 32, or of 16 with long heads
-    for tokens, dim, way in ((4, 64, "k_attend_rowsIfLi0ELi64ELi1ELi4E"), (5, 64, "k_attend_wideILi0ELi64E"), (5, 200, "k_attend_rowsIfLi0ELi256ELi1ELi1E")):
+    for tokens, dim, way in ((4, 64, "k_attend_rowsIfLi0ELi64ELi1ELi4E"), (5, 64, "k_attend_wideILi0ELi64E"), (5, 96, "k_attend_wideILi0ELi96E"), (5, 200, "k_attend_rowsIfLi0ELi256ELi1ELi1E")):
         assert call(vf, ctx, "attend", type=0, format=0, n_seq=1, tokens=tokens, head_dim=dim, ldq=8 * dim, ldo=8 * dim, longest_kv=1000, **long) == OK
         assert any(way in name for name, _ in names(stub))
+    assert call(vf, ctx, "attend", type=0, format=0, n_seq=1, tokens=50, longest_kv=500, **long) == OK
+    assert "k_attend_rowsIfLi0ELi64ELi1ELi1E" in names(stub)[0][0]
     # a window bounds the keys that the work is split by
     assert call(vf, ctx, "attend", n_seq=1, tokens=1, longest_kv=100000, window=100, **long) == OK
     assert [("k_attend_rows" in name) for name, _ in names(stub)] == [True]
