@@ -9,6 +9,13 @@
 // keys and values are fetched once for them.  Products are made as S^T = K Q^T and out^T = V^T P^T: a lane then holds scores of one row only, and the
 // scores come out in the lanes and registers in which the second product takes them, up to the order of the keys in it, which is free as
 // long as the values follow it.
+//
+// In bf16 the weights are rounded to bf16 for the second product: by 2^-8 of each at most, as outputs are; in two
+// parts they would cost half as many matrix instructions again.  Error to the outputs' size in root mean square 1.9 - 2.3e-3, of exact outputs rounded 1.7e-3.
+//
+// Which kernel takes a call goes by what the host knows: rows of the longest sequence times heads that share one of the cache's, and the longest length.
+// Up to 16 such rows: k_attend_rows; more: k_attend_tile in bf16, k_attend_wide or k_attend_rows in fp32.  Where there would be fewer workgroups than run at a
+// time, several share the keys of a row block and k_attend_join joins them.
 #include <math.h>
 
 #include "vf_internal.h"
@@ -81,6 +88,13 @@ __device__ __forceinline__ float weight_of(float m, float top) { return exp2_(m 
 // Rows of a search that go on from the same prefix have the same pages in front.  GROUP takes single tokens of up to 16 / group sequences that begin
 // with the same page as the rows of one product: keys and values of blocks whose pages are the same are fetched once for all of them, others for one sequence at a
 // time, with the other sequences' rows not seeing them.
+//
+// What bounds it is the memory, with few workgroups its latency: keys, values and pages of a step are asked for one step before.  Values lie with their numbers side by
+// side, and the product wants keys side by side: the numbers of eight keys, eight of each, are turned around in registers, halves by halves, 32 instructions
+// for 8 products, which memory's time hides.
+// MI355X: 4 rows of 32 heads of 128 behind 131,072 keys of 8 heads in 8 bits, 1.1 GB, 199 us = 5.6 TB/s (503 with a step's loads behind the step before, 235 with pages
+// by vector loads); 64 rows behind 2001 keys in bf16 95 us = 5.5 TB/s; 1024 rows behind 501 keys of 64 prefixes, 16 over 4 heads of 64, 41 us and 9 for the groups (72
+// apart); one row behind 1001 keys 11 us, of which 5 are there without keys.
 enum { SHARE, ROWWISE, SEQWISE, GROUP, SHARE8 };   // SHARE8: eight waves, where there are few workgroups
 
 template <typename T, int FMT, int DP> struct Shape;
@@ -915,6 +929,13 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const Att
 // memory (numbers in 8 bits through registers, where they become bf16); which lane fetches a piece says where it lies: piece x of key t at place x ^ key_turn(t), so
 // that the 16 keys whose pieces lanes read at a time meet all banks, and values in pairs of pieces at pair ^ value_turn(t).  S^T is made by products of
 // 32 keys by 32 rows; values are read with the reads that turn a 4 by 16 block around, so that a lane gets four keys' numbers of one column.
+//
+// Two workgroups a compute unit: while waves of one are at their weights, those of the other may be at their products.  MI355X: prompt of 8192 tokens, 32 over 8 heads of
+// 128, 575 us = 960 TFLOP/s (the vendor library's product of 8192^3 reaches 1280); without weights and maxima, in a copy that leaves them out, 538 of then 604 us,
+// without loads too 462: products, their reads and one barrier a tile are three quarters of it.  Matrix cores are busy 40 % of the cycles, the vector unit 38 %.  Tried and slower:
+// scores of the next tile beside this one's weights (spills), 64 rows a wave with one wave a SIMD (790 us), a higher priority at products (614), operands' reads ordered
+// by hand (610).  16384 sequences of 50 tokens, 4 over 2 heads of 64: 340 us, 3.7 TB/s; a workgroup is one tile there, and its chain of loads (length, pages, keys) is
+// what three workgroups a unit overlap.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 

@@ -1,6 +1,10 @@
 // vf_kv_append and vf_kv_read: rows of keys and values into a paged cache and out of it, rotary positions on the way.
 //
-// Both move every number once and are bound by the memory's rate, or for few rows by the latency of a launch.
+// Both move every number once and are bound by the memory's rate, or for few rows by the latency of a launch.  A workgroup takes up to 8 (16) rows of a
+// sequence with all their heads: rows are contiguous in the call's matrices and a page's rows of a head in the cache, so that both sides move
+// in whole lines, and what a row needs once (page, angles) is there once.
+// MI355X: prompt of 16384 tokens, 32 + 2 x 8 heads of 128 in bf16, 403 MB, 86 us = 4.7 TB/s (104 with one head at a time); 64 prefixes of up to
+// 4096 tokens, 8 heads of 128, from 8 bits to bf16, 823 MB, 174 us = 4.7 TB/s (252); a copy reaches 5.2.  One token: 4.2 and 3.8 us.
 #include "vf_internal.h"
 #include "vf_kv_dev.h"
 

@@ -167,7 +167,8 @@ int vf_kv_attend(vf_ctx *c, const vf_kv *kv, const vf_kv_seqs *seqs, int32_t typ
                  int32_t window, float scale, int64_t longest_kv, void *out, int64_t ld_out) {
   if (!c || !kv || !seqs || !is_type(type) || !kv_ok(kv, type) || !seqs_ok(seqs, kv)) return VF_EINVAL;
   if (heads < 1 || heads > 65536 || heads % kv->kv_heads != 0) return VF_EINVAL;
-  if (causal < 0 || causal > 1 || window < 0 || (window > 0 && !causal) || !(scale >= 0.0f) || !isfinite(scale) || longest_kv < 0) return VF_EINVAL;
+  // (scores are powers of two inside: the scale times log2(e) has to be a number too)
+  if (causal < 0 || causal > 1 || window < 0 || (window > 0 && !causal) || !(scale >= 0.0f) || !isfinite(scale * 1.5f) || longest_kv < 0) return VF_EINVAL;
   // (rows of one head of the cache are counted in 32 bits)
   if (seqs->tokens * (int64_t)(heads / kv->kv_heads) >= ((int64_t)1 << 31)) return VF_EINVAL;
   const int64_t HD = (int64_t)heads * kv->head_dim;

@@ -210,3 +210,18 @@ def test_rows_of_32_a_wave(vf, ctx, cache, dim):  # noqa: F811
                     assert not np.isfinite(a[dim // 2])
                 else:
                     assert np.array_equal(a, b)
+
+
+def test_outputs_in_place(vf, ctx):  # noqa: F811
+    """Outputs in the queries' place, in every way that attention takes."""
+    for kind, new, keys, extra in (("bf16", [1], [40], 1), ("bf16", [1], [9000], 1), ("bf16", [3, 40, 200], [9, 40, 700], 1), ("fp32", [3, 40], [9, 40], 1),
+                                   ("fp32", [40, 200], [40, 700], 40), ("bf16", [1] * 2100, [20] * 2100, 1)):
+        c = Case(vf, kind, kind, 8, 2, 64, new, keys, 16, extra=extra, ragged=len(new) < 9)
+        q = c.matrix(512)
+        kept = q.clone()
+        table, lengths = c.where()
+        off = c.dev(c.offsets)
+        apart = vf.vf_kv_attend(ctx, c.cache, q, table, lengths, offsets=off)
+        assert vf.vf_kv_attend(ctx, c.cache, q, table, lengths, offsets=off, out=q) is q
+        live = slice(2, -2) if c.offsets is not None else slice(None)
+        assert c.torch.equal(q[live], apart[live]) and not c.torch.equal(q[live], kept[live])

@@ -65,7 +65,7 @@ def refused(stub, vf, ctx):
                 dict(freq_dev=P + 4), dict(magnitude=NAN), dict(magnitude=INF)],
         read=[dict(type=2), dict(type=-1)],
         attend=[dict(heads=0), dict(heads=7), dict(heads=-2), dict(q=None), dict(out=None), dict(ldq=511), dict(ldo=511), dict(q=P + 1), dict(out=P + 1), dict(causal=2),
-                dict(window=-1), dict(causal=0, window=5), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(longest_kv=-1), dict(type=0), dict(type=3)])
+                dict(window=-1), dict(causal=0, window=5), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(scale=3e38), dict(ldo=-5), dict(longest_kv=-1), dict(type=0), dict(type=3)])
     for what in ("append", "read", "attend"):
         for good in ({}, EIGHT, dict(offsets_dev=P, tokens=7), dict(max_pages=0, ld_table=0, table_dev=None)):
             stub.stub_clear()
