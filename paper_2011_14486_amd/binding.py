@@ -794,6 +794,8 @@ def vf_kv_attend(ctx, cache, q, table, lengths, causal=True, window=0, scale=Non
     wide, dtype = heads * cache.head_dim, q.dtype
     ld_q = _rows_of(ctx, q, tokens, wide, dtype, "q")
     out, ld_o = _like(ctx, out, q, ld_q, tokens, wide, dtype)
+    if window and not 0 < window < 1 << 31:
+        _fail(f"window: 0 or 1 to 2^31 - 1 is wanted, not {window}")
     if longest_kv is None:
         longest_kv = seqs.max_pages * cache.page
     _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, _addr(q), ld_q, 1 if causal else 0, window,

@@ -196,7 +196,8 @@ def test_binding_refuses():
     table, lengths = i32(3, 4), i32(3)
     q, k = torch.zeros((6, 512), dtype=torch.bfloat16), torch.zeros((6, 128), dtype=torch.bfloat16)
     for more in (dict(table=i32(3, 4, 1)), dict(table=table.long()), dict(table=i32(4, 3).t()), dict(lengths=i32(4)), dict(lengths=lengths.long()),
-                 dict(lengths=i32(6)[::2]), dict(offsets=i32(3)), dict(table=i32(4, 4), lengths=i32(4)), dict(q=q[:, :100]), dict(q=q.half()), dict(q=q[:, ::2])):
+                 dict(lengths=i32(6)[::2]), dict(offsets=i32(3)), dict(table=i32(4, 4), lengths=i32(4)), dict(q=q[:, :100]), dict(q=q.half()), dict(q=q[:, ::2]),
+                 dict(window=(1 << 32) + 5), dict(window=-1)):
         args = dict(dict(q=q, table=table, lengths=lengths), **more)
         with pytest.raises(ValueError):
             vf.vf_kv_attend(ctx, cache, args.pop("q"), args.pop("table"), args.pop("lengths"), **args)
