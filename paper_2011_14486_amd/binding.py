@@ -129,7 +129,7 @@ class Context:
         self.device = torch.device("cuda", device)
         with torch.cuda.device(self.device):
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
-        self.index, self.raw_stream = device, self.stream.cuda_stream
+        self.index, self.raw_stream, self.current = device, self.stream.cuda_stream, torch._C._cuda_getCurrentRawStream
         h = C.c_void_p()
         rc = lib().vf_create(C.byref(h), device, C.c_void_p(self.stream.cuda_stream))
         self.handle = h if rc == VF_OK else None
@@ -443,10 +443,12 @@ def _mx_empty(ctx, rows, cols, fmt):
 
 def _call(ctx, fn, args, tensors):
     """Runs a library call on the context's stream, ordered with torch's current one."""
-    torch = ctx.torch
-    if torch._C._cuda_getCurrentRawStream(ctx.index) == ctx.raw_stream:
-        _check(ctx, fn(ctx.handle, *args))
+    if ctx.current(ctx.index) == ctx.raw_stream:
+        rc = fn(ctx.handle, *args)
+        if rc != VF_OK:
+            _check(ctx, rc)
         return
+    torch = ctx.torch
     here = torch.cuda.current_stream(ctx.device)
     ctx.stream.wait_stream(here)
     for t in tensors:
@@ -730,11 +732,18 @@ def _like(ctx, out, t, ld_t, rows, cols, dtype):
     return out, ld_t if out is t else _rows_of(ctx, out, rows, cols, dtype, "out")
 
 
-def _heads_of(cache, t, name):
-    """Heads in the rows of a matrix."""
-    if t.dim() != 2 or t.shape[1] % cache.head_dim != 0:
-        _fail(f"{name}: rows of heads of {cache.head_dim} are wanted, got {tuple(t.shape)}")
-    return t.shape[1] // cache.head_dim
+def _queries(ctx, cache, q, tokens, dtype):
+    """Checks a matrix of heads; returns its rows, columns, heads and the distance of its rows."""
+    shape = q.shape
+    if len(shape) != 2 or shape[1] % cache.head_dim != 0:
+        _fail(f"q: rows of heads of {cache.head_dim} are wanted, got {tuple(shape)}")
+    rows, cols = shape
+    if (tokens is not None and rows != tokens) or q.dtype != dtype or q.device != ctx.device:
+        _fail(f"q: {dtype} [{rows if tokens is None else tokens}][{cols}] on {ctx.device} is wanted, got {q.dtype} {tuple(shape)} on {q.device}")
+    ld, step = q.stride()
+    if step != 1 and cols > 1 and rows > 0:
+        _fail("q: the last dimension has to be dense")
+    return rows, cols, cols // cache.head_dim, ld if rows > 1 or ld > cols else cols
 
 
 def vf_kv_append(ctx, cache, k, v, table, lengths, q=None, rope=None, offsets=None, longest=None, q_out=None):
@@ -752,9 +761,7 @@ def vf_kv_append(ctx, cache, k, v, table, lengths, q=None, rope=None, offsets=No
     ld_v = _rows_of(ctx, v, tokens, wide, dtype, "v")
     heads = ld_q = ld_o = 0
     if q is not None:
-        heads = _heads_of(cache, q, "q")
-        wide = heads * cache.head_dim
-        ld_q = _rows_of(ctx, q, tokens, wide, dtype, "q")
+        _, wide, heads, ld_q = _queries(ctx, cache, q, tokens, dtype)
         q_out, ld_o = _like(ctx, q_out, q, ld_q, tokens, wide, dtype)
     elif q_out is not None:
         _fail("q_out without q")
@@ -788,17 +795,16 @@ def vf_kv_attend(ctx, cache, q, table, lengths, causal=True, window=0, scale=Non
     heads is a multiple of the cache's; rows, table, lengths, offsets and longest as for vf_kv_append.  causal: row i of m sees the keys up
     to position lengths[s] - m + i, with a window only the last `window` of them; otherwise all lengths[s] keys.  scale: default
     head_dim ** -0.5.  longest_kv: the longest length (default: what the table can hold).  Rows without keys are zeros."""
-    torch = ctx.torch
-    kind, tokens, heads = _type_of(torch, q), q.shape[0], _heads_of(cache, q, "q")
+    dtype = q.dtype
+    kind = _type_of(ctx.torch, q)
+    tokens, wide, heads, ld_q = _queries(ctx, cache, q, None, dtype)
     seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
-    wide, dtype = heads * cache.head_dim, q.dtype
-    ld_q = _rows_of(ctx, q, tokens, wide, dtype, "q")
     out, ld_o = _like(ctx, out, q, ld_q, tokens, wide, dtype)
     if window and not 0 < window < 1 << 31:
         _fail(f"window: 0 or 1 to 2^31 - 1 is wanted, not {window}")
     if longest_kv is None:
         longest_kv = seqs.max_pages * cache.page
-    _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, _addr(q), ld_q, 1 if causal else 0, window,
-                                    cache.head_dim ** -0.5 if scale is None else scale, longest_kv, _addr(out), ld_o),
+    _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, q.data_ptr(), ld_q, 1 if causal else 0, window,
+                                    cache.head_dim ** -0.5 if scale is None else scale, longest_kv, out.data_ptr(), ld_o),
           (q, out, table, lengths, offsets, *cache.tensors))
     return out
