@@ -793,8 +793,8 @@ def vf_kv_attend(ctx, cache, q, table, lengths, causal=True, window=0, scale=Non
     """Attention of the rows q [tokens][heads head_dim] over their sequences' keys and values in the cache: [tokens][heads head_dim].
 
     heads is a multiple of the cache's; rows, table, lengths, offsets and longest as for vf_kv_append.  causal: row i of m sees the keys up
-    to position lengths[s] - m + i, with a window only the last `window` of them; otherwise all lengths[s] keys.  scale: default
-    head_dim ** -0.5.  longest_kv: the longest length (default: what the table can hold).  Rows without keys are zeros."""
+    to position lengths[s] - m + i, with a window only the last `window` of them; otherwise all lengths[s] keys, whatever the window.
+    scale: default head_dim ** -0.5.  longest_kv: the longest length (default: what the table can hold).  Rows without keys are zeros."""
     dtype = q.dtype
     kind = _type_of(ctx.torch, q)
     tokens, wide, heads, ld_q = _queries(ctx, cache, q, None, dtype)
@@ -804,7 +804,7 @@ def vf_kv_attend(ctx, cache, q, table, lengths, causal=True, window=0, scale=Non
         _fail(f"window: 0 or 1 to 2^31 - 1 is wanted, not {window}")
     if longest_kv is None:
         longest_kv = seqs.max_pages * cache.page
-    _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, q.data_ptr(), ld_q, 1 if causal else 0, window,
+    _call(ctx, lib().vf_kv_attend, (cache.ref, C.byref(seqs), kind, heads, q.data_ptr(), ld_q, 1 if causal else 0, window if causal else 0,
                                     cache.head_dim ** -0.5 if scale is None else scale, longest_kv, out.data_ptr(), ld_o),
           (q, out, table, lengths, offsets, *cache.tensors))
     return out
