@@ -334,8 +334,7 @@ def run(state):
         return (q, *vf.vf_kv_read(ctx, cache, *where, s["tokens"], offsets=s["offsets"], longest=case["longest"], out_type=ids[case["type"]]))
     if op == "read":
         return vf.vf_kv_read(ctx, cache, *where, s["tokens"], offsets=s["offsets"], longest=case["longest"], out_type=ids[case["type"]])
-    window = case["window"] if case["causal"] else 0   # (where every row sees all keys there is none)
-    return vf.vf_kv_attend(ctx, cache, s["q"], *where, causal=case["causal"], window=window, scale=s["scale"], offsets=s["offsets"],
+    return vf.vf_kv_attend(ctx, cache, s["q"], *where, causal=case["causal"], window=case["window"], scale=s["scale"], offsets=s["offsets"],
                            longest=case["longest"], longest_kv=s["longest_kv"])
 
 
