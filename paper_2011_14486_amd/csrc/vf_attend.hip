@@ -760,7 +760,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const Att
       };
       // (what is fetched of an entry that is no page, and behind a row's end, is not used)
       auto page_of = [&](const Pages &p, int kb) { return (unsigned)p.entry[kb] < (unsigned)c.pages ? p.entry[kb] : 0; };
-      const int own_d = VW * n < width ? VW * n : 0;
+      const int own_d = VW * n < width ? VW * n : 0;   // (a row's width is a multiple of VW, see launch)
       auto ask_keys = [&](int st, const Pages &p) {
         const int64_t row = row_of(c, n < 16 ? page_of(p, 0) : page_of(p, 1), head, from + st * STEP + n);
         const E *k = reinterpret_cast<const E *>(c.k) + row * width;
@@ -1577,7 +1577,8 @@ int launch(vf_ctx *c, AttendArgs &a, int64_t longest_kv) {
     if ((int64_t)a.longest * a.group.by > 16 && a.c.dim <= 128 && longest_kv >= 512) {
       if (a.c.dim <= 32) return launch_wide<FMT, 32>(c, a, longest_kv);
       if (a.c.dim <= 64) return launch_wide<FMT, 64>(c, a, longest_kv);
-      if (FMT == VF_FP32 && a.c.dim <= 96) return launch_wide<FMT, FMT == VF_FP32 ? 96 : 128>(c, a, longest_kv);
+      // (a lane of the instance for 96 takes three numbers of a value, which only rows of 72 and 96 consist of: of others a lane's three would end behind the row)
+      if (FMT == VF_FP32 && a.c.dim <= 96 && a.c.width % 3 == 0) return launch_wide<FMT, FMT == VF_FP32 ? 96 : 128>(c, a, longest_kv);
       return launch_wide<FMT, 128>(c, a, longest_kv);
     }
   }
