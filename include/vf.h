@@ -406,8 +406,9 @@ int vf_kv_read(vf_ctx *ctx, const vf_kv *cache_host, const vf_kv_seqs *seqs_host
  * of `type`; heads is a multiple of kv_heads, head h meets head h / (heads / kv_heads) of the cache; the cache's format is `type` or
  * VF_E4M3; out may be q itself with its row distance.  0 <= scale < 2^127.  causal: a row at position t sees keys 0..t, with a window w > 0 only the last w of them; a row with
  * a negative position sees none.  Otherwise every row sees all keys, however many rows there are, and the window is 0.  A key that a row does not see takes no
- * part in it, whatever it and its value hold.  Rows that see no key, and rows all of whose scores are -inf, are zeros.  In bf16 the weights p are rounded to bf16 for
- * their products with the values, and numbers that are not finite may come out as NaN where they would be infinite.  longest_kv: the longest length, which sets how
+ * part in it, whatever it and its value hold.  Rows that see no key, and rows all of whose scores are -inf, are zeros.  In bf16 the weights p of calls
+ * with longest times heads / kv_heads above 16 are rounded to bf16 for their products with the values, of others to 2^-15 of each; numbers that are not finite may
+ * come out as NaN where they would be infinite.  longest_kv: the longest length, which sets how
  * the work is split (longer ones are right, but slow).  A call may keep scratch in the context until vf_destroy, up to 260 MiB for a call and 1 GiB
  * in all (few rows behind many keys are split along the keys); a call whose stream is being captured takes no new scratch and does without.  A
  * graph that holds such a call is replayed on the context's stream, or ordered with it. */

@@ -10,8 +10,10 @@
 // scores come out in the lanes and registers in which the second product takes them, up to the order of the keys in it, which is free as
 // long as the values follow it.
 //
-// In bf16 the weights are rounded to bf16 for the second product: by 2^-8 of each at most, as outputs are; in two
-// parts they would cost half as many matrix instructions again.  Error to the outputs' size in root mean square 1.9 - 2.3e-3, of exact outputs rounded 1.7e-3.
+// In bf16 the second product takes the weights as bf16.  Few rows, whose time is the memory's, have them as two numbers of bf16 each, right to 2^-15: one token
+// behind 1001 keys 11.2 us for 11.0 with one number, 64 rows behind 2001 keys 104.4 for 104.4, 4 rows behind 131,072 keys in 8 bits 199.0 for 198.2, 1024 rows of 64 prefixes
+// 52.7 for 51.4.  Many rows, whose time is the products', have one, rounded by 2^-8 of it at most, as outputs are: with two a prompt of 8192 tokens takes 797 us
+// for 569, chunks from 8 bits 461 for 340, short whole sequences 356 for 338.  Their error to the outputs' size in root mean square is 1.8 - 2.3e-3, of exact outputs rounded 1.7e-3.
 //
 // Which kernel takes a call goes by what the host knows: rows of the longest sequence times heads that share one of the cache's, and the longest length.
 // Up to 16 such rows: k_attend_rows; more: k_attend_tile in bf16, k_attend_wide or k_attend_rows in fp32.  Where there would be fewer workgroups than run at a
@@ -122,6 +124,14 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t marks_of(uint32_t w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0x3f80u : 0) | ((w & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0);
+}
+
+// Two weights as pairs of bf16 whose sums they are to 2^-15: their upper halves, and what is left of them, which is never negative.  (The rest
+// of a weight that is not zero is not zero either, so that an infinite value stays infinite in both products.)
+__device__ __forceinline__ void two_parts(float a, float b, uint32_t &upper, uint32_t &rest) {
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  upper = __builtin_amdgcn_perm(y, x, 0x07060302u);
+  rest = pack2(fmaxf(a - __uint_as_float(x & 0xffff0000u), a * 0x1p-24f), fmaxf(b - __uint_as_float(y & 0xffff0000u), b * 0x1p-24f));
 }
 
 // First of the eight numbers (four in fp32) of k-step ks that a lane of quarter g holds: whole pieces of 16 bytes of a row.
@@ -560,10 +570,15 @@ __global__ void __launch_bounds__(MODE == SHARE8 ? 512 : 256, MODE == GROUP && D
                 for (int b = 0; b < RB; ++b) acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, sc[b][0][i], acc[b][h * VW + x], 0, 0, 0);
               }
         } else {
-          bf16x8 p[RB];
+          bf16x8 p[RB], rest[RB];
 #pragma unroll
-          for (int b = 0; b < RB; ++b)
-            p[b] = as_bf16x8(pack2(sc[b][0][0], sc[b][0][1]), pack2(sc[b][0][2], sc[b][0][3]), pack2(sc[b][1][0], sc[b][1][1]), pack2(sc[b][1][2], sc[b][1][3]));
+          for (int b = 0; b < RB; ++b) {
+            uint32_t w[4], r[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) two_parts(sc[b][e >> 1][2 * (e & 1)], sc[b][e >> 1][2 * (e & 1) + 1], w[e], r[e]);
+            p[b] = as_bf16x8(w[0], w[1], w[2], w[3]);
+            rest[b] = as_bf16x8(r[0], r[1], r[2], r[3]);
+          }
 #pragma unroll
           for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -594,6 +609,9 @@ __global__ void __launch_bounds__(MODE == SHARE8 ? 512 : 256, MODE == GROUP && D
 #pragma unroll
               for (int b = 0; b < RB; ++b)
                 acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w[0], w[1], w[2], w[3]), p[b], acc[b][h * VW + x], 0, 0, 0);
+#pragma unroll
+              for (int b = 0; b < RB; ++b)
+                acc[b][h * VW + x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w[0], w[1], w[2], w[3]), rest[b], acc[b][h * VW + x], 0, 0, 0);
             }
         }
         if (next.st < steps) ask_values(next);
