@@ -173,6 +173,7 @@ int vf_kv_attend(vf_ctx *c, const vf_kv *kv, const vf_kv_seqs *seqs, int32_t typ
   if (seqs->tokens * (int64_t)(heads / kv->kv_heads) >= ((int64_t)1 << 31)) return VF_EINVAL;
   const int64_t HD = (int64_t)heads * kv->head_dim;
   if (!matrix_ok(q, ld_q, seqs->tokens, HD, type) || !matrix_ok(out, ld_out, seqs->tokens, HD, type)) return VF_EINVAL;
+  if (out == q && ld_out != ld_q && seqs->tokens > 1) return VF_EINVAL;
   DeviceGuard g(c->device);
   return vfk_kv_attend(c, vf_kv_call{kv, seqs, type}, heads, q, ld_q, causal != 0, window, scale, longest_kv, out, ld_out);
 }

@@ -1,10 +1,19 @@
-"""What the Python side of the attention operators hands to the library, and which calls it takes, on the CPU."""
+"""What the Python side of the attention operators hands to the library, and which calls are taken, on the CPU."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
-from paper_2011_14486_amd import binding as vf
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+sys.path.insert(0, ROOT)
+
+from paper_2011_14486_amd import binding as vf  # noqa: E402
+from tests.test_host_kv import EINVAL, OK, P, call, library, make_library  # noqa: E402
+from tests.test_host_ops import stub_path  # noqa: E402, F401
 
 
 class Thing:
@@ -37,3 +46,26 @@ def test_a_window_without_causality_is_none(monkeypatch, window):
     for bad in (-1, 1 << 31):
         with pytest.raises(ValueError):
             handed(monkeypatch, vf.vf_kv_attend, q, i32(3, 4), i32(3), causal=False, window=bad)
+
+
+def in_place(stub, vf, ctx):  # noqa: F811
+    """Outputs in the queries' place have the queries' row distance: with another one rows would lie over queries that are still to be read."""
+    stub.stub_clear()
+    for other in (513, 1024):
+        assert call(vf, ctx, "attend", out=5 * P, ldo=other) == EINVAL
+        assert call(vf, ctx, "attend", out=5 * P, ldo=other, n_seq=1, tokens=300) == EINVAL
+    assert stub.stub_log() == b""
+    assert call(vf, ctx, "attend", out=5 * P) == OK
+    assert call(vf, ctx, "attend", out=5 * P, ldq=1024, ldo=1024) == OK
+    assert call(vf, ctx, "attend", out=5 * P, ldo=1024, n_seq=1, tokens=1) == OK   # (one row has no distance)
+    assert call(vf, ctx, "attend", out=5 * P, ldo=1024, n_seq=1, tokens=0) == OK
+
+
+@pytest.mark.parametrize("case", ["in_place"])
+def test_on_a_runtime_without_a_gpu(stub_path, case):  # noqa: F811
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), stub_path, case], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+if __name__ == "__main__":
+    globals()[sys.argv[2]](*library(*make_library(sys.argv[1])))
