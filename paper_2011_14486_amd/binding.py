@@ -773,10 +773,13 @@ def vf_kv_append(ctx, cache, k, v, table, lengths, q=None, rope=None, offsets=No
     return q_out
 
 
-def vf_kv_read(ctx, cache, table, lengths, tokens, offsets=None, longest=None, out_type=VF_BF16, out=None):
+def vf_kv_read(ctx, cache, table, lengths, tokens, offsets=None, longest=None, out_type=None, out=None):
     """Keys and values of the last positions of every sequence, `tokens` rows in all, as vf_kv_append deals rows to sequences: (k, v),
-    each [tokens][kv_heads head_dim] of out_type; out: a pair of matrices to write to, either may be None and is then not read."""
+    each [tokens][kv_heads head_dim] of out_type (default: the cache's type, VF_BF16 of 8 bits); out: a pair of matrices to write to,
+    either may be None and is then not read."""
     seqs = _kv_seqs(ctx, cache, table, lengths, tokens, offsets, longest)
+    if out_type is None:
+        out_type = VF_BF16 if cache.fmt == VF_E4M3 else cache.fmt
     dtype, wide = _dtype_of(ctx.torch, out_type), cache.kv_heads * cache.head_dim
     if out is None:
         k = ctx.empty((tokens, wide), dtype)

@@ -48,6 +48,19 @@ def test_a_window_without_causality_is_none(monkeypatch, window):
             handed(monkeypatch, vf.vf_kv_attend, q, i32(3, 4), i32(3), causal=False, window=bad)
 
 
+def test_rows_are_read_as_the_cache_holds_them(monkeypatch):
+    """Without a type rows come out in the cache's own, those of 8 bits in bf16: nothing is rounded unasked."""
+    where = i32(3, 4), i32(3), 6
+    for fmt, kind, dtype in ((vf.VF_FP32, vf.VF_FP32, torch.float32), (vf.VF_BF16, vf.VF_BF16, torch.bfloat16), (vf.VF_E4M3, vf.VF_BF16, torch.bfloat16)):
+        a, out = handed(monkeypatch, vf.vf_kv_read, *where, fmt=fmt)
+        assert a[2] == kind and all(t.dtype == dtype for t in out)
+        own = torch.empty((6, 128), dtype=dtype), None
+        assert handed(monkeypatch, vf.vf_kv_read, *where, fmt=fmt, out=own)[1] is own
+        for asked, dt in ((vf.VF_FP32, torch.float32), (vf.VF_BF16, torch.bfloat16)):
+            a, out = handed(monkeypatch, vf.vf_kv_read, *where, fmt=fmt, out_type=asked)
+            assert a[2] == asked and all(t.dtype == dt for t in out)
+
+
 def in_place(stub, vf, ctx):  # noqa: F811
     """Outputs in the queries' place have the queries' row distance: with another one rows would lie over queries that are still to be read."""
     stub.stub_clear()
