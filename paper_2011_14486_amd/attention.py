@@ -26,7 +26,8 @@ from .ssm import sums_of_ranges
 class AttentionState:
     """What the rows of a search have behind them: a cache per block, the rows' pages, their lengths and the sums of their predictions.
 
-    rows: at most this many at a time; stages: no row gets longer.  `longest` is the longest length that the calls so far may have made."""
+    rows: at most this many at a time; stages: no row gets longer.  `longest` is the longest length that a row may have, as far as the host knows:
+    it grows with the calls, and is looked up on the GPU where it would leave no place."""
 
     def __init__(self, torch, caches, rows, wide, device):
         self.caches, self.page, self.rows, self.wide, self.longest = caches, caches[0].page, rows, wide, 0
@@ -57,6 +58,10 @@ class AttentionValue:
         wide = -(-stages // page)
         caches = [vf.KvCache.zeros(fmt, rows * wide, page, self.kv_heads, self.head_dim, self.ctx.device) for _ in self.blocks or [None]]
         return AttentionState(self.torch, caches, rows, wide, self.ctx.device)
+
+    def _capturing(self):
+        """Whether torch's current stream is being captured, so that nothing can be looked up."""
+        return self.torch.cuda.is_current_stream_capturing()
 
     def _tokens(self, x, caches, table, lengths, offsets, longest, longest_kv):
         """Predictions [tokens] of x [tokens][F], the last tokens of sequences of these lengths."""
@@ -109,10 +114,12 @@ class AttentionValue:
         else:
             if state.lengths.shape[0] != n_seq:
                 raise ValueError(f"the state has {state.lengths.shape[0]} rows, not {n_seq}")
-            longest_kv = state.longest + longest
-            if longest_kv > state.wide * state.page:
-                raise ValueError(f"the state has place for {state.wide * state.page} stages a row, not {longest_kv}")
+            longest_kv, room = state.longest + longest, state.wide * state.page
             caches, table, lengths = state.caches, state.table, state.lengths + counts
+            if longest_kv > room and not self._capturing():
+                longest_kv = int(lengths.max())   # (rows have forked to shorter ones, or others have been the longest in turn)
+            if longest_kv > room:
+                raise ValueError(f"the state has place for {room} stages a row, not {longest_kv}")
         each = self._tokens(x, caches, table, lengths, offsets, longest, longest_kv)
         value = each.reshape(n_seq, -1).sum(1) if offsets is None else sums_of_ranges(torch, each, offsets.long())
         if state is not None:

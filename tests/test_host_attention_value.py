@@ -1,0 +1,114 @@
+"""The attention value network's keeping of lengths, pages and rows on the CPU, with the operators' rules for pages and positions in place of the
+operators: a stage's prediction is the sum of all stages' first features that it sees, whole numbers, so that every value is exact."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2011_14486_amd import attention
+
+
+class Pool:
+    """A cache of one number a token."""
+
+    def __init__(self, pages, page):
+        self.k, self.page = torch.full((pages, 1, page, 8), float("nan")), page
+        self.tensors = (self.k, None)
+
+
+class Thing:
+    pass
+
+
+def network(monkeypatch, capturing=False):
+    net = object.__new__(attention.AttentionValue)
+    net.ctx, net.torch, net.blocks, net.kv_heads, net.head_dim = Thing(), torch, [None], 1, 8
+    net.ctx.device, net.ctx.torch = torch.device("cpu"), torch
+    net.ctx.empty = lambda shape, dtype: torch.full(shape, float("nan"))
+    net.capturing, net.pages = capturing, []
+    monkeypatch.setattr(attention.AttentionValue, "_capturing", lambda self: self.capturing, raising=False)
+
+    def cache(fmt, head_dim, k, v):
+        c = Pool(0, k.shape[2])
+        c.k, c.tensors = k, (k, v)
+        return c
+
+    monkeypatch.setattr(attention.vf, "KvCache", cache)
+
+    def tokens(x, caches, table, lengths, offsets, longest, longest_kv):
+        pool, wide = caches[0].k, table.shape[1]
+        page, n, each = pool.shape[2], len(lengths), len(x) // len(lengths)
+        net.pages.append(pool.shape[0])
+        out = torch.full((len(x),), float("nan"))
+        for write in (True, False):
+            for s in range(n):
+                first, end = (s * each, (s + 1) * each) if offsets is None else (int(offsets[s]), int(offsets[s + 1]))
+                if not 0 <= first <= end <= len(x):
+                    continue
+                length = min(max(int(lengths[s]), 0), wide * page)
+                place = lambda t: (int(table[s, t // page]), t % page)   # noqa: E731
+                for i in range(end - first):
+                    t = length - (end - first) + i
+                    if write and t >= 0 and 0 <= place(t)[0] < len(pool):
+                        pool[place(t)[0], 0, place(t)[1], 0] = x[first + i, 0]
+                    if not write:
+                        keys = [pool[place(u)[0], 0, place(u)[1], 0] if 0 <= place(u)[0] < len(pool) else float("nan") for u in range(t + 1)]
+                        out[first + i] = float(sum(keys))
+        return out
+
+    net._tokens = tokens
+    return net
+
+
+def state_of(rows, stages, page=16):
+    wide = -(-stages // page)
+    return attention.AttentionState(torch, [Pool(rows * wide, page)], rows, wide, torch.device("cpu"))
+
+
+def value_of(xs):
+    return float(sum(sum(xs[:t + 1]) for t in range(len(xs))))
+
+
+def stages(rng, n):
+    return torch.from_numpy(rng.integers(-9, 10, (n, 3)).astype(np.float32))
+
+
+def test_a_state_is_used_again(monkeypatch):
+    """Rows that fork to a short one have the place of a short one, however long the longest has been, and ragged calls add what rows have got."""
+    net, rng = network(monkeypatch), np.random.default_rng(1)
+    state = state_of(4, 32)
+    net.fork(state, torch.zeros(2, dtype=torch.int32))
+    first = stages(rng, 33)
+    net.score(first, 2, 30, torch.tensor([0, 30, 33], dtype=torch.int32), state)
+    net.fork(state, torch.tensor([1], dtype=torch.int32))
+    keep = first[30:33, 0].tolist()
+    for _ in range(29):
+        y = stages(rng, 1)
+        keep.append(float(y[0, 0]))
+        assert net.extend(y, state).tolist() == [value_of(keep)]
+    with pytest.raises(ValueError):
+        net.extend(stages(rng, 1), state)      # 33 stages
+    assert state.lengths.tolist() == [32]
+    # a further search from nothing
+    state.lengths.zero_()
+    state.total.zero_()
+    x = stages(rng, 32)
+    assert net.score(x, 1, state=state).tolist() == [value_of(x[:, 0].tolist())]
+    with pytest.raises(ValueError):
+        net.extend(stages(rng, 1), state)
+
+
+def test_turns_of_the_longest_row(monkeypatch):
+    """Ragged calls in which another row is the longest each time."""
+    net, rng = network(monkeypatch), np.random.default_rng(2)
+    state = state_of(2, 32)
+    kept = [[], []]
+    for counts in ([20, 1], [1, 20], [5, 5]):
+        x = stages(rng, sum(counts))
+        off = np.concatenate([[0], np.cumsum(counts)])
+        got = net.score(x, 2, max(counts), torch.from_numpy(off.astype(np.int32)), state)
+        for r in range(2):
+            kept[r] += x[off[r]:off[r + 1], 0].tolist()
+        assert got.tolist() == [value_of(k) for k in kept]
+    with pytest.raises(ValueError):
+        net.score(stages(rng, 8), 2, 7, torch.tensor([0, 7, 8], dtype=torch.int32), state)
+    assert state.lengths.tolist() == [26, 26]
