@@ -91,26 +91,34 @@ class AttentionValue:
     def score(self, x, n_seq=1, longest=None, offsets=None, state=None):
         """Values [n_seq] of whole sequences x bf16 [tokens][F]: sequence s has rows offsets[s] .. offsets[s + 1] - 1 (int32 [n_seq + 1]; None:
         all have tokens / n_seq), behind row s of `state`, which then has them too.  longest: no sequence has more tokens (default: without offsets
-        their number, with offsets all tokens).  Without a state every sequence begins from nothing and nothing is kept."""
+        their number, with offsets looked up on the GPU, or in a captured call all tokens).  Without a state every sequence begins from nothing and
+        nothing is kept."""
         torch, tokens = self.torch, x.shape[0]
-        if longest is None:
-            longest = tokens if offsets is not None or n_seq == 0 else tokens // n_seq
-        longest = min(longest, tokens)
         if n_seq == 0 or tokens == 0:
             return x.new_zeros(n_seq, dtype=torch.float32) if state is None else state.total.clone()
         if offsets is None:
             if tokens % n_seq:
                 raise ValueError(f"{tokens} rows cannot be dealt to {n_seq} sequences; offsets are wanted")
             counts = torch.full((n_seq,), tokens // n_seq, dtype=torch.int32, device=self.ctx.device)
+            longest = tokens // n_seq if longest is None else min(longest, tokens)
         else:
             begin, end = offsets[:-1], offsets[1:]
             counts = torch.where((begin >= 0) & (end >= begin) & (end <= tokens), end - begin, 0).to(torch.int32)
+            if longest is None and not self._capturing():
+                longest = int(counts.max())
+            longest = tokens if longest is None else min(longest, tokens)
         if state is None:
             # (one cache does for all blocks: a block's keys are not looked at after it)
             wide = max(1, -(-longest // 16))
-            new = [self.ctx.empty((n_seq * wide, self.kv_heads, 16, (self.head_dim + 7) // 8 * 8), torch.bfloat16) for _ in range(2)]
+            if offsets is None:
+                pages, table = n_seq * wide, torch.arange(n_seq * wide, dtype=torch.int32, device=self.ctx.device).reshape(n_seq, wide)
+            else:   # a sequence's pages behind those of the ones before: at most a page more than its tokens fill
+                need = (counts + 15) // 16
+                pages = tokens // 16 + n_seq
+                table = ((need.cumsum(0) - need)[:, None] + torch.arange(wide, device=self.ctx.device)).to(torch.int32)
+            new = [self.ctx.empty((pages, self.kv_heads, 16, (self.head_dim + 7) // 8 * 8), torch.bfloat16) for _ in range(2)]
             caches = [vf.KvCache(vf.VF_BF16, self.head_dim, *new)] * len(self.blocks)
-            table, lengths, longest_kv = torch.arange(n_seq * wide, dtype=torch.int32, device=self.ctx.device).reshape(n_seq, wide), counts, longest
+            lengths, longest_kv = counts, longest
         else:
             if state.lengths.shape[0] != n_seq:
                 raise ValueError(f"the state has {state.lengths.shape[0]} rows, not {n_seq}")

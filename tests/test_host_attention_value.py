@@ -112,3 +112,47 @@ def test_turns_of_the_longest_row(monkeypatch):
     with pytest.raises(ValueError):
         net.score(stages(rng, 8), 2, 7, torch.tensor([0, 7, 8], dtype=torch.int32), state)
     assert state.lengths.tolist() == [26, 26]
+
+
+def test_ragged_sequences_without_a_longest(monkeypatch):
+    """Without `longest` it is looked up: pages for the tokens there are, and a state's place is each row's own."""
+    net, rng = network(monkeypatch), np.random.default_rng(3)
+    counts = rng.integers(0, 40, 200)
+    counts[7] = 300
+    x = stages(rng, int(counts.sum()))
+    off = np.concatenate([[0], np.cumsum(counts)])
+    got = net.score(x, 200, offsets=torch.from_numpy(off.astype(np.int32)))
+    assert got.tolist() == [value_of(x[a:b, 0].tolist()) for a, b in zip(off[:-1], off[1:])]
+    assert net.pages[-1] <= len(x) // 16 + 200
+    state = state_of(6, 32)
+    net.fork(state, torch.zeros(6, dtype=torch.int32))
+    for counts in ([20, 30, 5, 0, 1, 16], [12, 2, 3, 32, 1, 16]):
+        x = stages(rng, sum(counts))
+        off = np.concatenate([[0], np.cumsum(counts)])
+        net.score(x, 6, offsets=torch.from_numpy(off.astype(np.int32)), state=state)
+    assert state.lengths.tolist() == [32, 32, 8, 32, 2, 32] and state.longest == 32
+    with pytest.raises(ValueError):
+        net.score(x[:3], 6, offsets=torch.tensor([0, 0, 0, 0, 0, 0, 3], dtype=torch.int32), state=state)
+
+
+def test_ranges_in_any_order(monkeypatch):
+    """Ranges that lie in no order, that leave rows out, and ones that do not lie in the tokens."""
+    net, rng = network(monkeypatch), np.random.default_rng(4)
+    x = stages(rng, 100)
+    off = torch.tensor([3, 40, 90, 90, 200], dtype=torch.int32)
+    for more in (dict(), dict(longest=50), dict(longest=100)):
+        got = net.score(x, 4, offsets=off, **more)
+        assert got.tolist() == [value_of(x[a:b, 0].tolist()) for a, b in ((3, 40), (40, 90), (90, 90), (0, 0))]
+
+
+def test_captured_calls_look_nothing_up(monkeypatch):
+    """While a stream is captured all tokens are taken as the longest, and nothing is read back."""
+    net, rng = network(monkeypatch, capturing=True), np.random.default_rng(5)
+    x = stages(rng, 60)
+    off = torch.tensor([0, 25, 60], dtype=torch.int32)
+    want = [value_of(x[:25, 0].tolist()), value_of(x[25:, 0].tolist())]
+    monkeypatch.setattr(torch.Tensor, "__int__", lambda self: pytest.fail("looked up"))
+    taken = []
+    net._tokens = lambda x, caches, table, lengths, offsets, longest, longest_kv: (taken.append((longest, tuple(table.shape))), x[:, 0])[1]
+    net.score(x, 2, offsets=off)
+    assert taken == [(60, (2, 4))]
