@@ -27,13 +27,15 @@ class AttentionState:
     """What the rows of a search have behind them: a cache per block, the rows' pages, their lengths and the sums of their predictions.
 
     rows: at most this many at a time; stages: no row gets longer.  `longest` is the longest length that a row may have, as far as the host knows:
-    it grows with the calls, and is looked up on the GPU where it would leave no place."""
+    it grows with the calls, and is looked up on the GPU where it would leave no place.  Once a graph holds a call (`captured`) its replays
+    add what the host does not know of: then a row without a place has NaN as its value from there on, and is not lengthened."""
 
     def __init__(self, torch, caches, rows, wide, device):
         self.caches, self.page, self.rows, self.wide, self.longest = caches, caches[0].page, rows, wide, 0
         self.table = torch.arange(rows * wide, dtype=torch.int32, device=device).reshape(rows, wide)
         self.lengths = torch.zeros(rows, dtype=torch.int32, device=device)
         self.total = torch.zeros(rows, device=device)
+        self.captured = False
 
 
 class AttentionValue:
@@ -90,21 +92,24 @@ class AttentionValue:
 
     def score(self, x, n_seq=1, longest=None, offsets=None, state=None):
         """Values [n_seq] of whole sequences x bf16 [tokens][F]: sequence s has rows offsets[s] .. offsets[s + 1] - 1 (int32 [n_seq + 1]; None:
-        all have tokens / n_seq), behind row s of `state`, which then has them too.  longest: no sequence has more tokens (default: without offsets
-        their number, with offsets looked up on the GPU, or in a captured call all tokens).  Without a state every sequence begins from nothing and
-        nothing is kept."""
+        all have tokens / n_seq), behind row s of `state`, which then has them too.  longest: with offsets, no sequence has more tokens, and one that has
+        is not taken: its value is NaN (default: looked up on the GPU, in a captured call all tokens).  Without a state every sequence begins from nothing
+        and nothing is kept."""
         torch, tokens = self.torch, x.shape[0]
         if n_seq == 0 or tokens == 0:
             return x.new_zeros(n_seq, dtype=torch.float32) if state is None else state.total.clone()
+        over = None   # sequences that are not taken
         if offsets is None:
             if tokens % n_seq:
                 raise ValueError(f"{tokens} rows cannot be dealt to {n_seq} sequences; offsets are wanted")
             counts = torch.full((n_seq,), tokens // n_seq, dtype=torch.int32, device=self.ctx.device)
-            longest = tokens // n_seq if longest is None else min(longest, tokens)
+            longest = tokens // n_seq
         else:
             begin, end = offsets[:-1], offsets[1:]
             counts = torch.where((begin >= 0) & (end >= begin) & (end <= tokens), end - begin, 0).to(torch.int32)
-            if longest is None and not self._capturing():
+            if longest is not None:
+                over = counts > longest
+            elif not self._capturing():
                 longest = int(counts.max())
             longest = tokens if longest is None else min(longest, tokens)
         if state is None:
@@ -124,16 +129,24 @@ class AttentionValue:
                 raise ValueError(f"the state has {state.lengths.shape[0]} rows, not {n_seq}")
             longest_kv, room = state.longest + longest, state.wide * state.page
             caches, table, lengths = state.caches, state.table, state.lengths + counts
-            if longest_kv > room and not self._capturing():
+            state.captured = state.captured or self._capturing()
+            if state.captured:
+                over = lengths > room if over is None else over | (lengths > room)
+                longest_kv = min(longest_kv, room)
+            elif longest_kv > room:
                 longest_kv = int(lengths.max())   # (rows have forked to shorter ones, or others have been the longest in turn)
-            if longest_kv > room:
-                raise ValueError(f"the state has place for {room} stages a row, not {longest_kv}")
-        each = self._tokens(x, caches, table, lengths, offsets, longest, longest_kv)
+                if longest_kv > room:
+                    raise ValueError(f"the state has place for {room} stages a row, not {longest_kv}")
+        # (a sequence of length 0 has no positions: its tokens are written nowhere, see nothing and cost nothing else)
+        where = lengths if over is None else torch.where(over, 0, lengths)
+        each = self._tokens(x, caches, table, where, offsets, longest, longest_kv)
         value = each.reshape(n_seq, -1).sum(1) if offsets is None else sums_of_ranges(torch, each, offsets.long())
+        if over is not None:
+            value = torch.where(over, float("nan"), value)
         if state is not None:
             value = value + state.total
             state.total.copy_(value)
-            state.lengths.copy_(lengths)
+            state.lengths.copy_(lengths if over is None else torch.where(over, state.lengths, lengths))
             state.longest = longest_kv
         return value
 

@@ -156,3 +156,66 @@ def test_captured_calls_look_nothing_up(monkeypatch):
     net._tokens = lambda x, caches, table, lengths, offsets, longest, longest_kv: (taken.append((longest, tuple(table.shape))), x[:, 0])[1]
     net.score(x, 2, offsets=off)
     assert taken == [(60, (2, 4))]
+
+
+NAN = float("nan")
+
+
+def same(got, want):
+    return np.array_equal(np.array(got.tolist()), np.array(want), equal_nan=True)
+
+
+def test_a_longest_below_the_truth(monkeypatch):
+    """Sequences with more tokens have NaN as their value, never another number, and a state's row is not lengthened by them; without offsets the
+    host knows better."""
+    net, rng = network(monkeypatch), np.random.default_rng(6)
+    counts = [20, 50, 33, 32, 0]
+    x = stages(rng, sum(counts))
+    off = np.concatenate([[0], np.cumsum(counts)])
+    each, offsets = [value_of(x[a:b, 0].tolist()) for a, b in zip(off[:-1], off[1:])], torch.from_numpy(off.astype(np.int32))
+    assert same(net.score(x, 5, 32, offsets), [each[0], NAN, NAN, each[3], 0.0])
+    assert same(net.score(x, 5, 1, offsets), [NAN, NAN, NAN, NAN, 0.0])
+    got = net.score(x[:120], 3, 10)
+    assert same(got, [value_of(x[a:a + 40, 0].tolist()) for a in (0, 40, 80)])
+    state = state_of(5, 48)
+    net.fork(state, torch.zeros(5, dtype=torch.int32))
+    got = net.score(x, 5, 40, offsets, state)
+    assert same(got, [each[0], NAN, each[2], each[3], 0.0]) and same(state.total, got.tolist())
+    assert state.lengths.tolist() == [20, 0, 33, 32, 0] and state.longest == 40
+    more = stages(rng, 5)
+    keep = [x[a:b, 0].tolist() + [float(v)] for a, b, v in zip(off[:-1], off[1:], more[:, 0])]
+    assert same(net.extend(more, state), [value_of(k) if r != 1 else NAN for r, k in enumerate(keep)])
+
+
+def test_replays_past_the_place(monkeypatch):
+    """A captured extension that is replayed more often than there is place for: NaN from there on, and pages that rows share stay as they were."""
+    net, rng = network(monkeypatch), np.random.default_rng(7)
+    state = state_of(4, 16)
+    net.fork(state, torch.zeros(1, dtype=torch.int32))
+    x = stages(rng, 16)
+    net.score(x, 1, state=state)
+    net.fork(state, torch.zeros(4, dtype=torch.int32))      # (four rows of 16 stages that share one full page)
+    before = state.caches[0].k.clone()
+    net.capturing = True
+    for _ in range(3):
+        assert same(net.extend(stages(rng, 4), state), [NAN] * 4)
+    assert torch.equal(before.nan_to_num(-1e9), state.caches[0].k.nan_to_num(-1e9))
+    # and rows with some place left, replayed on the same tensors
+    state = state_of(2, 16)
+    net.fork(state, torch.zeros(2, dtype=torch.int32))
+    x = stages(rng, 2 * 14)
+    net.capturing = False
+    net.score(x, 2, state=state)
+    net.capturing = True
+    keep = [x[:14, 0].tolist(), x[14:, 0].tolist()]
+    lengths, total = state.lengths, state.total
+    for turn in range(4):
+        y = stages(rng, 2)
+        got = net.extend(y, state)
+        keep = [k + [float(v)] for k, v in zip(keep, y[:, 0])]
+        assert same(got, [value_of(k) if turn < 2 else NAN for k in keep])
+        assert state.lengths is lengths and state.total is total
+    # what replays have added the host does not know: calls after them go by the rows' own lengths too
+    net.capturing = False
+    state.longest = 1
+    assert same(net.extend(stages(rng, 2), state), [NAN, NAN])
