@@ -50,6 +50,7 @@ class AttentionValue:
         self.rope = vf.Rope(dev(weights["freq"]), interleaved, magnitude)
         self.w_in, self.gain = four(weights["w_in"]), dev(weights["gain"])
         self.w_head, self.b_head = four(weights["w_head"]), dev(weights["b_head"])
+        self.ends = torch.tensor([0.0, float("nan")], device=ctx.device)
         self.blocks = [(dev(b["gain"]), four(b["w_qkv"]), four(b["w_out"]),
                         (dev(b["gain_up"]), four(b["w_up"]), four(b["w_down"])) if weights["hidden"] else None) for b in weights["blocks"]]
 
@@ -156,14 +157,19 @@ class AttentionValue:
 
     def fork(self, state, parents):
         """Row r of the state goes on from what row parents[r] (int32 or int64 [n], n at most state.rows) has had, as many rows as there are
-        parents.  Full pages are shared, the page that a row goes on in is its own.  The state has other tables and lengths afterwards, and pages that
+        parents; -1: from nothing; any other parent that is no row makes a row whose values are NaN.  Full pages are shared, the page that a row goes on in is its own.  The state has other tables and lengths afterwards, and pages that
         no row has are written over, so that a graph holds extensions, not forks."""
         torch, wide, page = self.torch, state.wide, state.page
         n, device = parents.shape[0], self.ctx.device
         if n > state.rows:
             raise ValueError(f"the state has place for {state.rows} rows, not {n}")
-        parents = parents.long()
-        lengths, old = state.lengths[parents], state.table[parents]
+        # lengths and sums with those of a row from nothing and of one that is not there behind them
+        rows = state.lengths.shape[0]
+        at = parents.clamp(-2, rows).long()
+        at = torch.where(at == -1, rows, torch.where((at < 0) | (at == rows), rows + 1, at))
+        lengths = torch.cat((state.lengths, state.lengths.new_zeros(2)))[at]
+        total = torch.cat((state.total, self.ends))[at]
+        old = state.table[at.clamp(max=rows - 1)] if rows else state.table.new_zeros((n, wide))
         full = (lengths // page).long()
         at = torch.arange(wide, device=device)
         own = at >= full[:, None]
@@ -181,4 +187,4 @@ class AttentionValue:
             for pool in cache.tensors:
                 if pool is not None:
                     pool.index_copy_(0, to, pool.index_select(0, source))
-        state.table, state.lengths, state.total = table, lengths, state.total[parents]
+        state.table, state.lengths, state.total = table, lengths, total

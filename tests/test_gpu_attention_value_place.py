@@ -151,3 +151,26 @@ def test_captured_calls(vf, weights):  # noqa: F811
         torch.cuda.synchronize()
         assert torch.isnan(net.extend(z, state)).all()      # an eager call behind the replays
     vf.vf_destroy(ctx)
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+def test_parents_that_are_not_there(vf, ctx, weights, fmt):  # noqa: F811
+    """-1 begins from nothing; any other parent that is no row makes a row whose value is NaN; the others are as without these."""
+    import torch
+    from paper_2011_14486_amd import attention
+    net = attention.AttentionValue(ctx, weights)
+    x, off, _ = ragged([20, 32, 0])
+    y = dev(bf16(np.random.default_rng(7).standard_normal((7, 32))))
+    got = []
+    for parents in ([1, -1, 3, 1, -2, 0, 2 ** 31 - 1], [1, 2, 2, 1, 2, 0, 2]):     # (row 2 has nothing either)
+        state = net.state(7, 48, fmt=fmt)
+        net.fork(state, torch.zeros(3, dtype=torch.int32, device="cuda"))
+        net.score(dev(x), 3, 32, off, state)
+        net.fork(state, dev(np.array(parents), torch.int32))
+        got.append(net.extend(y, state))
+        assert state.lengths.tolist() == [33, 1, 1, 33, 1, 21, 1]
+    there = [0, 1, 3, 5]
+    assert torch.equal(got[0][there], got[1][there]) and torch.isfinite(got[1]).all() and torch.isnan(got[0][[2, 4, 6]]).all()
+    net.fork(state, torch.zeros(0, dtype=torch.int32, device="cuda"))
+    net.fork(state, dev(np.array([-1]), torch.int32))
+    assert torch.equal(net.extend(y[1:2], state), net.extend(y[1:2], net.state(1, 48, fmt=fmt)))

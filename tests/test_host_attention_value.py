@@ -7,6 +7,9 @@ import torch
 from paper_2011_14486_amd import attention
 
 
+NAN = float("nan")
+
+
 class Pool:
     """A cache of one number a token."""
 
@@ -22,7 +25,7 @@ class Thing:
 def network(monkeypatch, capturing=False):
     net = object.__new__(attention.AttentionValue)
     net.ctx, net.torch, net.blocks, net.kv_heads, net.head_dim = Thing(), torch, [None], 1, 8
-    net.ctx.device, net.ctx.torch = torch.device("cpu"), torch
+    net.ctx.device, net.ctx.torch, net.ends = torch.device("cpu"), torch, torch.tensor([0.0, NAN])
     net.ctx.empty = lambda shape, dtype: torch.full(shape, float("nan"))
     net.capturing, net.pages = capturing, []
     monkeypatch.setattr(attention.AttentionValue, "_capturing", lambda self: self.capturing, raising=False)
@@ -158,9 +161,6 @@ def test_captured_calls_look_nothing_up(monkeypatch):
     assert taken == [(60, (2, 4))]
 
 
-NAN = float("nan")
-
-
 def same(got, want):
     return np.array_equal(np.array(got.tolist()), np.array(want), equal_nan=True)
 
@@ -219,3 +219,27 @@ def test_replays_past_the_place(monkeypatch):
     net.capturing = False
     state.longest = 1
     assert same(net.extend(stages(rng, 2), state), [NAN, NAN])
+
+
+@pytest.mark.parametrize("kind", [torch.int32, torch.int64])
+def test_parents_that_are_not_there(monkeypatch, kind):
+    """-1 begins from nothing; any other parent that is no row makes a row whose value is NaN; the same parent may come many times."""
+    net, rng = network(monkeypatch), np.random.default_rng(8)
+    state = state_of(7, 48)
+    net.fork(state, torch.zeros(3, dtype=kind))
+    counts = [20, 32, 0]
+    x = stages(rng, sum(counts))
+    off = np.concatenate([[0], np.cumsum(counts)])
+    net.score(x, 3, 32, torch.from_numpy(off.astype(np.int32)), state)
+    prefix = [x[a:b, 0].tolist() for a, b in zip(off[:-1], off[1:])]
+    parents = [1, -1, 3, 1, -2, 0, 2 ** 31 - 1]
+    net.fork(state, torch.tensor(parents, dtype=kind))
+    y = stages(rng, 7)
+    want = [value_of(([] if p == -1 else prefix[p]) + [float(v)]) if -1 <= p < 3 else NAN for p, v in zip(parents, y[:, 0])]
+    assert same(net.extend(y, state), want)
+    assert state.lengths.tolist() == [33, 1, 1, 33, 1, 21, 1]
+    # a state without rows, and rows from nothing again
+    net.fork(state, torch.zeros(0, dtype=kind))
+    assert net.extend(y[:0], state).shape == (0,)
+    net.fork(state, torch.tensor([-1, 0], dtype=kind))
+    assert same(net.extend(y[:2], state), [float(y[0, 0]), NAN])
