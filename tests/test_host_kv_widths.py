@@ -1,8 +1,8 @@
 """Which attention kernel takes a head's size, and that no lane of it fetches past the end of a cache's row, on a runtime without a GPU.
 
 A lane takes a fixed number of neighbouring numbers of a row; one whose first number lies in the row takes them from there, others from
-the row's begin.  So the numbers from a first one inside have to lie inside too, for every width that comes to a kernel: the last row of the last page
-ends with the cache."""
+the row's begin.  (Three numbers at a time, which rows of 80 and 88 do not consist of, are taken from before where they would end behind the row.)  So the
+numbers from a first one inside have to lie inside too, for every width that comes to a kernel: the last row of the last page ends with the cache."""
 import os
 import re
 import subprocess
@@ -19,12 +19,15 @@ from tests.test_host_kv import EIGHT, OK, call, library, make_library, names  # 
 from tests.test_host_ops import stub_path  # noqa: E402, F401
 
 
-def fetches(name):
-    """(first numbers, how many) of every fetch of a row by the kernel's lanes, and the widest row that it holds."""
+def fetches(name, w):
+    """(first numbers, how many) of every fetch of a row of w numbers by the kernel's lanes, and the widest row that it holds."""
     m = re.search(r"k_attend_wideILi(\d)ELi(\d+)E", name)
     if m:
         fmt, DP = int(m[1]), int(m[2])
-        return [([8 * x + 4 * g for x in range(DP // 8) for g in range(2)], 4), ([DP // 32 * n for n in range(32)], DP // 32)], DP
+        VW = DP // 32
+        values = [VW * n if VW * n >= w or VW != 3 else min(VW * n, w - VW) for n in range(32)]
+        assert set(range(w)) <= {f + x for f in values for x in range(VW)}
+        return [([8 * x + 4 * g for x in range(DP // 8) for g in range(2)], 4), (values, VW)], DP
     m = re.search(r"k_attend_rowsI([tf])Li(\d)ELi(\d+)E", name)
     if m:
         f32, fmt, DP = m[1] == "f", int(m[2]), int(m[3])
@@ -50,7 +53,7 @@ def widths(stub, vf, ctx):
                 assert call(vf, ctx, "attend", **dict(EIGHT if fmt == 2 else {}, format=fmt), type=kind, head_dim=dim, n_seq=1, tokens=tokens, ldq=8 * dim, ldo=8 * dim,
                             longest_kv=keys, max_pages=1 << 14, ld_table=1 << 14) == OK
                 name = names(stub)[0][0]
-                each, widest = fetches(name)
+                each, widest = fetches(name, w)
                 assert widest >= dim, (name, dim)
                 for firsts, n in each:
                     assert all(f + n <= w for f in firsts if f < w), (name, dim, w)
