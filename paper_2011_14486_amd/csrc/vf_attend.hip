@@ -95,7 +95,7 @@ __device__ __forceinline__ float weight_of(float m, float top) { return exp2_(m 
 // side, and the product wants keys side by side: the numbers of eight keys, eight of each, are turned around in registers, halves by halves, 32 instructions
 // for 8 products, which memory's time hides.
 // MI355X: 4 rows of 32 heads of 128 behind 131,072 keys of 8 heads in 8 bits, 1.1 GB, 199 us = 5.6 TB/s (503 with a step's loads behind the step before, 235 with pages
-// by vector loads); 64 rows behind 2001 keys in bf16 95 us = 5.5 TB/s; 1024 rows behind 501 keys of 64 prefixes, 16 over 4 heads of 64, 41 us and 9 for the groups (72
+// by vector loads); 64 rows behind 2001 keys in bf16 105 us = 5.0 TB/s, in 8 bits 45; 1024 rows behind 501 keys of 64 prefixes, 16 over 4 heads of 64, 42 us and 10 for the groups (57
 // apart); one row behind 1001 keys 11 us, of which 5 are there without keys.
 enum { SHARE, ROWWISE, SEQWISE, GROUP, SHARE8 };   // SHARE8: eight waves, where there are few workgroups
 
@@ -710,7 +710,7 @@ __global__ void __launch_bounds__(MODE == SHARE8 ? 512 : 256, MODE == GROUP && D
 // Products of 32 by 32 numbers, two of the sum at a time, take so long that one wave a SIMD keeps the matrix cores busy as long as its operands are
 // there: a step's keys are sent for behind the scores of the step before, its values behind the outputs.  Lane n of half g holds key n, and takes the
 // numbers d = 8 x + 4 g + e for product (x, e); of value 8 (i / 4) + 4 g + i % 4, whose weight is in register i, it takes the VW numbers at VW n, one for each of VW products.
-// MI355X: a prompt of 2048 tokens, 32 heads of 128 over 8 of the cache, 390 us = 88 TFLOP/s, of the 154 that the vendor library's product reaches: matrix cores busy
+// MI355X: a prompt of 2048 tokens, 32 heads of 128 over 8 of the cache, 400 us = 86 TFLOP/s, of the 154 that the vendor library's product reaches: matrix cores busy
 // 54 % of the cycles, the rest is weights and moves beside them, which nothing else hides with one wave a SIMD.
 template <int FMT, int DP>
 __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const AttendArgs a) {
@@ -961,7 +961,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 2 : 1) k_attend_wide(const Att
 // 32 keys by 32 rows; values are read with the reads that turn a 4 by 16 block around, so that a lane gets four keys' numbers of one column.
 //
 // Two workgroups a compute unit: while waves of one are at their weights, those of the other may be at their products.  MI355X: prompt of 8192 tokens, 32 over 8 heads of
-// 128, 575 us = 960 TFLOP/s (the vendor library's product of 8192^3 reaches 1280); without weights and maxima, in a copy that leaves them out, 538 of then 604 us,
+// 128, 570 - 620 us from card to card = 890 - 965 TFLOP/s (the vendor library's product of 8192^3 reaches 1280); without weights and maxima, in a copy that leaves them out, 538 of then 604 us,
 // without loads too 462: products, their reads and one barrier a tile are three quarters of it.  Matrix cores are busy 40 % of the cycles, the vector unit 38 %.  Tried and slower:
 // scores of the next tile beside this one's weights (spills), 64 rows a wave with one wave a SIMD (790 us), a higher priority at products (614), operands' reads ordered
 // by hand (610).  16384 sequences of 50 tokens, 4 over 2 heads of 64: 340 us, 3.7 TB/s; a workgroup is one tile there, and its chain of loads (length, pages, keys) is
@@ -1330,7 +1330,7 @@ __global__ void __launch_bounds__(256, DP <= 64 ? 3 : DP <= 128 ? 2 : 1) k_atten
 // Sorts sequences by their first page and cuts them into groups of up to `most` that have the same: order[n] = (sequence, its length), items[n + 1] = first
 // places of the groups (behind the last one n).  A sequence without keys is a group of its own.  One workgroup, a bitonic network of 64-bit keys (page,
 // sequence), key 1024 r + t in register r of thread t: neighbours up to 32 apart are exchanged between lanes, up to 512 through the LDS.
-// MI355X: 1024 sequences 9 us.
+// MI355X: 1024 sequences 10 us.
 constexpr int MAX_GROUPED = 4096;
 template <int PER>
 __global__ void __launch_bounds__(1024) k_attend_group(const AttendArgs a, int2 *order, int32_t *items, int most) {
@@ -1472,6 +1472,10 @@ int blocks_of(int64_t longest, int rows, int heads) {
 }
 
 // (about 70 us at the memory's rate; below, the 10 us that finding the groups takes are more than what sharing saves)
+// Whether rows do share pages the host does not know.  MI355X, us, in groups / each by itself: 1024 rows of 64 prefixes of 501 keys, 16 over 4 heads of 64, 52 / 57; 256 of 16 prefixes of
+// 2001, 32 over 8 heads of 128, 106 / 150.  What the rule costs where nothing is shared: 1000 rows of 501 keys 133 / 99, 256 of 2001 373 / 362, 64 of 4001, 8 heads of 128, 193 / 182, 4000 of
+// 101, 16 over 8 heads of 64, 364 / 174; and where there are few groups, whose keys no more workgroups share than before, 64 rows of one prefix of 4001 113 / 80; or short
+// prefixes, 4000 of 250 prefixes of 101 184 / 117.
 constexpr int64_t GROUP_BYTES = 384 << 20;
 
 template <typename T, int FMT, int DP>
