@@ -50,7 +50,7 @@ class AttentionValue:
         self.rope = vf.Rope(dev(weights["freq"]), interleaved, magnitude)
         self.w_in, self.gain = four(weights["w_in"]), dev(weights["gain"])
         self.w_head, self.b_head = four(weights["w_head"]), dev(weights["b_head"])
-        self.ends = torch.tensor([0.0, float("nan")], device=ctx.device)
+        self.not_there = torch.zeros(3, dtype=torch.int32, device=ctx.device), torch.tensor([float("nan"), float("nan"), 0.0], device=ctx.device)
         self.blocks = [(dev(b["gain"]), four(b["w_qkv"]), four(b["w_out"]),
                         (dev(b["gain_up"]), four(b["w_up"]), four(b["w_down"])) if weights["hidden"] else None) for b in weights["blocks"]]
 
@@ -116,12 +116,14 @@ class AttentionValue:
         if state is None:
             # (one cache does for all blocks: a block's keys are not looked at after it)
             wide = max(1, -(-longest // 16))
-            if offsets is None:
-                pages, table = n_seq * wide, torch.arange(n_seq * wide, dtype=torch.int32, device=self.ctx.device).reshape(n_seq, wide)
-            else:   # a sequence's pages behind those of the ones before: at most a page more than its tokens fill
-                need = (counts + 15) // 16
-                pages = tokens // 16 + n_seq
-                table = ((need.cumsum(0) - need)[:, None] + torch.arange(wide, device=self.ctx.device)).to(torch.int32)
+            pages, least = n_seq * wide, tokens // 16 + n_seq
+            if pages <= 2 * least:
+                table = torch.arange(pages, dtype=torch.int32, device=self.ctx.device).reshape(n_seq, wide)
+            else:
+                # most sequences are much shorter than the longest: each has as many pages as it needs, at most one more than its tokens fill, the
+                # last of them first
+                ends = ((counts + 15) >> 4).cumsum(0, dtype=torch.int32)
+                pages, table = least, ends[:, None] + torch.arange(-1, -1 - wide, -1, dtype=torch.int32, device=self.ctx.device)
             new = [self.ctx.empty((pages, self.kv_heads, 16, (self.head_dim + 7) // 8 * 8), torch.bfloat16) for _ in range(2)]
             caches = [vf.KvCache(vf.VF_BF16, self.head_dim, *new)] * len(self.blocks)
             lengths, longest_kv = counts, longest
@@ -138,12 +140,12 @@ class AttentionValue:
                 longest_kv = int(lengths.max())   # (rows have forked to shorter ones, or others have been the longest in turn)
                 if longest_kv > room:
                     raise ValueError(f"the state has place for {room} stages a row, not {longest_kv}")
-        # (a sequence of length 0 has no positions: its tokens are written nowhere, see nothing and cost nothing else)
-        where = lengths if over is None else torch.where(over, 0, lengths)
+        # (a row of length 0 has no positions: its tokens are written nowhere and see nothing.  Without a state pages are a sequence's own)
+        where = lengths if over is None or state is None else torch.where(over, 0, lengths)
         each = self._tokens(x, caches, table, where, offsets, longest, longest_kv)
         value = each.reshape(n_seq, -1).sum(1) if offsets is None else sums_of_ranges(torch, each, offsets.long())
         if over is not None:
-            value = torch.where(over, float("nan"), value)
+            value.masked_fill_(over, float("nan"))
         if state is not None:
             value = value + state.total
             state.total.copy_(value)
@@ -163,13 +165,11 @@ class AttentionValue:
         n, device = parents.shape[0], self.ctx.device
         if n > state.rows:
             raise ValueError(f"the state has place for {state.rows} rows, not {n}")
-        # lengths and sums with those of a row from nothing and of one that is not there behind them
+        # (lengths and sums with three numbers behind them: past the end, -2 and -1 as indexes)
         rows = state.lengths.shape[0]
         at = parents.clamp(-2, rows).long()
-        at = torch.where(at == -1, rows, torch.where((at < 0) | (at == rows), rows + 1, at))
-        lengths = torch.cat((state.lengths, state.lengths.new_zeros(2)))[at]
-        total = torch.cat((state.total, self.ends))[at]
-        old = state.table[at.clamp(max=rows - 1)] if rows else state.table.new_zeros((n, wide))
+        lengths, total = (torch.cat((have, ends))[at] for have, ends in zip((state.lengths, state.total), self.not_there))
+        old = state.table[at.clamp(0, rows - 1)] if rows else state.table.new_zeros((n, wide))
         full = (lengths // page).long()
         at = torch.arange(wide, device=device)
         own = at >= full[:, None]

@@ -36,9 +36,20 @@ def test_ragged_sequences_without_a_longest(vf, ctx, weights):  # noqa: F811
     held = torch.cuda.memory_allocated()
     got = net.score(x, 2000, offsets=off)
     torch.cuda.synchronize()
-    # (keys and values: 2000 x 4 pages x 16 x 2 x 64 x 2 x 2 bytes = 33 MB at most; the tokens' matrices take 60)
-    assert torch.cuda.max_memory_allocated() - held < 200 << 20
+    # (keys and values: 2 x 2000 x 4 pages x 16 x 2 x 64 x 2 bytes = 66 MB; what 50,000 tokens have at a time in a block, 512 + 256 + 4 x 96 numbers of
+    # bf16 and as many of 8 bits, 180; with all tokens taken as the longest keys and values would be 51 GB)
+    assert torch.cuda.max_memory_allocated() - held < 400 << 20
     assert torch.equal(got, net.score(x, 2000, 50, off)) and got[0] == 0
+    # one sequence much longer than the others
+    counts[5] = 1000
+    x, off, _ = ragged(counts)
+    x = dev(x)
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    got = net.score(x, 2000, offsets=off)
+    torch.cuda.synchronize()
+    assert torch.cuda.max_memory_allocated() - held < 400 << 20
+    assert torch.equal(got, net.score(x, 2000, 1000, off, net.state(2000, 1000))) and torch.isfinite(got).all()
     small, off3, _ = ragged([20, 1, 0, 37], 3)
     each = predictions(weights, small, [20, 1, 0, 37], False)
     want = np.array([each[:20].sum(), each[20], 0.0, each[21:].sum()])

@@ -25,7 +25,8 @@ class Thing:
 def network(monkeypatch, capturing=False):
     net = object.__new__(attention.AttentionValue)
     net.ctx, net.torch, net.blocks, net.kv_heads, net.head_dim = Thing(), torch, [None], 1, 8
-    net.ctx.device, net.ctx.torch, net.ends = torch.device("cpu"), torch, torch.tensor([0.0, NAN])
+    net.ctx.device, net.ctx.torch = torch.device("cpu"), torch
+    net.not_there = torch.zeros(3, dtype=torch.int32), torch.tensor([NAN, NAN, 0.0])
     net.ctx.empty = lambda shape, dtype: torch.full(shape, float("nan"))
     net.capturing, net.pages = capturing, []
     monkeypatch.setattr(attention.AttentionValue, "_capturing", lambda self: self.capturing, raising=False)
