@@ -405,7 +405,7 @@ int vf_kv_read(vf_ctx *ctx, const vf_kv *cache_host, const vf_kv_seqs *seqs_host
 /* out[r][h] = sum_t p[t] v[t], p = softmax over the keys t that row r sees of scale q[r][h] . k[t].  q and out [tokens][heads head_dim]
  * of `type`; heads is a multiple of kv_heads, head h meets head h / (heads / kv_heads) of the cache; the cache's format is `type` or
  * VF_E4M3; out may be q itself with its row distance.  0 <= scale < 2^127.  causal: a row at position t sees keys 0..t, with a window w > 0 only the last w of them; a row with
- * a negative position sees none.  Otherwise every row sees all keys, however many rows there are, and the window is 0.  A key that a row does not see takes no
+ * a negative position sees none.  Otherwise every row sees all keys, however many rows there are, and the window has to be 0.  A key that a row does not see takes no
  * part in it, whatever it and its value hold.  Rows that see no key, and rows all of whose scores are -inf, are zeros.  In bf16 the weights p of calls
  * with longest times heads / kv_heads above 16 are rounded to bf16 for their products with the values, of others to 2^-15 of each; numbers that are not finite may
  * come out as NaN where they would be infinite.  longest_kv: the longest length, which sets how
